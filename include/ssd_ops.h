@@ -105,6 +105,110 @@ ssd_status ssd_gemv_noalloc(const void* W, int32_t dtype, int32_t rows, int32_t 
                             const float* x_dev, int32_t M, float* y_dev, int32_t* err_dev,
                             void* stream);
 
+/* ------------------------------------------------------------------------
+ * A KV cache held in 8 bits, and what a verification pass over it needs: rows
+ * into the cache, attention over it, and the log-probabilities of tokens (the
+ * paper has no counterpart; its cache is in the model's type).  These calls
+ * take no context.  They enqueue on `stream` (NULL: the legacy default stream),
+ * whose device must be the current one, do not synchronise, allocate nothing and
+ * keep nothing between calls, so they can be captured into graphs; the first
+ * call of a kind on a device sets kernel attributes and has to come before a
+ * capture.  Calls on different streams can run at the same time where they
+ * share no output and no workspace; so can captured ones.  The returned
+ * status covers the host-side checks and the launches, ssd_last_error(NULL) has
+ * its message; what only the device can see sets bits (SSD error bits) in
+ * *err_dev (device int32, may be NULL), which the caller clears. */
+#define SSD_KV8_BLOCK 64       /* positions that share a scale */
+#define SSD_KV8_MAX_SEQS 4096
+#define SSD_DEV_ERR_TOKEN 1    /* a token id outside [0, vocab) */
+#define SSD_DEV_ERR_CAPACITY 2 /* positions outside the cache */
+#define SSD_DEV_ERR_CONTROL 4  /* a number of rows outside 0..M */
+
+/* Cache of one layer for n_seq sequences (all memory the caller's, device).
+ * k, v: e4m3 codes [n_seq][n_kv_heads][max_seq][head_dim], 16-byte aligned; k_scale,
+ * v_scale: fp32 [n_seq][n_kv_heads][max_seq / 64].  A value is code * scale of
+ * its block of 64 positions.  A scale is the smallest power of two, 2^-120 to
+ * 2^111, that brings the block's largest magnitude to 448 or less (beyond
+ * 448 * 2^111 values are cut to that).  max_seq: a multiple of 64; head_dim 64 or 128
+ * (SSD_ERR_UNSUPPORTED otherwise).  Nothing has to be initialised: positions that
+ * were not appended are never used. */
+typedef struct {
+  int32_t n_seq, n_kv_heads, head_dim, max_seq;
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+} ssd_kv8_cache;
+
+/* Appends: rows m < rows[b] of sequence b (rows: device [n_seq], NULL: M each;
+ * 0 leaves the sequence alone) go to positions pos[b] + m (pos: device [n_seq]).
+ * k, v: device, dtype SSD_DTYPE_F32 or _BF16, row m of sequence b at element
+ * (b M + m) row_stride, its heads one behind the other: a product's rows q | k | v
+ * can be read in place; pointers and row_stride in multiples of 16 bytes.
+ * Positions from pos[b] on in its block count as free (a rollback needs no call):
+ * the block's scale is the larger of that of the positions in front of pos[b] and
+ * the new rows' own.  Where it grows, the codes in front are rounded to it again
+ * (nothing but values below 2^-6 of the new scale can change).  Codes from
+ * pos[b] + rows[b] on are not written, but stand under a new scale in that block.
+ * NaN and infinities are stored as NaN and take no part in a scale.
+ * A sequence whose positions do not lie in 0 .. max_seq - 1, or whose rows[b] does
+ * not in 0 .. M, is left alone, with its error bit. */
+ssd_status ssd_kv8_append(const ssd_kv8_cache* cache, const void* k, const void* v, int32_t dtype,
+                          int64_t row_stride, int32_t M, const int32_t* pos, const int32_t* rows,
+                          int32_t* err_dev, void* stream);
+
+/* Bytes of device workspace that ssd_kv8_attention needs for these sizes,
+ * whatever the lengths (0: invalid). */
+size_t ssd_kv8_attention_bytes(const ssd_kv8_cache* cache, int32_t dtype, int32_t n_heads,
+                               int32_t M);
+
+/* Attention over the cache, softmax scale 1/sqrt(head_dim), query head h reading KV
+ * head h / (n_heads / n_kv_heads): row m < rows[b] of sequence b sits at position
+ * p = pos[b] + m and sees the keys j <= p with j >= first[b] (device [n_seq], NULL: 0;
+ * a padded batch) and, with window > 0, j > p - window.  The rows' own keys must
+ * have been appended.  q and out: device, dtype SSD_DTYPE_F32 or _BF16 (both the
+ * same), row m of sequence b at element (b M + m) q_stride (out_stride), heads one
+ * behind the other; pointers and strides in multiples of 16 bytes; out may be q.
+ * A row that sees no key is zero.  Rows from rows[b] on are left as they were,
+ * and so are sequences with bad positions or row numbers (error bits as above).
+ * What stands in a key or value that a row does not see never reaches it, NaN
+ * neither.  Scores, sums and outputs are fp32; bf16 queries are exact, probabilities
+ * keep 11 bits (bf16) or 22 (fp32).  Equal calls give equal bits.
+ * Any M >= 1, any n_heads / n_kv_heads; SSD_ERR_CAPACITY where n_seq x M x max_seq is
+ * so large that the work has more than 2^31 parts.  workspace: 256-byte aligned,
+ * used by this call until it has run. */
+ssd_status ssd_kv8_attention(const ssd_kv8_cache* cache, const void* q, int32_t dtype,
+                             int32_t n_heads, int64_t q_stride, int32_t M, const int32_t* pos,
+                             const int32_t* rows, const int32_t* first, int32_t window, void* out,
+                             int64_t out_stride, void* workspace, size_t workspace_bytes,
+                             int32_t* err_dev, void* stream);
+
+/* Bytes of device workspace that ssd_token_logprobs needs (0: invalid sizes). */
+size_t ssd_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t top_n);
+
+#define SSD_MAX_TOP 32 /* most probable tokens of a row, at most */
+
+/* Log-probabilities over rows of logits z at temperature t (0.001..1000): of
+ * softmax(z / t), each row's lse = ln sum e^(z/t), entropy in nats, the n_tokens given
+ * tokens' log-probabilities z/t - lse and the top_n (0..32) most probable tokens (lower
+ * id first on ties) with theirs.  logits: device, dtype SSD_DTYPE_F32 or _BF16, row r
+ * at element r row_stride (>= vocab; any alignment of an element).  tokens: device
+ * [n_rows][n_tokens], logprob the same in fp32 (both may be NULL when n_tokens is 0); id
+ * -1 marks a place without a token, its result is 0; any other id outside [0, vocab)
+ * gives NaN and its error bit.  lse, entropy: device fp32 [n_rows], each may be NULL.
+ * top_id, top_logprob: device [n_rows][top_n], in descending order; where a row has
+ * fewer than top_n logits above -inf, the places left are id -1, -inf.
+ * A logit of -inf is a token of probability 0.  A row of nothing else has lse -inf,
+ * its entropy and tokens NaN.  A NaN or +inf logit makes a row's lse, entropy and
+ * log-probabilities NaN; its top_id are those of the numbers in it.
+ * workspace: device, 256-byte aligned, this call's until it has run. */
+ssd_status ssd_token_logprobs(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab,
+                              int64_t row_stride, const int32_t* tokens, int32_t n_tokens,
+                              float temperature, int32_t top_n, float* logprob, float* lse,
+                              float* entropy, int32_t* top_id, float* top_logprob,
+                              void* workspace, size_t workspace_bytes, int32_t* err_dev,
+                              void* stream);
+
 /* Test fixture: fills dst (device, n elements of dtype) with the seeded
  * synthetic weights of tensor `tid` (see synth/synth.h): element i is
  * synth_weight_f32(seed, tid, i, sigma), rounded to bf16 for SSD_DTYPE_BF16.

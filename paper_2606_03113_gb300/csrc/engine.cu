@@ -21,6 +21,7 @@
 #include <vector>
 
 #include "kernels.h"
+#include "kv8.cuh"
 #include "pipe.cuh"
 
 using namespace ssd;
@@ -528,6 +529,23 @@ int kcap_for(const ssd_ctx* x, int budget) {
 }
 
 }  // namespace
+
+namespace ssd {
+ssd_status fail_op(ssd_status s, const char* msg) noexcept {
+  try {
+    g_init_error = msg;
+  } catch (...) {  // no memory for the message: the status still says what failed
+  }
+  return s;
+}
+ssd_status fail_op_cuda(const char* what, cudaError_t e) noexcept {
+  try {
+    g_init_error = std::string(what) + ": " + cudaGetErrorString(e);
+  } catch (...) {
+  }
+  return SSD_ERR_CUDA;
+}
+}  // namespace ssd
 
 // =================================================================== C ABI
 

@@ -1,0 +1,67 @@
+// kv8.cuh -- the 8-bit KV cache of the kernel-level entry points: layout,
+// argument blocks and the numeric conversions its kernels share.
+//
+// Codes are e4m3 (4 significant bits, largest value 448).  kKv8Block positions
+// of one KV head share one fp32 scale, K and V apart; a scale is the smallest
+// power of two 2^e, kKv8MinExp <= e <= kKv8MaxExp, that brings the block's largest
+// magnitude to 448 or less.  A power of two costs e4m3 nothing (the codes are
+// floating-point numbers already), and it makes a product of code and scale
+// exact, a change of scale a shift of exponents, and the scale itself free to
+// move between the factors of a product.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "kernels.h"
+#include "pipe.cuh"
+
+namespace ssd {
+
+constexpr int kKv8Block = SSD_KV8_BLOCK;
+constexpr int kKv8MinExp = -120, kKv8MaxExp = 111;
+
+// 2^e for -126 <= e <= 127.
+__host__ __device__ __forceinline__ float pow2i(int e) {
+  union {
+    uint32_t u;
+    float f;
+  } x{(uint32_t)(e + 127) << 23};
+  return x.f;
+}
+
+// Exponent of the scale of a block whose largest finite magnitude is amax.
+__device__ __forceinline__ int kv8_scale_exp(float amax) {
+  const uint32_t b = __float_as_uint(amax);
+  if (b < 0x00800000u) return kKv8MinExp;  // zero or below 2^-126
+  // amax = f 2^x, 1 <= f < 2; 448 = 1.75 * 2^8
+  const int x = (int)(b >> 23) - 127;
+  const int e = (b & 0x007fffffu) <= 0x00600000u ? x - 8 : x - 7;
+  return min(max(e, kKv8MinExp), kKv8MaxExp);
+}
+
+// Two values as e4m3 codes, a in the low byte: nearest, ties to even, beyond
+// 448 saturated, NaN kept.
+__device__ __forceinline__ uint32_t e4m3_pair(float a, float b) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+  return r;
+}
+// Two e4m3 codes (low 16 bits) as f16, exact.
+__device__ __forceinline__ uint32_t e4m3_to_half2(uint32_t codes) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)codes));
+  return r;
+}
+// Nonzero where one of the four codes is NaN.
+__device__ __forceinline__ uint32_t e4m3_nan_mask(uint32_t w) {
+  return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+}
+
+// Message for ssd_last_error(NULL); returns s.  Does not throw.
+ssd_status fail_op(ssd_status s, const char* msg) noexcept;
+ssd_status fail_op_cuda(const char* what, cudaError_t e) noexcept;
+
+// Checks of a cache that every entry point makes; null: fine.
+const char* check_kv8(const ssd_kv8_cache* c) noexcept;
+
+}  // namespace ssd

@@ -1,0 +1,719 @@
+// kv8_attention.cu -- attention of new rows over the 8-bit cache (kv8.cuh), for
+// 1 row a sequence (decoding) up to prompt chunks, with grouped queries:
+//   o_r = sum_j p_rj v_j / sum_j p_rj,  p_rj = e^(q_r . k_j / sqrt(hd) - max),
+// over the keys j that row r sees: first .. its own position, at most `window`.
+//
+// k_kv8_rows: a block takes a stretch of the plan's units (kv8_plan.cuh); its
+// eight warps take the 16-key steps of an item in turn, each with its own running
+// maximum, sum and output, and the block joins the warps once per item.  Queries
+// and probabilities are f16 operands of mma.sync against the codes, which f16
+// holds exactly; a row of queries is first brought near f16's upper end by a
+// power of two, so a bf16 query is exact down to 2^-28 of its row's largest, and
+// the probabilities are scaled by 2^15, so those above 2^-29 of the running
+// maximum keep f16's 11 bits.  fp32 queries and probabilities enter as two f16
+// parts, 22 bits.  Scores, sums and outputs are fp32.
+//
+// The places of a lane in the matrix fragments can be any as long as both
+// operands agree, so they are chosen such that a lane's codes lie in 16
+// consecutive bytes of a key, which it copies itself to shared memory
+// (cp.async, kRing steps ahead) and reads back without a bank conflict or a
+// barrier.
+//
+// A key that some row of the tile does not see can hold anything: its scores are
+// dropped by position, and a NaN code of such a value row is zeroed before the
+// product and put back, row by row, for the rows that see it.
+#include <math.h>
+
+#include <mutex>
+
+#include "kv8_plan.cuh"
+#include "mma.cuh"
+
+namespace ssd {
+
+namespace {
+
+constexpr int kRT = 16;       // query rows of a tile
+constexpr int kStep = 16;     // keys of a warp's step
+constexpr int kRing = 6;      // steps in flight per warp
+constexpr int kVWarps = 8;
+constexpr int kVThreads = kVWarps * 32;
+constexpr int kKv8MaxBlocks = 320;
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
+                                        uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+      "{%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t half2_bits(float x, float y) {
+  const __half2 h = __floats2half2_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 half2_floats(uint32_t u) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&u));
+}
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, int bytes, bool valid) {
+  if (bytes == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
+                 "r"(valid ? 16 : 0)
+                 : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src),
+                 "r"(valid ? 8 : 0)
+                 : "memory");
+}
+
+// A lane's share of a step: K chunks of 16 bytes (kKC), V chunks of HD / 8 bytes.
+template <int HD>
+struct RowsL {
+  static constexpr int kKC = 2 * HD / 64;         // K chunks: two keys x HD / 64
+  static constexpr int kVB = HD / 8;              // bytes of a V chunk (four keys)
+  static constexpr uint32_t kKBytes = kKC * 512;
+  static constexpr uint32_t kStepBytes = kKBytes + 4 * 32 * kVB;
+  static constexpr uint32_t kWarpBytes = kRing * kStepBytes;
+  static constexpr int kOPad = HD + 4;            // floats of a row in the warps' exchange
+  static constexpr uint32_t kQOff = kVWarps * kWarpBytes;
+  template <int PARTS>
+  static constexpr uint32_t total() {
+    return kQOff + PARTS * kRT * HD * 2;
+  }
+  static_assert(kVWarps * kRT * kOPad * 4 <= kVWarps * kWarpBytes, "the exchange fits the ring");
+};
+
+
+__device__ __forceinline__ void load_query8(const float* p, float (&f)[8]) {
+  const float4 x = __ldg(reinterpret_cast<const float4*>(p));
+  const float4 y = __ldg(reinterpret_cast<const float4*>(p) + 1);
+  f[0] = x.x, f[1] = x.y, f[2] = x.z, f[3] = x.w;
+  f[4] = y.x, f[5] = y.y, f[6] = y.z, f[7] = y.w;
+}
+__device__ __forceinline__ void load_query8(const __nv_bfloat16* p, float (&f)[8]) {
+  Elem<__nv_bfloat16>::unpack(__ldg(reinterpret_cast<const uint4*>(p)), f);
+}
+__device__ __forceinline__ void store_out8(float* p, const float (&f)[8]) {
+  *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+  *(reinterpret_cast<float4*>(p) + 1) = make_float4(f[4], f[5], f[6], f[7]);
+}
+__device__ __forceinline__ void store_out8(__nv_bfloat16* p, const float (&f)[8]) {
+  uint32_t u[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+    u[j] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+}
+// 2^(m - max), the weight of a part whose maximum is m; 0 for a part without keys.
+__device__ __forceinline__ float part_weight(float m, float mx) {
+  return exp2f(m - (mx == -INFINITY ? 0.f : mx));
+}
+
+}  // namespace
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
+  using L = RowsL<HD>;
+  constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
+  constexpr int NT = HD / 8;   // 8-column tiles of the output
+  constexpr int KS = HD / 16;  // 16-column steps of a score
+  extern __shared__ __align__(1024) unsigned char smem[];
+  __shared__ int s_plan[kVWarps + 2];
+  __shared__ float s_qs[kRT];  // scores = dot * s_qs * key scale
+  __shared__ float s_m[kVWarps][kRT], s_l[kVWarps][kRT], s_ref[kVWarps];
+  __shared__ int s_nan;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int t = lane & 3, n8 = lane >> 2;
+  unsigned char* const wring = smem + warp * L::kWarpBytes;
+  unsigned char* const Qs = smem + L::kQOff;
+  float* const Ox = reinterpret_cast<float*>(smem);
+
+  const Kv8Cursor cur = kv8_plan<kRT, kVThreads>(a, s_plan);
+  pdl_launch_dependents();
+  if (tid == 0) a.desc[blockIdx.x].valid = 0;
+  int w = cur.w0, e = cur.e, off = cur.off;
+  while (w < cur.w1) {
+    const Kv8Item it = kv8_entry<kRT>(a, e);
+    if (off >= it.units * a.Hkv) {
+      off = 0;
+      ++e;
+      continue;
+    }
+    const int g = off / it.units, u0 = off - g * it.units;
+    const int nu = min(it.units - u0, cur.w1 - w);
+    w += nu;
+    off += nu;
+
+    // ---- queries of the tile, in the order of the matrix fragments
+    if (tid == 0) s_nan = 0;
+    {
+      constexpr int kLanes = HD / 8;  // lanes of a row
+      const int row = tid / kLanes, ch = tid % kLanes;
+      float f[8], amax = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = 0.f;
+      if (row < it.nr) {
+        const int r = it.r0 + row, m = r / a.G, h = g * a.G + r - m * a.G;
+        load_query8(static_cast<const T*>(a.q) + ((int64_t)it.b * a.M + m) * a.q_stride +
+                        (int64_t)h * HD + ch * 8,
+                    f);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(f[j]));
+#pragma unroll
+      for (int x = kLanes / 2; x > 0; x >>= 1)
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, x));
+      // the row's largest magnitude to [2^13, 2^14)
+      const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127 - 13, -100), 115);
+      const float inv = pow2i(-ex);
+      if (row < kRT) {
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          const float x = f[j] * inv, y = f[j + 1] * inv;
+          const uint32_t hi = half2_bits(x, y);
+          const int c = ch * 8 + j;  // lane c / 16 % 4 of the row, its step c / 64 * 4 + c / 4 % 4
+          unsigned char* p = Qs + (((c / 64 * 4 + c / 4 % 4) * 32 + (row & 7) * 4 + c / 16 % 4) * 4 +
+                                   (c % 4) + (row >> 3)) *
+                                      4;
+          *reinterpret_cast<uint32_t*>(p) = hi;
+          if constexpr (PARTS == 2) {
+            const float2 v = half2_floats(hi);
+            *reinterpret_cast<uint32_t*>(p + kRT * HD * 2) = half2_bits(x - v.x, y - v.y);
+          }
+        }
+        if (ch == 0) s_qs[row] = pow2i(ex) * a.scale;
+      }
+    }
+    __syncthreads();
+
+    // ---- keys of the segment, by 16-key steps
+    const int seg0 = (it.blk0 + u0) * kKv8Block;
+    const int kb = max(it.lo & ~(kStep - 1), seg0);
+    const int ke = min(it.hi + 1, seg0 + nu * kKv8Block);
+    const int nsteps = ke > kb ? (ke - kb + kStep - 1) / kStep : 0;
+    const size_t slab = (size_t)it.b * a.Hkv + g;
+    const uint8_t* kp = a.k + slab * a.max_seq * HD;
+    const uint8_t* vp = a.v + slab * a.max_seq * HD;
+    const float* ksp = a.ks + slab * (a.max_seq / kKv8Block);
+    const float* vsp = a.vs + slab * (a.max_seq / kKv8Block);
+    // every row sees keys full_lo .. full_hi
+    const int full_lo = kv8_row_lo(it, it.hi, a.window);
+    const int full_hi = kv8_row_pos(it, it.r0, a.G);
+    int plo[2], phi[2];
+    float qs[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = n8 + 8 * i;
+      phi[i] = row < it.nr ? kv8_row_pos(it, it.r0 + row, a.G) : -1;  // no row here: sees none
+      plo[i] = row < it.nr ? kv8_row_lo(it, phi[i], a.window) : 0;
+      qs[i] = s_qs[row];
+    }
+    uint32_t qf[PARTS == 1 ? KS : 1][4];
+    if constexpr (PARTS == 1)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const uint4 u = *reinterpret_cast<const uint4*>(Qs + (k * 32 + lane) * 16);
+        qf[k][0] = u.x, qf[k][1] = u.y, qf[k][2] = u.z, qf[k][3] = u.w;
+      }
+
+    auto issue = [&](int s) {  // this lane's codes of step s
+      if (s < nsteps) {
+        const int k0 = kb + s * kStep;
+        const uint32_t dst = smem_u32(wring) + (uint32_t)((s / kVWarps) % kRing) * L::kStepBytes;
+#pragma unroll
+        for (int c = 0; c < L::kKC; ++c) {
+          const int key = k0 + 8 * (c / (HD / 64)) + n8;
+          const bool in = key >= it.lo && key <= it.hi;
+          cp_async(dst + c * 512 + lane * 16,
+                   kp + (size_t)(in ? key : it.hi) * HD + (c % (HD / 64)) * 64 + t * 16, 16, in);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int key = k0 + 2 * t + (c & 1) + 8 * (c >> 1);
+          const bool in = key >= it.lo && key <= it.hi;
+          cp_async(dst + L::kKBytes + (c * 32 + lane) * L::kVB,
+                   vp + (size_t)(in ? key : it.hi) * HD + n8 * L::kVB, L::kVB, in);
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+
+    float o[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[j][i] = 0.f;
+    // running maximum and sum of the lane's rows; the output stands in units
+    // of ref, the largest value scale so far
+    float mx[2] = {-INFINITY, -INFINITY}, ls[2] = {0.f, 0.f}, ref = pow2i(-126);
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i) issue(warp + i * kVWarps);
+    float nks = 0.f, nvs = 0.f;
+    if (warp < nsteps) {
+      nks = __ldg(ksp + (kb + warp * kStep) / kKv8Block);
+      nvs = __ldg(vsp + (kb + warp * kStep) / kKv8Block);
+    }
+    for (int s = warp; s < nsteps; s += kVWarps) {
+      issue(s + (kRing - 1) * kVWarps);
+      const float ks = nks, vs = nvs;
+      if (s + kVWarps < nsteps) {
+        nks = __ldg(ksp + (kb + (s + kVWarps) * kStep) / kKv8Block);
+        nvs = __ldg(vsp + (kb + (s + kVWarps) * kStep) / kKv8Block);
+      }
+      asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+      const int k0 = kb + s * kStep;
+      const unsigned char* sp = wring + (uint32_t)((s / kVWarps) % kRing) * L::kStepBytes;
+
+      // scores: 2 tiles of 8 keys, even and odd 16-column steps summed apart
+      float sc[2][2][4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) sc[i][n][x] = 0.f;
+#pragma unroll
+      for (int hf = 0; hf < HD / 64; ++hf) {
+        uint4 kw[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+          kw[n] = *reinterpret_cast<const uint4*>(sp + (n * (HD / 64) + hf) * 512 + lane * 16);
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const int k = hf * 4 + q4;
+          uint32_t kf[2][2];
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const uint32_t x = q4 == 0 ? kw[n].x : q4 == 1 ? kw[n].y : q4 == 2 ? kw[n].z : kw[n].w;
+            kf[n][0] = e4m3_to_half2(x);
+            kf[n][1] = e4m3_to_half2(x >> 16);
+          }
+          if constexpr (PARTS == 1) {
+            mma_f16(sc[q4 & 1][0], qf[k], kf[0][0], kf[0][1]);
+            mma_f16(sc[q4 & 1][1], qf[k], kf[1][0], kf[1][1]);
+          } else {
+#pragma unroll
+            for (int p = PARTS - 1; p >= 0; --p) {
+              const uint4 u =
+                  *reinterpret_cast<const uint4*>(Qs + p * kRT * HD * 2 + (k * 32 + lane) * 16);
+              const uint32_t qa[4] = {u.x, u.y, u.z, u.w};
+              mma_f16(sc[q4 & 1][0], qa, kf[0][0], kf[0][1]);
+              mma_f16(sc[q4 & 1][1], qa, kf[1][0], kf[1][1]);
+            }
+          }
+        }
+      }
+      const bool full = k0 >= full_lo && k0 + kStep - 1 <= full_hi;
+      float z[2][4], nm[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          z[n][x] = (sc[0][n][x] + sc[1][n][x]) * (qs[x >> 1] * ks);
+          if (!full) {
+            const int key = k0 + 8 * n + 2 * t + (x & 1);
+            if (key < plo[x >> 1] || key > phi[x >> 1]) z[n][x] = -INFINITY;
+          }
+          nm[x >> 1] = fmaxf(nm[x >> 1], z[n][x]);
+        }
+      float f[2];
+      bool moved = vs > ref;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        nm[i] = fmaxf(nm[i], __shfl_xor_sync(0xffffffffu, nm[i], 1));
+        nm[i] = fmaxf(nm[i], __shfl_xor_sync(0xffffffffu, nm[i], 2));
+        nm[i] = fmaxf(nm[i], mx[i]);
+        f[i] = nm[i] == mx[i] ? 1.f : exp2f(mx[i] - nm[i]);
+        moved |= nm[i] != mx[i];
+        mx[i] = nm[i];
+        ls[i] *= f[i];
+      }
+      if (__any_sync(0xffffffffu, moved)) {
+        const float down = vs > ref ? ref / vs : 1.f;
+        if (vs > ref) ref = vs;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[j][x] *= f[x >> 1] * down;
+      }
+      const float vrel = vs / ref;
+      uint32_t pf[PARTS][4];
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float top = mx[i] == -INFINITY ? 0.f : mx[i] - 15.f;
+          const float x = exp2f(z[n][2 * i] - top), y = exp2f(z[n][2 * i + 1] - top);
+          ls[i] += x + y;
+          pf[0][2 * n + i] = half2_bits(x * vrel, y * vrel);
+          if constexpr (PARTS == 2) {
+            const float2 v = half2_floats(pf[0][2 * n + i]);
+            pf[1][2 * n + i] = half2_bits(x * vrel - v.x, y * vrel - v.y);
+          }
+        }
+      // values: words of the lane's four keys
+      uint32_t vw[4][NT / 4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const unsigned char* p = sp + L::kKBytes + (c * 32 + lane) * L::kVB;
+        if constexpr (HD == 128) {
+          const uint4 u = *reinterpret_cast<const uint4*>(p);
+          vw[c][0] = u.x, vw[c][1] = u.y, vw[c][2] = u.z, vw[c][3] = u.w;
+        } else {
+          const uint2 u = *reinterpret_cast<const uint2*>(p);
+          vw[c][0] = u.x, vw[c][1] = u.y;
+        }
+      }
+      if (!full) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int j = 0; j < NT / 4; ++j) {
+            const uint32_t m = e4m3_nan_mask(vw[c][j]);
+            any |= m;
+            vw[c][j] &= ~((m >> 7) * 0xffu);
+          }
+        if (any) s_nan = 1;
+      }
+#pragma unroll
+      for (int j4 = 0; j4 < NT / 4; ++j4) {
+        // bytes (key, key + 1) of columns j4 * 4 .. + 3
+        const uint32_t a01 = __byte_perm(vw[0][j4], vw[1][j4], 0x5140);
+        const uint32_t a23 = __byte_perm(vw[0][j4], vw[1][j4], 0x7362);
+        const uint32_t b01 = __byte_perm(vw[2][j4], vw[3][j4], 0x5140);
+        const uint32_t b23 = __byte_perm(vw[2][j4], vw[3][j4], 0x7362);
+        const uint32_t lo[4] = {e4m3_to_half2(a01), e4m3_to_half2(a01 >> 16), e4m3_to_half2(a23),
+                                e4m3_to_half2(a23 >> 16)};
+        const uint32_t hi[4] = {e4m3_to_half2(b01), e4m3_to_half2(b01 >> 16), e4m3_to_half2(b23),
+                                e4m3_to_half2(b23 >> 16)};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p) mma_f16(o[j4 * 4 + j], pf[p], lo[j], hi[j]);
+        }
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+
+    // ---- the warps' parts together
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 1);
+      ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 2);
+      if (t == 0) {
+        s_m[warp][n8 + 8 * i] = mx[i];
+        s_l[warp][n8 + 8 * i] = ls[i];
+      }
+    }
+    if (lane == 0) s_ref[warp] = ref;
+    __syncthreads();  // nobody reads the ring any more
+    const int nw = min(nsteps, kVWarps);
+    if (warp < nw) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = n8 + 8 * (i >> 1);
+        if (row < it.nr) {
+          float* p = Ox + (size_t)(warp * kRT + row) * L::kOPad + (2 * t + (i & 1)) * NT;
+#pragma unroll
+          for (int j = 0; j < NT; j += 4)
+            *reinterpret_cast<float4*>(p + j) =
+                make_float4(o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]);
+        }
+      }
+    }
+    __syncthreads();
+    const bool whole = nu == it.units;
+    const int slot = 2 * blockIdx.x + (u0 == 0);
+    {
+      const int row = tid / NT, c8 = (tid % NT) * 8;
+      if (row < it.nr) {
+        const int r = it.r0 + row, m = r / a.G, h = g * a.G + r - m * a.G;
+        const int p = kv8_row_pos(it, r, a.G), lo = kv8_row_lo(it, p, a.window);
+        float gm = -INFINITY, Ls = 0.f;
+        for (int x = 0; x < nw; ++x) gm = fmaxf(gm, s_m[x][row]);
+        for (int x = 0; x < nw; ++x) Ls = fmaf(part_weight(s_m[x][row], gm), s_l[x][row], Ls);
+        float acc[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+        if (Ls != 0.f)
+          for (int x = 0; x < nw; ++x) {
+            const float wt = part_weight(s_m[x][row], gm) / Ls, rf = s_ref[x];
+            const float* ox = Ox + (size_t)(x * kRT + row) * L::kOPad + c8;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] = fmaf(ox[j] * wt, rf, acc[j]);
+          }
+        if (s_nan) {  // a NaN value belongs to the rows that see its key
+          for (int key = kb; key < ke; ++key) {
+            const int k0 = key & ~(kStep - 1);  // the key's step (kb is one's first key)
+            if (k0 >= full_lo && k0 + kStep - 1 <= full_hi) continue;  // nothing was zeroed there
+            if (key < lo || key > p) continue;
+            const uint2 u = *reinterpret_cast<const uint2*>(vp + (size_t)key * HD + c8);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const uint32_t code = ((j < 4 ? u.x : u.y) >> (8 * (j & 3))) & 0x7fu;
+              if (code == 0x7fu) acc[j] = __uint_as_float(0x7fffffffu);
+            }
+          }
+        }
+        if (whole) {
+          if (p < lo) {  // sees no key
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+          } else if (Ls == 0.f) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] = __uint_as_float(0x7fffffffu);
+          }
+          store_out8(static_cast<T*>(a.out) + ((int64_t)it.b * a.M + m) * a.out_stride +
+                         (int64_t)h * HD + c8,
+                     acc);
+        } else {
+          store_out8(a.part + ((size_t)slot * kRT + row) * HD + c8, acc);
+          if (c8 == 0) a.ml[(size_t)slot * kRT + row] = make_float2(gm, Ls);
+        }
+      }
+    }
+    if (!whole && u0 == 0 && tid == 0) {
+      // the unit behind the item's last one, counted from the line's start
+      const long long end = (long long)w - nu + it.units;
+      a.desc[blockIdx.x] = Kv8Desc{1,  it.b, it.rt, g, (int)((end * gridDim.x - 1) / cur.total),
+                                   cur.total};
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the parts of the items that several blocks shared: block i those of the
+// item that begins in block i's stretch.  Fixed order, first part to last.
+template <typename T, int HD, int RT>
+__global__ void __launch_bounds__(256) k_kv8_merge(const Kv8Attn a) {
+  constexpr int kL = HD / 8;           // lanes of a row
+  constexpr int kRows = 256 / kL;      // rows of a pass
+  __shared__ float s_w[kRows][kKv8MaxBlocks + 1];
+  __shared__ int s_slot[kKv8MaxBlocks + 1];
+  pdl_wait();
+  const int i = blockIdx.x, P = gridDim.x, tid = threadIdx.x;
+  const Kv8Desc d = a.desc[i];
+  if (!d.valid) return;
+  // its parts: one of each block i .. last, or, with fewer units than blocks, one
+  // of each unit's block
+  const int u0 = kv8_start(i, P, d.total);
+  const bool dense = d.total >= P;
+  const int n = dense ? d.last - i + 1 : kv8_start(d.last, P, d.total) - u0 + 1;
+  for (int x = tid; x < n; x += 256) {
+    const int j = dense ? i + x : (int)(((long long)(u0 + x + 1) * P - 1) / d.total);
+    s_slot[x] = 2 * j + (x == 0);
+  }
+  __syncthreads();
+  const Kv8Item it = kv8_entry<RT>(a, d.b * a.n_rt + d.rt);
+  const int lane = tid % kL, c8 = lane * 8;
+  for (int r0 = blockIdx.y * kRows; r0 < it.nr; r0 += gridDim.y * kRows) {
+    const int rl = tid / kL, row = min(r0 + rl, it.nr - 1);
+    float gm = -INFINITY;
+    for (int x = lane; x < n; x += kL) gm = fmaxf(gm, __ldcg(&a.ml[(size_t)s_slot[x] * RT + row]).x);
+#pragma unroll
+    for (int o = kL / 2; o > 0; o >>= 1) gm = fmaxf(gm, __shfl_xor_sync(0xffffffffu, gm, o));
+    float Ls = 0.f;
+    for (int x = lane; x < n; x += kL) {
+      const float2 v = __ldcg(&a.ml[(size_t)s_slot[x] * RT + row]);
+      const float wt = part_weight(v.x, gm) * v.y;
+      s_w[rl][x] = wt;
+      Ls += wt;
+    }
+#pragma unroll
+    for (int o = kL / 2; o > 0; o >>= 1) Ls += __shfl_xor_sync(0xffffffffu, Ls, o);
+    __syncwarp();
+    float acc[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+    const float inv = 1.f / Ls;
+#pragma unroll 4
+    for (int x = 0; x < n; ++x) {
+      const float4* p = reinterpret_cast<const float4*>(a.part + ((size_t)s_slot[x] * RT + row) * HD + c8);
+      const float4 u = __ldcg(p), v = __ldcg(p + 1);
+      const float wt = s_w[rl][x] * inv;
+      acc[0] = fmaf(wt, u.x, acc[0]);
+      acc[1] = fmaf(wt, u.y, acc[1]);
+      acc[2] = fmaf(wt, u.z, acc[2]);
+      acc[3] = fmaf(wt, u.w, acc[3]);
+      acc[4] = fmaf(wt, v.x, acc[4]);
+      acc[5] = fmaf(wt, v.y, acc[5]);
+      acc[6] = fmaf(wt, v.z, acc[6]);
+      acc[7] = fmaf(wt, v.w, acc[7]);
+    }
+    __syncwarp();
+    if (r0 + rl < it.nr) {
+      const int r = it.r0 + row, m = r / a.G, h = d.g * a.G + r - m * a.G;
+      const int p = kv8_row_pos(it, r, a.G);
+      if (p < kv8_row_lo(it, p, a.window)) {  // sees no key
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+      }
+      store_out8(static_cast<T*>(a.out) + ((int64_t)it.b * a.M + m) * a.out_stride +
+                     (int64_t)h * HD + c8,
+                 acc);
+    }
+  }
+}
+
+// ------------------------------------------------------------- host side
+
+namespace {
+
+struct Kv8Device {
+  bool ready = false;
+  int sms = 0;
+};
+std::mutex g_kv8_mu;
+Kv8Device g_kv8_dev[64];
+
+template <typename T, int HD>
+cudaError_t prep_rows() {
+  return cudaFuncSetAttribute(k_kv8_rows<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)RowsL<HD>::template total<sizeof(T) == 4 ? 2 : 1>());
+}
+
+// SMs of the current device; its kernels' limits of shared memory are set on
+// the first call there.
+cudaError_t kv8_device(int* sms) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(g_kv8_mu);
+  Kv8Device& d = g_kv8_dev[dev];
+  if (!d.ready) {
+    if ((e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess ||
+        (e = prep_rows<float, 64>()) != cudaSuccess || (e = prep_rows<float, 128>()) != cudaSuccess ||
+        (e = prep_rows<__nv_bfloat16, 64>()) != cudaSuccess ||
+        (e = prep_rows<__nv_bfloat16, 128>()) != cudaSuccess)
+      return e;
+    d.ready = true;
+  }
+  *sms = d.sms;
+  return cudaSuccess;
+}
+
+// Workspace of an attention call: descriptors, (max, sum) pairs, parts.
+struct Kv8Work {
+  size_t ml, part, total;
+};
+Kv8Work kv8_work(int blocks, int rt, int hd) {
+  Kv8Work w;
+  w.ml = ((size_t)blocks * sizeof(Kv8Desc) + 255) / 256 * 256;
+  w.part = w.ml + ((size_t)2 * blocks * rt * sizeof(float2) + 255) / 256 * 256;
+  w.total = w.part + (size_t)2 * blocks * rt * hd * sizeof(float);
+  return w;
+}
+
+template <typename T, int HD>
+cudaError_t rows_launch(const Kv8Attn& a, int P, cudaStream_t st) {
+  const size_t smem = RowsL<HD>::template total<sizeof(T) == 4 ? 2 : 1>();
+  k_kv8_rows<T, HD><<<P, kVThreads, smem, st>>>(a);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(P);
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = g_pdl_enabled ? 1 : 0;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_kv8_merge<T, HD, kRT>, a);
+}
+
+// What both attention entry points check; null: fine.
+const char* check_attention(const ssd_kv8_cache* c, int32_t dtype, int32_t n_heads, int32_t M) {
+  if (const char* why = check_kv8(c)) return why;
+  if (dtype != SSD_DTYPE_F32 && dtype != SSD_DTYPE_BF16) return "dtype must be fp32 or bf16";
+  if (n_heads < c->n_kv_heads || n_heads % c->n_kv_heads || n_heads > 65536)
+    return "n_heads must be a multiple of the cache's n_kv_heads";
+  if (M < 1) return "M must be at least 1";
+  return nullptr;
+}
+
+}  // namespace
+}  // namespace ssd
+
+extern "C" size_t ssd_kv8_attention_bytes(const ssd_kv8_cache* c, int32_t dtype, int32_t n_heads,
+                                          int32_t M) {
+  using namespace ssd;
+  if (const char* why = check_attention(c, dtype, n_heads, M)) {
+    fail_op(SSD_ERR_INVALID_ARG, why);
+    return 0;
+  }
+  return kv8_work(kKv8MaxBlocks, kRT, c->head_dim).total;
+}
+
+extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, int32_t dtype,
+                                        int32_t n_heads, int64_t q_stride, int32_t M,
+                                        const int32_t* pos, const int32_t* rows,
+                                        const int32_t* first, int32_t window, void* out,
+                                        int64_t out_stride, void* workspace,
+                                        size_t workspace_bytes, int32_t* err_dev, void* stream) {
+  using namespace ssd;
+  if (const char* why = check_attention(c, dtype, n_heads, M))
+    return fail_op(c && c->head_dim != 64 && c->head_dim != 128 ? SSD_ERR_UNSUPPORTED
+                                                                : SSD_ERR_INVALID_ARG, why);
+  const int elt = dtype == SSD_DTYPE_BF16 ? 2 : 4;
+  const int64_t len = (int64_t)n_heads * c->head_dim;
+  if (!q || !out || !pos || ((uintptr_t)q & 15u) || ((uintptr_t)out & 15u))
+    return fail_op(SSD_ERR_INVALID_ARG, "q, out or pos: NULL or unaligned pointer");
+  if (q_stride < len || out_stride < len || q_stride > (1ll << 40) || out_stride > (1ll << 40) ||
+      (q_stride * elt) % 16 || (out_stride * elt) % 16)
+    return fail_op(SSD_ERR_INVALID_ARG,
+                   "q_stride or out_stride: below a row's length, or not a multiple of 16 bytes");
+  if (window < 0) return fail_op(SSD_ERR_INVALID_ARG, "window must be 0 (none) or positive");
+  if (M > c->max_seq) return fail_op(SSD_ERR_CAPACITY, "more rows than the cache has positions");
+  const int G = n_heads / c->n_kv_heads;
+  const long long n_rt = ((long long)M * G + kRT - 1) / kRT;
+  const long long units = n_rt * c->n_seq * c->n_kv_heads * (c->max_seq / kKv8Block);
+  if (units > 0x7fffffffll)
+    return fail_op(SSD_ERR_CAPACITY, "n_seq x M x max_seq: more than 2^31 units of work");
+  const Kv8Work lay = kv8_work(kKv8MaxBlocks, kRT, c->head_dim);
+  if (!workspace || ((uintptr_t)workspace & 255u))
+    return fail_op(SSD_ERR_INVALID_ARG, "workspace must be non-NULL and 256-byte aligned");
+  if (workspace_bytes < lay.total) return fail_op(SSD_ERR_CAPACITY, "workspace too small");
+  int sms = 0;
+  cudaError_t e = kv8_device(&sms);
+  if (e != cudaSuccess) return fail_op_cuda("ssd_kv8_attention", e);
+  Kv8Attn a{};
+  a.k = static_cast<const uint8_t*>(c->k);
+  a.v = static_cast<const uint8_t*>(c->v);
+  a.ks = c->k_scale;
+  a.vs = c->v_scale;
+  a.q = q;
+  a.out = out;
+  a.pos = pos;
+  a.rows = rows;
+  a.first = first;
+  a.err = err_dev;
+  a.q_stride = q_stride;
+  a.out_stride = out_stride;
+  a.n_seq = c->n_seq;
+  a.Hkv = c->n_kv_heads;
+  a.G = G;
+  a.M = M;
+  a.max_seq = c->max_seq;
+  a.window = window;
+  a.n_rt = (int)n_rt;
+  a.entries = (int)n_rt * c->n_seq;
+  a.scale = (float)(1.4426950408889634 / sqrt((double)c->head_dim));
+  char* ws = static_cast<char*>(workspace);
+  a.desc = reinterpret_cast<Kv8Desc*>(ws);
+  a.ml = reinterpret_cast<float2*>(ws + lay.ml);
+  a.part = reinterpret_cast<float*>(ws + lay.part);
+  int P = sms < kKv8MaxBlocks ? sms : kKv8MaxBlocks;
+  if (units < P) P = (int)units;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool wide = c->head_dim == 128;
+  if (dtype == SSD_DTYPE_BF16)
+    e = wide ? rows_launch<__nv_bfloat16, 128>(a, P, st) : rows_launch<__nv_bfloat16, 64>(a, P, st);
+  else
+    e = wide ? rows_launch<float, 128>(a, P, st) : rows_launch<float, 64>(a, P, st);
+  return e == cudaSuccess ? SSD_OK : fail_op_cuda("ssd_kv8_attention", e);
+}

@@ -4,10 +4,13 @@
 GPU and fills them with the library's seeded synthetic-weight fixture (the
 same generator the CPU oracle reads).  `Engine` owns one ssd_ctx: workspace
 (KV cache, activations, control block) from PyTorch, work on a PyTorch stream.
+`KV8Cache` is a layer's KV cache held in 8 bits, with its append and attention;
+`token_logprobs` scores given tokens over rows of logits.
 """
 from __future__ import annotations
 
 import ctypes as C
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -238,3 +241,244 @@ def kernels_per_round(trace: dict, n_layers: int, kind: int, bf16: bool = True) 
         n += (trace["k"] - 1) * (1 + pass_launches(trace["lstar"], bf16) + 2)
     n += 1 + pass_launches(n_layers, bf16) + 1 + 1
     return n
+
+
+# ------------------------------------------- 8-bit KV cache, token scores
+
+_CODES = {torch.float32: S.SSD_DTYPE_F32, torch.bfloat16: S.SSD_DTYPE_BF16}
+
+
+def _dtype_code(t: torch.Tensor, what: str) -> int:
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what} must be float32 or bfloat16, not {t.dtype}")
+    return code
+
+
+def _on(t, device: torch.device, what: str) -> int:
+    """The device address of t, or 0 for None."""
+    if t is None:
+        return 0
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, not on {device}")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient: there is no backward pass")
+    return t.data_ptr()
+
+
+def _per_seq(t, n_seq: int, device: torch.device, what: str) -> int:
+    """The address of an int32 [n_seq] tensor, or 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n_seq or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 tensor of {n_seq} elements")
+    return _on(t, device, what)
+
+
+class _Stream:
+    """Makes `device` current and, with a stream, work and allocations its own; yields the
+    stream's address.  Without a stream it is the device's current one."""
+
+    __slots__ = ("device", "stream", "ctx")
+
+    def __init__(self, device: torch.device, stream):
+        self.device, self.stream, self.ctx = device, stream, None
+
+    def __enter__(self) -> int:
+        if self.device.type != "cuda":
+            raise ValueError(f"a CUDA device is needed, not {self.device}")
+        if self.stream is not None:
+            if self.stream.device != self.device:
+                raise ValueError(f"the stream is on {self.stream.device}, not on {self.device}")
+            self.ctx = torch.cuda.stream(self.stream)
+            self.ctx.__enter__()
+            return self.stream.cuda_stream
+        if torch.cuda.current_device() != self.device.index:
+            self.ctx = torch.cuda.device(self.device)
+            self.ctx.__enter__()
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+        return False
+
+
+class KV8Cache:
+    """The KV cache of one layer in 8 bits (ssd_kv8_cache, include/ssd_ops.h): e4m3 codes `k`, `v`
+    [n_seq, n_kv_heads, max_seq, head_dim], one scale per 64 positions and KV head in `k_scale`,
+    `v_scale` [n_seq, n_kv_heads, max_seq / 64].  `max_seq` is rounded up to a multiple of 64.
+
+    Calls enqueue on `stream`, or on the current stream of the cache's device, and do not
+    synchronise; the caller orders streams, and keeps tensors that another stream made alive
+    (`Tensor.record_stream`).  They can be captured into CUDA graphs after a first call outside
+    of a capture.  What only the device can see (positions outside the cache, bad row numbers)
+    leaves the sequence alone and sets a bit in `err`, which `check` reads."""
+
+    def __init__(self, n_kv_heads: int, head_dim: int, max_seq: int, n_seq: int = 1,
+                 device: str | torch.device = "cuda:0"):
+        device = torch.device(device)
+        if device.type == "cuda" and device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        if head_dim not in (64, 128):
+            raise ValueError(f"head_dim must be 64 or 128, not {head_dim}")
+        if n_kv_heads < 1 or max_seq < 1 or not 1 <= n_seq <= S.KV8_MAX_SEQS:
+            raise ValueError("n_kv_heads, max_seq and n_seq must be positive, "
+                             f"n_seq at most {S.KV8_MAX_SEQS}")
+        self.device, self.n_seq, self.n_kv_heads, self.head_dim = device, n_seq, n_kv_heads, head_dim
+        self.max_seq = (max_seq + S.KV8_BLOCK - 1) // S.KV8_BLOCK * S.KV8_BLOCK
+        shape = (n_seq, n_kv_heads, self.max_seq, head_dim)
+        scales = (n_seq, n_kv_heads, self.max_seq // S.KV8_BLOCK)
+        # zeros where nothing was appended, for whoever looks at the tensors
+        self.k = torch.zeros(shape, dtype=torch.float8_e4m3fn, device=device)
+        self.v = torch.zeros(shape, dtype=torch.float8_e4m3fn, device=device)
+        self.k_scale = torch.zeros(scales, dtype=torch.float32, device=device)
+        self.v_scale = torch.zeros(scales, dtype=torch.float32, device=device)
+        self.err = torch.zeros(1, dtype=torch.int32, device=device)
+        self._c = S.ssd_kv8_cache(n_seq, n_kv_heads, head_dim, self.max_seq, self.k.data_ptr(),
+                                  self.v.data_ptr(), self.k_scale.data_ptr(),
+                                  self.v_scale.data_ptr())
+        self._work = {}  # (dtype code, n_heads, M) -> workspace bytes
+
+    def _rows(self, x: torch.Tensor, heads: int, what: str) -> tuple[int, int]:
+        """(M, elements between rows) of x [n_seq, M, heads, head_dim]."""
+        if x.dim() != 4 or x.shape[0] != self.n_seq or x.shape[2] != heads or \
+                x.shape[3] != self.head_dim or x.shape[1] < 1:
+            raise ValueError(f"{what} must be [{self.n_seq}, M, {heads}, {self.head_dim}], "
+                             f"not {list(x.shape)}")
+        s0, s1, s2, s3 = x.stride()
+        M = x.shape[1]
+        row = s1 if M > 1 else (s0 if self.n_seq > 1 else heads * self.head_dim)
+        if s3 != 1 or (heads > 1 and s2 != self.head_dim) or \
+                (self.n_seq > 1 and s0 != M * row):
+            raise ValueError(f"{what}: a row's heads must lie one behind the other, and the rows "
+                             f"of all sequences at one distance; strides are {x.stride()}")
+        return M, row
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
+               rows: torch.Tensor | None = None, stream=None):
+        """Writes k[b, m], v[b, m] ([n_seq, M, n_kv_heads, head_dim]) for m < rows[b] (all M
+        without `rows`) to positions pos[b] + m.  Positions from pos[b] on count as free."""
+        code = _dtype_code(k, "k")
+        if v.dtype != k.dtype:
+            raise ValueError("k and v must have one type")
+        M, row = self._rows(k, self.n_kv_heads, "k")
+        if self._rows(v, self.n_kv_heads, "v") != (M, row):
+            raise ValueError("k and v must have the same rows and strides")
+        if pos is None:
+            raise ValueError("pos is missing")
+        kp, vp = _on(k, self.device, "k"), _on(v, self.device, "v")
+        pp = _per_seq(pos, self.n_seq, self.device, "pos")
+        rp = _per_seq(rows, self.n_seq, self.device, "rows")
+        with _Stream(self.device, stream) as st:
+            S.ssd_kv8_append(self._c, kp, vp, code, row, M, pp, rp, self.err.data_ptr(), st)
+
+    def attention(self, q: torch.Tensor, pos: torch.Tensor, rows: torch.Tensor | None = None,
+                  first: torch.Tensor | None = None, window: int = 0,
+                  out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+        """softmax(q k^T / sqrt(head_dim)) v for q [n_seq, M, n_heads, head_dim]: row m < rows[b]
+        of sequence b sits at position pos[b] + m, whose key has been appended, and sees the keys
+        up to its own from first[b] on, at most `window` of them (0: all).  A row that sees
+        none is zero.  Returns `out` (a new tensor without it, whose rows from rows[b] on are
+        zero; a given one keeps them)."""
+        code = _dtype_code(q, "q")
+        heads = q.shape[2] if q.dim() == 4 else 0
+        M, row = self._rows(q, heads, "q")
+        if heads < 1 or heads % self.n_kv_heads:
+            raise ValueError(f"q has {heads} heads: not a multiple of {self.n_kv_heads}")
+        if pos is None:
+            raise ValueError("pos is missing")
+        qp = _on(q, self.device, "q")
+        pp = _per_seq(pos, self.n_seq, self.device, "pos")
+        rp = _per_seq(rows, self.n_seq, self.device, "rows")
+        fp = _per_seq(first, self.n_seq, self.device, "first")
+        if out is not None:
+            if out.dtype != q.dtype:
+                raise ValueError("out must have q's type")
+            Mo, orow = self._rows(out, heads, "out")
+            if Mo != M:
+                raise ValueError("out must have q's rows")
+            _on(out, self.device, "out")
+        if not 0 <= window < 1 << 31:
+            raise ValueError(f"window must be 0 (none) or a positive int32, not {window}")
+        key = (code, heads, M)
+        nbytes = self._work.get(key)
+        if nbytes is None:
+            nbytes = S.ssd_kv8_attention_bytes(self._c, code, heads, M)
+            self._work[key] = nbytes
+        with _Stream(self.device, stream) as st:
+            if out is None:
+                out = torch.zeros((self.n_seq, M, heads, self.head_dim), dtype=q.dtype,
+                                  device=self.device)
+                orow = heads * self.head_dim
+            work = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            S.ssd_kv8_attention(self._c, qp, code, heads, row, M, pp, rp, fp, window,
+                                out.data_ptr(), orow, work.data_ptr(), nbytes,
+                                self.err.data_ptr(), st)
+        return out
+
+    def check(self):
+        """Waits for the device and raises SsdError if a call since the last check found bad
+        positions or row numbers there."""
+        bits = int(self.err.item())
+        if bits:
+            self.err.zero_()
+            raise S.SsdError(S.SSD_ERR_DEVICE_FLAG, "KV8Cache", f"device error bits {bits}")
+
+
+class TokenLogprobs(NamedTuple):
+    """Per row of logits: log-probabilities of the given tokens [rows, n] (None without tokens),
+    log-sum-exp and entropy [rows], ids and log-probabilities of the most probable tokens
+    [rows, top_n] (None for top_n 0), and the device word of error bits [1]."""
+    logprob: torch.Tensor | None
+    lse: torch.Tensor
+    entropy: torch.Tensor
+    top_id: torch.Tensor | None
+    top_logprob: torch.Tensor | None
+    err: torch.Tensor | None
+
+
+def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top_n: int = 0,
+                   temperature: float = 1.0, err: torch.Tensor | None = None,
+                   stream=None) -> TokenLogprobs:
+    """ssd_token_logprobs on logits [rows, vocab] (float32 or bfloat16, rows at any distance) and
+    tokens [rows, n] or [rows] (int32; -1: no token here, its result is 0).  Other ids outside the
+    vocabulary give NaN and set a bit in `err` (device int32 [1]) where one is given.  Enqueues on
+    `stream`, or on the current stream of the logits' device; does not synchronise."""
+    code = _dtype_code(logits, "logits")
+    if logits.dim() != 2 or logits.shape[0] < 1 or logits.shape[1] < 1:
+        raise ValueError(f"logits must be [rows, vocab], not {list(logits.shape)}")
+    n, vocab = logits.shape
+    if vocab > 1 and logits.stride(1) != 1:
+        raise ValueError("a row's logits must be consecutive")
+    if n > 1 and logits.stride(0) < vocab:
+        raise ValueError("rows of logits must not overlap")
+    if not 0 <= top_n <= S.MAX_TOP or top_n > vocab:
+        raise ValueError(f"top_n must be in 0..{S.MAX_TOP} and at most the vocabulary, not {top_n}")
+    dev = logits.device
+    zp = _on(logits, dev, "logits")
+    ntok, tp = 0, 0
+    if tokens is not None:
+        if tokens.dtype != torch.int32 or tokens.dim() not in (1, 2) or tokens.shape[0] != n or \
+                not tokens.is_contiguous():
+            raise ValueError(f"tokens must be a contiguous int32 tensor [{n}, n] or [{n}]")
+        ntok = 1 if tokens.dim() == 1 else tokens.shape[1]
+        tp = _on(tokens, dev, "tokens")
+    if err is not None and (err.dtype != torch.int32 or err.numel() < 1):
+        raise ValueError("err must be an int32 tensor")
+    ep = _on(err, dev, "err")
+    nbytes = S.ssd_token_logprobs_bytes(n, vocab, top_n)
+    with _Stream(dev, stream) as st:
+        lp = torch.empty(tokens.shape, dtype=torch.float32, device=dev) if tokens is not None else None
+        stats = torch.empty((2, n), dtype=torch.float32, device=dev)
+        ids = top = None
+        if top_n > 0:
+            ids = torch.empty((n, top_n), dtype=torch.int32, device=dev)
+            top = torch.empty((n, top_n), dtype=torch.float32, device=dev)
+        work = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=dev)
+        lse, entropy = stats.unbind()
+        S.ssd_token_logprobs(zp, code, n, vocab, logits.stride(0) if n > 1 else vocab,
+                             tp, ntok, temperature, top_n, lp.data_ptr() if ntok else 0,
+                             lse.data_ptr(), entropy.data_ptr(), ids.data_ptr() if top_n > 0 else 0,
+                             top.data_ptr() if top_n > 0 else 0, work.data_ptr(), nbytes, ep, st)
+    return TokenLogprobs(lp, lse, entropy, ids, top, err)

@@ -94,8 +94,21 @@ class ssd_exit_stats(C.Structure):
                     pmax=self.pmax, margin=self.margin)
 
 
+KV8_BLOCK = 64        # positions of the 8-bit cache that share a scale
+KV8_MAX_SEQS = 4096
+MAX_TOP = 32          # most probable tokens of ssd_token_logprobs
+DEV_ERR_TOKEN, DEV_ERR_CAPACITY, DEV_ERR_CONTROL = 1, 2, 4
+
+
+class ssd_kv8_cache(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("max_seq", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
 # Every exported entry point with its ctypes signature (restype, argtypes).
 _P, _I32, _U32, _U64, _SZ = C.c_void_p, C.c_int32, C.c_uint32, C.c_uint64, C.c_size_t
+_I64, _F32 = C.c_int64, C.c_float
 SIGNATURES = {
     "ssd_workspace_bytes": (_SZ, [C.POINTER(ssd_model_cfg)]),
     "ssd_init_model": (C.c_int, [C.POINTER(ssd_model_cfg), C.POINTER(ssd_weights), _P, _SZ, _P,
@@ -117,6 +130,13 @@ SIGNATURES = {
     "ssd_op_gemv": (C.c_int, [_P, _I32, _I32, _I32, _P, _P, _P]),
     "ssd_op_layer": (C.c_int, [_P, _I32, _I32, _I32, _I32, _P]),
     "ssd_gemv_noalloc": (C.c_int, [_P, _I32, _I32, _I32, _P, _I32, _P, _P, _P]),
+    "ssd_kv8_append": (C.c_int, [_P, _P, _P, _I32, _I64, _I32, _P, _P, _P, _P]),
+    "ssd_kv8_attention_bytes": (_SZ, [_P, _I32, _I32, _I32]),
+    "ssd_kv8_attention": (C.c_int, [_P, _P, _I32, _I32, _I64, _I32, _P, _P, _P, _I32, _P, _I64, _P,
+                                    _SZ, _P, _P]),
+    "ssd_token_logprobs_bytes": (_SZ, [_I32, _I32, _I32]),
+    "ssd_token_logprobs": (C.c_int, [_P, _I32, _I32, _I32, _I64, _P, _I32, _F32, _I32, _P, _P, _P,
+                                     _P, _P, _P, _SZ, _P, _P]),
     "ssd_synth_fill": (C.c_int, [_P, _I32, _U64, _U32, _U32, C.c_double, _P]),
     "ssd_read_probe": (C.c_int, [_P, _U64, _P, _P]),
 }
@@ -285,6 +305,47 @@ def ssd_gemv_noalloc(w_ptr: int, dtype: int, rows: int, cols: int, x_ptr: int, M
     err_ptr (device int32, optional) receives the kernel's error word."""
     _check(lib().ssd_gemv_noalloc(w_ptr, dtype, rows, cols, x_ptr, M, y_ptr, err_ptr or None,
                                   stream_ptr or None), "ssd_gemv_noalloc")
+
+
+def ssd_kv8_append(cache: ssd_kv8_cache, k_ptr: int, v_ptr: int, dtype: int, row_stride: int, M: int,
+                   pos_ptr: int, rows_ptr: int = 0, err_ptr: int = 0, stream_ptr: int = 0):
+    """Rows of K and V into the 8-bit cache (see ssd_ops.h)."""
+    _check(lib().ssd_kv8_append(C.addressof(cache), k_ptr, v_ptr, dtype, row_stride, M, pos_ptr,
+                                rows_ptr or None, err_ptr or None, stream_ptr or None),
+           "ssd_kv8_append")
+
+
+def ssd_kv8_attention_bytes(cache: ssd_kv8_cache, dtype: int, n_heads: int, M: int) -> int:
+    return lib().ssd_kv8_attention_bytes(C.addressof(cache), dtype, n_heads, M)
+
+
+def ssd_kv8_attention(cache: ssd_kv8_cache, q_ptr: int, dtype: int, n_heads: int, q_stride: int,
+                      M: int, pos_ptr: int, rows_ptr: int, first_ptr: int, window: int, out_ptr: int,
+                      out_stride: int, workspace_ptr: int, workspace_bytes: int, err_ptr: int = 0,
+                      stream_ptr: int = 0):
+    """Attention of new rows over the 8-bit cache (see ssd_ops.h)."""
+    _check(lib().ssd_kv8_attention(C.addressof(cache), q_ptr, dtype, n_heads, q_stride, M, pos_ptr,
+                                   rows_ptr or None, first_ptr or None, window, out_ptr, out_stride,
+                                   workspace_ptr, workspace_bytes, err_ptr or None,
+                                   stream_ptr or None), "ssd_kv8_attention")
+
+
+def ssd_token_logprobs_bytes(n_rows: int, vocab: int, top_n: int) -> int:
+    return lib().ssd_token_logprobs_bytes(n_rows, vocab, top_n)
+
+
+def ssd_token_logprobs(logits_ptr: int, dtype: int, n_rows: int, vocab: int, row_stride: int,
+                       tokens_ptr: int, n_tokens: int, temperature: float, top_n: int,
+                       logprob_ptr: int, lse_ptr: int, entropy_ptr: int, top_id_ptr: int,
+                       top_logprob_ptr: int, workspace_ptr: int, workspace_bytes: int,
+                       err_ptr: int = 0, stream_ptr: int = 0):
+    """Log-probabilities, entropy and most probable tokens of rows of logits (see ssd_ops.h)."""
+    _check(lib().ssd_token_logprobs(logits_ptr, dtype, n_rows, vocab, row_stride, tokens_ptr or None,
+                                    n_tokens, temperature, top_n, logprob_ptr or None,
+                                    lse_ptr or None, entropy_ptr or None, top_id_ptr or None,
+                                    top_logprob_ptr or None, workspace_ptr or None,
+                                    workspace_bytes, err_ptr or None, stream_ptr or None),
+           "ssd_token_logprobs")
 
 
 def ssd_synth_fill(dst_ptr: int, dtype: int, n: int, seed: int, tid: int, sigma: float,
