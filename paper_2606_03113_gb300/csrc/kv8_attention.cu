@@ -15,9 +15,10 @@
 //
 // The places of a lane in the matrix fragments can be any as long as both
 // operands agree, so they are chosen such that a lane's codes lie in 16
-// consecutive bytes of a key, which it copies itself to shared memory
-// (cp.async, kRing steps ahead) and reads back without a bank conflict or a
-// barrier.
+// consecutive bytes of a key.  Each warp copies its own steps to shared memory,
+// whole lines at a time (cp.async, kRing steps ahead; lane by lane, as the
+// fragments read them, the same copies reach 4.9 TB/s and not 6.3), and waits for no
+// other warp until the end of an item.
 //
 // A key that some row of the tile does not see can hold anything: its scores are
 // dropped by position, and a NaN code of such a value row is zeroed before the
@@ -25,9 +26,11 @@
 #include <math.h>
 
 #include <mutex>
+#include <type_traits>
 
 #include "kv8_plan.cuh"
 #include "mma.cuh"
+#include "tc.cuh"
 
 namespace ssd {
 
@@ -48,6 +51,12 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// 2^x, as close as the hardware's instruction (2 ulp; a result below 2^-126 is 0).
+__device__ __forceinline__ float ex2_approx(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 __device__ __forceinline__ uint32_t half2_bits(float x, float y) {
   const __half2 h = __floats2half2_rn(x, y);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -55,24 +64,13 @@ __device__ __forceinline__ uint32_t half2_bits(float x, float y) {
 __device__ __forceinline__ float2 half2_floats(uint32_t u) {
   return __half22float2(*reinterpret_cast<const __half2*>(&u));
 }
-__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, int bytes, bool valid) {
-  if (bytes == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
-                 "r"(valid ? 16 : 0)
-                 : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src),
-                 "r"(valid ? 8 : 0)
-                 : "memory");
-}
-
-// A lane's share of a step: K chunks of 16 bytes (kKC), V chunks of HD / 8 bytes.
+// The ring of a warp: steps of 16 keys, then their values, rows of HD bytes.
 template <int HD>
 struct RowsL {
-  static constexpr int kKC = 2 * HD / 64;         // K chunks: two keys x HD / 64
-  static constexpr int kVB = HD / 8;              // bytes of a V chunk (four keys)
-  static constexpr uint32_t kKBytes = kKC * 512;
-  static constexpr uint32_t kStepBytes = kKBytes + 4 * 32 * kVB;
+  static constexpr int kCpr = HD / 16;                  // 16-byte chunks of a row
+  static constexpr int kCopies = kStep * kCpr / 32;     // a lane's copies of a step's keys
+  static constexpr uint32_t kKBytes = kStep * HD;
+  static constexpr uint32_t kStepBytes = 2 * kKBytes;
   static constexpr uint32_t kWarpBytes = kRing * kStepBytes;
   static constexpr int kOPad = HD + 4;            // floats of a row in the warps' exchange
   static constexpr uint32_t kQOff = kVWarps * kWarpBytes;
@@ -80,9 +78,15 @@ struct RowsL {
   static constexpr uint32_t total() {
     return kQOff + PARTS * kRT * HD * 2;
   }
+  // Where chunk ch of key kk stands: its place in the row is moved by the key, so
+  // that eight lanes meet all banks, both as two keys x four chunks (scores) and
+  // as four keys of one parity x two chunks (values; two by two at HD 64).
+  __device__ static __forceinline__ uint32_t place(int kk, int ch) {
+    const int x = HD == 128 ? ((kk >> 1 & 3) << 1) ^ ((kk & 1) << 2) : kk >> 1 & 3;
+    return (uint32_t)(kk * HD + ((ch ^ x) << 4));
+  }
   static_assert(kVWarps * kRT * kOPad * 4 <= kVWarps * kWarpBytes, "the exchange fits the ring");
 };
-
 
 __device__ __forceinline__ void load_query8(const float* p, float (&f)[8]) {
   const float4 x = __ldg(reinterpret_cast<const float4*>(p));
@@ -130,21 +134,51 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
   unsigned char* const Qs = smem + L::kQOff;
   float* const Ox = reinterpret_cast<float*>(smem);
 
-  const Kv8Cursor cur = kv8_plan<kRT, kVThreads>(a, s_plan);
+  Kv8Cursor cur = kv8_plan<kRT, kKv8Block, kVThreads>(a, s_plan);
   pdl_launch_dependents();
-  if (tid == 0) a.desc[blockIdx.x].valid = 0;
-  int w = cur.w0, e = cur.e, off = cur.off;
-  while (w < cur.w1) {
-    const Kv8Item it = kv8_entry<kRT>(a, e);
-    if (off >= it.units * a.Hkv) {
-      off = 0;
-      ++e;
-      continue;
+  if (tid == 0) a.desc[blockIdx.x].nr = 0;
+  Kv8Seg sg;
+  while (kv8_next<kRT, kKv8Block>(a, cur, sg)) {
+    const Kv8Item& it = sg.it;
+    const int g = sg.g;
+
+    // ---- keys of the segment, by 16-key steps: on their way before the queries
+    const int seg0 = (it.unit0 + sg.u0) * kKv8Block;
+    const int kb = max(it.lo & ~(kStep - 1), seg0);
+    const int ke = min(it.hi + 1, seg0 + sg.nu * kKv8Block);
+    const int nsteps = ke > kb ? (ke - kb + kStep - 1) / kStep : 0;
+    const size_t slab = (size_t)it.b * a.Hkv + g;
+    const uint8_t* kp = a.k + slab * a.max_seq * HD;
+    const uint8_t* vp = a.v + slab * a.max_seq * HD;
+    const float* ksp = a.ks + slab * (a.max_seq / kKv8Block);
+    const float* vsp = a.vs + slab * (a.max_seq / kKv8Block);
+    // every row sees keys full_lo .. full_hi
+    const int full_lo = kv8_row_lo(it, it.hi, a.window);
+    const int full_hi = kv8_row_pos(it, it.r0, a.G);
+    auto issue = [&](int s) {  // the warp's codes of step s, whole lines at a time
+      if (s < nsteps) {
+        const int k0 = kb + s * kStep;
+        const uint32_t dst = smem_u32(wring) + (uint32_t)((s / kVWarps) % kRing) * L::kStepBytes;
+#pragma unroll
+        for (int i = 0; i < L::kCopies; ++i) {
+          const int kk = i * (32 / L::kCpr) + lane / L::kCpr, ch = lane % L::kCpr;
+          const bool in = k0 + kk >= it.lo && k0 + kk <= it.hi;
+          const size_t off = (size_t)(in ? k0 + kk : it.hi) * HD + ch * 16;
+          const uint32_t at = dst + L::place(kk, ch);
+          cp_async16(at, kp + off, in);
+          cp_async16(at + L::kKBytes, vp + off, in);
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i) issue(warp + i * kVWarps);
+    float nks = 0.f, nvs = 0.f;
+    if (warp < nsteps) {
+      nks = __ldg(ksp + (kb + warp * kStep) / kKv8Block);
+      nvs = __ldg(vsp + (kb + warp * kStep) / kKv8Block);
     }
-    const int g = off / it.units, u0 = off - g * it.units;
-    const int nu = min(it.units - u0, cur.w1 - w);
-    w += nu;
-    off += nu;
 
     // ---- queries of the tile, in the order of the matrix fragments
     if (tid == 0) s_nan = 0;
@@ -188,19 +222,7 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
     }
     __syncthreads();
 
-    // ---- keys of the segment, by 16-key steps
-    const int seg0 = (it.blk0 + u0) * kKv8Block;
-    const int kb = max(it.lo & ~(kStep - 1), seg0);
-    const int ke = min(it.hi + 1, seg0 + nu * kKv8Block);
-    const int nsteps = ke > kb ? (ke - kb + kStep - 1) / kStep : 0;
-    const size_t slab = (size_t)it.b * a.Hkv + g;
-    const uint8_t* kp = a.k + slab * a.max_seq * HD;
-    const uint8_t* vp = a.v + slab * a.max_seq * HD;
-    const float* ksp = a.ks + slab * (a.max_seq / kKv8Block);
-    const float* vsp = a.vs + slab * (a.max_seq / kKv8Block);
-    // every row sees keys full_lo .. full_hi
-    const int full_lo = kv8_row_lo(it, it.hi, a.window);
-    const int full_hi = kv8_row_pos(it, it.r0, a.G);
+
     int plo[2], phi[2];
     float qs[2];
 #pragma unroll
@@ -218,28 +240,6 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
         qf[k][0] = u.x, qf[k][1] = u.y, qf[k][2] = u.z, qf[k][3] = u.w;
       }
 
-    auto issue = [&](int s) {  // this lane's codes of step s
-      if (s < nsteps) {
-        const int k0 = kb + s * kStep;
-        const uint32_t dst = smem_u32(wring) + (uint32_t)((s / kVWarps) % kRing) * L::kStepBytes;
-#pragma unroll
-        for (int c = 0; c < L::kKC; ++c) {
-          const int key = k0 + 8 * (c / (HD / 64)) + n8;
-          const bool in = key >= it.lo && key <= it.hi;
-          cp_async(dst + c * 512 + lane * 16,
-                   kp + (size_t)(in ? key : it.hi) * HD + (c % (HD / 64)) * 64 + t * 16, 16, in);
-        }
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int key = k0 + 2 * t + (c & 1) + 8 * (c >> 1);
-          const bool in = key >= it.lo && key <= it.hi;
-          cp_async(dst + L::kKBytes + (c * 32 + lane) * L::kVB,
-                   vp + (size_t)(in ? key : it.hi) * HD + n8 * L::kVB, L::kVB, in);
-        }
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-
     float o[NT][4];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
@@ -248,14 +248,8 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
     // running maximum and sum of the lane's rows; the output stands in units
     // of ref, the largest value scale so far
     float mx[2] = {-INFINITY, -INFINITY}, ls[2] = {0.f, 0.f}, ref = pow2i(-126);
-#pragma unroll
-    for (int i = 0; i < kRing - 1; ++i) issue(warp + i * kVWarps);
-    float nks = 0.f, nvs = 0.f;
-    if (warp < nsteps) {
-      nks = __ldg(ksp + (kb + warp * kStep) / kKv8Block);
-      nvs = __ldg(vsp + (kb + warp * kStep) / kKv8Block);
-    }
     for (int s = warp; s < nsteps; s += kVWarps) {
+      __syncwarp();  // every lane has read the step whose place is filled now
       issue(s + (kRing - 1) * kVWarps);
       const float ks = nks, vs = nvs;
       if (s + kVWarps < nsteps) {
@@ -263,6 +257,7 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
         nvs = __ldg(vsp + (kb + (s + kVWarps) * kStep) / kKv8Block);
       }
       asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+      __syncwarp();
       const int k0 = kb + s * kStep;
       const unsigned char* sp = wring + (uint32_t)((s / kVWarps) % kRing) * L::kStepBytes;
 
@@ -279,7 +274,7 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
         uint4 kw[2];
 #pragma unroll
         for (int n = 0; n < 2; ++n)
-          kw[n] = *reinterpret_cast<const uint4*>(sp + (n * (HD / 64) + hf) * 512 + lane * 16);
+          kw[n] = *reinterpret_cast<const uint4*>(sp + L::place(8 * n + n8, hf * 4 + t));
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
           const int k = hf * 4 + q4;
@@ -357,7 +352,9 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
       uint32_t vw[4][NT / 4];
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const unsigned char* p = sp + L::kKBytes + (c * 32 + lane) * L::kVB;
+        const int kk = 2 * t + (c & 1) + 8 * (c >> 1);
+        const unsigned char* p = sp + L::kKBytes + (HD == 128 ? L::place(kk, n8)
+                                                              : L::place(kk, n8 >> 1) + 8 * (n8 & 1));
         if constexpr (HD == 128) {
           const uint4 u = *reinterpret_cast<const uint4*>(p);
           vw[c][0] = u.x, vw[c][1] = u.y, vw[c][2] = u.z, vw[c][3] = u.w;
@@ -425,8 +422,8 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
       }
     }
     __syncthreads();
-    const bool whole = nu == it.units;
-    const int slot = 2 * blockIdx.x + (u0 == 0);
+    const bool whole = sg.whole();
+    const int slot = 2 * blockIdx.x + (sg.u0 == 0);
     {
       const int row = tid / NT, c8 = (tid % NT) * 8;
       if (row < it.nr) {
@@ -475,86 +472,115 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
         }
       }
     }
-    if (!whole && u0 == 0 && tid == 0) {
-      // the unit behind the item's last one, counted from the line's start
-      const long long end = (long long)w - nu + it.units;
-      a.desc[blockIdx.x] = Kv8Desc{1,  it.b, it.rt, g, (int)((end * gridDim.x - 1) / cur.total),
-                                   cur.total};
-    }
+    if (!whole && sg.u0 == 0 && tid == 0) a.desc[blockIdx.x] = kv8_desc(cur, sg);
     __syncthreads();
   }
 }
 
-// Joins the parts of the items that several blocks shared: block i those of the
-// item that begins in block i's stretch.  Fixed order, first part to last.
+}  // namespace ssd
+
+#include "kv8_wide.cuh"
+
+namespace ssd {
+
+// Joins the parts of the items that several blocks shared: blocks (i, *) those of
+// the item that begins in block i's stretch, a warp per row, first part to last.
+// Bound by round trips to L2: a part's place depends on the item alone, so the
+// first parts are on their way while the weights are worked out.
+constexpr int kMWarps = 8;      // rows of a block at a time
+constexpr int kMRowBlocks = 8;  // blocks that share an item's rows, at most
+
 template <typename T, int HD, int RT>
-__global__ void __launch_bounds__(256) k_kv8_merge(const Kv8Attn a) {
-  constexpr int kL = HD / 8;           // lanes of a row
-  constexpr int kRows = 256 / kL;      // rows of a pass
-  __shared__ float s_w[kRows][kKv8MaxBlocks + 1];
+__global__ void __launch_bounds__(kMWarps * 32, RT == kRT ? 2 : 4) k_kv8_merge(const Kv8Attn a) {
+  constexpr int kC = HD / 32;                  // columns of a lane
+  constexpr int kBatch = RT == kRT ? 18 : 8;   // parts on their way
+  using Vec = typename std::conditional<HD == 128, float4, float2>::type;
+  __shared__ float2 s_ml[kMWarps][kKv8MaxBlocks + 1];
   __shared__ int s_slot[kKv8MaxBlocks + 1];
   pdl_wait();
-  const int i = blockIdx.x, P = gridDim.x, tid = threadIdx.x;
-  const Kv8Desc d = a.desc[i];
-  if (!d.valid) return;
+  const int i = blockIdx.x, P = gridDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int4 d0 = __ldcg(reinterpret_cast<const int4*>(a.desc + i));
+  const int4 d1 = __ldcg(reinterpret_cast<const int4*>(a.desc + i) + 1);
+  const int last = d1.x, total = d1.y;
   // its parts: one of each block i .. last, or, with fewer units than blocks, one
   // of each unit's block
-  const int u0 = kv8_start(i, P, d.total);
-  const bool dense = d.total >= P;
-  const int n = dense ? d.last - i + 1 : kv8_start(d.last, P, d.total) - u0 + 1;
-  for (int x = tid; x < n; x += 256) {
-    const int j = dense ? i + x : (int)(((long long)(u0 + x + 1) * P - 1) / d.total);
+  const int u0 = d0.x ? kv8_start(i, P, total) : 0;
+  const bool dense = total >= P;
+  const int n = !d0.x ? 0 : dense ? last - i + 1 : kv8_start(last, P, total) - u0 + 1;
+  if ((int)blockIdx.y * kMWarps >= d0.x) return;
+  for (int x = threadIdx.x; x < n; x += kMWarps * 32) {
+    const int j = dense ? i + x : ((u0 + x + 1) * P - 1) / total;
     s_slot[x] = 2 * j + (x == 0);
   }
   __syncthreads();
-  const Kv8Item it = kv8_entry<RT>(a, d.b * a.n_rt + d.rt);
-  const int lane = tid % kL, c8 = lane * 8;
-  for (int r0 = blockIdx.y * kRows; r0 < it.nr; r0 += gridDim.y * kRows) {
-    const int rl = tid / kL, row = min(r0 + rl, it.nr - 1);
-    float gm = -INFINITY;
-    for (int x = lane; x < n; x += kL) gm = fmaxf(gm, __ldcg(&a.ml[(size_t)s_slot[x] * RT + row]).x);
+  for (int row = blockIdx.y * kMWarps + warp; row < d0.x; row += gridDim.y * kMWarps) {
+    auto slot = [&](int x) -> size_t { return (size_t)s_slot[x] * RT + row; };
+    auto part = [&](int x) -> Vec {
+      return __ldcg(reinterpret_cast<const Vec*>(a.part + slot(x) * HD) + lane);
+    };
+    Vec pre[kBatch];
 #pragma unroll
-    for (int o = kL / 2; o > 0; o >>= 1) gm = fmaxf(gm, __shfl_xor_sync(0xffffffffu, gm, o));
-    float Ls = 0.f;
-    for (int x = lane; x < n; x += kL) {
-      const float2 v = __ldcg(&a.ml[(size_t)s_slot[x] * RT + row]);
+    for (int x = 0; x < kBatch; ++x)
+      if (x < n) pre[x] = part(x);
+    float gm = -INFINITY, Ls = 0.f;
+    for (int x = lane; x < n; x += 32) {
+      const float2 v = __ldcg(&a.ml[slot(x)]);
+      s_ml[warp][x] = v;
+      gm = fmaxf(gm, v.x);
+    }
+    gm = warp_max(gm);
+    for (int x = lane; x < n; x += 32) {
+      const float2 v = s_ml[warp][x];
       const float wt = part_weight(v.x, gm) * v.y;
-      s_w[rl][x] = wt;
+      s_ml[warp][x].y = wt;
       Ls += wt;
     }
-#pragma unroll
-    for (int o = kL / 2; o > 0; o >>= 1) Ls += __shfl_xor_sync(0xffffffffu, Ls, o);
+    Ls = warp_sum(Ls);
     __syncwarp();
-    float acc[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
     const float inv = 1.f / Ls;
-#pragma unroll 4
-    for (int x = 0; x < n; ++x) {
-      const float4* p = reinterpret_cast<const float4*>(a.part + ((size_t)s_slot[x] * RT + row) * HD + c8);
-      const float4 u = __ldcg(p), v = __ldcg(p + 1);
-      const float wt = s_w[rl][x] * inv;
-      acc[0] = fmaf(wt, u.x, acc[0]);
-      acc[1] = fmaf(wt, u.y, acc[1]);
-      acc[2] = fmaf(wt, u.z, acc[2]);
-      acc[3] = fmaf(wt, u.w, acc[3]);
-      acc[4] = fmaf(wt, v.x, acc[4]);
-      acc[5] = fmaf(wt, v.y, acc[5]);
-      acc[6] = fmaf(wt, v.z, acc[6]);
-      acc[7] = fmaf(wt, v.w, acc[7]);
-    }
-    __syncwarp();
-    if (r0 + rl < it.nr) {
-      const int r = it.r0 + row, m = r / a.G, h = d.g * a.G + r - m * a.G;
-      const int p = kv8_row_pos(it, r, a.G);
-      if (p < kv8_row_lo(it, p, a.window)) {  // sees no key
+    float acc[kC];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-      }
-      store_out8(static_cast<T*>(a.out) + ((int64_t)it.b * a.M + m) * a.out_stride +
-                     (int64_t)h * HD + c8,
-                 acc);
+    for (int j = 0; j < kC; ++j) acc[j] = 0.f;
+    for (int x0 = 0; x0 < n; x0 += kBatch) {
+      if (x0)
+#pragma unroll
+        for (int x = 0; x < kBatch; ++x)
+          if (x0 + x < n) pre[x] = part(x0 + x);
+#pragma unroll
+      for (int x = 0; x < kBatch; ++x)
+        if (x0 + x < n) {
+          const float wt = s_ml[warp][x0 + x].y * inv;
+          const float* f = reinterpret_cast<const float*>(&pre[x]);
+#pragma unroll
+          for (int j = 0; j < kC; ++j) acc[j] = fmaf(wt, f[j], acc[j]);
+        }
     }
+    const int r = d0.z + row, m = r / a.G, h = d0.w * a.G + r - m * a.G;
+    const int p = d1.z + m;
+    const int lo = a.window > 0 ? max(d1.w, p - a.window + 1) : d1.w;
+    if (p < lo)  // sees no key
+#pragma unroll
+      for (int j = 0; j < kC; ++j) acc[j] = 0.f;
+    T* out = static_cast<T*>(a.out) + ((int64_t)d0.y * a.M + m) * a.out_stride + (int64_t)h * HD +
+             lane * kC;
+    if constexpr (sizeof(T) == 4) {
+      Vec v;
+#pragma unroll
+      for (int j = 0; j < kC; ++j) reinterpret_cast<float*>(&v)[j] = acc[j];
+      *reinterpret_cast<Vec*>(out) = v;
+    } else {
+      uint32_t u[kC / 2];
+#pragma unroll
+      for (int j = 0; j < kC; j += 2) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(acc[j], acc[j + 1]);
+        u[j / 2] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+      if constexpr (HD == 128)
+        *reinterpret_cast<uint2*>(out) = make_uint2(u[0], u[1]);
+      else
+        *reinterpret_cast<uint32_t*>(out) = u[0];
+    }
+    __syncwarp();  // every lane has read the weights
   }
 }
 
@@ -588,7 +614,9 @@ cudaError_t kv8_device(int* sms) {
     if ((e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess ||
         (e = prep_rows<float, 64>()) != cudaSuccess || (e = prep_rows<float, 128>()) != cudaSuccess ||
         (e = prep_rows<__nv_bfloat16, 64>()) != cudaSuccess ||
-        (e = prep_rows<__nv_bfloat16, 128>()) != cudaSuccess)
+        (e = prep_rows<__nv_bfloat16, 128>()) != cudaSuccess ||
+        (e = cudaFuncSetAttribute(k_kv8_wide, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  (int)kWSmem)) != cudaSuccess)
       return e;
     d.ready = true;
   }
@@ -608,22 +636,41 @@ Kv8Work kv8_work(int blocks, int rt, int hd) {
   return w;
 }
 
-template <typename T, int HD>
-cudaError_t rows_launch(const Kv8Attn& a, int P, cudaStream_t st) {
-  const size_t smem = RowsL<HD>::template total<sizeof(T) == 4 ? 2 : 1>();
-  k_kv8_rows<T, HD><<<P, kVThreads, smem, st>>>(a);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
+template <typename T, int HD, int RT>
+cudaError_t merge_launch(const Kv8Attn& a, int P, cudaStream_t st) {
+  const int rows = a.M * a.G < RT ? a.M * a.G : RT;  // of a tile, at most
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(P);
-  cfg.blockDim = dim3(256);
+  const int ny = (rows + kMWarps - 1) / kMWarps;
+  cfg.gridDim = dim3(P, ny < kMRowBlocks ? ny : kMRowBlocks);
+  cfg.blockDim = dim3(kMWarps * 32);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = g_pdl_enabled ? 1 : 0;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_kv8_merge<T, HD, kRT>, a);
+  return cudaLaunchKernelEx(&cfg, k_kv8_merge<T, HD, RT>, a);
+}
+
+template <typename T, int HD>
+cudaError_t rows_launch(const Kv8Attn& a, int P, cudaStream_t st) {
+  const size_t smem = RowsL<HD>::template total<sizeof(T) == 4 ? 2 : 1>();
+  k_kv8_rows<T, HD><<<P, kVThreads, smem, st>>>(a);
+  const cudaError_t e = cudaGetLastError();
+  return e != cudaSuccess ? e : merge_launch<T, HD, kRT>(a, P, st);
+}
+
+cudaError_t wide_launch(const Kv8Attn& a, int P, cudaStream_t st) {
+  k_kv8_wide<<<P, kWThreads, kWSmem, st>>>(a);
+  const cudaError_t e = cudaGetLastError();
+  return e != cudaSuccess ? e : merge_launch<__nv_bfloat16, kWHd, kWRows>(a, P, st);
+}
+
+// The kernel of a call: tiles of 128 rows on tcgen05 where a KV head has more
+// query rows than kWideFrom and the type is bf16, tiles of 16 on mma.sync otherwise.
+constexpr int kWideFrom = 16;
+bool kv8_is_wide(int dtype, int hd, long long rows) {
+  return dtype == SSD_DTYPE_BF16 && hd == kWHd && rows > kWideFrom;
 }
 
 // What both attention entry points check; null: fine.
@@ -646,7 +693,8 @@ extern "C" size_t ssd_kv8_attention_bytes(const ssd_kv8_cache* c, int32_t dtype,
     fail_op(SSD_ERR_INVALID_ARG, why);
     return 0;
   }
-  return kv8_work(kKv8MaxBlocks, kRT, c->head_dim).total;
+  const bool wide = kv8_is_wide(dtype, c->head_dim, (long long)M * (n_heads / c->n_kv_heads));
+  return kv8_work(kKv8MaxBlocks, wide ? kWRows : kRT, c->head_dim).total;
 }
 
 extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, int32_t dtype,
@@ -670,11 +718,13 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   if (window < 0) return fail_op(SSD_ERR_INVALID_ARG, "window must be 0 (none) or positive");
   if (M > c->max_seq) return fail_op(SSD_ERR_CAPACITY, "more rows than the cache has positions");
   const int G = n_heads / c->n_kv_heads;
-  const long long n_rt = ((long long)M * G + kRT - 1) / kRT;
-  const long long units = n_rt * c->n_seq * c->n_kv_heads * (c->max_seq / kKv8Block);
+  const bool tc = kv8_is_wide(dtype, c->head_dim, (long long)M * G);
+  const int rt = tc ? kWRows : kRT, ku = tc ? kWKeys : kKv8Block;
+  const long long n_rt = ((long long)M * G + rt - 1) / rt;
+  const long long units = n_rt * c->n_seq * c->n_kv_heads * ((c->max_seq + ku - 1) / ku);
   if (units > 0x7fffffffll)
     return fail_op(SSD_ERR_CAPACITY, "n_seq x M x max_seq: more than 2^31 units of work");
-  const Kv8Work lay = kv8_work(kKv8MaxBlocks, kRT, c->head_dim);
+  const Kv8Work lay = kv8_work(kKv8MaxBlocks, rt, c->head_dim);
   if (!workspace || ((uintptr_t)workspace & 255u))
     return fail_op(SSD_ERR_INVALID_ARG, "workspace must be non-NULL and 256-byte aligned");
   if (workspace_bytes < lay.total) return fail_op(SSD_ERR_CAPACITY, "workspace too small");
@@ -707,11 +757,14 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   a.desc = reinterpret_cast<Kv8Desc*>(ws);
   a.ml = reinterpret_cast<float2*>(ws + lay.ml);
   a.part = reinterpret_cast<float*>(ws + lay.part);
-  int P = sms < kKv8MaxBlocks ? sms : kKv8MaxBlocks;
+  int P = tc ? 2 * sms : sms;
+  if (P > kKv8MaxBlocks) P = kKv8MaxBlocks;
   if (units < P) P = (int)units;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool wide = c->head_dim == 128;
-  if (dtype == SSD_DTYPE_BF16)
+  if (tc)
+    e = wide_launch(a, P, st);
+  else if (dtype == SSD_DTYPE_BF16)
     e = wide ? rows_launch<__nv_bfloat16, 128>(a, P, st) : rows_launch<__nv_bfloat16, 64>(a, P, st);
   else
     e = wide ? rows_launch<float, 128>(a, P, st) : rows_launch<float, 64>(a, P, st);

@@ -1,0 +1,598 @@
+// kv8_wide.cuh -- attention over the 8-bit cache for many query rows a KV head
+// (wide verifications, grouped queries, prompt chunks; bf16, head_dim 128), on
+// the 5th-generation tensor cores.  Included by kv8_attention.cu.
+//
+// A block serves tiles of 128 query rows (the plan's items) and walks their keys a
+// cache block (64) at a time; two blocks share an SM.  Its warps work side by side:
+//  - four convert: they read the codes a step ahead into registers and write them to
+//    shared memory as f16, exact, rows of 128 bytes with the 128-byte swizzle, two
+//    steps deep: keys as a K-major operand, values, whose columns lie one behind
+//    the other, as an MN-major one;
+//  - one thread issues S = Q K^T (tcgen05.mma, 128 x 64 x 128, fp32 in tensor memory, two
+//    buffers) for a step while the softmax of the step before is at work, another
+//    one O += P V, P read from tensor memory, as soon as a softmax is done;
+//  - four do the softmax, a thread per row: the row's 64 scores into registers, their
+//    maximum, p = 2^(s - ref + 7) as f16, which takes the place of S.  ref is the row's
+//    maximum as of the last time it grew by more than 8 (in powers of two), so O is
+//    rescaled in tensor memory only then, and p stays below 2^15.
+// Queries are scaled to f16 and value scales moved into p as in k_kv8_rows.
+//
+// Bound, per 128 keys and SM: 1280 cycles of tensor pipe (the queries' operand is
+// read from shared memory for 64 keys at a time), 1536 of shared memory (operands
+// and conversions), 512 of code conversions (one warp instruction a cycle), 512 of
+// exponentials.
+#pragma once
+
+namespace ssd {
+
+namespace {
+
+constexpr int kWRows = 128;   // query rows of a tile
+constexpr int kWKeys = kKv8Block;  // keys of a step: one scale
+constexpr int kWHd = 128;
+constexpr int kWThreads = 10 * 32;  // softmax: warps 0-3, conversion: 4-7, products: 8, 9
+constexpr uint32_t kWQHalf = kWRows * 128;       // bytes of 64 f16 columns of the queries
+constexpr uint32_t kWKHalf = kWKeys * 128;       // of a step's keys or values
+constexpr uint32_t kWKTile = 2 * kWKHalf;
+constexpr uint32_t kWSmem = 2 * kWQHalf + 4 * kWKTile + 1024;  // queries, keys and values; alignment
+constexpr uint32_t kWCols = 256;                 // tensor memory: S and P (2 x 64), O
+constexpr float kWBase = 7.f, kWGrow = 8.f;
+
+// Byte of 16-byte chunk ch (0..7, eight f16 each) of row r in 64 columns.
+__device__ __forceinline__ uint32_t w_place(int r, int ch) {
+  return (uint32_t)(r * 128 + ((ch ^ (r & 7)) << 4));
+}
+
+// Instruction descriptors: f16 operands, fp32 accumulator, M = 128, N = the keys of a
+// step or the columns of the output; bit 16: B is MN-major.
+constexpr uint32_t kWIdesc = (1u << 4) | ((uint32_t)(kWKeys >> 3) << 17) | ((128u >> 4) << 24);
+constexpr uint32_t kWIdescV = (1u << 4) | (1u << 16) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+
+// MN-major operand of 128-byte rows (64 columns) with the 128-byte swizzle: the
+// leading offset leads to the next 64 columns, the stride offset to the next 8 rows.
+__device__ __forceinline__ uint64_t w_desc_mn(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(kWKHalf >> 4) << 16;
+  d |= (uint64_t)(1024u >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+__device__ __forceinline__ void w_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+      : "memory");
+}
+// A from tensor memory.
+__device__ __forceinline__ void w_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
+                                         bool acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+      : "memory");
+}
+
+// Columns of the thread's lane, there on return.
+__device__ __forceinline__ void w_ld16(uint32_t t, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
+      "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15"
+      "}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
+        "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(t)
+      : "memory");
+}
+__device__ __forceinline__ void w_ld32(uint32_t t, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+      "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31"
+      "}, [%32];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
+        "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
+        "=r"(r[30]), "=r"(r[31])
+      : "r"(t)
+      : "memory");
+}
+__device__ __forceinline__ void w_ld64(uint32_t t, uint32_t (&r)[64]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+      "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+      "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+      "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63"
+      "}, [%64];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
+        "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
+        "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]),
+        "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]),
+        "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+        "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]),
+        "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]),
+        "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+      : "r"(t)
+      : "memory");
+}
+__device__ __forceinline__ void w_st16(uint32_t t, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(t),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void w_st32(uint32_t t, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(t),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+      "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+      "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+      "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void w_st_wait() {
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+// Writes of this thread to shared memory, for the tensor cores to read.
+__device__ __forceinline__ void w_smem_fence() {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+
+// Codes that are read once, a step ahead of their use (volatile: the load stays
+// where it is issued).
+__device__ __forceinline__ uint4 w_load16(const void* p) {
+  uint4 r;
+  asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+               : "l"(p));
+  return r;
+}
+
+// The larger of three.
+__device__ __forceinline__ float w_max3(float x, float y, float z) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+  return r;
+}
+// (x, y) * c + d and sums, two values an instruction.
+__device__ __forceinline__ uint64_t w_pack(float x, float y) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+__device__ __forceinline__ float2 w_unpack(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t w_fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t w_add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// Barriers of the two buffers: keys and values stored, scores there (and the keys'
+// place free), probabilities there, output added (the values' and their place
+// free); queries of the segment stored.
+struct WideBars {
+  uint64_t k_full[2], v_full[2], s_done[2], p_full[2], o_done[2], q_full;
+};
+
+// Keys of step i of a segment.
+__device__ __forceinline__ int w_key0(const Kv8Seg& s, int i) {
+  return (s.it.unit0 + s.u0 + i) * kWKeys;
+}
+
+// Waits for a barrier's phase, asleep for up to a millisecond at a time (a
+// poll without that hint comes back at once, and the polls of nine waiting warps take
+// the issue slots of those at work); false after a few seconds.
+__device__ __forceinline__ bool w_sleep(uint64_t* b, uint32_t parity) {
+  for (int i = 0; i < 4096; ++i) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(smem_u32(b)), "r"(parity), "r"(1000000u)
+        : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+// The phase that step n completes on its buffer's barrier; after a wait that gave
+// up, no thread of this role waits again: it runs through its steps, meets its
+// barriers and reports.
+__device__ __forceinline__ void w_wait(uint64_t (&b)[2], uint32_t n, bool& bad) {
+  if (!bad) bad = !w_sleep(&b[n & 1], (n >> 1) & 1);
+}
+
+}  // namespace
+
+__global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ int s_plan[kWThreads / 32 + 2];
+  __shared__ WideBars bar;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_nan, s_fail;
+  unsigned char* const smem =
+      reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  unsigned char* const Qs = smem;
+  unsigned char* const Ks = Qs + 2 * kWQHalf;   // [2 buffers]
+  unsigned char* const Vs = Ks + 2 * kWKTile;
+  const int tid = threadIdx.x, warp = tid >> 5;
+
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bar.k_full[i], 128);
+      mbar_init(&bar.v_full[i], 128);
+      mbar_init(&bar.p_full[i], 128);
+      mbar_init(&bar.s_done[i], 1);
+      mbar_init(&bar.o_done[i], 1);
+    }
+    mbar_init(&bar.q_full, 128);
+    mbar_init_fence();
+    s_nan = s_fail = 0;
+    a.desc[blockIdx.x].nr = 0;
+  }
+  if (warp == 8) tc_alloc(&s_tmem, kWCols);
+  tc_fence_before();
+  Kv8Cursor cur = kv8_plan<kWRows, kWKeys, kWThreads>(a, s_plan);  // (with block barriers)
+  tc_fence_after();
+  pdl_launch_dependents();
+  const uint32_t tm = s_tmem, tmO = tm + 2 * kWKeys;
+  Kv8Seg sg;
+  uint32_t n = 0;  // steps so far: the barriers' phases
+  bool bad = false;
+
+  // registers: 128 x 120 + 128 x 72 + 64 x 96 = 320 x 96, what the block was launched with
+  if (warp == 8) {
+    // ------------------------------------------------------------ scores
+    if ((tid & 31) == 0) {
+      const uint64_t dq = sdesc_k128(smem_u32(Qs)), dk = sdesc_k128(smem_u32(Ks));
+      for (uint32_t seg = 0; kv8_next<kWRows, kWKeys>(a, cur, sg); ++seg) {
+        if (!bad) bad = !w_sleep(&bar.q_full, seg & 1);
+        for (int i = 0; i < sg.nu; ++i, ++n) {
+          w_wait(bar.k_full, n, bad);
+          if (n >= 2) w_wait(bar.o_done, n - 2, bad);  // P of that step was read there
+          tc_fence_after();
+          const uint32_t buf = n & 1;
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            w_mma(tm + buf * kWKeys, dq + (((k >> 2) * kWQHalf + (k & 3) * 32) >> 4),
+                  dk + ((buf * kWKTile + (k >> 2) * kWKHalf + (k & 3) * 32) >> 4), kWIdesc, k > 0);
+          tc_commit(&bar.s_done[buf]);
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 9) {
+    // ------------------------------------------------------------ outputs
+    if ((tid & 31) == 0) {
+      const uint64_t dv = w_desc_mn(smem_u32(Vs));
+      while (kv8_next<kWRows, kWKeys>(a, cur, sg))
+        for (int i = 0; i < sg.nu; ++i, ++n) {
+          w_wait(bar.v_full, n, bad);
+          w_wait(bar.p_full, n, bad);
+          tc_fence_after();
+          const uint32_t buf = n & 1;
+#pragma unroll
+          for (int k = 0; k < kWKeys / 16; ++k)  // 16 keys: 8 words of P, two 8-row groups of V
+            w_mma_ts(tmO, tm + buf * kWKeys + 8 * k, dv + ((buf * kWKTile + k * 2048) >> 4),
+                     kWIdescV, i > 0 || k > 0);
+          tc_commit(&bar.o_done[buf]);
+        }
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    // ------------------------------------------------------------ codes to f16
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    const int ct = tid - 128;
+    uint4 kc[4], vc[4];
+    // rows ct / 8 + 16 j of a step, 16 codes each
+    auto load = [&](const Kv8Seg& s, int i, const uint8_t* base, uint4 (&c)[4]) {
+      const int key = w_key0(s, i) + ct / 8;
+      const uint8_t* p = base + (((size_t)s.it.b * a.Hkv + s.g) * a.max_seq + key) * kWHd + (ct % 8) * 16;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        c[j] = key + 16 * j >= s.it.lo && key + 16 * j <= s.it.hi ? w_load16(p + 16 * j * kWHd)
+                                                                  : make_uint4(0, 0, 0, 0);
+    };
+    // eight lanes hold a row, 128 bytes of each half; the upper four store their two
+    // chunks the other way round, so that all eight meet different banks
+    const bool up = ct & 4;
+    const uint32_t row0 = (ct & 4 ? kWKHalf : 0) + (ct / 8) * 128;
+    const uint32_t at0 = row0 + (((2 * (ct & 3) + up) ^ (ct / 8 & 7)) << 4);
+    const uint32_t at1 = row0 + (((2 * (ct & 3) + !up) ^ (ct / 8 & 7)) << 4);
+    auto store = [&](unsigned char* tile, const uint4 (&c)[4]) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t w0 = up ? c[j].z : c[j].x, w1 = up ? c[j].w : c[j].y;
+        const uint32_t w2 = up ? c[j].x : c[j].z, w3 = up ? c[j].y : c[j].w;
+        *reinterpret_cast<uint4*>(tile + at0 + j * 2048) =
+            make_uint4(e4m3_to_half2(w0), e4m3_to_half2(w0 >> 16), e4m3_to_half2(w1),
+                       e4m3_to_half2(w1 >> 16));
+        *reinterpret_cast<uint4*>(tile + at1 + j * 2048) =
+            make_uint4(e4m3_to_half2(w2), e4m3_to_half2(w2 >> 16), e4m3_to_half2(w3),
+                       e4m3_to_half2(w3 >> 16));
+      }
+      w_smem_fence();
+    };
+    Kv8Cursor ahead = cur;  // one segment ahead: its first codes are loaded early
+    Kv8Seg nx;
+    bool more = kv8_next<kWRows, kWKeys>(a, ahead, nx);
+    if (more) {
+      load(nx, 0, a.k, kc);
+      load(nx, 0, a.v, vc);
+    }
+    while (more) {
+      sg = nx;
+      more = kv8_next<kWRows, kWKeys>(a, ahead, nx);
+      const int full_lo = kv8_row_lo(sg.it, sg.it.hi, a.window);
+      const int full_hi = kv8_row_pos(sg.it, sg.it.r0, a.G);
+      for (int i = 0; i < sg.nu; ++i, ++n) {
+        const uint32_t buf = (n & 1) * kWKTile;
+        if (n >= 2) w_wait(bar.s_done, n - 2, bad);
+        store(Ks + buf, kc);
+        mbar_arrive(&bar.k_full[n & 1]);
+        if (i + 1 < sg.nu) load(sg, i + 1, a.k, kc);
+        else if (more) load(nx, 0, a.k, kc);
+        const int k0 = w_key0(sg, i);
+        if (k0 < full_lo || k0 + kWKeys - 1 > full_hi) {  // not every row sees every key
+          uint32_t any = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(&vc[j]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t m = e4m3_nan_mask(w[x]);
+              any |= m;
+              w[x] &= ~((m >> 7) * 0xffu);
+            }
+          }
+          if (any) s_nan = 1;  // (published by the arrival below)
+        }
+        if (n >= 2) w_wait(bar.o_done, n - 2, bad);
+        store(Vs + buf, vc);
+        mbar_arrive(&bar.v_full[n & 1]);
+        if (i + 1 < sg.nu) load(sg, i + 1, a.v, vc);
+        else if (more) load(nx, 0, a.v, vc);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
+    const int row = tid;
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    while (kv8_next<kWRows, kWKeys>(a, cur, sg)) {
+      const Kv8Item& it = sg.it;
+      const int g = sg.g;
+      // the thread's row of queries as f16 (a row past the last: the last one's, not
+      // used); the products of the segment before are done with theirs
+      const int rq = it.r0 + min(row, it.nr - 1), mq = rq / a.G, hq = g * a.G + rq - mq * a.G;
+      float qs;  // scores = products * qs * key scale
+      {
+        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) +
+                                 ((int64_t)it.b * a.M + mq) * a.q_stride + (int64_t)hq * kWHd;
+        uint4 u[16];
+#pragma unroll
+        for (int ch = 0; ch < 16; ++ch) u[ch] = __ldg(reinterpret_cast<const uint4*>(q) + ch);
+        __nv_bfloat162 am = __float2bfloat162_rn(0.f);
+#pragma unroll
+        for (int ch = 0; ch < 16; ++ch) {
+          const __nv_bfloat162* w = reinterpret_cast<const __nv_bfloat162*>(&u[ch]);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) am = __hmax2(am, __habs2(w[x]));
+        }
+        const float amax = fmaxf(__low2float(am), __high2float(am));
+        const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127 - 13, -100), 115);
+        const float inv = pow2i(-ex);
+        qs = pow2i(ex) * a.scale;
+#pragma unroll
+        for (int ch = 0; ch < 16; ++ch) {
+          float f[8];
+          Elem<__nv_bfloat16>::unpack(u[ch], f);
+          *reinterpret_cast<uint4*>(Qs + (ch >> 3) * kWQHalf + w_place(row, ch & 7)) =
+              make_uint4(half2_bits(f[0] * inv, f[1] * inv), half2_bits(f[2] * inv, f[3] * inv),
+                         half2_bits(f[4] * inv, f[5] * inv), half2_bits(f[6] * inv, f[7] * inv));
+        }
+      }
+      w_smem_fence();
+      tc_fence_before();
+      mbar_arrive(&bar.q_full);
+      const bool live = warp * 32 < it.nr;  // the warp has rows
+      const size_t slab = (size_t)it.b * a.Hkv + g;
+      const int b0 = it.unit0 + sg.u0;
+      const float* ksp = a.ks + slab * (a.max_seq / kKv8Block) + b0;
+      const float* vsp = a.vs + slab * (a.max_seq / kKv8Block) + b0;
+      const int full_lo = kv8_row_lo(it, it.hi, a.window);
+      const int full_hi = kv8_row_pos(it, it.r0, a.G);
+      const int phi = row < it.nr ? kv8_row_pos(it, it.r0 + row, a.G) : -1;
+      const int plo = row < it.nr ? kv8_row_lo(it, phi, a.window) : 0;
+      float ref = -INFINITY, ls = 0.f;   // of the row
+      float vref = pow2i(-126);          // the output's unit, as in k_kv8_rows
+      // (rows that see nothing have no block whose scale means something)
+      const bool any = it.lo <= it.hi;
+      float nks = any ? __ldg(ksp) : 0.f, nvs = any ? __ldg(vsp) : 0.f;
+      for (int i = 0; i < sg.nu; ++i, ++n) {
+        const float ks = nks, vs = nvs;
+        if (i + 1 < sg.nu) {
+          nks = __ldg(ksp + i + 1);
+          nvs = __ldg(vsp + i + 1);
+        }
+        w_wait(bar.s_done, n, bad);
+        __syncwarp();
+        tc_fence_after();
+        if (live) {
+          const int k0 = w_key0(sg, i);
+          const bool full = k0 >= full_lo && k0 + kWKeys - 1 <= full_hi;
+          const uint32_t at = tm + lanes + (n & 1) * kWKeys;
+          const float c = qs * ks;
+          uint32_t r[64];
+          w_ld64(at, r);
+          if (!full) {
+            const int lo = plo - k0, hi = phi - k0;
+#pragma unroll
+            for (int x = 0; x < 64; ++x)
+              if (x < lo || x > hi) r[x] = 0xff800000u;  // -inf
+          }
+          float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int x = 0; x < 64; x += 8)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              m[y] = w_max3(m[y], __uint_as_float(r[x + 2 * y]), __uint_as_float(r[x + 2 * y + 1]));
+          float mx = fmaxf(w_max3(m[0], m[1], m[2]), m[3]);
+          if (mx > -INFINITY) mx *= c;
+          const bool grow = mx > ref + kWGrow || (ref == -INFINITY && mx > ref);
+          if (__any_sync(0xffffffffu, grow) || vs > vref) {
+            float f = 1.f;
+            if (grow) {
+              f = ref == -INFINITY ? 0.f : exp2f(ref - mx);
+              ref = mx;
+              ls *= f;
+            }
+            if (vs > vref) {
+              f *= vref / vs;
+              vref = vs;
+            }
+            if (i > 0) {
+              w_wait(bar.o_done, n - 1, bad);
+              __syncwarp();
+              tc_fence_after();
+#pragma unroll 1
+              for (int q = 0; q < 8; ++q) {
+                uint32_t o[16];
+                w_ld16(tmO + lanes + 16 * q, o);
+#pragma unroll
+                for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+                w_st16(tmO + lanes + 16 * q, o);
+              }
+            }
+          }
+          const float top = ref == -INFINITY ? 0.f : ref - kWBase;
+          const float rel = vs / vref;
+          const uint64_t c2 = w_pack(c, c), t2 = w_pack(-top, -top);
+          uint64_t sum2 = 0;
+#pragma unroll
+          for (int x = 0; x < 64; x += 2) {
+            const float2 z =
+                w_unpack(w_fma2(w_pack(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), c2, t2));
+            float e0 = ex2_approx(z.x), e1 = ex2_approx(z.y);
+            sum2 = w_add2(sum2, w_pack(e0, e1));
+            r[x / 2] = half2_bits(e0 * rel, e1 * rel);
+          }
+          const float2 sum = w_unpack(sum2);
+          ls += sum.x + sum.y;
+          w_st32(at, r);
+          w_st_wait();
+        }
+        tc_fence_before();
+        mbar_arrive(&bar.p_full[n & 1]);
+      }
+      w_wait(bar.o_done, n - 1, bad);
+      __syncwarp();
+      tc_fence_after();
+      // ---- the rows' outputs, or the block's part of them
+      if (live) {
+        const bool whole = sg.whole(), nan = *(volatile int*)&s_nan;
+        const int slot = 2 * blockIdx.x + (sg.u0 == 0);
+        const bool in = row < it.nr, sees = plo <= phi;
+        const float unit = ls == 0.f ? 0.f : 1.f / ls;
+        // 64 columns at a time through the warp's part of the queries' place, which
+        // is free now, so that a row is stored in one piece
+        unsigned char* const xs = Qs + warp * 8192;
+        const int lane = tid & 31, c4 = lane & 15;
+#pragma unroll 1
+        for (int q = 0; q < 4; ++q) {
+          uint32_t o[32];
+          w_ld32(tmO + lanes + 32 * q, o);
+          float f[32];
+#pragma unroll
+          for (int x = 0; x < 32; ++x) f[x] = ls == 0.f ? 0.f : __uint_as_float(o[x]) * unit * vref;
+          if (nan && in) {
+            // a NaN value belongs to the rows that see its key (zeroed in steps that not
+            // every row sees whole)
+            const uint8_t* vp = a.v + slab * a.max_seq * kWHd + 32 * q;
+            const int kb = max(w_key0(sg, 0), plo), ke = min(w_key0(sg, sg.nu) - 1, phi);
+            for (int key = kb; key <= ke; ++key) {
+              const int s0 = key & ~(kWKeys - 1);
+              if (s0 >= full_lo && s0 + kWKeys - 1 <= full_hi) continue;
+#pragma unroll
+              for (int x = 0; x < 32; ++x)
+                if ((vp[(size_t)key * kWHd + x] & 0x7f) == 0x7f) f[x] = __uint_as_float(0x7fffffffu);
+            }
+          }
+          if (whole && (!sees || ls == 0.f)) {
+#pragma unroll
+            for (int x = 0; x < 32; ++x) f[x] = sees ? __uint_as_float(0x7fffffffu) : 0.f;
+          }
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+            *reinterpret_cast<float4*>(xs + lane * 256 + ((((q & 1) * 8 + x) ^ (lane & 15)) << 4)) =
+                make_float4(f[4 * x], f[4 * x + 1], f[4 * x + 2], f[4 * x + 3]);
+          if (!(q & 1)) continue;
+          __syncwarp();
+          const int rows = min(32, it.nr - warp * 32);
+          for (int y = lane >> 4; y < rows; y += 2) {
+            const float4 v = *reinterpret_cast<const float4*>(xs + y * 256 + ((c4 ^ (y & 15)) << 4));
+            const int col = (q >> 1) * 64 + c4 * 4;
+            if (whole) {
+              const int r = it.r0 + warp * 32 + y, m = r / a.G, h = g * a.G + r - m * a.G;
+              const __nv_bfloat162 b0 = __floats2bfloat162_rn(v.x, v.y);
+              const __nv_bfloat162 b1 = __floats2bfloat162_rn(v.z, v.w);
+              *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) +
+                                        ((int64_t)it.b * a.M + m) * a.out_stride +
+                                        (int64_t)h * kWHd + col) =
+                  make_uint2(*reinterpret_cast<const uint32_t*>(&b0),
+                             *reinterpret_cast<const uint32_t*>(&b1));
+            } else {
+              *reinterpret_cast<float4*>(
+                  a.part + ((size_t)slot * kWRows + warp * 32 + y) * kWHd + col) = v;
+            }
+          }
+          __syncwarp();
+        }
+        // (max, sum) as the merge weighs parts: p stands against 2^(ref - kWBase)
+        if (in && !whole) a.ml[(size_t)slot * kWRows + row] = make_float2(ref, ls);
+      }
+      named_sync(1, 128);  // the next segment's queries go where outputs were exchanged
+      if (row == 0 && !sg.whole() && sg.u0 == 0) a.desc[blockIdx.x] = kv8_desc(cur, sg);
+      tc_fence_before();  // the next segment's products overwrite O, behind its p_full
+    }
+  }
+  if (bad) s_fail = 1;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (tid == 0 && s_fail && a.err) atomicOr(a.err, (int)kErrTimeout);
+  if (warp == 8) tc_dealloc(tm, kWCols);
+}
+
+}  // namespace ssd

@@ -10,6 +10,7 @@ same generator the CPU oracle reads).  `Engine` owns one ssd_ctx: workspace
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import NamedTuple
 
 import numpy as np
@@ -275,33 +276,25 @@ def _per_seq(t, n_seq: int, device: torch.device, what: str) -> int:
     return _on(t, device, what)
 
 
-class _Stream:
-    """Makes `device` current and, with a stream, work and allocations its own; yields the
-    stream's address.  Without a stream it is the device's current one."""
+# The address of a device's current stream (its index given), without a Stream object.
+_current_stream = torch._C._cuda_getCurrentRawStream
 
-    __slots__ = ("device", "stream", "ctx")
 
-    def __init__(self, device: torch.device, stream):
-        self.device, self.stream, self.ctx = device, stream, None
+def _elsewhere(device: torch.device, stream):
+    """None where a call's work belongs on the current stream of the current device; else a
+    context that makes it so (`stream`'s, or `device`'s current one)."""
+    if device.type != "cuda":
+        raise ValueError(f"a CUDA device is needed, not {device}")
+    if stream is not None:
+        if stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, not on {device}")
+        return torch.cuda.stream(stream)
+    return None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
-    def __enter__(self) -> int:
-        if self.device.type != "cuda":
-            raise ValueError(f"a CUDA device is needed, not {self.device}")
-        if self.stream is not None:
-            if self.stream.device != self.device:
-                raise ValueError(f"the stream is on {self.stream.device}, not on {self.device}")
-            self.ctx = torch.cuda.stream(self.stream)
-            self.ctx.__enter__()
-            return self.stream.cuda_stream
-        if torch.cuda.current_device() != self.device.index:
-            self.ctx = torch.cuda.device(self.device)
-            self.ctx.__enter__()
-        return torch.cuda.current_stream().cuda_stream
 
-    def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
-        return False
+@functools.lru_cache(maxsize=256)
+def _logprobs_bytes(n: int, vocab: int, top_n: int) -> int:
+    return S.ssd_token_logprobs_bytes(n, vocab, top_n)
 
 
 class KV8Cache:
@@ -338,6 +331,7 @@ class KV8Cache:
         self._c = S.ssd_kv8_cache(n_seq, n_kv_heads, head_dim, self.max_seq, self.k.data_ptr(),
                                   self.v.data_ptr(), self.k_scale.data_ptr(),
                                   self.v_scale.data_ptr())
+        self._err = self.err.data_ptr()
         self._work = {}  # (dtype code, n_heads, M) -> workspace bytes
 
     def _rows(self, x: torch.Tensor, heads: int, what: str) -> tuple[int, int]:
@@ -370,8 +364,12 @@ class KV8Cache:
         kp, vp = _on(k, self.device, "k"), _on(v, self.device, "v")
         pp = _per_seq(pos, self.n_seq, self.device, "pos")
         rp = _per_seq(rows, self.n_seq, self.device, "rows")
-        with _Stream(self.device, stream) as st:
-            S.ssd_kv8_append(self._c, kp, vp, code, row, M, pp, rp, self.err.data_ptr(), st)
+        there = _elsewhere(self.device, stream)
+        if there is not None:
+            with there:
+                return self.append(k, v, pos, rows)
+        S.ssd_kv8_append(self._c, kp, vp, code, row, M, pp, rp, self._err,
+                         _current_stream(self.device.index))
 
     def attention(self, q: torch.Tensor, pos: torch.Tensor, rows: torch.Tensor | None = None,
                   first: torch.Tensor | None = None, window: int = 0,
@@ -406,15 +404,17 @@ class KV8Cache:
         if nbytes is None:
             nbytes = S.ssd_kv8_attention_bytes(self._c, code, heads, M)
             self._work[key] = nbytes
-        with _Stream(self.device, stream) as st:
-            if out is None:
-                out = torch.zeros((self.n_seq, M, heads, self.head_dim), dtype=q.dtype,
-                                  device=self.device)
-                orow = heads * self.head_dim
-            work = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-            S.ssd_kv8_attention(self._c, qp, code, heads, row, M, pp, rp, fp, window,
-                                out.data_ptr(), orow, work.data_ptr(), nbytes,
-                                self.err.data_ptr(), st)
+        there = _elsewhere(self.device, stream)
+        if there is not None:
+            with there:
+                return self.attention(q, pos, rows, first, window, out)
+        if out is None:
+            make = torch.empty if rows is None else torch.zeros
+            out = make((self.n_seq, M, heads, self.head_dim), dtype=q.dtype, device=self.device)
+            orow = heads * self.head_dim
+        work = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        S.ssd_kv8_attention(self._c, qp, code, heads, row, M, pp, rp, fp, window, out.data_ptr(), orow,
+                            work.data_ptr(), nbytes, self._err, _current_stream(self.device.index))
         return out
 
     def check(self):
@@ -467,18 +467,24 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top
     if err is not None and (err.dtype != torch.int32 or err.numel() < 1):
         raise ValueError("err must be an int32 tensor")
     ep = _on(err, dev, "err")
-    nbytes = S.ssd_token_logprobs_bytes(n, vocab, top_n)
-    with _Stream(dev, stream) as st:
-        lp = torch.empty(tokens.shape, dtype=torch.float32, device=dev) if tokens is not None else None
-        stats = torch.empty((2, n), dtype=torch.float32, device=dev)
-        ids = top = None
-        if top_n > 0:
-            ids = torch.empty((n, top_n), dtype=torch.int32, device=dev)
-            top = torch.empty((n, top_n), dtype=torch.float32, device=dev)
-        work = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=dev)
-        lse, entropy = stats.unbind()
-        S.ssd_token_logprobs(zp, code, n, vocab, logits.stride(0) if n > 1 else vocab,
-                             tp, ntok, temperature, top_n, lp.data_ptr() if ntok else 0,
-                             lse.data_ptr(), entropy.data_ptr(), ids.data_ptr() if top_n > 0 else 0,
-                             top.data_ptr() if top_n > 0 else 0, work.data_ptr(), nbytes, ep, st)
+    there = _elsewhere(dev, stream)
+    if there is not None:
+        with there:
+            return token_logprobs(logits, tokens, top_n, temperature, err)
+    lp = ids = top = None
+    lpp = ip = lp_top = 0
+    if tokens is not None:
+        lp = torch.empty(tokens.shape, dtype=torch.float32, device=dev)
+        lpp = lp.data_ptr()
+    lse = torch.empty(n, dtype=torch.float32, device=dev)
+    entropy = torch.empty(n, dtype=torch.float32, device=dev)
+    if top_n > 0:
+        ids = torch.empty((n, top_n), dtype=torch.int32, device=dev)
+        top = torch.empty((n, top_n), dtype=torch.float32, device=dev)
+        ip, lp_top = ids.data_ptr(), top.data_ptr()
+    nbytes = _logprobs_bytes(n, vocab, top_n)
+    work = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    S.ssd_token_logprobs(zp, code, n, vocab, logits.stride(0) if n > 1 else vocab, tp, ntok,
+                         temperature, top_n, lpp, lse.data_ptr(), entropy.data_ptr(), ip, lp_top,
+                         work.data_ptr(), nbytes, ep, _current_stream(dev.index))
     return TokenLogprobs(lp, lse, entropy, ids, top, err)
