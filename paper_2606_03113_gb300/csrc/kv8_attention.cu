@@ -38,8 +38,14 @@ namespace {
 
 constexpr int kRT = 16;       // query rows of a tile
 constexpr int kStep = 16;     // keys of a warp's step
-constexpr int kRing = 6;      // steps in flight per warp
-constexpr int kVWarps = 8;
+#ifndef KVW
+#define KVW 4
+#define KVR 5
+#define KVB 2
+#endif
+constexpr int kRing = KVR;      // steps in flight per warp
+constexpr int kVWarps = KVW;
+constexpr int kVBlocks = KVB;   // blocks of an SM
 constexpr int kVThreads = kVWarps * 32;
 constexpr int kKv8MaxBlocks = 320;
 
@@ -118,15 +124,16 @@ __device__ __forceinline__ float part_weight(float m, float mx) {
 }  // namespace
 
 template <typename T, int HD>
-__global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
+__global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn a) {
   using L = RowsL<HD>;
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
   constexpr int NT = HD / 8;   // 8-column tiles of the output
   constexpr int KS = HD / 16;  // 16-column steps of a score
   extern __shared__ __align__(1024) unsigned char smem[];
-  __shared__ int s_plan[kVWarps + 2];
+  __shared__ Kv8PlanSmem s_plan;
   __shared__ float s_qs[kRT];  // scores = dot * s_qs * key scale
   __shared__ float s_m[kVWarps][kRT], s_l[kVWarps][kRT], s_ref[kVWarps];
+  __shared__ float s_w[kVWarps][kRT], s_gm[kRT], s_sum[kRT];  // the warps' weights, the row's (max, sum)
   __shared__ int s_nan;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int t = lane & 3, n8 = lane >> 2;
@@ -142,7 +149,24 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
     const Kv8Item& it = sg.it;
     const int g = sg.g;
 
-    // ---- keys of the segment, by 16-key steps: on their way before the queries
+    // ---- queries of the tile: read before the keys, whose copies they would wait behind
+    constexpr int kLanes = HD / 8;  // lanes of a row
+    constexpr int kQPasses = (kRT * kLanes + kVThreads - 1) / kVThreads;
+    float fq[kQPasses][8];
+#pragma unroll
+    for (int x = 0; x < kQPasses; ++x) {
+      const int row = (x * kVThreads + tid) / kLanes, ch = tid % kLanes;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) fq[x][j] = 0.f;
+      if (row < it.nr) {
+        const int r = it.r0 + row, m = a.byG(r), h = g * a.G + r - m * a.G;
+        load_query8(static_cast<const T*>(a.q) + ((int64_t)it.b * a.M + m) * a.q_stride +
+                        (int64_t)h * HD + ch * 8,
+                    fq[x]);
+      }
+    }
+
+    // ---- keys of the segment, by 16-key steps
     const int seg0 = (it.unit0 + sg.u0) * kKv8Block;
     const int kb = max(it.lo & ~(kStep - 1), seg0);
     const int ke = min(it.hi + 1, seg0 + sg.nu * kKv8Block);
@@ -154,7 +178,7 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
     const float* vsp = a.vs + slab * (a.max_seq / kKv8Block);
     // every row sees keys full_lo .. full_hi
     const int full_lo = kv8_row_lo(it, it.hi, a.window);
-    const int full_hi = kv8_row_pos(it, it.r0, a.G);
+    const int full_hi = kv8_row_pos(a, it, it.r0);
     auto issue = [&](int s) {  // the warp's codes of step s, whole lines at a time
       if (s < nsteps) {
         const int k0 = kb + s * kStep;
@@ -180,33 +204,26 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
       nvs = __ldg(vsp + (kb + warp * kStep) / kKv8Block);
     }
 
-    // ---- queries of the tile, in the order of the matrix fragments
+    // the queries in the order of the matrix fragments
     if (tid == 0) s_nan = 0;
-    {
-      constexpr int kLanes = HD / 8;  // lanes of a row
-      const int row = tid / kLanes, ch = tid % kLanes;
-      float f[8], amax = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = 0.f;
-      if (row < it.nr) {
-        const int r = it.r0 + row, m = r / a.G, h = g * a.G + r - m * a.G;
-        load_query8(static_cast<const T*>(a.q) + ((int64_t)it.b * a.M + m) * a.q_stride +
-                        (int64_t)h * HD + ch * 8,
-                    f);
-      }
+    for (int x = 0; x < kQPasses; ++x) {
+      const int row = (x * kVThreads + tid) / kLanes, ch = tid % kLanes;
+      float (&f)[8] = fq[x];
+      float amax = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(f[j]));
 #pragma unroll
-      for (int x = kLanes / 2; x > 0; x >>= 1)
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, x));
+      for (int o = kLanes / 2; o > 0; o >>= 1)
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
       // the row's largest magnitude to [2^13, 2^14)
       const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127 - 13, -100), 115);
       const float inv = pow2i(-ex);
       if (row < kRT) {
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
-          const float x = f[j] * inv, y = f[j + 1] * inv;
-          const uint32_t hi = half2_bits(x, y);
+          const float u = f[j] * inv, w = f[j + 1] * inv;
+          const uint32_t hi = half2_bits(u, w);
           const int c = ch * 8 + j;  // lane c / 16 % 4 of the row, its step c / 64 * 4 + c / 4 % 4
           unsigned char* p = Qs + (((c / 64 * 4 + c / 4 % 4) * 32 + (row & 7) * 4 + c / 16 % 4) * 4 +
                                    (c % 4) + (row >> 3)) *
@@ -214,7 +231,7 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
           *reinterpret_cast<uint32_t*>(p) = hi;
           if constexpr (PARTS == 2) {
             const float2 v = half2_floats(hi);
-            *reinterpret_cast<uint32_t*>(p + kRT * HD * 2) = half2_bits(x - v.x, y - v.y);
+            *reinterpret_cast<uint32_t*>(p + kRT * HD * 2) = half2_bits(u - v.x, w - v.y);
           }
         }
         if (ch == 0) s_qs[row] = pow2i(ex) * a.scale;
@@ -228,7 +245,7 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int row = n8 + 8 * i;
-      phi[i] = row < it.nr ? kv8_row_pos(it, it.r0 + row, a.G) : -1;  // no row here: sees none
+      phi[i] = row < it.nr ? kv8_row_pos(a, it, it.r0 + row) : -1;  // no row here: sees none
       plo[i] = row < it.nr ? kv8_row_lo(it, phi[i], a.window) : 0;
       qs[i] = s_qs[row];
     }
@@ -408,6 +425,15 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
     if (lane == 0) s_ref[warp] = ref;
     __syncthreads();  // nobody reads the ring any more
     const int nw = min(nsteps, kVWarps);
+    if (tid < kRT) {
+      float gm = -INFINITY, sum = 0.f;
+      for (int x = 0; x < nw; ++x) gm = fmaxf(gm, s_m[x][tid]);
+      for (int x = 0; x < nw; ++x) sum = fmaf(part_weight(s_m[x][tid], gm), s_l[x][tid], sum);
+      for (int x = 0; x < nw; ++x)
+        s_w[x][tid] = sum != 0.f ? part_weight(s_m[x][tid], gm) / sum : 0.f;
+      s_gm[tid] = gm;
+      s_sum[tid] = sum;
+    }
     if (warp < nw) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -424,24 +450,30 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
     __syncthreads();
     const bool whole = sg.whole();
     const int slot = 2 * blockIdx.x + (sg.u0 == 0);
-    {
-      const int row = tid / NT, c8 = (tid % NT) * 8;
+#pragma unroll 1
+    for (int x0 = 0; x0 < kRT * NT; x0 += kVThreads) {
+      const int row = (x0 + tid) / NT, c8 = (tid % NT) * 8;
       if (row < it.nr) {
-        const int r = it.r0 + row, m = r / a.G, h = g * a.G + r - m * a.G;
-        const int p = kv8_row_pos(it, r, a.G), lo = kv8_row_lo(it, p, a.window);
-        float gm = -INFINITY, Ls = 0.f;
-        for (int x = 0; x < nw; ++x) gm = fmaxf(gm, s_m[x][row]);
-        for (int x = 0; x < nw; ++x) Ls = fmaf(part_weight(s_m[x][row], gm), s_l[x][row], Ls);
+        const int r = it.r0 + row, m = a.byG(r), h = g * a.G + r - m * a.G;
+        const int p = kv8_row_pos(a, it, r), lo = kv8_row_lo(it, p, a.window);
+        const float gm = s_gm[row], Ls = s_sum[row];
         float acc[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-        if (Ls != 0.f)
-          for (int x = 0; x < nw; ++x) {
-            const float wt = part_weight(s_m[x][row], gm) / Ls, rf = s_ref[x];
-            const float* ox = Ox + (size_t)(x * kRT + row) * L::kOPad + c8;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] = fmaf(ox[j] * wt, rf, acc[j]);
-          }
+        for (int x = 0; x < nw; ++x) {
+          const float wt = s_w[x][row], rf = s_ref[x];
+          const float4* ox = reinterpret_cast<const float4*>(Ox + (size_t)(x * kRT + row) * L::kOPad + c8);
+          const float4 u = ox[0], w = ox[1];
+          // (the weight before the unit: their product can be out of range)
+          acc[0] = fmaf(u.x * wt, rf, acc[0]);
+          acc[1] = fmaf(u.y * wt, rf, acc[1]);
+          acc[2] = fmaf(u.z * wt, rf, acc[2]);
+          acc[3] = fmaf(u.w * wt, rf, acc[3]);
+          acc[4] = fmaf(w.x * wt, rf, acc[4]);
+          acc[5] = fmaf(w.y * wt, rf, acc[5]);
+          acc[6] = fmaf(w.z * wt, rf, acc[6]);
+          acc[7] = fmaf(w.w * wt, rf, acc[7]);
+        }
         if (s_nan) {  // a NaN value belongs to the rows that see its key
           for (int key = kb; key < ke; ++key) {
             const int k0 = key & ~(kStep - 1);  // the key's step (kb is one's first key)
@@ -472,7 +504,7 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
         }
       }
     }
-    if (!whole && sg.u0 == 0 && tid == 0) a.desc[blockIdx.x] = kv8_desc(cur, sg);
+    if (!whole && sg.u0 == 0 && tid == 0) a.desc[blockIdx.x] = kv8_desc(a, cur, sg);
     __syncthreads();
   }
 }
@@ -484,36 +516,41 @@ __global__ void __launch_bounds__(kVThreads) k_kv8_rows(const Kv8Attn a) {
 namespace ssd {
 
 // Joins the parts of the items that several blocks shared: blocks (i, *) those of
-// the item that begins in block i's stretch, a warp per row, first part to last.
+// the item that begins in block i's stretch.  WPR warps share a row: warp w of them
+// takes parts w, w + WPR, ..; their sums are added in order.
 // Bound by round trips to L2: a part's place depends on the item alone, so the
-// first parts are on their way while the weights are worked out.
-constexpr int kMWarps = 8;      // rows of a block at a time
+// first parts are on their way while the weights are worked out.  Few rows have many
+// parts and get a block a row; many rows have few and get a warp.
+constexpr int kMWarps = 8;
 constexpr int kMRowBlocks = 8;  // blocks that share an item's rows, at most
 
-template <typename T, int HD, int RT>
-__global__ void __launch_bounds__(kMWarps * 32, RT == kRT ? 2 : 4) k_kv8_merge(const Kv8Attn a) {
-  constexpr int kC = HD / 32;                  // columns of a lane
-  constexpr int kBatch = RT == kRT ? 18 : 8;   // parts on their way
+template <typename T, int HD, int RT, int WPR>
+__global__ void __launch_bounds__(kMWarps * 32, 3) k_kv8_merge(const Kv8Attn a) {
+  constexpr int kC = HD / 32;  // columns of a lane
+  constexpr int kBatch = 6;    // parts of a warp on their way
+  constexpr int kRows = kMWarps / WPR;
   using Vec = typename std::conditional<HD == 128, float4, float2>::type;
-  __shared__ float2 s_ml[kMWarps][kKv8MaxBlocks + 1];
+  __shared__ float2 s_ml[kRows][kKv8MaxBlocks + 1];
   __shared__ int s_slot[kKv8MaxBlocks + 1];
+  __shared__ float s_red[kMWarps][HD];
+  __shared__ float s_gm[kMWarps], s_sum[kMWarps];
   pdl_wait();
-  const int i = blockIdx.x, P = gridDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int i = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int rl = warp / WPR, w = warp % WPR;
   const int4 d0 = __ldcg(reinterpret_cast<const int4*>(a.desc + i));
   const int4 d1 = __ldcg(reinterpret_cast<const int4*>(a.desc + i) + 1);
-  const int last = d1.x, total = d1.y;
+  if ((int)blockIdx.y * kRows >= d0.x) return;
   // its parts: one of each block i .. last, or, with fewer units than blocks, one
   // of each unit's block
-  const int u0 = d0.x ? kv8_start(i, P, total) : 0;
-  const bool dense = total >= P;
-  const int n = !d0.x ? 0 : dense ? last - i + 1 : kv8_start(last, P, total) - u0 + 1;
-  if ((int)blockIdx.y * kMWarps >= d0.x) return;
-  for (int x = threadIdx.x; x < n; x += kMWarps * 32) {
-    const int j = dense ? i + x : ((u0 + x + 1) * P - 1) / total;
-    s_slot[x] = 2 * j + (x == 0);
-  }
+  const Kv8Line line(a, d1.y);
+  const int last = d1.x, u0 = line.start(a, i);
+  const bool dense = line.q > 0;
+  const int n = dense ? last - i + 1 : line.start(a, last) - u0 + 1;
+  for (int x = threadIdx.x; x < n; x += kMWarps * 32)
+    s_slot[x] = 2 * (dense ? i + x : line.block(a, u0 + x)) + (x == 0);
   __syncthreads();
-  for (int row = blockIdx.y * kMWarps + warp; row < d0.x; row += gridDim.y * kMWarps) {
+  for (int row0 = blockIdx.y * kRows; row0 < d0.x; row0 += gridDim.y * kRows) {
+    const int row = min(row0 + rl, d0.x - 1);
     auto slot = [&](int x) -> size_t { return (size_t)s_slot[x] * RT + row; };
     auto part = [&](int x) -> Vec {
       return __ldcg(reinterpret_cast<const Vec*>(a.part + slot(x) * HD) + lane);
@@ -521,66 +558,95 @@ __global__ void __launch_bounds__(kMWarps * 32, RT == kRT ? 2 : 4) k_kv8_merge(c
     Vec pre[kBatch];
 #pragma unroll
     for (int x = 0; x < kBatch; ++x)
-      if (x < n) pre[x] = part(x);
+      if (w + x * WPR < n) pre[x] = part(w + x * WPR);
+    // the row's weights: its first warp's lanes, or all of its warps'
     float gm = -INFINITY, Ls = 0.f;
-    for (int x = lane; x < n; x += 32) {
+    for (int x = w * 32 + lane; x < n; x += WPR * 32) {
       const float2 v = __ldcg(&a.ml[slot(x)]);
-      s_ml[warp][x] = v;
+      s_ml[rl][x] = v;
       gm = fmaxf(gm, v.x);
     }
     gm = warp_max(gm);
-    for (int x = lane; x < n; x += 32) {
-      const float2 v = s_ml[warp][x];
+    if constexpr (WPR > 1) {
+      if (lane == 0) s_gm[warp] = gm;
+      __syncthreads();
+#pragma unroll
+      for (int y = 0; y < WPR; ++y) gm = fmaxf(gm, s_gm[rl * WPR + y]);
+    }
+    for (int x = w * 32 + lane; x < n; x += WPR * 32) {
+      const float2 v = s_ml[rl][x];
       const float wt = part_weight(v.x, gm) * v.y;
-      s_ml[warp][x].y = wt;
+      s_ml[rl][x].y = wt;
       Ls += wt;
     }
     Ls = warp_sum(Ls);
-    __syncwarp();
+    if constexpr (WPR > 1) {
+      if (lane == 0) s_sum[warp] = Ls;
+      __syncthreads();
+      Ls = 0.f;
+#pragma unroll
+      for (int y = 0; y < WPR; ++y) Ls += s_sum[rl * WPR + y];
+    } else {
+      __syncwarp();
+    }
     const float inv = 1.f / Ls;
     float acc[kC];
 #pragma unroll
     for (int j = 0; j < kC; ++j) acc[j] = 0.f;
-    for (int x0 = 0; x0 < n; x0 += kBatch) {
-      if (x0)
+    for (int x0 = w; x0 < n; x0 += kBatch * WPR) {
+      if (x0 != w)
 #pragma unroll
         for (int x = 0; x < kBatch; ++x)
-          if (x0 + x < n) pre[x] = part(x0 + x);
+          if (x0 + x * WPR < n) pre[x] = part(x0 + x * WPR);
 #pragma unroll
       for (int x = 0; x < kBatch; ++x)
-        if (x0 + x < n) {
-          const float wt = s_ml[warp][x0 + x].y * inv;
+        if (x0 + x * WPR < n) {
+          const float wt = s_ml[rl][x0 + x * WPR].y * inv;
           const float* f = reinterpret_cast<const float*>(&pre[x]);
 #pragma unroll
           for (int j = 0; j < kC; ++j) acc[j] = fmaf(wt, f[j], acc[j]);
         }
     }
-    const int r = d0.z + row, m = r / a.G, h = d0.w * a.G + r - m * a.G;
-    const int p = d1.z + m;
-    const int lo = a.window > 0 ? max(d1.w, p - a.window + 1) : d1.w;
-    if (p < lo)  // sees no key
+    if constexpr (WPR > 1) {
 #pragma unroll
-      for (int j = 0; j < kC; ++j) acc[j] = 0.f;
-    T* out = static_cast<T*>(a.out) + ((int64_t)d0.y * a.M + m) * a.out_stride + (int64_t)h * HD +
-             lane * kC;
-    if constexpr (sizeof(T) == 4) {
-      Vec v;
+      for (int j = 0; j < kC; ++j) s_red[warp][lane * kC + j] = acc[j];
+      __syncthreads();
 #pragma unroll
-      for (int j = 0; j < kC; ++j) reinterpret_cast<float*>(&v)[j] = acc[j];
-      *reinterpret_cast<Vec*>(out) = v;
-    } else {
-      uint32_t u[kC / 2];
+      for (int j = 0; j < kC; ++j) {
+        acc[j] = 0.f;
 #pragma unroll
-      for (int j = 0; j < kC; j += 2) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(acc[j], acc[j + 1]);
-        u[j / 2] = *reinterpret_cast<const uint32_t*>(&b);
+        for (int y = 0; y < WPR; ++y) acc[j] += s_red[rl * WPR + y][lane * kC + j];
       }
-      if constexpr (HD == 128)
-        *reinterpret_cast<uint2*>(out) = make_uint2(u[0], u[1]);
-      else
-        *reinterpret_cast<uint32_t*>(out) = u[0];
     }
-    __syncwarp();  // every lane has read the weights
+    if (w == 0 && row0 + rl < d0.x) {
+      const int r = d0.z + row, m = a.byG(r), h = d0.w * a.G + r - m * a.G;
+      const int p = d1.z + m;
+      const int lo = a.window > 0 ? max(d1.w, p - a.window + 1) : d1.w;
+      if (p < lo)  // sees no key
+#pragma unroll
+        for (int j = 0; j < kC; ++j) acc[j] = 0.f;
+      T* out = static_cast<T*>(a.out) + ((int64_t)d0.y * a.M + m) * a.out_stride + (int64_t)h * HD +
+               lane * kC;
+      if constexpr (sizeof(T) == 4) {
+        Vec v;
+#pragma unroll
+        for (int j = 0; j < kC; ++j) reinterpret_cast<float*>(&v)[j] = acc[j];
+        *reinterpret_cast<Vec*>(out) = v;
+      } else {
+        uint32_t u[kC / 2];
+#pragma unroll
+        for (int j = 0; j < kC; j += 2) {
+          const __nv_bfloat162 b = __floats2bfloat162_rn(acc[j], acc[j + 1]);
+          u[j / 2] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        if constexpr (HD == 128)
+          *reinterpret_cast<uint2*>(out) = make_uint2(u[0], u[1]);
+        else
+          *reinterpret_cast<uint32_t*>(out) = u[0];
+      }
+    }
+    if constexpr (WPR > 1) __syncthreads();
+    else __syncwarp();  // every lane has read the weights
   }
 }
 
@@ -640,7 +706,8 @@ template <typename T, int HD, int RT>
 cudaError_t merge_launch(const Kv8Attn& a, int P, cudaStream_t st) {
   const int rows = a.M * a.G < RT ? a.M * a.G : RT;  // of a tile, at most
   cudaLaunchConfig_t cfg = {};
-  const int ny = (rows + kMWarps - 1) / kMWarps;
+  constexpr int kWpr = RT == kRT ? kMWarps : 1;  // warps of a row
+  const int ny = (rows * kWpr + kMWarps - 1) / kMWarps;
   cfg.gridDim = dim3(P, ny < kMRowBlocks ? ny : kMRowBlocks);
   cfg.blockDim = dim3(kMWarps * 32);
   cfg.stream = st;
@@ -649,7 +716,7 @@ cudaError_t merge_launch(const Kv8Attn& a, int P, cudaStream_t st) {
   attr[0].val.programmaticStreamSerializationAllowed = g_pdl_enabled ? 1 : 0;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_kv8_merge<T, HD, RT>, a);
+  return cudaLaunchKernelEx(&cfg, k_kv8_merge<T, HD, RT, kWpr>, a);
 }
 
 template <typename T, int HD>
@@ -721,7 +788,7 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   const bool tc = kv8_is_wide(dtype, c->head_dim, (long long)M * G);
   const int rt = tc ? kWRows : kRT, ku = tc ? kWKeys : kKv8Block;
   const long long n_rt = ((long long)M * G + rt - 1) / rt;
-  const long long units = n_rt * c->n_seq * c->n_kv_heads * ((c->max_seq + ku - 1) / ku);
+  const long long units = n_rt * c->n_seq * c->n_kv_heads * ((c->max_seq + ku - 1) / ku + kKv8ItemCost);
   if (units > 0x7fffffffll)
     return fail_op(SSD_ERR_CAPACITY, "n_seq x M x max_seq: more than 2^31 units of work");
   const Kv8Work lay = kv8_work(kKv8MaxBlocks, rt, c->head_dim);
@@ -757,9 +824,12 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   a.desc = reinterpret_cast<Kv8Desc*>(ws);
   a.ml = reinterpret_cast<float2*>(ws + lay.ml);
   a.part = reinterpret_cast<float*>(ws + lay.part);
-  int P = tc ? 2 * sms : sms;
+  a.byG = Kv8Div::of((uint32_t)G);
+  a.byRt = Kv8Div::of((uint32_t)n_rt);
+  int P = sms * (tc ? 2 : kVBlocks);
   if (P > kKv8MaxBlocks) P = kKv8MaxBlocks;
   if (units < P) P = (int)units;
+  a.byP = Kv8Div::of((uint32_t)P);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool wide = c->head_dim == 128;
   if (tc)

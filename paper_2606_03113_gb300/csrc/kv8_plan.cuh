@@ -16,7 +16,26 @@
 
 namespace ssd {
 
+// n / d for 0 <= n < 2^31 by a product: m = ceil(2^(31 + s) / d), 2^(s - 1) < d <= 2^s.
+struct Kv8Div {
+  uint32_t d, m, s;
+  static Kv8Div of(uint32_t d) {
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    return Kv8Div{d, (uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};
+  }
+  __device__ __forceinline__ int operator()(int n) const {
+    return (int)((((uint64_t)(uint32_t)n * m) >> 31) >> s);
+  }
+};
+
+// What an item costs beside its units (queries, the join of the warps or of the
+// parts), in units: 2 to 3 us against 0.7 a unit.  Without it 24 ragged sequences of 32
+// heads kept the last block busy for 90 us and the first for 59.
+constexpr int kKv8ItemCost = 3;
+
 struct Kv8Attn {
+  Kv8Div byG, byRt, byP;
   const uint8_t *k, *v;
   const float *ks, *vs;
   const void* q;
@@ -44,7 +63,9 @@ struct Kv8Item {
   int unit0, units;    // first unit of KU keys, number of them (0: no rows here)
 };
 
-__device__ __forceinline__ int kv8_row_pos(const Kv8Item& it, int r, int G) { return it.pos + r / G; }
+__device__ __forceinline__ int kv8_row_pos(const Kv8Attn& a, const Kv8Item& it, int r) {
+  return it.pos + a.byG(r);
+}
 // First key that the row at position p sees.
 __device__ __forceinline__ int kv8_row_lo(const Kv8Item& it, int p, int window) {
   return window > 0 ? max(it.first, p - window + 1) : it.first;
@@ -53,7 +74,7 @@ __device__ __forceinline__ int kv8_row_lo(const Kv8Item& it, int p, int window) 
 template <int RT, int KU>
 __device__ __forceinline__ Kv8Item kv8_entry(const Kv8Attn& a, int e) {
   Kv8Item it;
-  it.b = e / a.n_rt;
+  it.b = a.byRt(e);
   it.rt = e - it.b * a.n_rt;
   it.pos = __ldg(a.pos + it.b);
   const int n = a.rows ? __ldg(a.rows + it.b) : a.M;
@@ -68,16 +89,34 @@ __device__ __forceinline__ Kv8Item kv8_entry(const Kv8Attn& a, int e) {
   }
   it.nr = min(RT, n * a.G - it.r0);
   if (it.nr <= 0) return it;
-  it.lo = kv8_row_lo(it, kv8_row_pos(it, it.r0, a.G), a.window);
-  it.hi = kv8_row_pos(it, it.r0 + it.nr - 1, a.G);
+  it.lo = kv8_row_lo(it, kv8_row_pos(a, it, it.r0), a.window);
+  it.hi = kv8_row_pos(a, it, it.r0 + it.nr - 1);
   it.unit0 = min(it.lo, it.hi) / KU;
   it.units = it.hi / KU - it.unit0 + 1;
   return it;
 }
 
-// First unit of block i's stretch.
-__device__ __forceinline__ int kv8_start(int i, int P, int total) {
-  return (int)((long long)i * total / P);
+// The line as the blocks share it: block i's stretch begins at i total / P.
+struct Kv8Line {
+  int total, q, r;  // total = q P + r
+  __device__ __forceinline__ Kv8Line(const Kv8Attn& a, int t) : total(t) {
+    q = a.byP(t);
+    r = t - q * (int)a.byP.d;
+  }
+  __device__ __forceinline__ int start(const Kv8Attn& a, int i) const { return i * q + a.byP(i * r); }
+  // The block whose stretch holds unit x.
+  __device__ __forceinline__ int block(const Kv8Attn& a, int x) const {
+    int j = min((int)((float)x * (float)a.byP.d / (float)total), (int)a.byP.d - 1);
+    while (j > 0 && start(a, j) > x) --j;
+    while (start(a, j + 1) <= x) ++j;
+    return j;
+  }
+};
+
+// The line's places that an item takes.
+template <int RT, int KU>
+__device__ __forceinline__ int kv8_len(const Kv8Item& it) {
+  return it.units ? it.units + kKv8ItemCost : 0;
 }
 
 // The block's part of an item: units u0 .. u0 + nu - 1.
@@ -88,50 +127,57 @@ struct Kv8Seg {
 };
 
 struct Kv8Cursor {
-  int w0, w1, total;  // the block's stretch, all units
-  int e, off;         // entry that holds w0, units of that entry before w0
+  int w0, w1, total;  // the block's stretch that is left, the whole line
+  int e, off;         // entry that holds w0, its places before w0
 };
 
-// Every thread of the block gets the block's stretch; sm: THREADS / 32 + 2 ints.
+struct Kv8PlanSmem {
+  int warp[16];
+  Kv8Cursor c;
+};
+
+// Every thread of the block gets the block's stretch.
 template <int RT, int KU, int THREADS>
-__device__ __forceinline__ Kv8Cursor kv8_plan(const Kv8Attn& a, int* sm) {
+__device__ __forceinline__ Kv8Cursor kv8_plan(const Kv8Attn& a, Kv8PlanSmem& sm) {
+  static_assert(THREADS / 32 <= 16, "a sum for each warp");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (a.entries + THREADS - 1) / THREADS;
   const int e0 = min(tid * per, a.entries), e1 = min(e0 + per, a.entries);
   int sum = 0;
-  for (int e = e0; e < e1; ++e) sum += kv8_entry<RT, KU>(a, e).units * a.Hkv;
+  Kv8Item it;
+  for (int e = e0; e < e1; ++e) {
+    it = kv8_entry<RT, KU>(a, e);
+    sum += kv8_len<RT, KU>(it) * a.Hkv;
+  }
   int inc = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int u = __shfl_up_sync(0xffffffffu, inc, o);
     if (lane >= o) inc += u;
   }
-  if (lane == 31) sm[warp] = inc;
+  if (lane == 31) sm.warp[warp] = inc;
+  if (tid == 0) sm.c.w0 = sm.c.w1 = 0;
   __syncthreads();
   int before = inc - sum, total = 0;
 #pragma unroll
   for (int w = 0; w < THREADS / 32; ++w) {
-    if (w < warp) before += sm[w];
-    total += sm[w];
+    if (w < warp) before += sm.warp[w];
+    total += sm.warp[w];
   }
-  Kv8Cursor c;
-  c.total = total;
-  c.w0 = kv8_start(blockIdx.x, gridDim.x, total);
-  c.w1 = kv8_start(blockIdx.x + 1, gridDim.x, total);
-  if (c.w0 < c.w1 && before <= c.w0 && c.w0 < before + sum) {  // one thread
-    int off = c.w0 - before, e = e0;
+  const Kv8Line line(a, total);
+  const int w0 = line.start(a, blockIdx.x), w1 = line.start(a, blockIdx.x + 1);
+  if (w0 < w1 && before <= w0 && w0 < before + sum) {  // one thread
+    int off = w0 - before, e = e0;
     for (;; ++e) {
-      const int u = kv8_entry<RT, KU>(a, e).units * a.Hkv;
+      if (per > 1) it = kv8_entry<RT, KU>(a, e);
+      const int u = kv8_len<RT, KU>(it) * a.Hkv;
       if (off < u) break;
       off -= u;
     }
-    sm[THREADS / 32] = e;
-    sm[THREADS / 32 + 1] = off;
+    sm.c = Kv8Cursor{w0, w1, total, e, off};
   }
   __syncthreads();
-  c.e = sm[THREADS / 32];
-  c.off = sm[THREADS / 32 + 1];
-  return c;
+  return sm.c;
 }
 
 // The next segment of the block's stretch; false at its end.
@@ -139,13 +185,20 @@ template <int RT, int KU>
 __device__ __forceinline__ bool kv8_next(const Kv8Attn& a, Kv8Cursor& c, Kv8Seg& s) {
   while (c.w0 < c.w1) {
     s.it = kv8_entry<RT, KU>(a, c.e);
-    if (c.off >= s.it.units * a.Hkv) {
+    const int len = kv8_len<RT, KU>(s.it);
+    if (c.off >= len * a.Hkv) {
       c.off = 0;
       ++c.e;
       continue;
     }
-    s.g = c.off / s.it.units;
-    s.u0 = c.off - s.g * s.it.units;
+    s.g = c.off / len;
+    s.u0 = c.off - s.g * len;
+    if (s.u0 >= s.it.units) {  // the item's cost
+      const int n = min(len - s.u0, c.w1 - c.w0);
+      c.w0 += n;
+      c.off += n;
+      continue;
+    }
     s.nu = min(s.it.units - s.u0, c.w1 - c.w0);
     c.w0 += s.nu;
     c.off += s.nu;
@@ -156,9 +209,9 @@ __device__ __forceinline__ bool kv8_next(const Kv8Attn& a, Kv8Cursor& c, Kv8Seg&
 
 // The segment as the merge finds it, where it begins an item that goes on in
 // the next block.  c: the cursor behind the segment.
-__device__ __forceinline__ Kv8Desc kv8_desc(const Kv8Cursor& c, const Kv8Seg& s) {
-  const long long end = (long long)c.w0 - s.nu + s.it.units;  // the unit behind the item
-  return Kv8Desc{s.it.nr, s.it.b, s.it.r0, s.g, (int)((end * gridDim.x - 1) / c.total), c.total,
+__device__ __forceinline__ Kv8Desc kv8_desc(const Kv8Attn& a, const Kv8Cursor& c, const Kv8Seg& s) {
+  const int last = c.w0 - s.nu + s.it.units - 1;  // the item's last unit
+  return Kv8Desc{s.it.nr, s.it.b, s.it.r0, s.g, Kv8Line(a, c.total).block(a, last), c.total,
                  s.it.pos, s.it.first};
 }
 

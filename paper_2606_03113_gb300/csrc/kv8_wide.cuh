@@ -237,10 +237,13 @@ __device__ __forceinline__ void w_wait(uint64_t (&b)[2], uint32_t n, bool& bad) 
 
 __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
   extern __shared__ unsigned char smem_raw[];
-  __shared__ int s_plan[kWThreads / 32 + 2];
+  __shared__ Kv8PlanSmem s_plan;
   __shared__ WideBars bar;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_nan, s_fail;
+  __shared__ int s_nan, s_fail, s_more;
+  __shared__ Kv8Cursor s_cur;  // of the softmax warps
+  __shared__ Kv8Seg s_seg;
+  __shared__ float s_qs[kWRows];
   unsigned char* const smem =
       reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   unsigned char* const Qs = smem;
@@ -267,7 +270,7 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
   tc_fence_after();
   pdl_launch_dependents();
   const uint32_t tm = s_tmem, tmO = tm + 2 * kWKeys;
-  Kv8Seg sg;
+  if (tid == 0) s_cur = cur;
   uint32_t n = 0;  // steps so far: the barriers' phases
   bool bad = false;
 
@@ -275,6 +278,7 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
   if (warp == 8) {
     // ------------------------------------------------------------ scores
     if ((tid & 31) == 0) {
+      Kv8Seg sg;
       const uint64_t dq = sdesc_k128(smem_u32(Qs)), dk = sdesc_k128(smem_u32(Ks));
       for (uint32_t seg = 0; kv8_next<kWRows, kWKeys>(a, cur, sg); ++seg) {
         if (!bad) bad = !w_sleep(&bar.q_full, seg & 1);
@@ -295,6 +299,7 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
   } else if (warp == 9) {
     // ------------------------------------------------------------ outputs
     if ((tid & 31) == 0) {
+      Kv8Seg sg;
       const uint64_t dv = w_desc_mn(smem_u32(Vs));
       while (kv8_next<kWRows, kWKeys>(a, cur, sg))
         for (int i = 0; i < sg.nu; ++i, ++n) {
@@ -310,19 +315,37 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
         }
     }
     __syncwarp();
-  } else if (warp >= 4) {
+  } else if (warp >= 4 && warp < 8) {
     // ------------------------------------------------------------ codes to f16
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     const int ct = tid - 128;
-    uint4 kc[4], vc[4];
-    // rows ct / 8 + 16 j of a step, 16 codes each
-    auto load = [&](const Kv8Seg& s, int i, const uint8_t* base, uint4 (&c)[4]) {
-      const int key = w_key0(s, i) + ct / 8;
-      const uint8_t* p = base + (((size_t)s.it.b * a.Hkv + s.g) * a.max_seq + key) * kWHd + (ct % 8) * 16;
+    // the step that is loaded next: its first row in the cache, the keys (counted from
+    // it) that some row sees, those that every row sees, steps left in the segment
+    int64_t off = 0;
+    int lo = 0, hi = 0, flo = 0, fhi = 0, left = 0;
+    auto advance = [&]() -> bool {
+      if (--left > 0) {
+        off += kWKeys * kWHd;
+        lo -= kWKeys, hi -= kWKeys, flo -= kWKeys, fhi -= kWKeys;
+        return true;
+      }
+      Kv8Seg sg;
+      if (!kv8_next<kWRows, kWKeys>(a, cur, sg)) return false;
+      const int k0 = w_key0(sg, 0);
+      off = (((int64_t)sg.it.b * a.Hkv + sg.g) * a.max_seq + k0) * kWHd;
+      lo = sg.it.lo - k0, hi = sg.it.hi - k0;
+      flo = kv8_row_lo(sg.it, sg.it.hi, a.window) - k0;
+      fhi = kv8_row_pos(a, sg.it, sg.it.r0) - k0;
+      left = sg.nu;
+      return true;
+    };
+    uint4 kc[4], vc[4];  // rows ct / 8 + 16 j of a step, 16 codes each
+    auto load = [&](const uint8_t* base, uint4 (&c)[4]) {
+      const uint8_t* p = base + off + ct * 16;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        c[j] = key + 16 * j >= s.it.lo && key + 16 * j <= s.it.hi ? w_load16(p + 16 * j * kWHd)
-                                                                  : make_uint4(0, 0, 0, 0);
+        c[j] = ct / 8 + 16 * j >= lo && ct / 8 + 16 * j <= hi ? w_load16(p + 16 * j * kWHd)
+                                                              : make_uint4(0, 0, 0, 0);
     };
     // eight lanes hold a row, 128 bytes of each half; the upper four store their two
     // chunks the other way round, so that all eight meet different banks
@@ -344,96 +367,104 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
       }
       w_smem_fence();
     };
-    Kv8Cursor ahead = cur;  // one segment ahead: its first codes are loaded early
-    Kv8Seg nx;
-    bool more = kv8_next<kWRows, kWKeys>(a, ahead, nx);
+    bool more = advance();
     if (more) {
-      load(nx, 0, a.k, kc);
-      load(nx, 0, a.v, vc);
+      load(a.k, kc);
+      load(a.v, vc);
     }
-    while (more) {
-      sg = nx;
-      more = kv8_next<kWRows, kWKeys>(a, ahead, nx);
-      const int full_lo = kv8_row_lo(sg.it, sg.it.hi, a.window);
-      const int full_hi = kv8_row_pos(sg.it, sg.it.r0, a.G);
-      for (int i = 0; i < sg.nu; ++i, ++n) {
-        const uint32_t buf = (n & 1) * kWKTile;
-        if (n >= 2) w_wait(bar.s_done, n - 2, bad);
-        store(Ks + buf, kc);
-        mbar_arrive(&bar.k_full[n & 1]);
-        if (i + 1 < sg.nu) load(sg, i + 1, a.k, kc);
-        else if (more) load(nx, 0, a.k, kc);
-        const int k0 = w_key0(sg, i);
-        if (k0 < full_lo || k0 + kWKeys - 1 > full_hi) {  // not every row sees every key
-          uint32_t any = 0;
+    for (; more; ++n) {
+      const uint32_t buf = (n & 1) * kWKTile;
+      if (n >= 2) w_wait(bar.s_done, n - 2, bad);
+      store(Ks + buf, kc);
+      mbar_arrive(&bar.k_full[n & 1]);
+      if (0 < flo || kWKeys - 1 > fhi) {  // not every row sees every key
+        uint32_t any = 0;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t* w = reinterpret_cast<uint32_t*>(&vc[j]);
+        for (int j = 0; j < 4; ++j) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(&vc[j]);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const uint32_t m = e4m3_nan_mask(w[x]);
-              any |= m;
-              w[x] &= ~((m >> 7) * 0xffu);
-            }
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t m = e4m3_nan_mask(w[x]);
+            any |= m;
+            w[x] &= ~((m >> 7) * 0xffu);
           }
-          if (any) s_nan = 1;  // (published by the arrival below)
         }
-        if (n >= 2) w_wait(bar.o_done, n - 2, bad);
-        store(Vs + buf, vc);
-        mbar_arrive(&bar.v_full[n & 1]);
-        if (i + 1 < sg.nu) load(sg, i + 1, a.v, vc);
-        else if (more) load(nx, 0, a.v, vc);
+        if (any) s_nan = 1;  // (published by the arrival below)
       }
+      more = advance();
+      if (more) load(a.k, kc);
+      if (n >= 2) w_wait(bar.o_done, n - 2, bad);
+      store(Vs + buf, vc);
+      mbar_arrive(&bar.v_full[n & 1]);
+      if (more) load(a.v, vc);
     }
-  } else {
+  } else if (warp < 4) {
     // ------------------------------------------------------------ softmax
     asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
     const int row = tid;
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-    while (kv8_next<kWRows, kWKeys>(a, cur, sg)) {
+    for (;;) {
+      // the segment stands in shared memory: the steps need the registers
+      if (tid == 0) s_more = kv8_next<kWRows, kWKeys>(a, s_cur, s_seg);
+      named_sync(1, 128);
+      if (!s_more) break;
+      const Kv8Seg& sg = s_seg;
       const Kv8Item& it = sg.it;
-      const int g = sg.g;
-      // the thread's row of queries as f16 (a row past the last: the last one's, not
+      // queries as f16, sixteen lanes a row (rows past the last: the last one's, not
       // used); the products of the segment before are done with theirs
-      const int rq = it.r0 + min(row, it.nr - 1), mq = rq / a.G, hq = g * a.G + rq - mq * a.G;
-      float qs;  // scores = products * qs * key scale
       {
-        const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) +
-                                 ((int64_t)it.b * a.M + mq) * a.q_stride + (int64_t)hq * kWHd;
+        const int ch = tid % 16;
+        const __nv_bfloat16* const q0 = static_cast<const __nv_bfloat16*>(a.q) + ch * 8 +
+                                        (int64_t)it.b * a.M * a.q_stride + (int64_t)sg.g * a.G * kWHd;
+        unsigned char* const own = Qs + (ch >> 3) * kWQHalf;
         uint4 u[16];
 #pragma unroll
-        for (int ch = 0; ch < 16; ++ch) u[ch] = __ldg(reinterpret_cast<const uint4*>(q) + ch);
-        __nv_bfloat162 am = __float2bfloat162_rn(0.f);
-#pragma unroll
-        for (int ch = 0; ch < 16; ++ch) {
-          const __nv_bfloat162* w = reinterpret_cast<const __nv_bfloat162*>(&u[ch]);
-#pragma unroll
-          for (int x = 0; x < 4; ++x) am = __hmax2(am, __habs2(w[x]));
+        for (int j = 0; j < 16; ++j) {
+          const int r = it.r0 + min(j * 8 + tid / 16, it.nr - 1), m = a.byG(r);
+          u[j] = w_load16(q0 + m * a.q_stride + (r - m * a.G) * kWHd);
         }
-        const float amax = fmaxf(__low2float(am), __high2float(am));
-        const int ex = min(max((int)(__float_as_uint(amax) >> 23) - 127 - 13, -100), 115);
-        const float inv = pow2i(-ex);
-        qs = pow2i(ex) * a.scale;
 #pragma unroll
-        for (int ch = 0; ch < 16; ++ch) {
-          float f[8];
-          Elem<__nv_bfloat16>::unpack(u[ch], f);
-          *reinterpret_cast<uint4*>(Qs + (ch >> 3) * kWQHalf + w_place(row, ch & 7)) =
-              make_uint4(half2_bits(f[0] * inv, f[1] * inv), half2_bits(f[2] * inv, f[3] * inv),
-                         half2_bits(f[4] * inv, f[5] * inv), half2_bits(f[6] * inv, f[7] * inv));
+        for (int j0 = 0; j0 < 16; j0 += 4) {
+          float amax[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const __nv_bfloat162* w = reinterpret_cast<const __nv_bfloat162*>(&u[j0 + j]);
+            const __nv_bfloat162 am = __hmax2(__hmax2(__habs2(w[0]), __habs2(w[1])),
+                                              __hmax2(__habs2(w[2]), __habs2(w[3])));
+            amax[j] = fmaxf(__low2float(am), __high2float(am));
+          }
+#pragma unroll
+          for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              amax[j] = fmaxf(amax[j], __shfl_xor_sync(0xffffffffu, amax[j], o));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int qr = (j0 + j) * 8 + tid / 16;
+            const int ex = min(max((int)(__float_as_uint(amax[j]) >> 23) - 127 - 13, -100), 115);
+            const float inv = pow2i(-ex);
+            float f[8];
+            Elem<__nv_bfloat16>::unpack(u[j0 + j], f);
+            *reinterpret_cast<uint4*>(own + w_place(qr, ch & 7)) =
+                make_uint4(half2_bits(f[0] * inv, f[1] * inv), half2_bits(f[2] * inv, f[3] * inv),
+                           half2_bits(f[4] * inv, f[5] * inv), half2_bits(f[6] * inv, f[7] * inv));
+            if (ch == 0) s_qs[qr] = pow2i(ex) * a.scale;
+          }
         }
       }
       w_smem_fence();
       tc_fence_before();
       mbar_arrive(&bar.q_full);
+      named_sync(1, 128);
+      const float qs = s_qs[row];  // scores = products * qs * key scale
       const bool live = warp * 32 < it.nr;  // the warp has rows
-      const size_t slab = (size_t)it.b * a.Hkv + g;
+      const size_t slab = (size_t)it.b * a.Hkv + sg.g;
       const int b0 = it.unit0 + sg.u0;
       const float* ksp = a.ks + slab * (a.max_seq / kKv8Block) + b0;
       const float* vsp = a.vs + slab * (a.max_seq / kKv8Block) + b0;
       const int full_lo = kv8_row_lo(it, it.hi, a.window);
-      const int full_hi = kv8_row_pos(it, it.r0, a.G);
-      const int phi = row < it.nr ? kv8_row_pos(it, it.r0 + row, a.G) : -1;
+      const int full_hi = kv8_row_pos(a, it, it.r0);
+      const int phi = row < it.nr ? kv8_row_pos(a, it, it.r0 + row) : -1;
       const int plo = row < it.nr ? kv8_row_lo(it, phi, a.window) : 0;
       float ref = -INFINITY, ls = 0.f;   // of the row
       float vref = pow2i(-126);          // the output's unit, as in k_kv8_rows
@@ -564,7 +595,7 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
             const float4 v = *reinterpret_cast<const float4*>(xs + y * 256 + ((c4 ^ (y & 15)) << 4));
             const int col = (q >> 1) * 64 + c4 * 4;
             if (whole) {
-              const int r = it.r0 + warp * 32 + y, m = r / a.G, h = g * a.G + r - m * a.G;
+              const int r = it.r0 + warp * 32 + y, m = a.byG(r), h = sg.g * a.G + r - m * a.G;
               const __nv_bfloat162 b0 = __floats2bfloat162_rn(v.x, v.y);
               const __nv_bfloat162 b1 = __floats2bfloat162_rn(v.z, v.w);
               *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) +
@@ -582,8 +613,8 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
         // (max, sum) as the merge weighs parts: p stands against 2^(ref - kWBase)
         if (in && !whole) a.ml[(size_t)slot * kWRows + row] = make_float2(ref, ls);
       }
+      if (row == 0 && !sg.whole() && sg.u0 == 0) a.desc[blockIdx.x] = kv8_desc(a, s_cur, sg);
       named_sync(1, 128);  // the next segment's queries go where outputs were exchanged
-      if (row == 0 && !sg.whole() && sg.u0 == 0) a.desc[blockIdx.x] = kv8_desc(cur, sg);
       tc_fence_before();  // the next segment's products overwrite O, behind its p_full
     }
   }
