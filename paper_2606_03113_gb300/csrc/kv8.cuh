@@ -61,6 +61,9 @@ __device__ __forceinline__ uint32_t e4m3_nan_mask(uint32_t w) {
 ssd_status fail_op(ssd_status s, const char* msg) noexcept;
 ssd_status fail_op_cuda(const char* what, cudaError_t e) noexcept;
 
+// SMs of the current device (asked for once a device).
+cudaError_t device_sms(int* sms) noexcept;
+
 // Checks of a cache that every entry point makes; null: fine.
 const char* check_kv8(const ssd_kv8_cache* c) noexcept;
 

@@ -231,8 +231,9 @@ __device__ void chunk_top(const Row<T>& row, int v0, int v1, int top, float tmax
     // with at least `top` elements at or above it
     uint32_t lo = (uint32_t)(logit_key(bound > -INFINITY ? bound : -3.4028235e38f, 0) >> 32);
     uint32_t hi = 0xff800000u;  // +inf
-    while (lo < hi) {
-      const uint32_t mid = lo + (hi - lo + 1) / 2;
+    // (mostly the bound is that value itself, the one that so many logits have: one scan)
+    for (bool first = true; lo < hi; first = false) {
+      const uint32_t mid = first ? lo + 1 : lo + (hi - lo + 1) / 2;
       __syncthreads();
       if (tid == 0) sm.count = 0;
       __syncthreads();
@@ -304,7 +305,7 @@ __device__ void chunk_top(const Row<T>& row, int v0, int v1, int top, float tmax
 // What a finished row puts out: x: its statistics, keys: its top.
 template <typename T>
 __device__ __forceinline__ void finish_row(const LogpArgs& a, int r, const T* row, const Stat& x,
-                                           const uint64_t* keys) {
+                                           const uint64_t* keys, int threads) {
   constexpr float kLn2 = 0.6931471805599453f;
   // a row of -inf alone: lse is -inf, the rest NaN
   const bool none = x.S == 0.f;
@@ -314,7 +315,7 @@ __device__ __forceinline__ void finish_row(const LogpArgs& a, int r, const T* ro
     if (a.lse) a.lse[r] = none ? -INFINITY : fmaf(x.m, a.inv_t, log_s);
     if (a.entropy) a.entropy[r] = log_s - x.T / x.S * kLn2;
   }
-  for (int i = tid; i < a.ntok; i += kLThreads) {
+  for (int i = tid; i < a.ntok; i += threads) {
     const int v = __ldg(a.tok + (int64_t)r * a.ntok + i);
     float lp = 0.f;
     if (v >= 0 && v < a.vocab) {
@@ -325,7 +326,7 @@ __device__ __forceinline__ void finish_row(const LogpArgs& a, int r, const T* ro
     }
     a.logprob[(int64_t)r * a.ntok + i] = lp;
   }
-  for (int i = tid; i < a.top; i += kLThreads) {
+  for (int i = tid; i < a.top; i += threads) {
     const uint64_t k = keys[i];
     a.top_id[(int64_t)r * a.top + i] = k ? key_id(k) : -1;
     a.top_logprob[(int64_t)r * a.top + i] =
@@ -335,9 +336,15 @@ __device__ __forceinline__ void finish_row(const LogpArgs& a, int r, const T* ro
 
 }  // namespace
 
+// fp32 rows wait for memory: a thread has the next step's vectors on their way, at
+// three blocks an SM (1023 rows of 128256 without a top: 82 us, 144 without that).  bf16 rows
+// have twice the arithmetic a byte and run better as four blocks without (53, 62).
+template <typename T>
+constexpr bool kAhead = sizeof(T) == 4;
+
 // Grid (chunks, rows).
 template <typename T>
-__global__ void __launch_bounds__(kLThreads) k_logprobs(const LogpArgs a) {
+__global__ void __launch_bounds__(kLThreads, kAhead<T> ? 3 : 4) k_logprobs(const LogpArgs a) {
   constexpr int kE = Row<T>::kE;
   __shared__ LogpSmem sm;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -353,24 +360,34 @@ __global__ void __launch_bounds__(kLThreads) k_logprobs(const LogpArgs a) {
     const int v0 = min((int)blockIdx.x * a.vec_per_chunk, nv);
     const int v1 = blockIdx.x + 1 == gridDim.x ? nv : min(v0 + a.vec_per_chunk, nv);
 
-    // running statistics of the thread's vectors v0 + tid, + kLThreads, ...
+    // running statistics of the thread's vectors v0 + tid, + kLThreads, ..., kUnroll of
+    // them a step
     float tmax = -INFINITY;  // largest logit
     float m = 0.f;           // what the sums stand against: tmax once there is one
     uint64_t S2 = 0, T2 = 0, nm2 = 0;
-    for (int vb = v0 + tid; vb < v1; vb += kLThreads * kUnroll) {
-      uint32_t x[kUnroll][4];
+    const uint64_t c2 = pack2(c, c);
+    const int whole0 = row.skip > 0, whole1 = min(v1, (row.skip + row.n) / kE);
+    auto load = [&](int vb, uint4 (&x)[kUnroll]) {
+      if (vb >= whole0 && vb + (kUnroll - 1) * kLThreads < whole1) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          x[u] = __ldg(reinterpret_cast<const uint4*>(row.base) + vb + u * kLThreads);
+      } else {
+        constexpr uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;  // -inf
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          const int v = vb + u * kLThreads;
+          x[u] = v < v1 ? row.raw(v) : make_uint4(none, none, none, none);
+        }
+      }
+    };
+    auto add = [&](const uint4 (&x)[kUnroll]) {
+      uint32_t bw = x[0].x;
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        const int v = vb + u * kLThreads;
-        constexpr uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;  // -inf
-        const uint4 w = v < v1 ? row.raw(v) : make_uint4(none, none, none, none);
-        x[u][0] = w.x, x[u][1] = w.y, x[u][2] = w.z, x[u][3] = w.w;
+        bw = max_word(max_word(bw, x[u].x, T()), x[u].y, T());
+        bw = max_word(max_word(bw, x[u].z, T()), x[u].w, T());
       }
-      uint32_t bw = x[0][0];
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) bw = max_word(bw, x[u][j], T());
       const float bm = max_of_word(bw, T());
       if (bm > tmax) {
         if (tmax > -INFINITY) {
@@ -383,19 +400,43 @@ __global__ void __launch_bounds__(kLThreads) k_logprobs(const LogpArgs a) {
         nm2 = pack2(-m, -m);
       }
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
+      for (int u = 0; u < kUnroll; ++u) {
+        const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
 #pragma unroll
         for (int j = 0; j < kE; j += 2) {
-          const uint64_t z2 =
-              sizeof(T) == 4 ? pack2(__uint_as_float(x[u][j]), __uint_as_float(x[u][j + 1 < 4 ? j + 1 : 3]))
-                             : pack2(__uint_as_float(x[u][j / 2] << 16),
-                                     __uint_as_float(x[u][j / 2] & 0xffff0000u));
-          const float2 d = unpack2(mul2(add2(z2, nm2), pack2(c, c)));
+          const uint64_t z2 = sizeof(T) == 4
+                                  ? pack2(__uint_as_float(w[j]), __uint_as_float(w[j + 1 < 4 ? j + 1 : 3]))
+                                  : pack2(__uint_as_float(w[j / 2] << 16),
+                                          __uint_as_float(w[j / 2] & 0xffff0000u));
+          // (differences first: a row of the type's lowest value is a row of equal logits)
+          const float2 d = unpack2(mul2(add2(z2, nm2), c2));
           const uint64_t e2 = pack2(ex2(d.x), ex2(d.y));
           S2 = add2(S2, e2);
           // (a logit of -inf adds 0)
           T2 = fma2(e2, pack2(fmaxf(d.x, -1e30f), fmaxf(d.y, -1e30f)), T2);
         }
+      }
+    };
+    constexpr int kStep = kLThreads * kUnroll;
+    if constexpr (kAhead<T>) {
+      uint4 xa[kUnroll], xb[kUnroll];
+      int vb = v0 + tid;
+      if (vb < v1) load(vb, xa);
+      while (vb < v1) {
+        if (vb + kStep < v1) load(vb + kStep, xb);
+        add(xa);
+        vb += kStep;
+        if (vb >= v1) break;
+        if (vb + kStep < v1) load(vb + kStep, xa);
+        add(xb);
+        vb += kStep;
+      }
+    } else {
+      for (int vb = v0 + tid; vb < v1; vb += kStep) {
+        uint4 x[kUnroll];
+        load(vb, x);
+        add(x);
+      }
     }
     const float2 Sv = unpack2(S2), Tv = unpack2(T2);
     Stat st{m, Sv.x + Sv.y, Tv.x + Tv.y};
@@ -415,7 +456,7 @@ __global__ void __launch_bounds__(kLThreads) k_logprobs(const LogpArgs a) {
 #pragma unroll
     for (int w = 1; w < kLWarps; ++w) st = join(st, sm.stat[w], c);
     if (a.chunks == 1) {
-      finish_row<T>(a, r, zr, st, sm.top);
+      finish_row<T>(a, r, zr, st, sm.top, kLThreads);
     } else {
       const int64_t at = r64 * a.chunks + blockIdx.x;
       if (tid == 0) a.part[at] = make_float4(st.m, st.S, st.T, 0.f);
@@ -425,49 +466,75 @@ __global__ void __launch_bounds__(kLThreads) k_logprobs(const LogpArgs a) {
   }
 }
 
-// Joins a row's chunks.
+// Joins a row's chunks: one warp takes the largest of the lists' heads, a.top times.
+constexpr int kJThreads = 128;
+
 template <typename T>
-__global__ void __launch_bounds__(kLThreads) k_logprobs_merge(const LogpArgs a) {
+__global__ void __launch_bounds__(kJThreads) k_logprobs_merge(const LogpArgs a) {
   __shared__ uint64_t keys[kMaxChunks * kMaxTop];
   __shared__ uint64_t top[kMaxTop];
-  __shared__ float4 part[kMaxChunks];
+  static_assert(kMaxChunks == 64, "two lists a lane");
   pdl_wait();
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const float c = a.inv_t * 1.4426950408889634f;
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const int n = a.chunks * a.top;
-    for (int i = tid; i < n; i += kLThreads) keys[i] = __ldcg(a.part_top + r * n + i);
-    if (tid < a.chunks) part[tid] = __ldcg(a.part + r * a.chunks + tid);
-    if (tid < a.top) top[tid] = 0ull;
+#pragma unroll 8
+    for (int i = tid; i < n; i += kJThreads) keys[i] = __ldcg(a.part_top + r * n + i);
     __syncthreads();
-    // a key's rank: its place in its own chunk's list and those above it in the others
-    for (int i = tid; i < n; i += kLThreads) {
-      const uint64_t k = keys[i];
-      if (!k) continue;
-      const int own = i / a.top;
-      int rank = i - own * a.top;
-      for (int ch = 0; ch < a.chunks && rank < a.top; ++ch) {
-        if (ch == own) continue;
-        const uint64_t* l = keys + ch * a.top;
-        for (int j = 0; j < a.top && l[j] > k; ++j) ++rank;
+    if (tid < 32) {
+      Stat st{0.f, 0.f, 0.f};
+      int at[2];
+      uint64_t head[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int ch = lane + 32 * j;
+        at[j] = 0;
+        head[j] = 0ull;
+        if (ch < a.chunks) {
+          const float4 p = __ldcg(a.part + r * a.chunks + ch);
+          st = join(st, Stat{p.x, p.y, p.z}, c);
+          if (a.top > 0) head[j] = keys[ch * a.top];
+        }
       }
-      if (rank < a.top) top[rank] = k;
+      for (int i = 0; i < a.top; ++i) {
+        const uint64_t k = head[0] > head[1] ? head[0] : head[1];
+        const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32));
+        const uint32_t lo =
+            __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
+        const uint64_t best = (uint64_t)hi << 32 | lo;
+        if (lane == 0) top[i] = best;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          if (best && head[j] == best) {
+            ++at[j];
+            head[j] = at[j] < a.top ? keys[(lane + 32 * j) * a.top + at[j]] : 0ull;
+          }
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        Stat b;
+        b.m = __shfl_down_sync(0xffffffffu, st.m, o);
+        b.S = __shfl_down_sync(0xffffffffu, st.S, o);
+        b.T = __shfl_down_sync(0xffffffffu, st.T, o);
+        st = join(st, b, c);
+      }
+      st.m = __shfl_sync(0xffffffffu, st.m, 0);
+      st.S = __shfl_sync(0xffffffffu, st.S, 0);
+      st.T = __shfl_sync(0xffffffffu, st.T, 0);
+      __syncwarp();
+      finish_row<T>(a, (int)r, static_cast<const T*>(a.z) + r * a.stride, st, top, 32);
     }
-    __syncthreads();
-    Stat st{0.f, 0.f, 0.f};
-    for (int ch = 0; ch < a.chunks; ++ch) {
-      const float4 p = part[ch];
-      st = join(st, Stat{p.x, p.y, p.z}, a.inv_t * 1.4426950408889634f);
-    }
-    finish_row<T>(a, (int)r, static_cast<const T*>(a.z) + r * a.stride, st, top);
     __syncthreads();
   }
 }
 
 namespace {
 
-// Chunks of a row.
+// Chunks of a row: blocks enough for four on each of 152 SMs, and no chunk below 4096
+// logits (one step of a block for fp32, half of one for bf16).
 int logp_chunks(int rows, int vocab) {
-  const int per = kLThreads * kUnroll * 8;  // logits of a block's one step, at most
+  constexpr int per = kLThreads * kUnroll * 4;
   const int most = (vocab + per - 1) / per;
   int n = (152 * 4 + rows - 1) / rows;
   n = n < most ? n : most;
@@ -493,7 +560,7 @@ cudaError_t logp_launch(const LogpArgs& a, cudaStream_t st) {
   if (e != cudaSuccess || a.chunks == 1) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(gy);
-  cfg.blockDim = dim3(kLThreads);
+  cfg.blockDim = dim3(kJThreads);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -192,3 +192,15 @@ def test_rows_past_32_bits():
     part = type(got)(*[x[-3:] if x is not None else None for x in got])
     _check(last, tok[-3:], 1.0, 2, part)
     assert abs(float(got.lse[0]) - np.log(V)) < 1e-5 and got.top_id[0].tolist() == [0, 1]
+
+
+def test_many_rows_of_fp32_and_parts_of_steps():
+    """A block a row with a step in advance: rows that end within a step, at odd places."""
+    import torch
+    for V in (1023, 4096, 4100, 9001, 12288):
+        g = torch.Generator(device="cuda").manual_seed(V)
+        flat = torch.randn(700 * (V + 3), generator=g, device="cuda") * 3
+        z = flat.view(700, V + 3)[:, 1:V + 1]
+        tok = torch.randint(0, V, (700, 1), generator=g, device="cuda").int()
+        _check(z[:50], tok[:50], 0.8, 9, type(_run(z[:1]))(*[
+            x[:50] if x is not None else None for x in _run(z, tok, top_n=9, temperature=0.8)]))
