@@ -29,20 +29,49 @@ struct AppendArgs {
   int32_t M, heads, max_seq;
 };
 
-// Eight values of a row from p (16-byte aligned).
+// Eight values of a row as they stand in memory.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&f)[8]);
+struct Eight {
+  static constexpr int kWords = sizeof(T) / 2;  // 16-byte words
+  uint4 w[kWords];
+  __device__ __forceinline__ void load(const T* p) {  // 16-byte aligned
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ void values(float (&f)[8]) const {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      float x[Elem<T>::kPerChunk];
+      Elem<T>::unpack(w[i], x);
+#pragma unroll
+      for (int j = 0; j < Elem<T>::kPerChunk; ++j) f[i * Elem<T>::kPerChunk + j] = x[j];
+    }
+  }
+  // Largest magnitude, NaN aside.
+  __device__ __forceinline__ float amax() const;
+};
 template <>
-__device__ __forceinline__ void load8<float>(const float* p, float (&f)[8]) {
-  const float4 a = __ldg(reinterpret_cast<const float4*>(p));
-  const float4 b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-  f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w;
-  f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+__device__ __forceinline__ float Eight<float>::amax() const {
+  float f[8], m = 0.f;
+  values(f);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(f[j]));
+  return m;
 }
 template <>
-__device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float (&f)[8]) {
-  Elem<__nv_bfloat16>::unpack(__ldg(reinterpret_cast<const uint4*>(p)), f);
+__device__ __forceinline__ float Eight<__nv_bfloat16>::amax() const {
+  const uint32_t u[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+  __nv_bfloat162 m = __float2bfloat162_rn(0.f);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) m = __hmax2(m, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&u[j])));
+  return fmaxf(__low2float(m), __high2float(m));
 }
+
+constexpr float kMaxFloat = 3.4028235e38f;
 
 __device__ __forceinline__ uint2 codes8(const float (&f)[8]) {
   uint2 r;
@@ -72,35 +101,43 @@ __global__ void __launch_bounds__(kApThreads) k_kv8_append(const AppendArgs a) {
   const T* x = static_cast<const T*>(a.x[side]) + (int64_t)h * HD;
   const int64_t row0 = (int64_t)b * a.M + (k0 - p0);  // input row of position k0
 
-  float f[kPer][8];
-  float amax = 0.f;
+  Eight<T> f[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int c = tid + i * kApThreads, r = c / kCpr, off = (c % kCpr) * 8;
-    if (r >= lo && r < hi) {
-      load8<T>(x + (row0 + r) * a.stride + off, f[i]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) f[i][j] = 0.f;
-    }
+    if (r >= lo && r < hi) f[i].load(x + (row0 + r) * a.stride + off);
+    else f[i].zero();
   }
-#pragma unroll
-  for (int i = 0; i < kPer; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      // an infinity has no code: it is kept as NaN, and takes no part in the scale
-      if (!(fabsf(f[i][j]) <= 3.4028235e38f)) f[i][j] = __uint_as_float(0x7fffffffu);
-      amax = fmaxf(amax, fabsf(f[i][j]));
-    }
   const size_t slab = (size_t)b * a.heads + h;
   float* sp = a.scale[side] + slab * (a.max_seq / kKv8Block) + blk;
   const float old = lo > 0 ? *sp : 0.f;  // positions in front of lo hold codes at this scale
-  __shared__ float warp_amax[kApThreads / 32];
-  amax = warp_max(amax);
-  if ((tid & 31) == 0) warp_amax[tid >> 5] = amax;
-  __syncthreads();  // (every thread has read the old scale)
+  __shared__ float warp_amax[2][kApThreads / 32];
+  // the block's largest of m
+  auto block_amax = [&](float m, int at) {
+    m = warp_max(m);
+    if ((tid & 31) == 0) warp_amax[at][tid >> 5] = m;
+    __syncthreads();  // (every thread has read the old scale)
 #pragma unroll
-  for (int w = 0; w < kApThreads / 32; ++w) amax = fmaxf(amax, warp_amax[w]);
+    for (int w = 0; w < kApThreads / 32; ++w) m = fmaxf(m, warp_amax[at][w]);
+    return m;
+  };
+  float amax = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) amax = fmaxf(amax, f[i].amax());
+  amax = block_amax(amax, 0);
+  // an infinity has no code: it is kept as NaN, and takes no part in the scale
+  const bool infinite = amax > kMaxFloat;
+  if (infinite) {
+    amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      float v[8];
+      f[i].values(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(v[j]) <= kMaxFloat ? fabsf(v[j]) : 0.f);
+    }
+    amax = block_amax(amax, 1);
+  }
 
   const int e = kv8_scale_exp(amax);
   const float s = fmaxf(pow2i(e), old);
@@ -127,9 +164,14 @@ __global__ void __launch_bounds__(kApThreads) k_kv8_append(const AppendArgs a) {
   for (int i = 0; i < kPer; ++i) {
     const int c = tid + i * kApThreads, r = c / kCpr, off = (c % kCpr) * 8;
     if (r < lo || r >= hi) continue;
+    float v[8];
+    f[i].values(v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[i][j] *= inv;
-    *reinterpret_cast<uint2*>(code + (size_t)r * HD + off) = codes8(f[i]);
+    for (int j = 0; j < 8; ++j) {
+      if (infinite && !(fabsf(v[j]) <= kMaxFloat)) v[j] = __uint_as_float(0x7fffffffu);
+      v[j] *= inv;
+    }
+    *reinterpret_cast<uint2*>(code + (size_t)r * HD + off) = codes8(v);
   }
   if (tid == 0) *sp = s;
 }

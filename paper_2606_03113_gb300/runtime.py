@@ -483,8 +483,10 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top
         top = torch.empty((n, top_n), dtype=torch.float32, device=dev)
         ip, lp_top = ids.data_ptr(), top.data_ptr()
     nbytes = _logprobs_bytes(n, vocab, top_n)
-    work = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    # (256: rows that a block reads alone need none; it stays this call's until the launches)
+    work = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes > 256 else None
     S.ssd_token_logprobs(zp, code, n, vocab, logits.stride(0) if n > 1 else vocab, tp, ntok,
                          temperature, top_n, lpp, lse.data_ptr(), entropy.data_ptr(), ip, lp_top,
-                         work.data_ptr(), nbytes, ep, _current_stream(dev.index))
+                         work.data_ptr() if work is not None else 0, nbytes, ep,
+                         _current_stream(dev.index))
     return TokenLogprobs(lp, lse, entropy, ids, top, err)
