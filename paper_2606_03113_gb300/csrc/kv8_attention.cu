@@ -4,7 +4,7 @@
 // over the keys j that row r sees: first .. its own position, at most `window`.
 //
 // k_kv8_rows: a block takes a stretch of the plan's units (kv8_plan.cuh); its
-// eight warps take the 16-key steps of an item in turn, each with its own running
+// four warps take the 16-key steps of an item in turn, each with its own running
 // maximum, sum and output, and the block joins the warps once per item.  Queries
 // and probabilities are f16 operands of mma.sync against the codes, which f16
 // holds exactly; a row of queries is first brought near f16's upper end by a
@@ -38,14 +38,9 @@ namespace {
 
 constexpr int kRT = 16;       // query rows of a tile
 constexpr int kStep = 16;     // keys of a warp's step
-#ifndef KVW
-#define KVW 4
-#define KVR 5
-#define KVB 2
-#endif
-constexpr int kRing = KVR;      // steps in flight per warp
-constexpr int kVWarps = KVW;
-constexpr int kVBlocks = KVB;   // blocks of an SM
+constexpr int kRing = 5;      // steps in flight per warp
+constexpr int kVWarps = 4;
+constexpr int kVBlocks = 2;   // blocks of an SM
 constexpr int kVThreads = kVWarps * 32;
 constexpr int kKv8MaxBlocks = 320;
 
@@ -143,7 +138,7 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
 
   Kv8Cursor cur = kv8_plan<kRT, kKv8Block, kVThreads>(a, s_plan);
   pdl_launch_dependents();
-  if (tid == 0) a.desc[blockIdx.x].nr = 0;
+  if (tid == 0 && !a.whole) a.desc[blockIdx.x].nr = 0;
   Kv8Seg sg;
   while (kv8_next<kRT, kKv8Block>(a, cur, sg)) {
     const Kv8Item& it = sg.it;
@@ -724,7 +719,7 @@ cudaError_t rows_launch(const Kv8Attn& a, int P, cudaStream_t st) {
   const size_t smem = RowsL<HD>::template total<sizeof(T) == 4 ? 2 : 1>();
   k_kv8_rows<T, HD><<<P, kVThreads, smem, st>>>(a);
   const cudaError_t e = cudaGetLastError();
-  return e != cudaSuccess ? e : merge_launch<T, HD, kRT>(a, P, st);
+  return e != cudaSuccess || a.whole ? e : merge_launch<T, HD, kRT>(a, P, st);
 }
 
 cudaError_t wide_launch(const Kv8Attn& a, int P, cudaStream_t st) {
@@ -733,11 +728,39 @@ cudaError_t wide_launch(const Kv8Attn& a, int P, cudaStream_t st) {
   return e != cudaSuccess ? e : merge_launch<__nv_bfloat16, kWHd, kWRows>(a, P, st);
 }
 
-// The kernel of a call: tiles of 128 rows on tcgen05 where a KV head has more
-// query rows than kWideFrom and the type is bf16, tiles of 16 on mma.sync otherwise.
+// The kernel of a call.  Tiles of 128 rows on tcgen05 where a KV head has more
+// than 16 query rows, the type is bf16 and head_dim 128; tiles of 16 on mma.sync
+// otherwise.  us a call, mma.sync / tcgen05, by rows of 8 KV heads (of 32 in the last
+// line):          16           17           32           48          128
+//   500 keys   10.3/12.7    11.0/12.9    11.1/13.7    11.9/14.2    17.6/17.4
+//   16000      18.8/22.9    28.5/23.1    28.9/24.5    34.9/25.5    63.7/35.1
+//   100000     51.4/64.9    90.6/65.1    90.6/66.6     126/67.8     293/81.3
+//   16 x 1000  58.7/71.0    97.7/72.6    99.7/79.6     146/82.7     369/103
 constexpr int kWideFrom = 16;
-bool kv8_is_wide(int dtype, int hd, long long rows) {
-  return dtype == SSD_DTYPE_BF16 && hd == kWHd && rows > kWideFrom;
+// Caches of up to 512 positions: a block for each item and no join (mma.sync kernel).  us,
+// shared / whole, at full caches of 128, 256, 512 and 1024 positions:
+//   1 sequence, 8 KV heads, 4 rows each     8.3/5.9   8.4/7.1    8.6/9.5    8.9/14.1
+//   1, 40 heads, 2 rows                     8.7/6.1   9.0/7.3    9.8/9.5   11.0/14.2
+//   16, 8 heads, 4 rows                    10.5/6.0  12.7/7.3   15.1/9.7   17.8/14.4
+//   32, 32 heads, 1 row                    23.8/22.0 30.0/28.8  42.8/44.7  64.2/68.1
+// and a launch less, which the host takes 2 to 3 us for.
+constexpr int kWholeSeq = 512;
+
+struct Kv8Plan {
+  bool wide, whole;
+  int rt, ku;
+  long long n_rt, units;  // tiles of a sequence; the line's places, at most
+};
+Kv8Plan plan_of(const ssd_kv8_cache* c, int dtype, int n_heads, int M) {
+  Kv8Plan p;
+  const long long rows = (long long)M * (n_heads / c->n_kv_heads);
+  p.wide = dtype == SSD_DTYPE_BF16 && c->head_dim == kWHd && rows > kWideFrom;
+  p.whole = !p.wide && c->max_seq <= kWholeSeq;
+  p.rt = p.wide ? kWRows : kRT;
+  p.ku = p.wide ? kWKeys : kKv8Block;
+  p.n_rt = (rows + p.rt - 1) / p.rt;
+  p.units = p.n_rt * c->n_seq * c->n_kv_heads * ((c->max_seq + p.ku - 1) / p.ku + kKv8ItemCost);
+  return p;
 }
 
 // What both attention entry points check; null: fine.
@@ -760,8 +783,8 @@ extern "C" size_t ssd_kv8_attention_bytes(const ssd_kv8_cache* c, int32_t dtype,
     fail_op(SSD_ERR_INVALID_ARG, why);
     return 0;
   }
-  const bool wide = kv8_is_wide(dtype, c->head_dim, (long long)M * (n_heads / c->n_kv_heads));
-  return kv8_work(kKv8MaxBlocks, wide ? kWRows : kRT, c->head_dim).total;
+  const Kv8Plan p = plan_of(c, dtype, n_heads, M);
+  return p.whole ? 256 : kv8_work(kKv8MaxBlocks, p.rt, c->head_dim).total;
 }
 
 extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, int32_t dtype,
@@ -785,16 +808,13 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   if (window < 0) return fail_op(SSD_ERR_INVALID_ARG, "window must be 0 (none) or positive");
   if (M > c->max_seq) return fail_op(SSD_ERR_CAPACITY, "more rows than the cache has positions");
   const int G = n_heads / c->n_kv_heads;
-  const bool tc = kv8_is_wide(dtype, c->head_dim, (long long)M * G);
-  const int rt = tc ? kWRows : kRT, ku = tc ? kWKeys : kKv8Block;
-  const long long n_rt = ((long long)M * G + rt - 1) / rt;
-  const long long units = n_rt * c->n_seq * c->n_kv_heads * ((c->max_seq + ku - 1) / ku + kKv8ItemCost);
-  if (units > 0x7fffffffll)
+  const Kv8Plan plan = plan_of(c, dtype, n_heads, M);
+  if (plan.units > 0x7fffffffll)
     return fail_op(SSD_ERR_CAPACITY, "n_seq x M x max_seq: more than 2^31 units of work");
-  const Kv8Work lay = kv8_work(kKv8MaxBlocks, rt, c->head_dim);
+  const Kv8Work lay = kv8_work(kKv8MaxBlocks, plan.rt, c->head_dim);
   if (!workspace || ((uintptr_t)workspace & 255u))
     return fail_op(SSD_ERR_INVALID_ARG, "workspace must be non-NULL and 256-byte aligned");
-  if (workspace_bytes < lay.total) return fail_op(SSD_ERR_CAPACITY, "workspace too small");
+  if (workspace_bytes < (plan.whole ? 256 : lay.total)) return fail_op(SSD_ERR_CAPACITY, "workspace too small");
   int sms = 0;
   cudaError_t e = kv8_device(&sms);
   if (e != cudaSuccess) return fail_op_cuda("ssd_kv8_attention", e);
@@ -817,22 +837,24 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   a.M = M;
   a.max_seq = c->max_seq;
   a.window = window;
-  a.n_rt = (int)n_rt;
-  a.entries = (int)n_rt * c->n_seq;
+  a.n_rt = (int)plan.n_rt;
+  a.entries = (int)plan.n_rt * c->n_seq;
   a.scale = (float)(1.4426950408889634 / sqrt((double)c->head_dim));
   char* ws = static_cast<char*>(workspace);
   a.desc = reinterpret_cast<Kv8Desc*>(ws);
   a.ml = reinterpret_cast<float2*>(ws + lay.ml);
   a.part = reinterpret_cast<float*>(ws + lay.part);
   a.byG = Kv8Div::of((uint32_t)G);
-  a.byRt = Kv8Div::of((uint32_t)n_rt);
-  int P = sms * (tc ? 2 : kVBlocks);
+  a.byRt = Kv8Div::of((uint32_t)plan.n_rt);
+  int P = sms * (plan.wide ? 2 : kVBlocks);
   if (P > kKv8MaxBlocks) P = kKv8MaxBlocks;
-  if (units < P) P = (int)units;
+  if (plan.units < P) P = (int)plan.units;
+  a.whole = plan.whole;
+  if (plan.whole) P = a.entries * a.Hkv;
   a.byP = Kv8Div::of((uint32_t)P);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool wide = c->head_dim == 128;
-  if (tc)
+  if (plan.wide)
     e = wide_launch(a, P, st);
   else if (dtype == SSD_DTYPE_BF16)
     e = wide ? rows_launch<__nv_bfloat16, 128>(a, P, st) : rows_launch<__nv_bfloat16, 64>(a, P, st);

@@ -44,6 +44,7 @@ struct Kv8Attn {
   int32_t* err;
   int64_t q_stride, out_stride;  // elements between rows
   int32_t n_seq, Hkv, G, M, max_seq, window, n_rt, entries;
+  int32_t whole;  // a block for each item, which is not shared: no parts
   float scale;  // log2(e) / sqrt(head_dim)
   struct Kv8Desc* desc;
   float* part;  // [2 P][RT][hd] normalised partial outputs
@@ -83,7 +84,7 @@ __device__ __forceinline__ Kv8Item kv8_entry(const Kv8Attn& a, int e) {
   it.nr = 0;
   it.units = it.unit0 = it.lo = it.hi = 0;
   if (it.pos < 0 || n < 0 || n > a.M || it.pos > a.max_seq - n) {
-    if (it.rt == 0 && blockIdx.x == 0 && a.err)
+    if (it.rt == 0 && (blockIdx.x == 0 || a.whole) && a.err)
       atomicOr(a.err, n < 0 || n > a.M ? (int)kErrControl : (int)kErrCapacity);
     return it;
   }
@@ -141,6 +142,11 @@ template <int RT, int KU, int THREADS>
 __device__ __forceinline__ Kv8Cursor kv8_plan(const Kv8Attn& a, Kv8PlanSmem& sm) {
   static_assert(THREADS / 32 <= 16, "a sum for each warp");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (a.whole) {
+    const int e = (int)blockIdx.x / a.Hkv, g = (int)blockIdx.x - e * a.Hkv;
+    const Kv8Item own = kv8_entry<RT, KU>(a, e);
+    return Kv8Cursor{0, own.units, 0, e, g * kv8_len<RT, KU>(own)};
+  }
   const int per = (a.entries + THREADS - 1) / THREADS;
   const int e0 = min(tid * per, a.entries), e1 = min(e0 + per, a.entries);
   int sum = 0;

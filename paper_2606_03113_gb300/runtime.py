@@ -271,9 +271,11 @@ def _per_seq(t, n_seq: int, device: torch.device, what: str) -> int:
     """The address of an int32 [n_seq] tensor, or 0 for None."""
     if t is None:
         return 0
-    if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n_seq or not t.is_contiguous():
+    if t.dtype is not torch.int32 or t.shape != (n_seq,) or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous int32 tensor of {n_seq} elements")
-    return _on(t, device, what)
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, not on {device}")
+    return t.data_ptr()
 
 
 # The address of a device's current stream (its index given), without a Stream object.
@@ -336,17 +338,16 @@ class KV8Cache:
 
     def _rows(self, x: torch.Tensor, heads: int, what: str) -> tuple[int, int]:
         """(M, elements between rows) of x [n_seq, M, heads, head_dim]."""
-        if x.dim() != 4 or x.shape[0] != self.n_seq or x.shape[2] != heads or \
-                x.shape[3] != self.head_dim or x.shape[1] < 1:
-            raise ValueError(f"{what} must be [{self.n_seq}, M, {heads}, {self.head_dim}], "
-                             f"not {list(x.shape)}")
-        s0, s1, s2, s3 = x.stride()
-        M = x.shape[1]
-        row = s1 if M > 1 else (s0 if self.n_seq > 1 else heads * self.head_dim)
-        if s3 != 1 or (heads > 1 and s2 != self.head_dim) or \
-                (self.n_seq > 1 and s0 != M * row):
+        shape, strides = x.shape, x.stride()
+        n, hd = self.n_seq, self.head_dim
+        if len(shape) != 4 or shape[0] != n or shape[2] != heads or shape[3] != hd or shape[1] < 1:
+            raise ValueError(f"{what} must be [{n}, M, {heads}, {hd}], not {list(shape)}")
+        s0, s1, s2, s3 = strides
+        M = shape[1]
+        row = s1 if M > 1 else (s0 if n > 1 else heads * hd)
+        if s3 != 1 or (s2 != hd and heads > 1) or (n > 1 and s0 != M * row):
             raise ValueError(f"{what}: a row's heads must lie one behind the other, and the rows "
-                             f"of all sequences at one distance; strides are {x.stride()}")
+                             f"of all sequences at one distance; strides are {strides}")
         return M, row
 
     def append(self, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
@@ -377,8 +378,8 @@ class KV8Cache:
         """softmax(q k^T / sqrt(head_dim)) v for q [n_seq, M, n_heads, head_dim]: row m < rows[b]
         of sequence b sits at position pos[b] + m, whose key has been appended, and sees the keys
         up to its own from first[b] on, at most `window` of them (0: all).  A row that sees
-        none is zero.  Returns `out` (a new tensor without it, whose rows from rows[b] on are
-        zero; a given one keeps them)."""
+        none is zero.  Returns `out`, which keeps its rows from rows[b] on; without it a new
+        tensor, where those are zero (a sequence with bad positions leaves its own unset)."""
         code = _dtype_code(q, "q")
         heads = q.shape[2] if q.dim() == 4 else 0
         M, row = self._rows(q, heads, "q")
@@ -420,6 +421,7 @@ class KV8Cache:
     def check(self):
         """Waits for the device and raises SsdError if a call since the last check found bad
         positions or row numbers there."""
+        torch.cuda.synchronize(self.device)
         bits = int(self.err.item())
         if bits:
             self.err.zero_()

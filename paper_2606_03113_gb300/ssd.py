@@ -307,12 +307,16 @@ def ssd_gemv_noalloc(w_ptr: int, dtype: int, rows: int, cols: int, x_ptr: int, M
                                   stream_ptr or None), "ssd_gemv_noalloc")
 
 
+# The operators over an 8-bit cache and over logits are called once or more a token: these take
+# addresses of 0 as NULL as they are, and look at the status before anything else.
+
 def ssd_kv8_append(cache: ssd_kv8_cache, k_ptr: int, v_ptr: int, dtype: int, row_stride: int, M: int,
                    pos_ptr: int, rows_ptr: int = 0, err_ptr: int = 0, stream_ptr: int = 0):
     """Rows of K and V into the 8-bit cache (see ssd_ops.h)."""
-    _check(lib().ssd_kv8_append(C.addressof(cache), k_ptr, v_ptr, dtype, row_stride, M, pos_ptr,
-                                rows_ptr or None, err_ptr or None, stream_ptr or None),
-           "ssd_kv8_append")
+    st = (_lib or lib()).ssd_kv8_append(C.addressof(cache), k_ptr, v_ptr, dtype, row_stride, M, pos_ptr,
+                                        rows_ptr, err_ptr, stream_ptr)
+    if st:
+        _check(st, "ssd_kv8_append")
 
 
 def ssd_kv8_attention_bytes(cache: ssd_kv8_cache, dtype: int, n_heads: int, M: int) -> int:
@@ -324,10 +328,11 @@ def ssd_kv8_attention(cache: ssd_kv8_cache, q_ptr: int, dtype: int, n_heads: int
                       out_stride: int, workspace_ptr: int, workspace_bytes: int, err_ptr: int = 0,
                       stream_ptr: int = 0):
     """Attention of new rows over the 8-bit cache (see ssd_ops.h)."""
-    _check(lib().ssd_kv8_attention(C.addressof(cache), q_ptr, dtype, n_heads, q_stride, M, pos_ptr,
-                                   rows_ptr or None, first_ptr or None, window, out_ptr, out_stride,
-                                   workspace_ptr, workspace_bytes, err_ptr or None,
-                                   stream_ptr or None), "ssd_kv8_attention")
+    st = (_lib or lib()).ssd_kv8_attention(C.addressof(cache), q_ptr, dtype, n_heads, q_stride, M,
+                                           pos_ptr, rows_ptr, first_ptr, window, out_ptr, out_stride,
+                                           workspace_ptr, workspace_bytes, err_ptr, stream_ptr)
+    if st:
+        _check(st, "ssd_kv8_attention")
 
 
 def ssd_token_logprobs_bytes(n_rows: int, vocab: int, top_n: int) -> int:
@@ -340,12 +345,12 @@ def ssd_token_logprobs(logits_ptr: int, dtype: int, n_rows: int, vocab: int, row
                        top_logprob_ptr: int, workspace_ptr: int, workspace_bytes: int,
                        err_ptr: int = 0, stream_ptr: int = 0):
     """Log-probabilities, entropy and most probable tokens of rows of logits (see ssd_ops.h)."""
-    _check(lib().ssd_token_logprobs(logits_ptr, dtype, n_rows, vocab, row_stride, tokens_ptr or None,
-                                    n_tokens, temperature, top_n, logprob_ptr or None,
-                                    lse_ptr or None, entropy_ptr or None, top_id_ptr or None,
-                                    top_logprob_ptr or None, workspace_ptr or None,
-                                    workspace_bytes, err_ptr or None, stream_ptr or None),
-           "ssd_token_logprobs")
+    st = (_lib or lib()).ssd_token_logprobs(logits_ptr, dtype, n_rows, vocab, row_stride, tokens_ptr,
+                                            n_tokens, temperature, top_n, logprob_ptr, lse_ptr,
+                                            entropy_ptr, top_id_ptr, top_logprob_ptr, workspace_ptr,
+                                            workspace_bytes, err_ptr, stream_ptr)
+    if st:
+        _check(st, "ssd_token_logprobs")
 
 
 def ssd_synth_fill(dst_ptr: int, dtype: int, n: int, seed: int, tid: int, sigma: float,

@@ -169,6 +169,12 @@ ATTEND = [  # dtype, heads, kv heads, hd, n, M, seq, pos, rows, first, window
     ("bf16", 8, 1, 64, 2, 40, 256, [130, 0], [39, 40], [7, 0], 90),
     ("bf16", 5, 5, 128, 9, 1, 128, [127, 64, 63, 1, 0, 100, 90, 80, 70], [1] * 9, [0] * 9, 0),
     ("f32", 16, 2, 128, 1, 33, 192, [150], [33], [0], 0),
+    ("bf16", 8, 8, 64, 3, 2, 1024, [1000, 5, 513], [2, 2, 1], [0, 0, 400], 0),
+    ("f32", 6, 3, 64, 2, 4, 960, [950, 700], [4, 4], [10, 0], 300),
+    ("bf16", 16, 2, 128, 2, 30, 1088, [1058, 3], [30, 7], [0, 0], 500),
+    ("bf16", 4, 1, 128, 1, 160, 896, [730], [160], [729], 0),
+    ("bf16", 4, 2, 128, 300, 1, 640, [(37 * i) % 640 for i in range(300)], [1] * 300,
+     [(11 * i) % 90 for i in range(300)], 0),
 ]
 
 
@@ -200,9 +206,12 @@ def _check(case, q, vals, got, before):
     assert not bad[live].any(), (np.abs(out - ref)[live].max(), np.argwhere(bad)[:5])
 
 
+@pytest.mark.parametrize("room", [0, 640])
 @pytest.mark.parametrize("case", ATTEND, ids=lambda c: "-".join(str(x) for x in c[:7]))
-def test_attention_against_64_bits(case):
+def test_attention_against_64_bits(case, room):
+    """Also in a larger cache, where blocks share items and their parts are joined."""
     torch = _torch()
+    case = case[:6] + (case[6] + room,) + case[7:]
     dtype, heads, kvh, hd, n, M, seq, pos, rows, first, window = case
     dt = torch.float32 if dtype == "f32" else torch.bfloat16
     out = torch.full((n, M, heads + 1, hd), 0.625, device="cuda", dtype=dt)[:, :, :heads]
@@ -218,10 +227,11 @@ def test_attention_against_64_bits(case):
 
 @pytest.mark.parametrize("M,window", [(4, 0), (4, 3), (17, 0), (70, 0)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_a_nan_value_reaches_the_rows_that_see_it(dtype, M, window):
+@pytest.mark.parametrize("seq", [320, 1024])
+def test_a_nan_value_reaches_the_rows_that_see_it(dtype, M, window, seq):
     """NaN codes of keys and values: rows that do not see the key are as if it were not there."""
     torch = _torch()
-    case = (dtype, 8, 2, 128, 1, M, 320, [200], [M], [0], window)
+    case = (dtype, 8, 2, 128, 1, M, seq, [200], [M], [0], window)
     _, q, vals, clean = _attend(case, 5)
     c, _, _, _ = _attend(case, 5, q=q)
     at = 200 + M - 2  # the last row but one's own key
@@ -292,10 +302,15 @@ def test_scores_far_apart_and_scales_far_apart():
 def test_attention_leaves_bad_sequences_alone():
     from paper_2606_03113_gb300 import ssd as S
     torch = _torch()
-    c = _cache(2, 128, 128, n=5)
+    for seq in (128, 1024):
+        _bad_sequences(S, torch, seq)
+
+
+def _bad_sequences(S, torch, seq):
+    c = _cache(2, 128, seq, n=5)
     out = torch.full((5, 3, 4, 128), 5.0, device="cuda", dtype=torch.bfloat16)
     q = torch.ones_like(out)
-    c.attention(q, _ints([-1, 126, 0, 2 ** 31 - 1, 5]), rows=_ints([3, 3, 4, 1, 3]), out=out)
+    c.attention(q, _ints([-1, seq - 2, 0, 2 ** 31 - 1, 5]), rows=_ints([3, 3, 4, 1, 3]), out=out)
     with pytest.raises(S.SsdError):
         c.check()
     assert bool((out[:4] == 5.0).all()) and not bool((out[4] == 5.0).any())

@@ -17,7 +17,7 @@ BUF = 0x7f0000000000  # an address that is only looked at
 
 
 def cache(**kw):
-    base = dict(n_seq=2, n_kv_heads=4, head_dim=128, max_seq=256, k=BUF, v=BUF, k_scale=BUF,
+    base = dict(n_seq=2, n_kv_heads=4, head_dim=128, max_seq=1024, k=BUF, v=BUF, k_scale=BUF,
                 v_scale=BUF)
     base.update(kw)
     return S.ssd_kv8_cache(**base)
@@ -64,7 +64,7 @@ def test_bad_caches_are_refused(bad, status):
     (dict(k=0), S.SSD_ERR_INVALID_ARG), (dict(v=BUF + 4), S.SSD_ERR_INVALID_ARG),
     (dict(dtype=2), S.SSD_ERR_INVALID_ARG), (dict(stride=511), S.SSD_ERR_INVALID_ARG),
     (dict(stride=516), S.SSD_ERR_INVALID_ARG), (dict(stride=-512), S.SSD_ERR_INVALID_ARG),
-    (dict(M=0), S.SSD_ERR_INVALID_ARG), (dict(M=257), S.SSD_ERR_CAPACITY),
+    (dict(M=0), S.SSD_ERR_INVALID_ARG), (dict(M=1025), S.SSD_ERR_CAPACITY),
     (dict(pos=0), S.SSD_ERR_INVALID_ARG)])
 def test_append_refuses(kw, status):
     a = dict(k=BUF, v=BUF, dtype=S.SSD_DTYPE_BF16, stride=512, M=1, pos=BUF)
@@ -82,7 +82,7 @@ def test_append_refuses(kw, status):
     (dict(heads=6), S.SSD_ERR_INVALID_ARG), (dict(heads=0), S.SSD_ERR_INVALID_ARG),
     (dict(heads=2), S.SSD_ERR_INVALID_ARG), (dict(qs=1020), S.SSD_ERR_INVALID_ARG),
     (dict(os=1028), S.SSD_ERR_INVALID_ARG), (dict(M=0), S.SSD_ERR_INVALID_ARG),
-    (dict(M=300), S.SSD_ERR_CAPACITY), (dict(window=-1), S.SSD_ERR_INVALID_ARG),
+    (dict(M=1030), S.SSD_ERR_CAPACITY), (dict(window=-1), S.SSD_ERR_INVALID_ARG),
     (dict(pos=0), S.SSD_ERR_INVALID_ARG), (dict(ws=0), S.SSD_ERR_INVALID_ARG),
     (dict(ws=BUF + 16), S.SSD_ERR_INVALID_ARG), (dict(wb=1000), S.SSD_ERR_CAPACITY)])
 def test_attention_refuses(kw, status):
@@ -96,6 +96,18 @@ def test_attention_refuses(kw, status):
     with pytest.raises(S.SsdError) as e:  # more than 2^31 units of work
         S.ssd_kv8_attention(cache(max_seq=1 << 30, n_seq=4096), BUF, S.SSD_DTYPE_BF16, 8, 1024, 64, BUF,
                             0, 0, 0, BUF, 1024, BUF, 1 << 40)
+    assert e.value.status == S.SSD_ERR_CAPACITY
+
+
+def test_attention_workspace_sizes():
+    """Small caches need none to speak of, others the same for every length."""
+    assert S.ssd_kv8_attention_bytes(cache(max_seq=512), S.SSD_DTYPE_BF16, 8, 1) == 256
+    few = S.ssd_kv8_attention_bytes(cache(max_seq=576), S.SSD_DTYPE_BF16, 8, 1)
+    assert few == S.ssd_kv8_attention_bytes(cache(max_seq=1 << 20), S.SSD_DTYPE_BF16, 8, 8) > 256
+    assert S.ssd_kv8_attention_bytes(cache(max_seq=576), S.SSD_DTYPE_BF16, 8, 9) > few
+    with pytest.raises(S.SsdError) as e:
+        S.ssd_kv8_attention(cache(max_seq=512), BUF, S.SSD_DTYPE_BF16, 8, 1024, 1, BUF, 0, 0, 0, BUF, 1024,
+                            BUF, 255)
     assert e.value.status == S.SSD_ERR_CAPACITY
 
 
