@@ -52,12 +52,6 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// 2^x, as close as the hardware's instruction (2 ulp; a result below 2^-126 is 0).
-__device__ __forceinline__ float ex2_approx(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 __device__ __forceinline__ uint32_t half2_bits(float x, float y) {
   const __half2 h = __floats2half2_rn(x, y);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -127,7 +121,7 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
   extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ Kv8PlanSmem s_plan;
   __shared__ float s_qs[kRT];  // scores = dot * s_qs * key scale
-  __shared__ float s_m[kVWarps][kRT], s_l[kVWarps][kRT], s_ref[kVWarps];
+  __shared__ float s_m[kVWarps][kRT], s_l[kVWarps][kRT], s_ref[kVWarps][kRT];
   __shared__ float s_w[kVWarps][kRT], s_gm[kRT], s_sum[kRT];  // the warps' weights, the row's (max, sum)
   __shared__ int s_nan;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -234,7 +228,6 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
     }
     __syncthreads();
 
-
     int plo[2], phi[2];
     float qs[2];
 #pragma unroll
@@ -257,9 +250,9 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[j][i] = 0.f;
-    // running maximum and sum of the lane's rows; the output stands in units
-    // of ref, the largest value scale so far
-    float mx[2] = {-INFINITY, -INFINITY}, ls[2] = {0.f, 0.f}, ref = pow2i(-126);
+    // running maximum and sum of the lane's rows; a row's output stands in units of
+    // the largest value scale that it has seen, rref is one over that
+    float mx[2] = {-INFINITY, -INFINITY}, ls[2] = {0.f, 0.f}, rref[2] = {pow2i(126), pow2i(126)};
     for (int s = warp; s < nsteps; s += kVWarps) {
       __syncwarp();  // every lane has read the step whose place is filled now
       issue(s + (kRing - 1) * kVWarps);
@@ -326,32 +319,37 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
           nm[x >> 1] = fmaxf(nm[x >> 1], z[n][x]);
         }
       float f[2];
-      bool moved = vs > ref;
+      bool moved = false, up[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         nm[i] = fmaxf(nm[i], __shfl_xor_sync(0xffffffffu, nm[i], 1));
         nm[i] = fmaxf(nm[i], __shfl_xor_sync(0xffffffffu, nm[i], 2));
+        up[i] = vs * rref[i] > 1.f && nm[i] > -INFINITY;
         nm[i] = fmaxf(nm[i], mx[i]);
         f[i] = nm[i] == mx[i] ? 1.f : exp2f(mx[i] - nm[i]);
-        moved |= nm[i] != mx[i];
+        moved |= nm[i] != mx[i] || up[i];
         mx[i] = nm[i];
         ls[i] *= f[i];
       }
       if (__any_sync(0xffffffffu, moved)) {
-        const float down = vs > ref ? ref / vs : 1.f;
-        if (vs > ref) ref = vs;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (up[i]) {
+            f[i] *= 1.f / (vs * rref[i]);
+            rref[i] = 1.f / vs;
+          }
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) o[j][x] *= f[x >> 1] * down;
+          for (int x = 0; x < 4; ++x) o[j][x] *= f[x >> 1];
       }
-      const float vrel = vs / ref;
       uint32_t pf[PARTS][4];
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const float top = mx[i] == -INFINITY ? 0.f : mx[i] - 15.f;
+          const float vrel = fminf(vs * rref[i], 1.f);  // (above 1: a row that sees no key here)
           const float x = exp2f(z[n][2 * i] - top), y = exp2f(z[n][2 * i + 1] - top);
           ls[i] += x + y;
           pf[0][2 * n + i] = half2_bits(x * vrel, y * vrel);
@@ -415,9 +413,9 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
       if (t == 0) {
         s_m[warp][n8 + 8 * i] = mx[i];
         s_l[warp][n8 + 8 * i] = ls[i];
+        s_ref[warp][n8 + 8 * i] = 1.f / rref[i];
       }
     }
-    if (lane == 0) s_ref[warp] = ref;
     __syncthreads();  // nobody reads the ring any more
     const int nw = min(nsteps, kVWarps);
     if (tid < kRT) {
@@ -456,7 +454,7 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] = 0.f;
         for (int x = 0; x < nw; ++x) {
-          const float wt = s_w[x][row], rf = s_ref[x];
+          const float wt = s_w[x][row], rf = s_ref[x][row];
           const float4* ox = reinterpret_cast<const float4*>(Ox + (size_t)(x * kRT + row) * L::kOPad + c8);
           const float4 u = ox[0], w = ox[1];
           // (the weight before the unit: their product can be out of range)
@@ -805,6 +803,8 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
       (q_stride * elt) % 16 || (out_stride * elt) % 16)
     return fail_op(SSD_ERR_INVALID_ARG,
                    "q_stride or out_stride: below a row's length, or not a multiple of 16 bytes");
+  if (out == q && out_stride != q_stride)
+    return fail_op(SSD_ERR_INVALID_ARG, "out is q, but their strides differ");
   if (window < 0) return fail_op(SSD_ERR_INVALID_ARG, "window must be 0 (none) or positive");
   if (M > c->max_seq) return fail_op(SSD_ERR_CAPACITY, "more rows than the cache has positions");
   const int G = n_heads / c->n_kv_heads;

@@ -175,28 +175,6 @@ __device__ __forceinline__ float w_max3(float x, float y, float z) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
   return r;
 }
-// (x, y) * c + d and sums, two values an instruction.
-__device__ __forceinline__ uint64_t w_pack(float x, float y) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-  return r;
-}
-__device__ __forceinline__ float2 w_unpack(uint64_t v) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
-__device__ __forceinline__ uint64_t w_fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t w_add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-
 // Barriers of the two buffers: keys and values stored, scores there (and the keys'
 // place free), probabilities there, output added (the values' and their place
 // free); queries of the segment stored.
@@ -502,14 +480,15 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
           float mx = fmaxf(w_max3(m[0], m[1], m[2]), m[3]);
           if (mx > -INFINITY) mx *= c;
           const bool grow = mx > ref + kWGrow || (ref == -INFINITY && mx > ref);
-          if (__any_sync(0xffffffffu, grow) || vs > vref) {
+          const bool up = vs > vref && mx > -INFINITY;
+          if (__any_sync(0xffffffffu, grow || up)) {
             float f = 1.f;
             if (grow) {
               f = ref == -INFINITY ? 0.f : exp2f(ref - mx);
               ref = mx;
               ls *= f;
             }
-            if (vs > vref) {
+            if (up) {
               f *= vref / vs;
               vref = vs;
             }
@@ -528,18 +507,18 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
             }
           }
           const float top = ref == -INFINITY ? 0.f : ref - kWBase;
-          const float rel = vs / vref;
-          const uint64_t c2 = w_pack(c, c), t2 = w_pack(-top, -top);
+          const float rel = fminf(vs / vref, 1.f);  // (above 1: a row that sees no key here)
+          const uint64_t c2 = pack2(c, c), t2 = pack2(-top, -top);
           uint64_t sum2 = 0;
 #pragma unroll
           for (int x = 0; x < 64; x += 2) {
             const float2 z =
-                w_unpack(w_fma2(w_pack(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), c2, t2));
+                unpack2(fma2(pack2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), c2, t2));
             float e0 = ex2_approx(z.x), e1 = ex2_approx(z.y);
-            sum2 = w_add2(sum2, w_pack(e0, e1));
+            sum2 = add2(sum2, pack2(e0, e1));
             r[x / 2] = half2_bits(e0 * rel, e1 * rel);
           }
-          const float2 sum = w_unpack(sum2);
+          const float2 sum = unpack2(sum2);
           ls += sum.x + sum.y;
           w_st32(at, r);
           w_st_wait();

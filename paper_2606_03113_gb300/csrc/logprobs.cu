@@ -75,52 +75,19 @@ __device__ __forceinline__ float logit(const T* row, int v) { return Elem<T>::to
 struct Stat {
   float m, S, T;
 };
-// 2^x, as close as the hardware's instruction (2 ulp; a result below 2^-126 is 0).
-__device__ __forceinline__ float ex2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 // Two sets together; c: log2(e) / t.
 __device__ __forceinline__ Stat join(const Stat& a, const Stat& b, float c) {
   if (a.S == 0.f) return b;
   if (b.S == 0.f) return a;
   const float m = fmaxf(a.m, b.m);
   const float da = (a.m - m) * c, db = (b.m - m) * c;
-  const float ea = ex2(da), eb = ex2(db);
+  const float ea = ex2_approx(da), eb = ex2_approx(db);
   Stat r;
   r.m = m;
   r.S = a.S * ea + b.S * eb;
   // (a set 2^126 below the other adds nothing, even where its distance is infinite)
   r.T = (ea > 0.f || ea != ea ? ea * (a.T + da * a.S) : 0.f) +
         (eb > 0.f || eb != eb ? eb * (b.T + db * b.S) : 0.f);
-  return r;
-}
-
-// Two fp32 values as the operand of one packed instruction.
-__device__ __forceinline__ uint64_t pack2(float x, float y) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-  return r;
-}
-__device__ __forceinline__ float2 unpack2(uint64_t v) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
 
@@ -391,7 +358,7 @@ __global__ void __launch_bounds__(kLThreads, kAhead<T> ? 3 : 4) k_logprobs(const
       const float bm = max_of_word(bw, T());
       if (bm > tmax) {
         if (tmax > -INFINITY) {
-          const float d = (tmax - bm) * c, f = ex2(d);
+          const float d = (tmax - bm) * c, f = ex2_approx(d);
           const uint64_t f2 = pack2(f, f);
           T2 = f > 0.f ? mul2(f2, fma2(pack2(d, d), S2, T2)) : 0ull;
           S2 = mul2(f2, S2);
@@ -410,7 +377,7 @@ __global__ void __launch_bounds__(kLThreads, kAhead<T> ? 3 : 4) k_logprobs(const
                                           __uint_as_float(w[j / 2] & 0xffff0000u));
           // (differences first: a row of the type's lowest value is a row of equal logits)
           const float2 d = unpack2(mul2(add2(z2, nm2), c2));
-          const uint64_t e2 = pack2(ex2(d.x), ex2(d.y));
+          const uint64_t e2 = pack2(ex2_approx(d.x), ex2_approx(d.y));
           S2 = add2(S2, e2);
           // (a logit of -inf adds 0)
           T2 = fma2(e2, pack2(fmaxf(d.x, -1e30f), fmaxf(d.y, -1e30f)), T2);

@@ -299,6 +299,71 @@ def test_scores_far_apart_and_scales_far_apart():
             assert (np.abs(_values(got) - ref) <= tol).all(), (dtype, pos)
 
 
+@pytest.mark.parametrize("dtype,M,window", [("f32", 6, 50), ("bf16", 6, 50), ("bf16", 40, 50),
+                                            ("bf16", 40, 130)])
+@pytest.mark.parametrize("seq", [320, 1024])
+def test_large_values_behind_the_window_cost_nothing(dtype, M, window, seq):
+    """A block of values 2^40 above the others that only the first rows of a tile still see: the
+    others keep all their bits."""
+    torch = _torch()
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    c = _cache(2, 128, seq)
+    g = torch.Generator(device="cuda").manual_seed(31)
+    x = torch.randn(1, 300, 4, 128, generator=g, device="cuda")
+    x[:, 64:128, 2:] *= 2.0 ** 40
+    c.append(x[:, :, :2], x[:, :, 2:], _ints([0]))
+    vals = [_values(t) * np.repeat(s.cpu().numpy().astype(np.float64), 64, -1)[..., None]
+            for t, s in ((c.k, c.k_scale), (c.v, c.v_scale))]
+    q = torch.randn(1, M, 4, 128, generator=g, device="cuda").to(dt)
+    pos = 125 + window  # row 0 sees keys 126 .., row 2 none below 128
+    got = c.attention(q, _ints([pos]), window=window)
+    ref = np.zeros(got.shape)
+    mass, size = R.attend(_values(q), vals[0], vals[1], [pos], [M], [0], window, ref)
+    tol = R.attend_bound(ref, mass, size, 128, window, dtype == "bf16")
+    assert (np.abs(_values(got) - ref) <= tol).all()
+    c.check()
+
+
+@pytest.mark.parametrize("dtype,heads,hd,n,M,seq", [("bf16", 8, 128, 2, 3, 320), ("bf16", 8, 128, 2, 40, 640),
+                                                    ("f32", 4, 64, 3, 7, 2048)])
+def test_output_over_the_queries_of_fused_rows(dtype, heads, hd, n, M, seq):
+    """q, k and v read in place from a product's rows, the output written over q; what
+    stands behind it in the rows stays."""
+    torch = _torch()
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(5)
+    c = _cache(2, hd, seq, n)
+    old = torch.randn(n, 200, 4, hd, generator=g, device="cuda").to(dt)
+    c.append(old[:, :, :2], old[:, :, 2:], _ints([0] * n))
+    rows = torch.randn(n, M, heads + 4, hd, generator=g, device="cuda").to(dt)
+    pos = _ints([200 - 31 * b for b in range(n)])
+    c.append(rows[:, :, heads:heads + 2], rows[:, :, heads + 2:], pos)
+    want = c.attention(rows[:, :, :heads], pos)
+    kept = rows[:, :, heads:].clone()
+    got = c.attention(rows[:, :, :heads], pos, out=rows[:, :, :heads])
+    assert got.data_ptr() == rows.data_ptr() and torch.equal(got, want)
+    assert torch.equal(rows[:, :, heads:], kept)
+    c.check()
+
+
+def test_a_padded_sequence_in_anothers_place():
+    """Its pads are not appended; the scales of the sequence before it are zeroed."""
+    torch = _torch()
+    g = torch.Generator(device="cuda").manual_seed(6)
+    c, fresh = _cache(2, 64, 192, 2), _cache(2, 64, 192, 2)
+    x = torch.randn(2, 150, 2, 64, generator=g, device="cuda")
+    c.append(1e6 * x, 1e6 * x, _ints([0, 0]))
+    for t in (c.k_scale, c.v_scale):
+        t[1].zero_()
+    y = x[:, :40].contiguous()
+    q = torch.randn(2, 40, 4, 64, generator=g, device="cuda")
+    for d in (c, fresh):
+        d.append(y, y, _ints([0, 21]), rows=_ints([0, 40]))
+    a, b = (d.attention(q, _ints([0, 21]), rows=_ints([0, 40]), first=_ints([0, 21])) for d in (c, fresh))
+    assert torch.equal(a, b) and bool(a[1].isfinite().all()) and bool((a[1] != 0).any())
+    assert torch.equal(c.v_scale[1, :, 0], fresh.v_scale[1, :, 0])
+
+
 def test_attention_leaves_bad_sequences_alone():
     from paper_2606_03113_gb300 import ssd as S
     torch = _torch()
