@@ -130,8 +130,9 @@ ssd_status ssd_gemv_noalloc(const void* W, int32_t dtype, int32_t rows, int32_t 
  * its block of 64 positions.  A scale is the smallest power of two, 2^-120 to
  * 2^111, that brings the block's largest magnitude to 448 or less (beyond
  * 448 * 2^111 values are cut to that).  max_seq: a multiple of 64; head_dim 64 or 128
- * (SSD_ERR_UNSUPPORTED otherwise).  Nothing has to be initialised: positions that
- * were not appended are never used. */
+ * (SSD_ERR_UNSUPPORTED otherwise).  Codes need no initial value.  Scales need one, 0,
+ * only where a sequence begins inside of a block (a padded batch whose pads are not
+ * appended): what stands there counts as the scale of the positions in front. */
 typedef struct {
   int32_t n_seq, n_kv_heads, head_dim, max_seq;
   void* k;
@@ -168,12 +169,16 @@ size_t ssd_kv8_attention_bytes(const ssd_kv8_cache* cache, int32_t dtype, int32_
  * a padded batch) and, with window > 0, j > p - window.  The rows' own keys must
  * have been appended.  q and out: device, dtype SSD_DTYPE_F32 or _BF16 (both the
  * same), row m of sequence b at element (b M + m) q_stride (out_stride), heads one
- * behind the other; pointers and strides in multiples of 16 bytes; out may be q.
+ * behind the other; pointers and strides in multiples of 16 bytes; out may
+ * be q, then at the same stride, and overlaps it in no other way.
  * A row that sees no key is zero.  Rows from rows[b] on are left as they were,
  * and so are sequences with bad positions or row numbers (error bits as above).
  * What stands in a key or value that a row does not see never reaches it, NaN
- * neither.  Scores, sums and outputs are fp32; bf16 queries are exact, probabilities
- * keep 11 bits (bf16) or 22 (fp32).  Equal calls give equal bits.
+ * neither.  Scores, sums and outputs are fp32.  bf16 query elements above 2^-28 of their
+ * row's largest are exact, fp32 ones above 2^-15 keep 22 bits; a probability keeps 11
+ * bits (fp32: 22) where its product with its value's scale is above 2^-20 (fp32: 2^-17) of
+ * the row's largest probability times the largest value scale that the row sees.  Below
+ * these they lose bits one by one.  Equal calls give equal bits.
  * Any M >= 1, any n_heads / n_kv_heads; SSD_ERR_CAPACITY where n_seq x M x max_seq is
  * so large that the work has more than 2^31 parts.  workspace: 256-byte aligned,
  * used by this call until it has run. */

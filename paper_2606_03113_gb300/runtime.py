@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import operator
 from typing import NamedTuple
 
 import numpy as np
@@ -308,7 +309,16 @@ class KV8Cache:
     synchronise; the caller orders streams, and keeps tensors that another stream made alive
     (`Tensor.record_stream`).  They can be captured into CUDA graphs after a first call outside
     of a capture.  What only the device can see (positions outside the cache, bad row numbers)
-    leaves the sequence alone and sets a bit in `err`, which `check` reads."""
+    leaves the sequence alone and sets a bit in `err`, which `check` reads.
+
+    A sequence that takes over another's place and begins inside of a block of 64 positions (a
+    padded batch whose pads are not appended) has its `k_scale[b]` and `v_scale[b]` zeroed first:
+    the scale that stands there counts as that of the positions in front."""
+
+    # the tensors can be written, but not replaced: calls have their addresses
+    k, v = (property(operator.attrgetter(x)) for x in ("_k", "_v"))
+    k_scale, v_scale = (property(operator.attrgetter(x)) for x in ("_k_scale", "_v_scale"))
+    err = property(operator.attrgetter("_err"))
 
     def __init__(self, n_kv_heads: int, head_dim: int, max_seq: int, n_seq: int = 1,
                  device: str | torch.device = "cuda:0"):
@@ -325,15 +335,15 @@ class KV8Cache:
         shape = (n_seq, n_kv_heads, self.max_seq, head_dim)
         scales = (n_seq, n_kv_heads, self.max_seq // S.KV8_BLOCK)
         # zeros where nothing was appended, for whoever looks at the tensors
-        self.k = torch.zeros(shape, dtype=torch.float8_e4m3fn, device=device)
-        self.v = torch.zeros(shape, dtype=torch.float8_e4m3fn, device=device)
-        self.k_scale = torch.zeros(scales, dtype=torch.float32, device=device)
-        self.v_scale = torch.zeros(scales, dtype=torch.float32, device=device)
-        self.err = torch.zeros(1, dtype=torch.int32, device=device)
+        self._k = torch.zeros(shape, dtype=torch.float8_e4m3fn, device=device)
+        self._v = torch.zeros(shape, dtype=torch.float8_e4m3fn, device=device)
+        self._k_scale = torch.zeros(scales, dtype=torch.float32, device=device)
+        self._v_scale = torch.zeros(scales, dtype=torch.float32, device=device)
+        self._err = torch.zeros(1, dtype=torch.int32, device=device)
         self._c = S.ssd_kv8_cache(n_seq, n_kv_heads, head_dim, self.max_seq, self.k.data_ptr(),
                                   self.v.data_ptr(), self.k_scale.data_ptr(),
                                   self.v_scale.data_ptr())
-        self._err = self.err.data_ptr()
+        self._err_at = self._err.data_ptr()
         self._work = {}  # (dtype code, n_heads, M) -> workspace bytes
 
     def _rows(self, x: torch.Tensor, heads: int, what: str) -> tuple[int, int]:
@@ -369,7 +379,7 @@ class KV8Cache:
         if there is not None:
             with there:
                 return self.append(k, v, pos, rows)
-        S.ssd_kv8_append(self._c, kp, vp, code, row, M, pp, rp, self._err,
+        S.ssd_kv8_append(self._c, kp, vp, code, row, M, pp, rp, self._err_at,
                          _current_stream(self.device.index))
 
     def attention(self, q: torch.Tensor, pos: torch.Tensor, rows: torch.Tensor | None = None,
@@ -397,7 +407,8 @@ class KV8Cache:
             Mo, orow = self._rows(out, heads, "out")
             if Mo != M:
                 raise ValueError("out must have q's rows")
-            _on(out, self.device, "out")
+            if _on(out, self.device, "out") == qp and orow != row:
+                raise ValueError("out is q, but their strides differ")
         if not 0 <= window < 1 << 31:
             raise ValueError(f"window must be 0 (none) or a positive int32, not {window}")
         key = (code, heads, M)
@@ -415,7 +426,7 @@ class KV8Cache:
             orow = heads * self.head_dim
         work = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         S.ssd_kv8_attention(self._c, qp, code, heads, row, M, pp, rp, fp, window, out.data_ptr(), orow,
-                            work.data_ptr(), nbytes, self._err, _current_stream(self.device.index))
+                            work.data_ptr(), nbytes, self._err_at, _current_stream(self.device.index))
         return out
 
     def check(self):

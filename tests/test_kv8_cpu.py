@@ -177,6 +177,27 @@ def test_python_entry_points_refuse_wrong_tensors():
         token_logprobs(z, t)
 
 
+def test_an_output_over_its_queries_has_their_stride():
+    with pytest.raises(S.SsdError, match="strides differ"):
+        S.ssd_kv8_attention(cache(), BUF, S.SSD_DTYPE_BF16, 8, 1024, 3, BUF, 0, 0, 0, BUF, 2048, BUF, 1 << 30)
+    c = KV8Cache(2, 64, 64, device="cpu")
+    pos = torch.zeros(1, dtype=torch.int32)
+    buf = torch.zeros(1, 4, 4, 64)
+    with pytest.raises(ValueError, match="strides differ"):
+        c.attention(buf[:, ::2], pos, out=buf[:, :2])
+    with pytest.raises(ValueError, match="CUDA"):
+        c.attention(buf[:, ::2], pos, out=buf[:, ::2])
+
+
+def test_the_caches_tensors_are_written_not_replaced():
+    c = KV8Cache(2, 64, 64, device="cpu")
+    for name in ("k", "v", "k_scale", "v_scale", "err"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, torch.zeros(1))
+    c.k_scale.fill_(2.0)
+    assert bool((c.k_scale == 2.0).all())
+
+
 def test_row_strides_that_are_read_in_place():
     """Slices of a fused q | k | v row, single rows and single sequences."""
     c = KV8Cache(2, 64, 64, n_seq=3, device="cpu")
