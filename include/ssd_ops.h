@@ -188,9 +188,6 @@ ssd_status ssd_kv8_attention(const ssd_kv8_cache* cache, const void* q, int32_t 
                              int64_t out_stride, void* workspace, size_t workspace_bytes,
                              int32_t* err_dev, void* stream);
 
-/* Bytes of device workspace that ssd_token_logprobs needs (0: invalid sizes). */
-size_t ssd_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t top_n);
-
 #define SSD_MAX_TOP 32 /* most probable tokens of a row, at most */
 
 /* Log-probabilities over rows of logits z at temperature t (0.001..1000): of
@@ -205,14 +202,12 @@ size_t ssd_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t top_n);
  * fewer than top_n logits above -inf, the places left are id -1, -inf.
  * A logit of -inf is a token of probability 0.  A row of nothing else has lse -inf,
  * its entropy and tokens NaN.  A NaN or +inf logit makes a row's lse, entropy and
- * log-probabilities NaN; its top_id are those of the numbers in it.
- * workspace: device, 256-byte aligned, this call's until it has run. */
+ * log-probabilities NaN; its top_id are those of the numbers in it. */
 ssd_status ssd_token_logprobs(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab,
                               int64_t row_stride, const int32_t* tokens, int32_t n_tokens,
                               float temperature, int32_t top_n, float* logprob, float* lse,
                               float* entropy, int32_t* top_id, float* top_logprob,
-                              void* workspace, size_t workspace_bytes, int32_t* err_dev,
-                              void* stream);
+                              int32_t* err_dev, void* stream);
 
 /* Test fixture: fills dst (device, n elements of dtype) with the seeded
  * synthetic weights of tensor `tid` (see synth/synth.h): element i is

@@ -94,9 +94,6 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
 ssd_status fail_op(ssd_status s, const char* msg) noexcept;
 ssd_status fail_op_cuda(const char* what, cudaError_t e) noexcept;
 
-// SMs of the current device (asked for once a device).
-cudaError_t device_sms(int* sms) noexcept;
-
 // Checks of a cache that every entry point makes; null: fine.
 const char* check_kv8(const ssd_kv8_cache* c) noexcept;
 

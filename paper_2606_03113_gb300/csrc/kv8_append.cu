@@ -9,8 +9,6 @@
 //
 // Bound by bytes for prompts (a value is read once and its code written once)
 // and by the launch and one round trip of memory for a few rows.
-#include <atomic>
-
 #include "kv8.cuh"
 
 namespace ssd {
@@ -181,21 +179,6 @@ static cudaError_t append(const AppendArgs& a, int n_seq, cudaStream_t st) {
   const dim3 grid((a.M + kKv8Block - 2) / kKv8Block + 1, 2 * a.heads, n_seq);
   k_kv8_append<T, HD><<<grid, kApThreads, 0, st>>>(a);
   return cudaGetLastError();
-}
-
-cudaError_t device_sms(int* sms) noexcept {
-  static std::atomic<int> known[64];
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  int n = known[dev].load(std::memory_order_relaxed);
-  if (!n) {
-    if ((e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) return e;
-    known[dev].store(n, std::memory_order_relaxed);
-  }
-  *sms = n;
-  return cudaSuccess;
 }
 
 const char* check_kv8(const ssd_kv8_cache* c) noexcept {

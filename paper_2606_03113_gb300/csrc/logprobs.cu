@@ -14,15 +14,15 @@
 // more than kCand logits (ties, a spread that the threads' stride meets), the bound
 // is raised by bisection first.
 //
-// Few rows are cut into chunks, one block each, whose parts k_logprobs_merge joins
-// in order; a row that a block reads alone is finished there.
+// Few rows are cut into chunks, one for each block of a cluster; the first block reads
+// the others' parts from their shared memory and joins them in order.
 //
 // A logit of -inf has probability 0 and is none of the most probable; a NaN
 // takes no place among them either, and it or +inf make the row's lse, entropy
 // and log-probabilities NaN.
 #include <math.h>
 
-#include <mutex>
+#include <atomic>
 
 #include "kv8.cuh"
 
@@ -36,8 +36,10 @@ constexpr int kUnroll = 4;       // 16-byte vectors of a thread in flight
 constexpr int kGroups = 64;      // groups of threads whose maxima bound the top
 constexpr int kCand = 1024;      // candidates that are ranked
 constexpr int kMaxTop = SSD_MAX_TOP;
-constexpr int kMaxChunks = 64;   // chunks of a row
+constexpr int kMaxChunks = 16;   // chunks of a row: blocks of a cluster
 static_assert(kMaxTop <= kGroups, "a group for each of the most probable");
+static_assert(kMaxChunks <= 32, "a lane for each chunk");
+static_assert(kMaxChunks * kMaxTop <= kCand, "the chunks' lists fit the candidates' place");
 
 struct LogpArgs {
   const void* z;
@@ -51,8 +53,6 @@ struct LogpArgs {
   float* entropy;
   int32_t* top_id;
   float* top_logprob;
-  float4* part;      // [rows][chunks] (max of z, S, T, -)
-  uint64_t* part_top;  // [rows][chunks][top] keys
   int32_t* err;
 };
 
@@ -100,7 +100,33 @@ struct LogpSmem {
   int scan[kLWarps];
   uint64_t cand[kCand];
   uint64_t top[kMaxTop];
+  uint64_t best[kMaxTop];  // of all chunks
+  Stat all;                // of the block's chunk; in the first block then of all
 };
+
+// The address of p, of this block's shared memory, in block `rank` of the cluster.
+__device__ __forceinline__ uint32_t in_block(const void* p, int rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float ld_cluster_f32(uint32_t a) {
+  float r;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(r) : "r"(a) : "memory");
+  return r;
+}
+__device__ __forceinline__ uint64_t ld_cluster_u64(uint32_t a) {
+  uint64_t r;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(r) : "r"(a) : "memory");
+  return r;
+}
+// Every thread of the cluster is here, and what they wrote before can be read.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile(
+      "barrier.cluster.arrive.release.aligned;\n\t"
+      "barrier.cluster.wait.acquire.aligned;" ::
+          : "memory");
+}
 
 // A row's vectors: the 16-byte aligned places that hold its elements, the first
 // and last of them perhaps in part.
@@ -422,93 +448,63 @@ __global__ void __launch_bounds__(kLThreads, kAhead<T> ? 3 : 4) k_logprobs(const
     st = sm.stat[0];
 #pragma unroll
     for (int w = 1; w < kLWarps; ++w) st = join(st, sm.stat[w], c);
-    if (a.chunks == 1) {
-      finish_row<T>(a, r, zr, st, sm.top, kLThreads);
-    } else {
-      const int64_t at = r64 * a.chunks + blockIdx.x;
-      if (tid == 0) a.part[at] = make_float4(st.m, st.S, st.T, 0.f);
-      for (int i = tid; i < a.top; i += kLThreads) a.part_top[at * a.top + i] = sm.top[i];
-    }
-    __syncthreads();
-  }
-}
-
-// Joins a row's chunks: one warp takes the largest of the lists' heads, a.top times.
-constexpr int kJThreads = 128;
-
-template <typename T>
-__global__ void __launch_bounds__(kJThreads) k_logprobs_merge(const LogpArgs a) {
-  __shared__ uint64_t keys[kMaxChunks * kMaxTop];
-  __shared__ uint64_t top[kMaxTop];
-  static_assert(kMaxChunks == 64, "two lists a lane");
-  pdl_wait();
-  const int tid = threadIdx.x, lane = tid & 31;
-  const float c = a.inv_t * 1.4426950408889634f;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    const int n = a.chunks * a.top;
-#pragma unroll 8
-    for (int i = tid; i < n; i += kJThreads) keys[i] = __ldcg(a.part_top + r * n + i);
-    __syncthreads();
-    if (tid < 32) {
-      Stat st{0.f, 0.f, 0.f};
-      int at[2];
-      uint64_t head[2];
+    const uint64_t* top = sm.top;
+    if (a.chunks > 1) {
+      if (tid == 0) sm.all = st;
+      cluster_sync();
+      if (blockIdx.x == 0) {
+        for (int i = tid; i < a.chunks * a.top; i += kLThreads)
+          sm.cand[i] = ld_cluster_u64(in_block(&sm.top[i % a.top], i / a.top));
+        if (warp == 0) {
+          st = Stat{0.f, 0.f, 0.f};
+          if (lane < a.chunks)
+            st = Stat{ld_cluster_f32(in_block(&sm.all.m, lane)),
+                      ld_cluster_f32(in_block(&sm.all.S, lane)),
+                      ld_cluster_f32(in_block(&sm.all.T, lane))};
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int ch = lane + 32 * j;
-        at[j] = 0;
-        head[j] = 0ull;
-        if (ch < a.chunks) {
-          const float4 p = __ldcg(a.part + r * a.chunks + ch);
-          st = join(st, Stat{p.x, p.y, p.z}, c);
-          if (a.top > 0) head[j] = keys[ch * a.top];
-        }
-      }
-      for (int i = 0; i < a.top; ++i) {
-        const uint64_t k = head[0] > head[1] ? head[0] : head[1];
-        const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32));
-        const uint32_t lo =
-            __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
-        const uint64_t best = (uint64_t)hi << 32 | lo;
-        if (lane == 0) top[i] = best;
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          if (best && head[j] == best) {
-            ++at[j];
-            head[j] = at[j] < a.top ? keys[(lane + 32 * j) * a.top + at[j]] : 0ull;
+          for (int o = kMaxChunks / 2; o > 0; o >>= 1) {
+            Stat b;
+            b.m = __shfl_down_sync(0xffffffffu, st.m, o);
+            b.S = __shfl_down_sync(0xffffffffu, st.S, o);
+            b.T = __shfl_down_sync(0xffffffffu, st.T, o);
+            st = join(st, b, c);
           }
+          if (lane == 0) sm.all = st;
+        }
+        __syncthreads();
+        if (warp == 0) {  // the largest of the lists' heads, a.top times
+          int at = 0;
+          uint64_t head = a.top > 0 && lane < a.chunks ? sm.cand[lane * a.top] : 0ull;
+          for (int i = 0; i < a.top; ++i) {
+            const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(head >> 32));
+            const uint32_t lo =
+                __reduce_max_sync(0xffffffffu, (uint32_t)(head >> 32) == hi ? (uint32_t)head : 0u);
+            const uint64_t best = (uint64_t)hi << 32 | lo;
+            if (lane == 0) sm.best[i] = best;
+            if (best && head == best) head = ++at < a.top ? sm.cand[lane * a.top + at] : 0ull;
+          }
+        }
+        __syncthreads();
+        st = sm.all;
+        top = sm.best;
       }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        Stat b;
-        b.m = __shfl_down_sync(0xffffffffu, st.m, o);
-        b.S = __shfl_down_sync(0xffffffffu, st.S, o);
-        b.T = __shfl_down_sync(0xffffffffu, st.T, o);
-        st = join(st, b, c);
-      }
-      st.m = __shfl_sync(0xffffffffu, st.m, 0);
-      st.S = __shfl_sync(0xffffffffu, st.S, 0);
-      st.T = __shfl_sync(0xffffffffu, st.T, 0);
-      __syncwarp();
-      finish_row<T>(a, (int)r, static_cast<const T*>(a.z) + r * a.stride, st, top, 32);
     }
-    __syncthreads();
+    if (blockIdx.x == 0) finish_row<T>(a, r, zr, st, top, kLThreads);
+    if (a.chunks > 1) cluster_sync();  // the first block has read the others'
+    else __syncthreads();
   }
 }
 
 namespace {
 
-// Chunks of a row: blocks enough for four on each of 152 SMs, and no chunk below 4096
-// logits (one step of a block for fp32, half of one for bf16).
+// Chunks of a row: blocks enough for four on each of 152 SMs, a power of two of them, and
+// no chunk below 4096 logits (one step of a block for fp32, half of one for bf16).
 int logp_chunks(int rows, int vocab) {
   constexpr int per = kLThreads * kUnroll * 4;
-  const int most = (vocab + per - 1) / per;
-  int n = (152 * 4 + rows - 1) / rows;
-  n = n < most ? n : most;
-  return n < 1 ? 1 : (n > kMaxChunks ? kMaxChunks : n);
-}
-size_t logp_part_bytes(int rows, int chunks) {
-  return ((size_t)rows * chunks * sizeof(float4) + 255) / 256 * 256;
+  const int want = (152 * 4 + rows - 1) / rows, most = (vocab + per - 1) / per;
+  int n = 1;
+  while (n < kMaxChunks && n < want && 2 * n <= most) n *= 2;
+  return n;
 }
 
 const char* check_logp(int32_t rows, int32_t vocab, int32_t ntok, int32_t top) {
@@ -519,44 +515,51 @@ const char* check_logp(int32_t rows, int32_t vocab, int32_t ntok, int32_t top) {
   return nullptr;
 }
 
+// More than eight blocks in a cluster have to be allowed, once a device.
+template <typename T>
+cudaError_t allow_clusters() {
+  static std::atomic<bool> done[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  if (done[dev].load(std::memory_order_acquire)) return cudaSuccess;
+  e = cudaFuncSetAttribute(k_logprobs<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) done[dev].store(true, std::memory_order_release);
+  return e;
+}
+
 template <typename T>
 cudaError_t logp_launch(const LogpArgs& a, cudaStream_t st) {
   const int gy = a.rows < 32768 ? a.rows : 32768;
-  k_logprobs<T><<<dim3(a.chunks, gy), kLThreads, 0, st>>>(a);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess || a.chunks == 1) return e;
+  if (a.chunks == 1) {
+    k_logprobs<T><<<dim3(1, gy), kLThreads, 0, st>>>(a);
+    return cudaGetLastError();
+  }
+  const cudaError_t e = allow_clusters<T>();
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(gy);
-  cfg.blockDim = dim3(kJThreads);
+  cfg.gridDim = dim3(a.chunks, gy);
+  cfg.blockDim = dim3(kLThreads);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = g_pdl_enabled ? 1 : 0;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = a.chunks;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_logprobs_merge<T>, a);
+  return cudaLaunchKernelEx(&cfg, k_logprobs<T>, a);
 }
 
 }  // namespace
 }  // namespace ssd
 
-extern "C" size_t ssd_token_logprobs_bytes(int32_t n_rows, int32_t vocab, int32_t top_n) {
-  using namespace ssd;
-  if (const char* why = check_logp(n_rows, vocab, 0, top_n)) {
-    fail_op(SSD_ERR_INVALID_ARG, why);
-    return 0;
-  }
-  const int chunks = logp_chunks(n_rows, vocab);
-  if (chunks == 1) return 256;
-  return logp_part_bytes(n_rows, chunks) + (size_t)n_rows * chunks * top_n * sizeof(uint64_t) + 256;
-}
-
 extern "C" ssd_status ssd_token_logprobs(const void* logits, int32_t dtype, int32_t n_rows,
                                          int32_t vocab, int64_t row_stride, const int32_t* tokens,
                                          int32_t n_tokens, float temperature, int32_t top_n,
                                          float* logprob, float* lse, float* entropy,
-                                         int32_t* top_id, float* top_logprob, void* workspace,
-                                         size_t workspace_bytes, int32_t* err_dev, void* stream) {
+                                         int32_t* top_id, float* top_logprob, int32_t* err_dev,
+                                         void* stream) {
   using namespace ssd;
   if (const char* why = check_logp(n_rows, vocab, n_tokens, top_n))
     return fail_op(SSD_ERR_INVALID_ARG, why);
@@ -569,12 +572,7 @@ extern "C" ssd_status ssd_token_logprobs(const void* logits, int32_t dtype, int3
     return fail_op(SSD_ERR_INVALID_ARG, "NULL buffer of tokens or of the most probable");
   if (!(temperature >= 1e-3f && temperature <= 1e3f))
     return fail_op(SSD_ERR_INVALID_ARG, "temperature must be in 0.001..1000");
-  const size_t need = ssd_token_logprobs_bytes(n_rows, vocab, top_n);
   const int chunks = logp_chunks(n_rows, vocab);
-  if (chunks > 1 && (!workspace || ((uintptr_t)workspace & 255u)))
-    return fail_op(SSD_ERR_INVALID_ARG, "workspace must be non-NULL and 256-byte aligned");
-  if (chunks > 1 && workspace_bytes < need)
-    return fail_op(SSD_ERR_CAPACITY, "workspace too small");
   LogpArgs a{};
   a.z = logits;
   a.tok = tokens;
@@ -594,11 +592,6 @@ extern "C" ssd_status ssd_token_logprobs(const void* logits, int32_t dtype, int3
   a.top_id = top_id;
   a.top_logprob = top_logprob;
   a.err = err_dev;
-  if (chunks > 1) {
-    a.part = static_cast<float4*>(workspace);
-    a.part_top = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) +
-                                             logp_part_bytes(n_rows, chunks));
-  }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e =
       dtype == SSD_DTYPE_BF16 ? logp_launch<__nv_bfloat16>(a, st) : logp_launch<float>(a, st);

@@ -10,7 +10,6 @@ same generator the CPU oracle reads).  `Engine` owns one ssd_ctx: workspace
 from __future__ import annotations
 
 import ctypes as C
-import functools
 import operator
 from typing import NamedTuple
 
@@ -295,11 +294,6 @@ def _elsewhere(device: torch.device, stream):
     return None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
 
-@functools.lru_cache(maxsize=256)
-def _logprobs_bytes(n: int, vocab: int, top_n: int) -> int:
-    return S.ssd_token_logprobs_bytes(n, vocab, top_n)
-
-
 class KV8Cache:
     """The KV cache of one layer in 8 bits (ssd_kv8_cache, include/ssd_ops.h): e4m3 codes `k`, `v`
     [n_seq, n_kv_heads, max_seq, head_dim], one scale per 64 positions and KV head in `k_scale`,
@@ -495,11 +489,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top
         ids = torch.empty((n, top_n), dtype=torch.int32, device=dev)
         top = torch.empty((n, top_n), dtype=torch.float32, device=dev)
         ip, lp_top = ids.data_ptr(), top.data_ptr()
-    nbytes = _logprobs_bytes(n, vocab, top_n)
-    # (256: rows that a block reads alone need none; it stays this call's until the launches)
-    work = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes > 256 else None
     S.ssd_token_logprobs(zp, code, n, vocab, logits.stride(0) if n > 1 else vocab, tp, ntok,
                          temperature, top_n, lpp, lse.data_ptr(), entropy.data_ptr(), ip, lp_top,
-                         work.data_ptr() if work is not None else 0, nbytes, ep,
-                         _current_stream(dev.index))
+                         ep, _current_stream(dev.index))
     return TokenLogprobs(lp, lse, entropy, ids, top, err)

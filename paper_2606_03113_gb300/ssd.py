@@ -134,9 +134,8 @@ SIGNATURES = {
     "ssd_kv8_attention_bytes": (_SZ, [_P, _I32, _I32, _I32]),
     "ssd_kv8_attention": (C.c_int, [_P, _P, _I32, _I32, _I64, _I32, _P, _P, _P, _I32, _P, _I64, _P,
                                     _SZ, _P, _P]),
-    "ssd_token_logprobs_bytes": (_SZ, [_I32, _I32, _I32]),
     "ssd_token_logprobs": (C.c_int, [_P, _I32, _I32, _I32, _I64, _P, _I32, _F32, _I32, _P, _P, _P,
-                                     _P, _P, _P, _SZ, _P, _P]),
+                                     _P, _P, _P, _P]),
     "ssd_synth_fill": (C.c_int, [_P, _I32, _U64, _U32, _U32, C.c_double, _P]),
     "ssd_read_probe": (C.c_int, [_P, _U64, _P, _P]),
 }
@@ -335,20 +334,15 @@ def ssd_kv8_attention(cache: ssd_kv8_cache, q_ptr: int, dtype: int, n_heads: int
         _check(st, "ssd_kv8_attention")
 
 
-def ssd_token_logprobs_bytes(n_rows: int, vocab: int, top_n: int) -> int:
-    return lib().ssd_token_logprobs_bytes(n_rows, vocab, top_n)
-
-
 def ssd_token_logprobs(logits_ptr: int, dtype: int, n_rows: int, vocab: int, row_stride: int,
                        tokens_ptr: int, n_tokens: int, temperature: float, top_n: int,
                        logprob_ptr: int, lse_ptr: int, entropy_ptr: int, top_id_ptr: int,
-                       top_logprob_ptr: int, workspace_ptr: int, workspace_bytes: int,
-                       err_ptr: int = 0, stream_ptr: int = 0):
+                       top_logprob_ptr: int, err_ptr: int = 0, stream_ptr: int = 0):
     """Log-probabilities, entropy and most probable tokens of rows of logits (see ssd_ops.h)."""
     st = (_lib or lib()).ssd_token_logprobs(logits_ptr, dtype, n_rows, vocab, row_stride, tokens_ptr,
                                             n_tokens, temperature, top_n, logprob_ptr, lse_ptr,
-                                            entropy_ptr, top_id_ptr, top_logprob_ptr, workspace_ptr,
-                                            workspace_bytes, err_ptr, stream_ptr)
+                                            entropy_ptr, top_id_ptr, top_logprob_ptr, err_ptr,
+                                            stream_ptr)
     if st:
         _check(st, "ssd_token_logprobs")
 

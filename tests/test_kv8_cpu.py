@@ -120,19 +120,15 @@ def test_attention_workspace_sizes():
     (dict(t=float("nan")), S.SSD_ERR_INVALID_ARG), (dict(t=-1.0), S.SSD_ERR_INVALID_ARG),
     (dict(t=float("inf")), S.SSD_ERR_INVALID_ARG), (dict(top=33), S.SSD_ERR_INVALID_ARG),
     (dict(top=-1), S.SSD_ERR_INVALID_ARG), (dict(top=4, vocab=3, stride=3), S.SSD_ERR_INVALID_ARG),
-    (dict(ids=0), S.SSD_ERR_INVALID_ARG), (dict(tops=0), S.SSD_ERR_INVALID_ARG),
-    (dict(ws=0, vocab=128256, stride=128256), S.SSD_ERR_INVALID_ARG),
-    (dict(wb=16, vocab=128256, stride=128256), S.SSD_ERR_CAPACITY)])
+    (dict(ids=0), S.SSD_ERR_INVALID_ARG), (dict(tops=0), S.SSD_ERR_INVALID_ARG)])
 def test_token_logprobs_refuses(kw, status):
     a = dict(z=BUF, dtype=S.SSD_DTYPE_F32, rows=2, vocab=1000, stride=1000, tok=BUF, ntok=1, t=1.0,
-             top=4, lp=BUF, ids=BUF, tops=BUF, ws=BUF, wb=1 << 30)
+             top=4, lp=BUF, ids=BUF, tops=BUF)
     a.update(kw)
     with pytest.raises(S.SsdError) as e:
         S.ssd_token_logprobs(a["z"], a["dtype"], a["rows"], a["vocab"], a["stride"], a["tok"],
-                             a["ntok"], a["t"], a["top"], a["lp"], BUF, BUF, a["ids"], a["tops"],
-                             a["ws"], a["wb"])
+                             a["ntok"], a["t"], a["top"], a["lp"], BUF, BUF, a["ids"], a["tops"])
     assert e.value.status == status
-    assert S.ssd_token_logprobs_bytes(0, 5, 1) == 0
 
 
 def test_python_entry_points_refuse_wrong_tensors():
