@@ -660,6 +660,12 @@ cudaError_t prep_rows() {
                               (int)RowsL<HD>::template total<sizeof(T) == 4 ? 2 : 1>());
 }
 
+template <int TILES>
+cudaError_t prep_wide() {
+  return cudaFuncSetAttribute(k_kv8_wide<TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)WideL<TILES>::kSmem);
+}
+
 // SMs of the current device; its kernels' limits of shared memory are set on
 // the first call there.
 cudaError_t kv8_device(int* sms) {
@@ -674,8 +680,7 @@ cudaError_t kv8_device(int* sms) {
         (e = prep_rows<float, 64>()) != cudaSuccess || (e = prep_rows<float, 128>()) != cudaSuccess ||
         (e = prep_rows<__nv_bfloat16, 64>()) != cudaSuccess ||
         (e = prep_rows<__nv_bfloat16, 128>()) != cudaSuccess ||
-        (e = cudaFuncSetAttribute(k_kv8_wide, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  (int)kWSmem)) != cudaSuccess)
+        (e = prep_wide<1>()) != cudaSuccess || (e = prep_wide<2>()) != cudaSuccess)
       return e;
     d.ready = true;
   }
@@ -720,20 +725,29 @@ cudaError_t rows_launch(const Kv8Attn& a, int P, cudaStream_t st) {
   return e != cudaSuccess || a.whole ? e : merge_launch<T, HD, kRT>(a, P, st);
 }
 
+template <int TILES>
 cudaError_t wide_launch(const Kv8Attn& a, int P, cudaStream_t st) {
-  k_kv8_wide<<<P, kWThreads, kWSmem, st>>>(a);
+  using L = WideL<TILES>;
+  k_kv8_wide<TILES><<<P, L::kThreads, L::kSmem, st>>>(a);
   const cudaError_t e = cudaGetLastError();
-  return e != cudaSuccess ? e : merge_launch<__nv_bfloat16, kWHd, kWRows>(a, P, st);
+  return e != cudaSuccess ? e : merge_launch<__nv_bfloat16, kWHd, L::kRows>(a, P, st);
 }
 
-// The kernel of a call.  Tiles of 128 rows on tcgen05 where a KV head has more
-// than 16 query rows, the type is bf16 and head_dim 128; tiles of 16 on mma.sync
-// otherwise.  us a call, mma.sync / tcgen05, by rows of 8 KV heads (of 32 in the last
-// line):          16           17           32           48          128
-//   500 keys   10.3/12.7    11.0/12.9    11.1/13.7    11.9/14.2    17.6/17.4
-//   16000      18.8/22.9    28.5/23.1    28.9/24.5    34.9/25.5    63.7/35.1
-//   100000     51.4/64.9    90.6/65.1    90.6/66.6     126/67.8     293/81.3
-//   16 x 1000  58.7/71.0    97.7/72.6    99.7/79.6     146/82.7     369/103
+// The kernel of a call.  Tiles on tcgen05 where a KV head has more than 16 query rows,
+// the type is bf16 and head_dim 128, with one accumulator of 128 rows, or two where there
+// are more; tiles of 16 on mma.sync otherwise.  us a call, mma.sync / tcgen05, by rows of 8 KV
+// heads (of 32 in the last line):
+//                     16           17           32           48          128
+//   500 keys      10.3/12.7    11.0/12.9    11.1/13.7    11.9/14.2    17.6/17.4
+//   16000         18.8/22.9    28.5/23.1    28.9/24.5    34.9/25.5    63.7/35.1
+//   100000        51.4/64.9    90.6/65.1    90.6/66.6     126/67.8     293/81.3
+//   16 x 1000     58.7/71.0    97.7/72.6    99.7/79.6     146/82.7     369/103
+// and one / two accumulators, 8 KV heads:
+//                    129          256          300          512         1024
+//   500 keys      19.2/19.3    21.3/22.5    22.1/23.3    23.2/24.9    32.4/28.0
+//   16000         40.0/33.7    44.5/37.7    50.4/50.1    60.7/51.4    97.1/75.1
+//   100000         117/94.4     129/99.8     189/173      239/175      459/322
+//   16 x 1000     59.7/42.7    68.9/51.6    84.2/76.1     105/82.8     193/157
 constexpr int kWideFrom = 16;
 // Caches of up to 512 positions: a block for each item and no join (mma.sync kernel).  us,
 // shared / whole, at full caches of 128, 256, 512 and 1024 positions:
@@ -745,19 +759,22 @@ constexpr int kWideFrom = 16;
 constexpr int kWholeSeq = 512;
 
 struct Kv8Plan {
-  bool wide, whole;
-  int rt, ku;
+  int wide;  // accumulators of a wide tile, 0: not wide
+  bool whole;
+  int rt, ku, max_blocks;
   long long n_rt, units;  // tiles of a sequence; the line's places, at most
 };
 Kv8Plan plan_of(const ssd_kv8_cache* c, int dtype, int n_heads, int M) {
   Kv8Plan p;
   const long long rows = (long long)M * (n_heads / c->n_kv_heads);
-  p.wide = dtype == SSD_DTYPE_BF16 && c->head_dim == kWHd && rows > kWideFrom;
+  const bool wide = dtype == SSD_DTYPE_BF16 && c->head_dim == kWHd && rows > kWideFrom;
+  p.wide = !wide ? 0 : rows > kWRows ? 2 : 1;
   p.whole = !p.wide && c->max_seq <= kWholeSeq;
-  p.rt = p.wide ? kWRows : kRT;
+  p.rt = p.wide ? p.wide * kWRows : kRT;
+  p.max_blocks = p.wide == 2 ? kKv8MaxBlocks / 2 : kKv8MaxBlocks;
   p.ku = p.wide ? kWKeys : kKv8Block;
   p.n_rt = (rows + p.rt - 1) / p.rt;
-  p.units = p.n_rt * c->n_seq * c->n_kv_heads * ((c->max_seq + p.ku - 1) / p.ku + kKv8ItemCost);
+  p.units = p.n_rt * c->n_seq * c->n_kv_heads * ((c->max_seq + p.ku - 1) / p.ku + (p.wide == 2 ? kKv8ItemCost<256> : kKv8ItemCost<kRT>));
   return p;
 }
 
@@ -782,7 +799,7 @@ extern "C" size_t ssd_kv8_attention_bytes(const ssd_kv8_cache* c, int32_t dtype,
     return 0;
   }
   const Kv8Plan p = plan_of(c, dtype, n_heads, M);
-  return p.whole ? 256 : kv8_work(kKv8MaxBlocks, p.rt, c->head_dim).total;
+  return p.whole ? 256 : kv8_work(p.max_blocks, p.rt, c->head_dim).total;
 }
 
 extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, int32_t dtype,
@@ -811,7 +828,7 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   const Kv8Plan plan = plan_of(c, dtype, n_heads, M);
   if (plan.units > 0x7fffffffll)
     return fail_op(SSD_ERR_CAPACITY, "n_seq x M x max_seq: more than 2^31 units of work");
-  const Kv8Work lay = kv8_work(kKv8MaxBlocks, plan.rt, c->head_dim);
+  const Kv8Work lay = kv8_work(plan.max_blocks, plan.rt, c->head_dim);
   if (!workspace || ((uintptr_t)workspace & 255u))
     return fail_op(SSD_ERR_INVALID_ARG, "workspace must be non-NULL and 256-byte aligned");
   if (workspace_bytes < (plan.whole ? 256 : lay.total)) return fail_op(SSD_ERR_CAPACITY, "workspace too small");
@@ -846,8 +863,8 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   a.part = reinterpret_cast<float*>(ws + lay.part);
   a.byG = Kv8Div::of((uint32_t)G);
   a.byRt = Kv8Div::of((uint32_t)plan.n_rt);
-  int P = sms * (plan.wide ? 2 : kVBlocks);
-  if (P > kKv8MaxBlocks) P = kKv8MaxBlocks;
+  int P = sms * (plan.wide == 2 ? 1 : 2);  // blocks of an SM
+  if (P > plan.max_blocks) P = plan.max_blocks;
   if (plan.units < P) P = (int)plan.units;
   a.whole = plan.whole;
   if (plan.whole) P = a.entries * a.Hkv;
@@ -855,7 +872,7 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool wide = c->head_dim == 128;
   if (plan.wide)
-    e = wide_launch(a, P, st);
+    e = plan.wide == 2 ? wide_launch<2>(a, P, st) : wide_launch<1>(a, P, st);
   else if (dtype == SSD_DTYPE_BF16)
     e = wide ? rows_launch<__nv_bfloat16, 128>(a, P, st) : rows_launch<__nv_bfloat16, 64>(a, P, st);
   else

@@ -30,9 +30,12 @@ struct Kv8Div {
 };
 
 // What an item costs beside its units (queries, the join of the warps or of the
-// parts), in units: 2 to 3 us against 0.7 a unit.  Without it 24 ragged sequences of 32
-// heads kept the last block busy for 90 us and the first for 59.
-constexpr int kKv8ItemCost = 3;
+// parts), in units.  Tiles of 16 and 128 rows: 2 to 3 us against 0.7 a unit; without it 24
+// ragged sequences of 32 heads kept the last block busy for 90 us and the first for 59.
+// Tiles of 256: 8 us against 1 (512 rows of 32 heads over 8 x 7936 keys: 2 % slower at 5, the
+// same at 11).
+template <int RT>
+constexpr int kKv8ItemCost = RT > 128 ? 8 : 3;
 
 struct Kv8Attn {
   Kv8Div byG, byRt, byP;
@@ -117,7 +120,7 @@ struct Kv8Line {
 // The line's places that an item takes.
 template <int RT, int KU>
 __device__ __forceinline__ int kv8_len(const Kv8Item& it) {
-  return it.units ? it.units + kKv8ItemCost : 0;
+  return it.units ? it.units + kKv8ItemCost<RT> : 0;
 }
 
 // The block's part of an item: units u0 .. u0 + nu - 1.
@@ -133,14 +136,14 @@ struct Kv8Cursor {
 };
 
 struct Kv8PlanSmem {
-  int warp[16];
+  int warp[32];
   Kv8Cursor c;
 };
 
 // Every thread of the block gets the block's stretch.
 template <int RT, int KU, int THREADS>
 __device__ __forceinline__ Kv8Cursor kv8_plan(const Kv8Attn& a, Kv8PlanSmem& sm) {
-  static_assert(THREADS / 32 <= 16, "a sum for each warp");
+  static_assert(THREADS / 32 <= 32, "a sum for each warp");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (a.whole) {
     const int e = (int)blockIdx.x / a.Hkv, g = (int)blockIdx.x - e * a.Hkv;

@@ -2,40 +2,56 @@
 // (wide verifications, grouped queries, prompt chunks; bf16, head_dim 128), on
 // the 5th-generation tensor cores.  Included by kv8_attention.cu.
 //
-// A block serves tiles of 128 query rows (the plan's items) and walks their keys a
-// cache block (64) at a time; two blocks share an SM.  Its warps work side by side:
+// A tile (the plan's items) has one or two accumulators of 128 query rows each.  A block
+// walks its keys a cache block (64) at a time; two blocks share an SM, of two
+// accumulators one has it alone.  Its warps work side by side:
 //  - four convert: they read the codes a step ahead into registers and write them to
 //    shared memory as f16, exact, rows of 128 bytes with the 128-byte swizzle, two
 //    steps deep: keys as a K-major operand, values, whose columns lie one behind
-//    the other, as an MN-major one;
-//  - one thread issues S = Q K^T (tcgen05.mma, 128 x 64 x 128, fp32 in tensor memory, two
-//    buffers) for a step while the softmax of the step before is at work, another
+//    the other, as an MN-major one (two accumulators: four for keys and four for values,
+//    which both then use);
+//  - one an accumulator issues S = Q K^T (tcgen05.mma, 128 x 64 x 128, fp32 in tensor memory,
+//    two buffers) for a step while the softmax of the step before is at work, another
 //    one O += P V, P read from tensor memory, as soon as a softmax is done;
-//  - four do the softmax, a thread per row: the row's 64 scores into registers, their
-//    maximum, p = 2^(s - ref + 7) as f16, which takes the place of S.  ref is the row's
-//    maximum as of the last time it grew by more than 8 (in powers of two), so O is
-//    rescaled in tensor memory only then, and p stays below 2^15.
+//  - four an accumulator do the softmax, a thread per row: the row's 64 scores into
+//    registers, their maximum, p = 2^(s - ref + 7) as f16, which takes the place of S.  ref is
+//    the row's maximum as of the last time it grew by more than 8 (in powers of two), so
+//    O is rescaled in tensor memory only then, and p stays below 2^15.
 // Queries are scaled to f16 and value scales moved into p as in k_kv8_rows.
 //
-// Bound, per 128 keys and SM: 1280 cycles of tensor pipe (the queries' operand is
-// read from shared memory for 64 keys at a time), 1536 of shared memory (operands
-// and conversions), 512 of code conversions (one warp instruction a cycle), 512 of
-// exponentials.
+// Bound, per 64 keys and accumulator: 640 cycles of tensor pipe (8 instructions of
+// 48 cycles for S, whose operands come from shared memory, 4 of 64 for O) and as much of
+// shared memory; 256 of code conversions (half with two accumulators), 256 of
+// exponentials; 700 of a scheduler's issue slots with two softmax warps there.  What it
+// takes is 1000 (1200 with one accumulator), the rest waits of one role for another.
+// 512 rows of 32 heads over 8 KV heads x 7936 keys: 77 us = 867 TFLOP/s, of which 6 are
+// the start (the plan, the queries), 4 the last outputs and 8 the join; a floor of 34 at
+// the library's bf16 rate.  17 rows of 64 heads over 8 x 16000
+// keys: 34 us.
 #pragma once
 
 namespace ssd {
 
 namespace {
 
-constexpr int kWRows = 128;   // query rows of a tile
+constexpr int kWRows = 128;   // query rows of an accumulator
 constexpr int kWKeys = kKv8Block;  // keys of a step: one scale
 constexpr int kWHd = 128;
-constexpr int kWThreads = 10 * 32;  // softmax: warps 0-3, conversion: 4-7, products: 8, 9
 constexpr uint32_t kWQHalf = kWRows * 128;       // bytes of 64 f16 columns of the queries
 constexpr uint32_t kWKHalf = kWKeys * 128;       // of a step's keys or values
 constexpr uint32_t kWKTile = 2 * kWKHalf;
-constexpr uint32_t kWSmem = 2 * kWQHalf + 4 * kWKTile + 1024;  // queries, keys and values; alignment
-constexpr uint32_t kWCols = 256;                 // tensor memory: S and P (2 x 64), O
+// A block's tile of TILES accumulators.
+template <int TILES>
+struct WideL {
+  static constexpr int kRows = TILES * kWRows;
+  // warps: 4 TILES softmax, 4 TILES conversion (two: keys, then values), then the
+  // accumulators' scores and outputs
+  static constexpr int kSoft = 4 * TILES, kQk = 2 * kSoft, kPv = kQk + TILES;
+  static constexpr int kThreads = 320 * TILES;
+  static constexpr int kBlocks = 3 - TILES;  // of an SM
+  static constexpr uint32_t kSmem = 2 * TILES * kWQHalf + 4 * kWKTile + 1024;  // queries, keys and values; alignment
+  static constexpr uint32_t kCols = 256 * TILES;  // tensor memory: S and P (2 x 64 each), O
+};
 constexpr float kWBase = 7.f, kWGrow = 8.f;
 
 // Byte of 16-byte chunk ch (0..7, eight f16 each) of row r in 64 columns.
@@ -60,23 +76,39 @@ __device__ __forceinline__ uint64_t w_desc_mn(uint32_t smem_addr) {
   return d;
 }
 
-__device__ __forceinline__ void w_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
+// A whole warp comes here, and the lane with `one` issues: where a branch leaves one lane
+// alone, the operands have to be brought into the warp's registers for each instruction,
+// and it took up to 125 cycles to issue what the tensor cores need 48 for.
+__device__ __forceinline__ void w_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc,
+                                      uint32_t one) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc), "r"(one)
       : "memory");
 }
 // A from tensor memory.
 __device__ __forceinline__ void w_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
-                                         bool acc) {
+                                         bool acc, uint32_t one) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "setp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc), "r"(one)
+      : "memory");
+}
+// 1 in one lane of the warp.
+__device__ __forceinline__ uint32_t w_elect() {
+  uint32_t r;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
-      : "memory");
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r));
+  return r;
 }
 
 // Columns of the thread's lane, there on return.
@@ -178,8 +210,9 @@ __device__ __forceinline__ float w_max3(float x, float y, float z) {
 // Barriers of the two buffers: keys and values stored, scores there (and the keys'
 // place free), probabilities there, output added (the values' and their place
 // free); queries of the segment stored.
+template <int TILES>
 struct WideBars {
-  uint64_t k_full[2], v_full[2], s_done[2], p_full[2], o_done[2], q_full;
+  uint64_t k_full[2], v_full[2], s_done[TILES][2], p_full[TILES][2], o_done[TILES][2], q_full[TILES];
 };
 
 // Keys of step i of a segment.
@@ -213,19 +246,22 @@ __device__ __forceinline__ void w_wait(uint64_t (&b)[2], uint32_t n, bool& bad) 
 
 }  // namespace
 
-__global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
+template <int TILES>
+__global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
+    k_kv8_wide(const Kv8Attn a) {
+  using L = WideL<TILES>;
   extern __shared__ unsigned char smem_raw[];
   __shared__ Kv8PlanSmem s_plan;
-  __shared__ WideBars bar;
+  __shared__ WideBars<TILES> bar;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_nan, s_fail, s_more;
-  __shared__ Kv8Cursor s_cur;  // of the softmax warps
-  __shared__ Kv8Seg s_seg;
-  __shared__ float s_qs[kWRows];
+  __shared__ int s_nan, s_fail, s_more[TILES];
+  __shared__ Kv8Cursor s_cur[TILES];  // of the softmax warps
+  __shared__ Kv8Seg s_seg[TILES];
+  __shared__ float s_qs[L::kRows];
   unsigned char* const smem =
       reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   unsigned char* const Qs = smem;
-  unsigned char* const Ks = Qs + 2 * kWQHalf;   // [2 buffers]
+  unsigned char* const Ks = Qs + 2 * TILES * kWQHalf;   // [2 buffers]
   unsigned char* const Vs = Ks + 2 * kWKTile;
   const int tid = threadIdx.x, warp = tid >> 5;
 
@@ -233,70 +269,82 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bar.k_full[i], 128);
       mbar_init(&bar.v_full[i], 128);
-      mbar_init(&bar.p_full[i], 128);
-      mbar_init(&bar.s_done[i], 1);
-      mbar_init(&bar.o_done[i], 1);
+      for (int t = 0; t < TILES; ++t) {
+        mbar_init(&bar.p_full[t][i], 128);
+        mbar_init(&bar.s_done[t][i], 1);
+        mbar_init(&bar.o_done[t][i], 1);
+      }
     }
-    mbar_init(&bar.q_full, 128);
+    for (int t = 0; t < TILES; ++t) mbar_init(&bar.q_full[t], 128);
     mbar_init_fence();
     s_nan = s_fail = 0;
     a.desc[blockIdx.x].nr = 0;
   }
-  if (warp == 8) tc_alloc(&s_tmem, kWCols);
+  if (warp == L::kQk) tc_alloc(&s_tmem, L::kCols);
   tc_fence_before();
-  Kv8Cursor cur = kv8_plan<kWRows, kWKeys, kWThreads>(a, s_plan);  // (with block barriers)
+  Kv8Cursor cur = kv8_plan<L::kRows, kWKeys, L::kThreads>(a, s_plan);  // (with block barriers)
   tc_fence_after();
   pdl_launch_dependents();
-  const uint32_t tm = s_tmem, tmO = tm + 2 * kWKeys;
-  if (tid == 0) s_cur = cur;
+  // tensor memory: the accumulators' scores, two buffers each, then their outputs
+  const uint32_t tm = s_tmem;
+  constexpr uint32_t kS = 2 * kWKeys, kO = TILES * kS;
+  if (warp < L::kSoft && (tid & 127) == 0) s_cur[tid >> 7] = cur;
   uint32_t n = 0;  // steps so far: the barriers' phases
   bool bad = false;
 
-  // registers: 128 x 120 + 128 x 72 + 64 x 96 = 320 x 96, what the block was launched with
-  if (warp == 8) {
+  // registers: 128 x 120 + 128 x 72 + 64 x 96 = 320 x 96, what the block was launched with;
+  // two accumulators: 256 x 136 + 256 x 72 + 128 x 64 = 640 x 96
+  if (TILES == 2 && warp >= L::kQk) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+  if (warp >= L::kQk && warp < L::kPv) {
     // ------------------------------------------------------------ scores
-    if ((tid & 31) == 0) {
-      Kv8Seg sg;
-      const uint64_t dq = sdesc_k128(smem_u32(Qs)), dk = sdesc_k128(smem_u32(Ks));
-      for (uint32_t seg = 0; kv8_next<kWRows, kWKeys>(a, cur, sg); ++seg) {
-        if (!bad) bad = !w_sleep(&bar.q_full, seg & 1);
-        for (int i = 0; i < sg.nu; ++i, ++n) {
-          w_wait(bar.k_full, n, bad);
-          if (n >= 2) w_wait(bar.o_done, n - 2, bad);  // P of that step was read there
-          tc_fence_after();
-          const uint32_t buf = n & 1;
+    Kv8Seg sg;
+    const uint32_t one = w_elect();
+    const int t = warp - L::kQk;
+    const uint32_t tmS = tm + t * kS;
+    const uint64_t dq = sdesc_k128(smem_u32(Qs)) + (2 * t * kWQHalf >> 4);
+    const uint64_t dk = sdesc_k128(smem_u32(Ks));
+    for (uint32_t seg = 0; kv8_next<L::kRows, kWKeys>(a, cur, sg); ++seg) {
+      if (!bad) bad = !w_sleep(&bar.q_full[t], seg & 1);
+      for (int i = 0; i < sg.nu; ++i, ++n) {
+        w_wait(bar.k_full, n, bad);
+        if (n >= 2) w_wait(bar.o_done[t], n - 2, bad);  // P of that step was read there
+        __syncwarp();
+        tc_fence_after();
+        const uint32_t buf = n & 1;
+        if (t == 0 || sg.it.nr > t * kWRows)
 #pragma unroll
           for (int k = 0; k < 8; ++k)
-            w_mma(tm + buf * kWKeys, dq + (((k >> 2) * kWQHalf + (k & 3) * 32) >> 4),
-                  dk + ((buf * kWKTile + (k >> 2) * kWKHalf + (k & 3) * 32) >> 4), kWIdesc, k > 0);
-          tc_commit(&bar.s_done[buf]);
-        }
+            w_mma(tmS + buf * kWKeys, dq + (((k >> 2) * kWQHalf + (k & 3) * 32) >> 4),
+                  dk + ((buf * kWKTile + (k >> 2) * kWKHalf + (k & 3) * 32) >> 4), kWIdesc, k > 0,
+                  one);
+        if (one) tc_commit(&bar.s_done[t][buf]);
       }
     }
-    __syncwarp();
-  } else if (warp == 9) {
+  } else if (warp >= L::kPv && warp < L::kPv + TILES) {
     // ------------------------------------------------------------ outputs
-    if ((tid & 31) == 0) {
-      Kv8Seg sg;
-      const uint64_t dv = w_desc_mn(smem_u32(Vs));
-      while (kv8_next<kWRows, kWKeys>(a, cur, sg))
-        for (int i = 0; i < sg.nu; ++i, ++n) {
-          w_wait(bar.v_full, n, bad);
-          w_wait(bar.p_full, n, bad);
-          tc_fence_after();
-          const uint32_t buf = n & 1;
+    Kv8Seg sg;
+    const uint32_t one = w_elect();
+    const int t = warp - L::kPv;
+    const uint32_t tmS = tm + t * kS, tmO = tm + kO + t * kWHd;
+    const uint64_t dv = w_desc_mn(smem_u32(Vs));
+    while (kv8_next<L::kRows, kWKeys>(a, cur, sg))
+      for (int i = 0; i < sg.nu; ++i, ++n) {
+        w_wait(bar.v_full, n, bad);
+        w_wait(bar.p_full[t], n, bad);
+        __syncwarp();
+        tc_fence_after();
+        const uint32_t buf = n & 1;
+        if (t == 0 || sg.it.nr > t * kWRows)
 #pragma unroll
           for (int k = 0; k < kWKeys / 16; ++k)  // 16 keys: 8 words of P, two 8-row groups of V
-            w_mma_ts(tmO, tm + buf * kWKeys + 8 * k, dv + ((buf * kWKTile + k * 2048) >> 4),
-                     kWIdescV, i > 0 || k > 0);
-          tc_commit(&bar.o_done[buf]);
-        }
-    }
-    __syncwarp();
-  } else if (warp >= 4 && warp < 8) {
+            w_mma_ts(tmO, tmS + buf * kWKeys + 8 * k, dv + ((buf * kWKTile + k * 2048) >> 4),
+                     kWIdescV, i > 0 || k > 0, one);
+        if (one) tc_commit(&bar.o_done[t][buf]);
+      }
+  } else if (warp >= L::kSoft && warp < L::kQk) {
     // ------------------------------------------------------------ codes to f16
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    const int ct = tid - 128;
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");  // (64: spills, 88 us for 77)
+    const int ct = tid & 127;
     // the step that is loaded next: its first row in the cache, the keys (counted from
     // it) that some row sees, those that every row sees, steps left in the segment
     int64_t off = 0;
@@ -308,7 +356,7 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
         return true;
       }
       Kv8Seg sg;
-      if (!kv8_next<kWRows, kWKeys>(a, cur, sg)) return false;
+      if (!kv8_next<L::kRows, kWKeys>(a, cur, sg)) return false;
       const int k0 = w_key0(sg, 0);
       off = (((int64_t)sg.it.b * a.Hkv + sg.g) * a.max_seq + k0) * kWHd;
       lo = sg.it.lo - k0, hi = sg.it.hi - k0;
@@ -317,7 +365,7 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
       left = sg.nu;
       return true;
     };
-    uint4 kc[4], vc[4];  // rows ct / 8 + 16 j of a step, 16 codes each
+    // rows ct / 8 + 16 j of a step, 16 codes each
     auto load = [&](const uint8_t* base, uint4 (&c)[4]) {
       const uint8_t* p = base + off + ct * 16;
 #pragma unroll
@@ -345,48 +393,72 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
       }
       w_smem_fence();
     };
-    bool more = advance();
-    if (more) {
-      load(a.k, kc);
-      load(a.v, vc);
-    }
-    for (; more; ++n) {
-      const uint32_t buf = (n & 1) * kWKTile;
-      if (n >= 2) w_wait(bar.s_done, n - 2, bad);
-      store(Ks + buf, kc);
-      mbar_arrive(&bar.k_full[n & 1]);
-      if (0 < flo || kWKeys - 1 > fhi) {  // not every row sees every key
-        uint32_t any = 0;
+    // NaN codes of values to zero, in a step that not every row sees whole
+    auto zero_nan = [&](uint4 (&c)[4]) {
+      uint32_t any = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          uint32_t* w = reinterpret_cast<uint32_t*>(&vc[j]);
+      for (int j = 0; j < 4; ++j) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&c[j]);
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const uint32_t m = e4m3_nan_mask(w[x]);
-            any |= m;
-            w[x] &= ~((m >> 7) * 0xffu);
-          }
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t m = e4m3_nan_mask(w[x]);
+          any |= m;
+          w[x] &= ~((m >> 7) * 0xffu);
         }
-        if (any) s_nan = 1;  // (published by the arrival below)
       }
-      more = advance();
-      if (more) load(a.k, kc);
-      if (n >= 2) w_wait(bar.o_done, n - 2, bad);
-      store(Vs + buf, vc);
-      mbar_arrive(&bar.v_full[n & 1]);
-      if (more) load(a.v, vc);
+      if (any) s_nan = 1;  // (published by the arrival that follows)
+    };
+    bool more = advance();
+    if constexpr (TILES == 1) {  // keys and values in turn, a step ahead
+      uint4 kc[4], vc[4];
+      if (more) {
+        load(a.k, kc);
+        load(a.v, vc);
+      }
+      for (; more; ++n) {
+        const uint32_t buf = (n & 1) * kWKTile;
+        if (n >= 2) w_wait(bar.s_done[0], n - 2, bad);
+        store(Ks + buf, kc);
+        mbar_arrive(&bar.k_full[n & 1]);
+        if (0 < flo || kWKeys - 1 > fhi) zero_nan(vc);
+        more = advance();
+        if (more) load(a.k, kc);
+        if (n >= 2) w_wait(bar.o_done[0], n - 2, bad);
+        store(Vs + buf, vc);
+        mbar_arrive(&bar.v_full[n & 1]);
+        if (more) load(a.v, vc);
+      }
+    } else {  // four warps each
+      const bool values = warp >= L::kSoft + 4;
+      const uint8_t* const base = values ? a.v : a.k;
+      unsigned char* const tile = values ? Vs : Ks;
+      uint4 c[4];
+      if (more) load(base, c);
+      for (; more; ++n) {
+        if (values && (0 < flo || kWKeys - 1 > fhi)) zero_nan(c);
+        if (n >= 2)
+#pragma unroll
+          for (int t = 0; t < TILES; ++t) w_wait(values ? bar.o_done[t] : bar.s_done[t], n - 2, bad);
+        store(tile + (n & 1) * kWKTile, c);
+        mbar_arrive(values ? &bar.v_full[n & 1] : &bar.k_full[n & 1]);
+        more = advance();
+        if (more) load(base, c);
+      }
     }
-  } else if (warp < 4) {
+  } else if (warp < L::kSoft) {
     // ------------------------------------------------------------ softmax
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
-    const int row = tid;
-    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    if constexpr (TILES == 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
+    const int t = TILES == 1 ? 0 : warp >> 2, ttid = tid & 127;  // the accumulator, its thread
+    const int row = tid;  // of the tile
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t tmS = tm + t * kS + lanes, tmO = tm + kO + t * kWHd + lanes;
     for (;;) {
       // the segment stands in shared memory: the steps need the registers
-      if (tid == 0) s_more = kv8_next<kWRows, kWKeys>(a, s_cur, s_seg);
-      named_sync(1, 128);
-      if (!s_more) break;
-      const Kv8Seg& sg = s_seg;
+      if (ttid == 0) s_more[t] = kv8_next<L::kRows, kWKeys>(a, s_cur[t], s_seg[t]);
+      named_sync(1 + t, 128);
+      if (!s_more[t]) break;
+      const Kv8Seg& sg = s_seg[t];
       const Kv8Item& it = sg.it;
       // queries as f16, sixteen lanes a row (rows past the last: the last one's, not
       // used); the products of the segment before are done with theirs
@@ -394,11 +466,11 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
         const int ch = tid % 16;
         const __nv_bfloat16* const q0 = static_cast<const __nv_bfloat16*>(a.q) + ch * 8 +
                                         (int64_t)it.b * a.M * a.q_stride + (int64_t)sg.g * a.G * kWHd;
-        unsigned char* const own = Qs + (ch >> 3) * kWQHalf;
+        unsigned char* const own = Qs + (2 * t + (ch >> 3)) * kWQHalf;
         uint4 u[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const int r = it.r0 + min(j * 8 + tid / 16, it.nr - 1), m = a.byG(r);
+          const int r = it.r0 + min(t * kWRows + j * 8 + ttid / 16, it.nr - 1), m = a.byG(r);
           u[j] = w_load16(q0 + m * a.q_stride + (r - m * a.G) * kWHd);
         }
 #pragma unroll
@@ -418,7 +490,7 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
               amax[j] = fmaxf(amax[j], __shfl_xor_sync(0xffffffffu, amax[j], o));
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int qr = (j0 + j) * 8 + tid / 16;
+            const int qr = (j0 + j) * 8 + ttid / 16;
             const int ex = min(max((int)(__float_as_uint(amax[j]) >> 23) - 127 - 13, -100), 115);
             const float inv = pow2i(-ex);
             float f[8];
@@ -426,14 +498,14 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
             *reinterpret_cast<uint4*>(own + w_place(qr, ch & 7)) =
                 make_uint4(half2_bits(f[0] * inv, f[1] * inv), half2_bits(f[2] * inv, f[3] * inv),
                            half2_bits(f[4] * inv, f[5] * inv), half2_bits(f[6] * inv, f[7] * inv));
-            if (ch == 0) s_qs[qr] = pow2i(ex) * a.scale;
+            if (ch == 0) s_qs[t * kWRows + qr] = pow2i(ex) * a.scale;
           }
         }
       }
       w_smem_fence();
       tc_fence_before();
-      mbar_arrive(&bar.q_full);
-      named_sync(1, 128);
+      mbar_arrive(&bar.q_full[t]);
+      named_sync(1 + t, 128);
       const float qs = s_qs[row];  // scores = products * qs * key scale
       const bool live = warp * 32 < it.nr;  // the warp has rows
       const size_t slab = (size_t)it.b * a.Hkv + sg.g;
@@ -455,13 +527,13 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
           nks = __ldg(ksp + i + 1);
           nvs = __ldg(vsp + i + 1);
         }
-        w_wait(bar.s_done, n, bad);
+        w_wait(bar.s_done[t], n, bad);
         __syncwarp();
         tc_fence_after();
         if (live) {
           const int k0 = w_key0(sg, i);
           const bool full = k0 >= full_lo && k0 + kWKeys - 1 <= full_hi;
-          const uint32_t at = tm + lanes + (n & 1) * kWKeys;
+          const uint32_t at = tmS + (n & 1) * kWKeys;
           const float c = qs * ks;
           uint32_t r[64];
           w_ld64(at, r);
@@ -493,16 +565,16 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
               vref = vs;
             }
             if (i > 0) {
-              w_wait(bar.o_done, n - 1, bad);
+              w_wait(bar.o_done[t], n - 1, bad);
               __syncwarp();
               tc_fence_after();
 #pragma unroll 1
               for (int q = 0; q < 8; ++q) {
                 uint32_t o[16];
-                w_ld16(tmO + lanes + 16 * q, o);
+                w_ld16(tmO + 16 * q, o);
 #pragma unroll
                 for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
-                w_st16(tmO + lanes + 16 * q, o);
+                w_st16(tmO + 16 * q, o);
               }
             }
           }
@@ -514,7 +586,7 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
           for (int x = 0; x < 64; x += 2) {
             const float2 z =
                 unpack2(fma2(pack2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), c2, t2));
-            float e0 = ex2_approx(z.x), e1 = ex2_approx(z.y);
+            const float e0 = ex2_approx(z.x), e1 = ex2_approx(z.y);
             sum2 = add2(sum2, pack2(e0, e1));
             r[x / 2] = half2_bits(e0 * rel, e1 * rel);
           }
@@ -524,9 +596,9 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
           w_st_wait();
         }
         tc_fence_before();
-        mbar_arrive(&bar.p_full[n & 1]);
+        mbar_arrive(&bar.p_full[t][n & 1]);
       }
-      w_wait(bar.o_done, n - 1, bad);
+      w_wait(bar.o_done[t], n - 1, bad);
       __syncwarp();
       tc_fence_after();
       // ---- the rows' outputs, or the block's part of them
@@ -542,7 +614,7 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
 #pragma unroll 1
         for (int q = 0; q < 4; ++q) {
           uint32_t o[32];
-          w_ld32(tmO + lanes + 32 * q, o);
+          w_ld32(tmO + 32 * q, o);
           float f[32];
 #pragma unroll
           for (int x = 0; x < 32; ++x) f[x] = ls == 0.f ? 0.f : __uint_as_float(o[x]) * unit * vref;
@@ -584,16 +656,16 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
                              *reinterpret_cast<const uint32_t*>(&b1));
             } else {
               *reinterpret_cast<float4*>(
-                  a.part + ((size_t)slot * kWRows + warp * 32 + y) * kWHd + col) = v;
+                  a.part + ((size_t)slot * L::kRows + warp * 32 + y) * kWHd + col) = v;
             }
           }
           __syncwarp();
         }
         // (max, sum) as the merge weighs parts: p stands against 2^(ref - kWBase)
-        if (in && !whole) a.ml[(size_t)slot * kWRows + row] = make_float2(ref, ls);
+        if (in && !whole) a.ml[(size_t)slot * L::kRows + row] = make_float2(ref, ls);
       }
-      if (row == 0 && !sg.whole() && sg.u0 == 0) a.desc[blockIdx.x] = kv8_desc(a, s_cur, sg);
-      named_sync(1, 128);  // the next segment's queries go where outputs were exchanged
+      if (row == 0 && !sg.whole() && sg.u0 == 0) a.desc[blockIdx.x] = kv8_desc(a, s_cur[0], sg);
+      named_sync(1 + t, 128);  // the next segment's queries go where outputs were exchanged
       tc_fence_before();  // the next segment's products overwrite O, behind its p_full
     }
   }
@@ -602,7 +674,7 @@ __global__ void __launch_bounds__(kWThreads, 2) k_kv8_wide(const Kv8Attn a) {
   __syncthreads();
   tc_fence_after();
   if (tid == 0 && s_fail && a.err) atomicOr(a.err, (int)kErrTimeout);
-  if (warp == 8) tc_dealloc(tm, kWCols);
+  if (warp == L::kQk) tc_dealloc(tm, L::kCols);
 }
 
 }  // namespace ssd
