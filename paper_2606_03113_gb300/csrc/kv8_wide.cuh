@@ -23,7 +23,7 @@
 // 48 cycles for S, whose operands come from shared memory, 4 of 64 for O) and as much of
 // shared memory; 256 of code conversions (half with two accumulators), 256 of
 // exponentials; 700 of a scheduler's issue slots with two softmax warps there.  What it
-// takes is 1000 (1200 with one accumulator), the rest waits of one role for another.
+// takes is about 1050 (1200 with one accumulator), the rest waits of one role for another.
 // 512 rows of 32 heads over 8 KV heads x 7936 keys: 77 us = 867 TFLOP/s, of which 6 are
 // the start (the plan, the queries), 4 the last outputs and 8 the join; a floor of 34 at
 // the library's bf16 rate.  17 rows of 64 heads over 8 x 16000

@@ -14,6 +14,9 @@
 // more than kCand logits (ties, a spread that the threads' stride meets), the bound
 // is raised by bisection first.
 //
+// Bound by issue slots beside the loads: 1023 rows of 128256 bf16 logits, top 8, 58 us = 4.5
+// TB/s; in fp32 106 us = 5.0 TB/s; 13 rows in fp32, top 20, 9.0 us.
+//
 // Few rows are cut into chunks, one for each block of a cluster; the first block reads
 // the others' parts from their shared memory and joins them in order.
 //
