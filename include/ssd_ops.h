@@ -159,7 +159,7 @@ ssd_status ssd_kv8_append(const ssd_kv8_cache* cache, const void* k, const void*
                           int32_t* err_dev, void* stream);
 
 /* Bytes of device workspace that ssd_kv8_attention needs for these sizes,
- * whatever the lengths (0: invalid). */
+ * whatever the lengths (0: invalid; 256: it uses none, and takes NULL). */
 size_t ssd_kv8_attention_bytes(const ssd_kv8_cache* cache, int32_t dtype, int32_t n_heads,
                                int32_t M);
 

@@ -497,8 +497,8 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
                          (int64_t)h * HD + c8,
                      acc);
         } else {
-          store_out8(a.part + ((size_t)slot * kRT + row) * HD + c8, acc);
-          if (c8 == 0) a.ml[(size_t)slot * kRT + row] = make_float2(gm, Ls);
+          store_out8(a.part + ((size_t)slot * a.part_rows + row) * HD + c8, acc);
+          if (c8 == 0) a.ml[(size_t)slot * a.part_rows + row] = make_float2(gm, Ls);
         }
       }
     }
@@ -550,7 +550,7 @@ __global__ void __launch_bounds__(kMWarps * 32, 3) k_kv8_merge(const Kv8Attn a) 
   __syncthreads();
   for (int row0 = blockIdx.y * kRows; row0 < d0.x; row0 += gridDim.y * kRows) {
     const int row = min(row0 + rl, d0.x - 1);
-    auto slot = [&](int x) -> size_t { return (size_t)s_slot[x] * RT + row; };
+    auto slot = [&](int x) -> size_t { return (size_t)s_slot[x] * a.part_rows + row; };
     auto part = [&](int x) -> Vec {
       return __ldcg(reinterpret_cast<const Vec*>(a.part + slot(x) * HD) + lane);
     };
@@ -698,20 +698,19 @@ cudaError_t kv8_device(int* sms) {
 struct Kv8Work {
   size_t ml, part, total;
 };
-Kv8Work kv8_work(int blocks, int rt, int hd) {
+Kv8Work kv8_work(int blocks, int rows, int hd) {
   Kv8Work w;
   w.ml = ((size_t)blocks * sizeof(Kv8Desc) + 255) / 256 * 256;
-  w.part = w.ml + ((size_t)2 * blocks * rt * sizeof(float2) + 255) / 256 * 256;
-  w.total = w.part + (size_t)2 * blocks * rt * hd * sizeof(float);
+  w.part = w.ml + ((size_t)2 * blocks * rows * sizeof(float2) + 255) / 256 * 256;
+  w.total = w.part + (size_t)2 * blocks * rows * hd * sizeof(float);
   return w;
 }
 
 template <typename T, int HD, int RT>
 cudaError_t merge_launch(const Kv8Attn& a, int P, cudaStream_t st) {
-  const int rows = a.M * a.G < RT ? a.M * a.G : RT;  // of a tile, at most
   cudaLaunchConfig_t cfg = {};
   constexpr int kWpr = RT == kRT ? kMWarps : 1;  // warps of a row
-  const int ny = (rows * kWpr + kMWarps - 1) / kMWarps;
+  const int ny = (a.part_rows * kWpr + kMWarps - 1) / kMWarps;
   cfg.gridDim = dim3(P, ny < kMRowBlocks ? ny : kMRowBlocks);
   cfg.blockDim = dim3(kMWarps * 32);
   cfg.stream = st;
@@ -767,7 +766,8 @@ constexpr int kWholeSeq = 512;
 struct Kv8Plan {
   int wide;  // accumulators of a wide tile, 0: not wide
   bool whole;
-  int rt, ku, max_blocks;
+  int rt, ku;
+  int max_blocks, part_rows;
   long long n_rt, units;  // tiles of a sequence; the line's places, at most
 };
 Kv8Plan plan_of(const ssd_kv8_cache* c, int dtype, int n_heads, int M) {
@@ -777,10 +777,12 @@ Kv8Plan plan_of(const ssd_kv8_cache* c, int dtype, int n_heads, int M) {
   p.wide = !wide ? 0 : rows > kWRows ? 2 : 1;
   p.whole = !p.wide && c->max_seq <= kWholeSeq;
   p.rt = p.wide ? p.wide * kWRows : kRT;
-  p.max_blocks = p.wide == 2 ? kKv8MaxBlocks / 2 : kKv8MaxBlocks;
+  p.part_rows = rows < p.rt ? (int)rows : p.rt;
   p.ku = p.wide ? kWKeys : kKv8Block;
   p.n_rt = (rows + p.rt - 1) / p.rt;
   p.units = p.n_rt * c->n_seq * c->n_kv_heads * ((c->max_seq + p.ku - 1) / p.ku + (p.wide == 2 ? kKv8ItemCost<256> : kKv8ItemCost<kRT>));
+  p.max_blocks = p.wide == 2 ? kKv8MaxBlocks / 2 : kKv8MaxBlocks;
+  if (p.units < p.max_blocks) p.max_blocks = (int)p.units;
   return p;
 }
 
@@ -805,7 +807,7 @@ extern "C" size_t ssd_kv8_attention_bytes(const ssd_kv8_cache* c, int32_t dtype,
     return 0;
   }
   const Kv8Plan p = plan_of(c, dtype, n_heads, M);
-  return p.whole ? 256 : kv8_work(p.max_blocks, p.rt, c->head_dim).total;
+  return p.whole ? 256 : kv8_work(p.max_blocks, p.part_rows, c->head_dim).total;
 }
 
 extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, int32_t dtype,
@@ -834,10 +836,12 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   const Kv8Plan plan = plan_of(c, dtype, n_heads, M);
   if (plan.units > 0x7fffffffll)
     return fail_op(SSD_ERR_CAPACITY, "n_seq x M x max_seq: more than 2^31 units of work");
-  const Kv8Work lay = kv8_work(plan.max_blocks, plan.rt, c->head_dim);
-  if (!workspace || ((uintptr_t)workspace & 255u))
-    return fail_op(SSD_ERR_INVALID_ARG, "workspace must be non-NULL and 256-byte aligned");
-  if (workspace_bytes < (plan.whole ? 256 : lay.total)) return fail_op(SSD_ERR_CAPACITY, "workspace too small");
+  const Kv8Work lay = kv8_work(plan.max_blocks, plan.part_rows, c->head_dim);
+  if (!plan.whole) {
+    if (!workspace || ((uintptr_t)workspace & 255u))
+      return fail_op(SSD_ERR_INVALID_ARG, "workspace must be non-NULL and 256-byte aligned");
+    if (workspace_bytes < lay.total) return fail_op(SSD_ERR_CAPACITY, "workspace too small");
+  }
   int sms = 0;
   cudaError_t e = kv8_device(&sms);
   if (e != cudaSuccess) return fail_op_cuda("ssd_kv8_attention", e);
@@ -871,7 +875,7 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   a.byRt = Kv8Div::of((uint32_t)plan.n_rt);
   int P = sms * (plan.wide == 2 ? 1 : 2);  // blocks of an SM
   if (P > plan.max_blocks) P = plan.max_blocks;
-  if (plan.units < P) P = (int)plan.units;
+  a.part_rows = plan.part_rows;
   a.whole = plan.whole;
   if (plan.whole) P = a.entries * a.Hkv;
   a.byP = Kv8Div::of((uint32_t)P);

@@ -47,11 +47,12 @@ struct Kv8Attn {
   int32_t* err;
   int64_t q_stride, out_stride;  // elements between rows
   int32_t n_seq, Hkv, G, M, max_seq, window, n_rt, entries;
+  int32_t part_rows;  // rows of a tile, at most
   int32_t whole;  // a block for each item, which is not shared: no parts
   float scale;  // log2(e) / sqrt(head_dim)
   struct Kv8Desc* desc;
-  float* part;  // [2 P][RT][hd] normalised partial outputs
-  float2* ml;   // [2 P][RT] their (max, sum), max in powers of two
+  float* part;  // [2 P][part_rows][hd] normalised partial outputs
+  float2* ml;   // [2 P][part_rows] their (max, sum), max in powers of two
 };
 
 // What block i of the attention left to be joined: the item that begins in its

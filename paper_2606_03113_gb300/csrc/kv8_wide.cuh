@@ -656,13 +656,13 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
                              *reinterpret_cast<const uint32_t*>(&b1));
             } else {
               *reinterpret_cast<float4*>(
-                  a.part + ((size_t)slot * L::kRows + warp * 32 + y) * kWHd + col) = v;
+                  a.part + ((size_t)slot * a.part_rows + warp * 32 + y) * kWHd + col) = v;
             }
           }
           __syncwarp();
         }
         // (max, sum) as the merge weighs parts: p stands against 2^(ref - kWBase)
-        if (in && !whole) a.ml[(size_t)slot * L::kRows + row] = make_float2(ref, ls);
+        if (in && !whole) a.ml[(size_t)slot * a.part_rows + row] = make_float2(ref, ls);
       }
       if (row == 0 && !sg.whole() && sg.u0 == 0) a.desc[blockIdx.x] = kv8_desc(a, s_cur[0], sg);
       named_sync(1 + t, 128);  // the next segment's queries go where outputs were exchanged

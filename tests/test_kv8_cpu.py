@@ -100,15 +100,17 @@ def test_attention_refuses(kw, status):
 
 
 def test_attention_workspace_sizes():
-    """Small caches need none to speak of, others the same for every length."""
+    """Small caches need none, others what their parts take, the same for every length."""
     assert S.ssd_kv8_attention_bytes(cache(max_seq=512), S.SSD_DTYPE_BF16, 8, 1) == 256
     few = S.ssd_kv8_attention_bytes(cache(max_seq=576), S.SSD_DTYPE_BF16, 8, 1)
-    assert few == S.ssd_kv8_attention_bytes(cache(max_seq=1 << 20), S.SSD_DTYPE_BF16, 8, 8) > 256
-    assert S.ssd_kv8_attention_bytes(cache(max_seq=576), S.SSD_DTYPE_BF16, 8, 9) > few
-    with pytest.raises(S.SsdError) as e:
-        S.ssd_kv8_attention(cache(max_seq=512), BUF, S.SSD_DTYPE_BF16, 8, 1024, 1, BUF, 0, 0, 0, BUF, 1024,
-                            BUF, 255)
-    assert e.value.status == S.SSD_ERR_CAPACITY
+    more = S.ssd_kv8_attention_bytes(cache(max_seq=1 << 14), S.SSD_DTYPE_BF16, 8, 8)
+    assert 256 < few < more == S.ssd_kv8_attention_bytes(cache(max_seq=1 << 20), S.SSD_DTYPE_BF16, 8, 8)
+    assert S.ssd_kv8_attention_bytes(cache(max_seq=1 << 14), S.SSD_DTYPE_BF16, 8, 9) > more
+    for ws, nbytes, status in ((BUF, few - 1, S.SSD_ERR_CAPACITY), (0, few, S.SSD_ERR_INVALID_ARG)):
+        with pytest.raises(S.SsdError) as e:
+            S.ssd_kv8_attention(cache(max_seq=576), BUF, S.SSD_DTYPE_BF16, 8, 1024, 1, BUF, 0, 0, 0, BUF,
+                                1024, ws, nbytes)
+        assert e.value.status == status
 
 
 @pytest.mark.parametrize("kw,status", [
