@@ -90,6 +90,38 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   return r;
 }
 
+// The address of p, of this block's shared memory, in block `rank` of the cluster.
+__device__ __forceinline__ uint32_t in_block(const void* p, int rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float ld_cluster_f32(uint32_t a) {
+  float r;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(r) : "r"(a) : "memory");
+  return r;
+}
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t a) {
+  float4 r;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(r.x), "=f"(r.y), "=f"(r.z), "=f"(r.w)
+               : "r"(a)
+               : "memory");
+  return r;
+}
+__device__ __forceinline__ uint64_t ld_cluster_u64(uint32_t a) {
+  uint64_t r;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(r) : "r"(a) : "memory");
+  return r;
+}
+// Every thread of the cluster is here, and what they wrote before can be read.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile(
+      "barrier.cluster.arrive.release.aligned;\n\t"
+      "barrier.cluster.wait.acquire.aligned;" ::
+          : "memory");
+}
+
 // Message for ssd_last_error(NULL); returns s.  Does not throw.
 ssd_status fail_op(ssd_status s, const char* msg) noexcept;
 ssd_status fail_op_cuda(const char* what, cudaError_t e) noexcept;

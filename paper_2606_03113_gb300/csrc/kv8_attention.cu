@@ -3,7 +3,8 @@
 //   o_r = sum_j p_rj v_j / sum_j p_rj,  p_rj = e^(q_r . k_j / sqrt(hd) - max),
 // over the keys j that row r sees: first .. its own position, at most `window`.
 //
-// k_kv8_rows: a block takes a stretch of the plan's units (kv8_plan.cuh); its
+// k_kv8_rows: a block takes a stretch of the plan's units (kv8_plan.cuh), or, for short
+// caches, a cluster of blocks an item; a block's
 // four warps take the 16-key steps of an item in turn, each with its own running
 // maximum, sum and output, and the block joins the warps once per item.  Queries
 // and probabilities are f16 operands of mma.sync against the codes, which f16
@@ -48,6 +49,7 @@ constexpr int kVWarps = 4;
 constexpr int kVBlocks = 2;   // blocks of an SM
 constexpr int kVThreads = kVWarps * 32;
 constexpr int kKv8MaxBlocks = 320;
+constexpr int kSplitMax = 8;  // blocks of a short cache's item, a cluster, at most
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
                                         uint32_t b1) {
@@ -128,6 +130,7 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
   __shared__ float s_qs[kRT];  // scores = dot * s_qs * key scale
   __shared__ float s_m[kVWarps][kRT], s_l[kVWarps][kRT], s_ref[kVWarps][kRT];
   __shared__ float s_w[kVWarps][kRT], s_gm[kRT], s_sum[kRT];  // the warps' weights, the row's (max, sum)
+  __shared__ __align__(16) float s_part[kRT][HD];  // the block's part of a cluster's item
   __shared__ int s_nan;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int t = lane & 3, n8 = lane >> 2;
@@ -137,7 +140,8 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
 
   Kv8Cursor cur = kv8_plan<kRT, kKv8Block, kVThreads>(a, s_plan);
   pdl_launch_dependents();
-  if (tid == 0 && !a.whole) a.desc[blockIdx.x].nr = 0;
+  if (tid == 0 && !a.split) a.desc[blockIdx.x].nr = 0;
+  if (tid < kRT) s_sum[tid] = 0.f;
   Kv8Seg sg;
   while (kv8_next<kRT, kKv8Block>(a, cur, sg)) {
     const Kv8Item& it = sg.it;
@@ -485,7 +489,9 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
             }
           }
         }
-        if (whole) {
+        if (a.split > 1) {
+          store_out8(&s_part[row][c8], acc);
+        } else if (whole) {
           if (p < lo) {  // sees no key
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[j] = 0.f;
@@ -502,8 +508,54 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
         }
       }
     }
-    if (!whole && sg.u0 == 0 && tid == 0) a.desc[blockIdx.x] = kv8_desc(a, cur, sg);
+    if (!a.split && !whole && sg.u0 == 0 && tid == 0) a.desc[blockIdx.x] = kv8_desc(a, cur, sg);
     __syncthreads();
+  }
+  if (a.split > 1) {  // the cluster's parts together, each block some of the columns
+    const int i = (int)blockIdx.x / a.split, rank = (int)blockIdx.x - i * a.split;
+    const int e = i / a.Hkv, g = i - e * a.Hkv;
+    const Kv8Item it = kv8_entry<kRT, kKv8Block>(a, e);
+    cluster_sync();
+    for (int x = rank * kVThreads + tid; x < it.nr * NT; x += a.split * kVThreads) {
+      const int row = x / NT, c8 = (x % NT) * 8;
+      float w[kSplitMax], m[kSplitMax], gm = -INFINITY, sum = 0.f, acc[8];
+#pragma unroll
+      for (int y = 0; y < kSplitMax; ++y) {
+        w[y] = y < a.split ? ld_cluster_f32(in_block(&s_sum[row], y)) : 0.f;
+        m[y] = y < a.split ? ld_cluster_f32(in_block(&s_gm[row], y)) : 0.f;
+      }
+#pragma unroll
+      for (int y = 0; y < kSplitMax; ++y)  // (a sum of 0: the row sees none of the part's keys)
+        gm = fmaxf(gm, w[y] != 0.f ? m[y] : -INFINITY);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+#pragma unroll
+      for (int y = 0; y < kSplitMax; ++y) {
+        if (w[y] == 0.f) continue;
+        const uint32_t at = in_block(&s_part[row][c8], y);
+        const float4 u = ld_cluster_f32x4(at), v = ld_cluster_f32x4(at + 16);
+        const float wt = part_weight(m[y], gm) * w[y];
+        sum += wt;
+        acc[0] = fmaf(wt, u.x, acc[0]);
+        acc[1] = fmaf(wt, u.y, acc[1]);
+        acc[2] = fmaf(wt, u.z, acc[2]);
+        acc[3] = fmaf(wt, u.w, acc[3]);
+        acc[4] = fmaf(wt, v.x, acc[4]);
+        acc[5] = fmaf(wt, v.y, acc[5]);
+        acc[6] = fmaf(wt, v.z, acc[6]);
+        acc[7] = fmaf(wt, v.w, acc[7]);
+      }
+      const int r = it.r0 + row, mr = a.byG(r), h = g * a.G + r - mr * a.G;
+      const int p = kv8_row_pos(a, it, r);
+      const bool sees = kv8_row_lo(it, p, a.window) <= p;
+      const float inv = 1.f / sum;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] = sees ? acc[j] * inv : 0.f;
+      store_out8(static_cast<T*>(a.out) + ((int64_t)it.b * a.M + mr) * a.out_stride +
+                     (int64_t)h * HD + c8,
+                 acc);
+    }
+    cluster_sync();  // everybody has read this block's part
   }
 }
 
@@ -662,8 +714,11 @@ Kv8Device g_kv8_dev[64];
 
 template <typename T, int HD>
 cudaError_t prep_rows() {
-  return cudaFuncSetAttribute(k_kv8_rows<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)RowsL<HD>::template total<sizeof(T) == 4 ? 2 : 1>());
+  const cudaError_t e =
+      cudaFuncSetAttribute(k_kv8_rows<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           (int)RowsL<HD>::template total<sizeof(T) == 4 ? 2 : 1>());
+  if (e != cudaSuccess) return e;  // (clusters of more than eight have to be allowed)
+  return cudaFuncSetAttribute(k_kv8_rows<T, HD>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
 }
 
 template <int TILES>
@@ -725,9 +780,23 @@ cudaError_t merge_launch(const Kv8Attn& a, int P, cudaStream_t st) {
 template <typename T, int HD>
 cudaError_t rows_launch(const Kv8Attn& a, int P, cudaStream_t st) {
   const size_t smem = RowsL<HD>::template total<sizeof(T) == 4 ? 2 : 1>();
+  if (a.split > 1) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(P);
+    cfg.blockDim = dim3(kVThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = a.split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k_kv8_rows<T, HD>, a);
+  }
   k_kv8_rows<T, HD><<<P, kVThreads, smem, st>>>(a);
   const cudaError_t e = cudaGetLastError();
-  return e != cudaSuccess || a.whole ? e : merge_launch<T, HD, kRT>(a, P, st);
+  return e != cudaSuccess || a.split ? e : merge_launch<T, HD, kRT>(a, P, st);
 }
 
 template <int TILES>
@@ -754,18 +823,21 @@ cudaError_t wide_launch(const Kv8Attn& a, int P, cudaStream_t st) {
 //   100000         117/94.4     129/99.8     189/173      239/175      459/322
 //   16 x 1000     59.7/42.7    68.9/51.6    84.2/76.1     105/82.8     193/157
 constexpr int kWideFrom = 16;
-// Caches of up to 512 positions: a block for each item and no join (mma.sync kernel).  us,
-// shared / whole, at full caches of 128, 256, 512 and 1024 positions:
-//   1 sequence, 8 KV heads, 4 rows each     8.3/5.9   8.4/7.1    8.6/9.5    8.9/14.1
-//   1, 40 heads, 2 rows                     8.7/6.1   9.0/7.3    9.8/9.5   11.0/14.2
-//   16, 8 heads, 4 rows                    10.5/6.0  12.7/7.3   15.1/9.7   17.8/14.4
-//   32, 32 heads, 1 row                    23.8/22.0 30.0/28.8  42.8/44.7  64.2/68.1
-// and a launch less, which the host takes 2 to 3 us for.
-constexpr int kWholeSeq = 512;
+// Short caches: a cluster of blocks for each item, which joins its parts itself (mma.sync
+// kernel): of 1, 2, 4 or 8 blocks with 128 keys or more each, as long as there is room for
+// all, two on each of 152 SMs; up to 512 keys a block and 2048 in all.  us, line / clusters,
+// at full caches of 128, 512, 1024, 2048 and 4096 positions:
+//   1 sequence, 8 KV heads, 4 rows each     8.6/5.8   8.7/7.8   9.0/8.6   9.9/10.0  10.8/12.6
+//   1, 40 heads, 2 rows                     9.1/6.2  10.2/8.6  11.2/10.4 12.9/13.5  17.6/19.9
+//   4, 8 heads, 4 rows                      9.3/6.1  10.7/8.2  11.0/9.9  12.8/11.7  16.3/15.3
+//   16, 8 heads, 4 rows                    10.9/6.3  15.4/10.7 18.4/14.2 24.3/20.6  37.9/34.8
+// (sequences of one length, for which clusters are at their best), and a launch and a
+// workspace less, which the host takes 6 to 8 us for.
+constexpr int kSplitKeys = 128, kSplitBlocks = 304, kSplitSeq = 512, kSplitMost = 2048;
 
 struct Kv8Plan {
   int wide;  // accumulators of a wide tile, 0: not wide
-  bool whole;
+  int split;     // blocks of an item's own, 0: the line
   int rt, ku;
   int max_blocks, part_rows;
   long long n_rt, units;  // tiles of a sequence; the line's places, at most
@@ -775,12 +847,17 @@ Kv8Plan plan_of(const ssd_kv8_cache* c, int dtype, int n_heads, int M) {
   const long long rows = (long long)M * (n_heads / c->n_kv_heads);
   const bool wide = dtype == SSD_DTYPE_BF16 && c->head_dim == kWHd && rows > kWideFrom;
   p.wide = !wide ? 0 : rows > kWRows ? 2 : 1;
-  p.whole = !p.wide && c->max_seq <= kWholeSeq;
   p.rt = p.wide ? p.wide * kWRows : kRT;
   p.part_rows = rows < p.rt ? (int)rows : p.rt;
   p.ku = p.wide ? kWKeys : kKv8Block;
   p.n_rt = (rows + p.rt - 1) / p.rt;
   p.units = p.n_rt * c->n_seq * c->n_kv_heads * ((c->max_seq + p.ku - 1) / p.ku + (p.wide == 2 ? kKv8ItemCost<256> : kKv8ItemCost<kRT>));
+  const long long items = p.n_rt * c->n_seq * c->n_kv_heads;
+  p.split = 1;
+  while (p.split < kSplitMax && c->max_seq > kSplitKeys * p.split &&
+         items * p.split * 2 <= kSplitBlocks)
+    p.split *= 2;
+  if (p.wide || c->max_seq > kSplitSeq * p.split || c->max_seq > kSplitMost) p.split = 0;
   p.max_blocks = p.wide == 2 ? kKv8MaxBlocks / 2 : kKv8MaxBlocks;
   if (p.units < p.max_blocks) p.max_blocks = (int)p.units;
   return p;
@@ -807,7 +884,7 @@ extern "C" size_t ssd_kv8_attention_bytes(const ssd_kv8_cache* c, int32_t dtype,
     return 0;
   }
   const Kv8Plan p = plan_of(c, dtype, n_heads, M);
-  return p.whole ? 256 : kv8_work(p.max_blocks, p.part_rows, c->head_dim).total;
+  return p.split ? 256 : kv8_work(p.max_blocks, p.part_rows, c->head_dim).total;
 }
 
 extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, int32_t dtype,
@@ -837,7 +914,7 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   if (plan.units > 0x7fffffffll)
     return fail_op(SSD_ERR_CAPACITY, "n_seq x M x max_seq: more than 2^31 units of work");
   const Kv8Work lay = kv8_work(plan.max_blocks, plan.part_rows, c->head_dim);
-  if (!plan.whole) {
+  if (!plan.split) {
     if (!workspace || ((uintptr_t)workspace & 255u))
       return fail_op(SSD_ERR_INVALID_ARG, "workspace must be non-NULL and 256-byte aligned");
     if (workspace_bytes < lay.total) return fail_op(SSD_ERR_CAPACITY, "workspace too small");
@@ -876,8 +953,8 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   int P = sms * (plan.wide == 2 ? 1 : 2);  // blocks of an SM
   if (P > plan.max_blocks) P = plan.max_blocks;
   a.part_rows = plan.part_rows;
-  a.whole = plan.whole;
-  if (plan.whole) P = a.entries * a.Hkv;
+  a.split = plan.split;
+  if (plan.split) P = a.entries * a.Hkv * plan.split;
   a.byP = Kv8Div::of((uint32_t)P);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool wide = c->head_dim == 128;

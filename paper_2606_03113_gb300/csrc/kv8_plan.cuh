@@ -9,7 +9,8 @@
 // the lengths are; they are read from device memory, so a captured launch serves
 // growing sequences.  A block's stretch of the line can begin and end inside an
 // item: it then leaves the item's partial sums in the workspace, and k_kv8_merge
-// joins them.
+// joins them.  Short caches have a cluster of blocks for each item instead, which joins its
+// sums itself.
 #pragma once
 
 #include "kv8.cuh"
@@ -48,7 +49,7 @@ struct Kv8Attn {
   int64_t q_stride, out_stride;  // elements between rows
   int32_t n_seq, Hkv, G, M, max_seq, window, n_rt, entries;
   int32_t part_rows;  // rows of a tile, at most
-  int32_t whole;  // a block for each item, which is not shared: no parts
+  int32_t split;  // 0: the line; else each item's own blocks, a cluster: no parts
   float scale;  // log2(e) / sqrt(head_dim)
   struct Kv8Desc* desc;
   float* part;  // [2 P][part_rows][hd] normalised partial outputs
@@ -88,7 +89,7 @@ __device__ __forceinline__ Kv8Item kv8_entry(const Kv8Attn& a, int e) {
   it.nr = 0;
   it.units = it.unit0 = it.lo = it.hi = 0;
   if (it.pos < 0 || n < 0 || n > a.M || it.pos > a.max_seq - n) {
-    if (it.rt == 0 && (blockIdx.x == 0 || a.whole) && a.err)
+    if (it.rt == 0 && (blockIdx.x == 0 || a.split) && a.err)
       atomicOr(a.err, n < 0 || n > a.M ? (int)kErrControl : (int)kErrCapacity);
     return it;
   }
@@ -146,10 +147,12 @@ template <int RT, int KU, int THREADS>
 __device__ __forceinline__ Kv8Cursor kv8_plan(const Kv8Attn& a, Kv8PlanSmem& sm) {
   static_assert(THREADS / 32 <= 32, "a sum for each warp");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (a.whole) {
-    const int e = (int)blockIdx.x / a.Hkv, g = (int)blockIdx.x - e * a.Hkv;
+  if (a.split) {
+    const int i = (int)blockIdx.x / a.split, rank = (int)blockIdx.x - i * a.split;
+    const int e = i / a.Hkv, g = i - e * a.Hkv;
     const Kv8Item own = kv8_entry<RT, KU>(a, e);
-    return Kv8Cursor{0, own.units, 0, e, g * kv8_len<RT, KU>(own)};
+    const int w0 = own.units * rank / a.split, w1 = own.units * (rank + 1) / a.split;
+    return Kv8Cursor{w0, w1, 0, e, g * kv8_len<RT, KU>(own) + w0};
   }
   const int per = (a.entries + THREADS - 1) / THREADS;
   const int e0 = min(tid * per, a.entries), e1 = min(e0 + per, a.entries);

@@ -206,10 +206,11 @@ def _check(case, q, vals, got, before):
     assert not bad[live].any(), (np.abs(out - ref)[live].max(), np.argwhere(bad)[:5])
 
 
-@pytest.mark.parametrize("room", [0, 640])
+@pytest.mark.parametrize("room", [0, 640, 2112])
 @pytest.mark.parametrize("case", ATTEND, ids=lambda c: "-".join(str(x) for x in c[:7]))
 def test_attention_against_64_bits(case, room):
-    """Also in a larger cache, where blocks share items and their parts are joined."""
+    """Also in larger caches: items of several blocks, a cluster, and of blocks that share all
+    items evenly, whose parts are joined behind them."""
     torch = _torch()
     case = case[:6] + (case[6] + room,) + case[7:]
     dtype, heads, kvh, hd, n, M, seq, pos, rows, first, window = case
@@ -227,7 +228,7 @@ def test_attention_against_64_bits(case, room):
 
 @pytest.mark.parametrize("M,window", [(4, 0), (4, 3), (17, 0), (70, 0)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("seq", [320, 1024])
+@pytest.mark.parametrize("seq", [320, 1024, 2560])
 def test_a_nan_value_reaches_the_rows_that_see_it(dtype, M, window, seq):
     """NaN codes of keys and values: rows that do not see the key are as if it were not there."""
     torch = _torch()
@@ -301,7 +302,7 @@ def test_scores_far_apart_and_scales_far_apart():
 
 @pytest.mark.parametrize("dtype,M,window", [("f32", 6, 50), ("bf16", 6, 50), ("bf16", 40, 50),
                                             ("bf16", 40, 130)])
-@pytest.mark.parametrize("seq", [320, 1024])
+@pytest.mark.parametrize("seq", [320, 1024, 2560])
 def test_large_values_behind_the_window_cost_nothing(dtype, M, window, seq):
     """A block of values 2^40 above the others that only the first rows of a tile still see: the
     others keep all their bits."""
@@ -325,7 +326,7 @@ def test_large_values_behind_the_window_cost_nothing(dtype, M, window, seq):
 
 
 @pytest.mark.parametrize("dtype,heads,hd,n,M,seq", [("bf16", 8, 128, 2, 3, 320), ("bf16", 8, 128, 2, 40, 640),
-                                                    ("f32", 4, 64, 3, 7, 2048)])
+                                                    ("f32", 4, 64, 3, 7, 2048), ("bf16", 4, 128, 1, 5, 2560)])
 def test_output_over_the_queries_of_fused_rows(dtype, heads, hd, n, M, seq):
     """q, k and v read in place from a product's rows, the output written over q; what
     stands behind it in the rows stays."""
@@ -367,7 +368,7 @@ def test_a_padded_sequence_in_anothers_place():
 def test_attention_leaves_bad_sequences_alone():
     from paper_2606_03113_gb300 import ssd as S
     torch = _torch()
-    for seq in (128, 1024):
+    for seq in (128, 1024, 2560):
         _bad_sequences(S, torch, seq)
 
 

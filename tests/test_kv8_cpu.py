@@ -83,14 +83,15 @@ def test_append_refuses(kw, status):
     (dict(heads=2), S.SSD_ERR_INVALID_ARG), (dict(qs=1020), S.SSD_ERR_INVALID_ARG),
     (dict(os=1028), S.SSD_ERR_INVALID_ARG), (dict(M=0), S.SSD_ERR_INVALID_ARG),
     (dict(M=1030), S.SSD_ERR_CAPACITY), (dict(window=-1), S.SSD_ERR_INVALID_ARG),
-    (dict(pos=0), S.SSD_ERR_INVALID_ARG), (dict(ws=0), S.SSD_ERR_INVALID_ARG),
-    (dict(ws=BUF + 16), S.SSD_ERR_INVALID_ARG), (dict(wb=1000), S.SSD_ERR_CAPACITY)])
+    (dict(pos=0), S.SSD_ERR_INVALID_ARG), (dict(seq=4096, ws=0), S.SSD_ERR_INVALID_ARG),
+    (dict(seq=4096, ws=BUF + 16), S.SSD_ERR_INVALID_ARG),
+    (dict(seq=4096, wb=1000), S.SSD_ERR_CAPACITY)])
 def test_attention_refuses(kw, status):
     a = dict(q=BUF, out=BUF, dtype=S.SSD_DTYPE_BF16, heads=8, qs=1024, os=1024, M=3, window=0, pos=BUF,
-             ws=BUF, wb=1 << 30)
+             ws=BUF, wb=1 << 30, seq=1024)
     a.update(kw)
     with pytest.raises(S.SsdError) as e:
-        S.ssd_kv8_attention(cache(), a["q"], a["dtype"], a["heads"], a["qs"], a["M"], a["pos"], 0, 0,
+        S.ssd_kv8_attention(cache(max_seq=a["seq"]), a["q"], a["dtype"], a["heads"], a["qs"], a["M"], a["pos"], 0, 0,
                             a["window"], a["out"], a["os"], a["ws"], a["wb"])
     assert e.value.status == status
     with pytest.raises(S.SsdError) as e:  # more than 2^31 units of work
@@ -102,13 +103,14 @@ def test_attention_refuses(kw, status):
 def test_attention_workspace_sizes():
     """Small caches need none, others what their parts take, the same for every length."""
     assert S.ssd_kv8_attention_bytes(cache(max_seq=512), S.SSD_DTYPE_BF16, 8, 1) == 256
-    few = S.ssd_kv8_attention_bytes(cache(max_seq=576), S.SSD_DTYPE_BF16, 8, 1)
+    assert S.ssd_kv8_attention_bytes(cache(max_seq=2048), S.SSD_DTYPE_BF16, 8, 1) == 256
+    few = S.ssd_kv8_attention_bytes(cache(max_seq=2112), S.SSD_DTYPE_BF16, 8, 1)
     more = S.ssd_kv8_attention_bytes(cache(max_seq=1 << 14), S.SSD_DTYPE_BF16, 8, 8)
     assert 256 < few < more == S.ssd_kv8_attention_bytes(cache(max_seq=1 << 20), S.SSD_DTYPE_BF16, 8, 8)
     assert S.ssd_kv8_attention_bytes(cache(max_seq=1 << 14), S.SSD_DTYPE_BF16, 8, 9) > more
     for ws, nbytes, status in ((BUF, few - 1, S.SSD_ERR_CAPACITY), (0, few, S.SSD_ERR_INVALID_ARG)):
         with pytest.raises(S.SsdError) as e:
-            S.ssd_kv8_attention(cache(max_seq=576), BUF, S.SSD_DTYPE_BF16, 8, 1024, 1, BUF, 0, 0, 0, BUF,
+            S.ssd_kv8_attention(cache(max_seq=2112), BUF, S.SSD_DTYPE_BF16, 8, 1024, 1, BUF, 0, 0, 0, BUF,
                                 1024, ws, nbytes)
         assert e.value.status == status
 
