@@ -4,9 +4,9 @@
 // over the keys j that row r sees: first .. its own position, at most `window`.
 //
 // k_kv8_rows: a block takes a stretch of the plan's units (kv8_plan.cuh), or, for short
-// caches, a cluster of blocks an item; a block's
-// four warps take the 16-key steps of an item in turn, each with its own running
-// maximum, sum and output, and the block joins the warps once per item.  Queries
+// caches, a cluster of blocks an item; its four warps take the 16-key steps of an item
+// in turn, each with its own running maximum, sum and output, and the block joins the
+// warps once per item.  Queries
 // and probabilities are f16 operands of mma.sync against the codes, which f16
 // holds exactly; a row of queries is first brought near f16's upper end by a
 // power of two, so a bf16 query is exact down to 2^-28 of its row's largest, and

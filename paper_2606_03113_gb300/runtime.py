@@ -454,12 +454,16 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top
     vocabulary give NaN and set a bit in `err` (device int32 [1]) where one is given.  Enqueues on
     `stream`, or on the current stream of the logits' device; does not synchronise."""
     code = _dtype_code(logits, "logits")
-    if logits.dim() != 2 or logits.shape[0] < 1 or logits.shape[1] < 1:
-        raise ValueError(f"logits must be [rows, vocab], not {list(logits.shape)}")
-    n, vocab = logits.shape
-    if vocab > 1 and logits.stride(1) != 1:
+    shape = logits.shape
+    if len(shape) != 2 or shape[0] < 1 or shape[1] < 1:
+        raise ValueError(f"logits must be [rows, vocab], not {list(shape)}")
+    n, vocab = shape
+    row, one = logits.stride()
+    if vocab > 1 and one != 1:
         raise ValueError("a row's logits must be consecutive")
-    if n > 1 and logits.stride(0) < vocab:
+    if n == 1:
+        row = vocab
+    elif row < vocab:
         raise ValueError("rows of logits must not overlap")
     if not 0 <= top_n <= S.MAX_TOP or top_n > vocab:
         raise ValueError(f"top_n must be in 0..{S.MAX_TOP} and at most the vocabulary, not {top_n}")
@@ -467,10 +471,11 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top
     zp = _on(logits, dev, "logits")
     ntok, tp = 0, 0
     if tokens is not None:
-        if tokens.dtype != torch.int32 or tokens.dim() not in (1, 2) or tokens.shape[0] != n or \
+        tshape = tokens.shape
+        if tokens.dtype is not torch.int32 or len(tshape) not in (1, 2) or tshape[0] != n or \
                 not tokens.is_contiguous():
             raise ValueError(f"tokens must be a contiguous int32 tensor [{n}, n] or [{n}]")
-        ntok = 1 if tokens.dim() == 1 else tokens.shape[1]
+        ntok = 1 if len(tshape) == 1 else tshape[1]
         tp = _on(tokens, dev, "tokens")
     if err is not None and (err.dtype != torch.int32 or err.numel() < 1):
         raise ValueError("err must be an int32 tensor")
@@ -479,18 +484,18 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, top
     if there is not None:
         with there:
             return token_logprobs(logits, tokens, top_n, temperature, err)
+    empty, f32 = torch.empty, torch.float32
     lp = ids = top = None
     lpp = ip = lp_top = 0
     if tokens is not None:
-        lp = torch.empty(tokens.shape, dtype=torch.float32, device=dev)
+        lp = empty(tshape, dtype=f32, device=dev)
         lpp = lp.data_ptr()
-    lse = torch.empty(n, dtype=torch.float32, device=dev)
-    entropy = torch.empty(n, dtype=torch.float32, device=dev)
+    lse = empty(n, dtype=f32, device=dev)
+    entropy = empty(n, dtype=f32, device=dev)
     if top_n > 0:
-        ids = torch.empty((n, top_n), dtype=torch.int32, device=dev)
-        top = torch.empty((n, top_n), dtype=torch.float32, device=dev)
+        ids = empty((n, top_n), dtype=torch.int32, device=dev)
+        top = empty((n, top_n), dtype=f32, device=dev)
         ip, lp_top = ids.data_ptr(), top.data_ptr()
-    S.ssd_token_logprobs(zp, code, n, vocab, logits.stride(0) if n > 1 else vocab, tp, ntok,
-                         temperature, top_n, lpp, lse.data_ptr(), entropy.data_ptr(), ip, lp_top,
-                         ep, _current_stream(dev.index))
+    S.ssd_token_logprobs(zp, code, n, vocab, row, tp, ntok, temperature, top_n, lpp, lse.data_ptr(),
+                         entropy.data_ptr(), ip, lp_top, ep, _current_stream(dev.index))
     return TokenLogprobs(lp, lse, entropy, ids, top, err)
