@@ -8,7 +8,7 @@
 // between blocks.
 //
 // Bound by bytes for prompts (a value is read once and its code written once): 2047
-// bf16 rows of 40 heads x 128, K and V, 14.6 us = 4.3 TB/s, the rows kept in
+// bf16 rows of 40 heads x 128, K and V, 12.8 us = 4.9 TB/s, the rows kept in
 // registers as they stand in memory.  By the launch and one round trip of memory for a few
 // rows: 16 sequences x 1 row of 8 heads 2.3 us.
 #include "kv8.cuh"
@@ -17,7 +17,9 @@ namespace ssd {
 
 namespace {
 
-constexpr int kApThreads = 256;
+// 2047 rows of 40 heads: 64 threads 14.1 us, 128 12.8, 256 14.0, 512 19.7; one row of 16
+// sequences: 2.9, 2.3, 2.2, 2.8.
+constexpr int kApThreads = 128;
 
 struct AppendArgs {
   uint8_t* code[2];
@@ -98,7 +100,7 @@ __global__ void __launch_bounds__(kApThreads) k_kv8_append(const AppendArgs a) {
   const int blk = p0 / kKv8Block + (int)blockIdx.x, k0 = blk * kKv8Block;
   if (n == 0 || k0 >= p0 + n) return;
   const int lo = max(p0 - k0, 0), hi = min(p0 + n - k0, kKv8Block);  // new rows of the block
-  const T* x = static_cast<const T*>(a.x[side]) + (int64_t)h * HD;
+  const T* x = static_cast<const T*>(side ? a.x[1] : a.x[0]) + (int64_t)h * HD;
   const int64_t row0 = (int64_t)b * a.M + (k0 - p0);  // input row of position k0
 
   Eight<T> f[kPer];
@@ -109,7 +111,7 @@ __global__ void __launch_bounds__(kApThreads) k_kv8_append(const AppendArgs a) {
     else f[i].zero();
   }
   const size_t slab = (size_t)b * a.heads + h;
-  float* sp = a.scale[side] + slab * (a.max_seq / kKv8Block) + blk;
+  float* sp = (side ? a.scale[1] : a.scale[0]) + slab * (a.max_seq / kKv8Block) + blk;
   const float old = lo > 0 ? *sp : 0.f;  // positions in front of lo hold codes at this scale
   __shared__ float warp_amax[2][kApThreads / 32];
   // the block's largest of m
@@ -142,7 +144,7 @@ __global__ void __launch_bounds__(kApThreads) k_kv8_append(const AppendArgs a) {
   const int e = kv8_scale_exp(amax);
   const float s = fmaxf(pow2i(e), old);
   const float inv = 1.0f / s;  // a power of two: exact
-  uint8_t* code = a.code[side] + (slab * a.max_seq + k0) * HD;
+  uint8_t* code = (side ? a.code[1] : a.code[0]) + (slab * a.max_seq + k0) * HD;
   if (s > old && lo > 0) {
     const float ratio = old / s;
     for (int c = tid; c < lo * kCpr; c += kApThreads) {
