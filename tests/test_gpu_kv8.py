@@ -175,6 +175,11 @@ ATTEND = [  # dtype, heads, kv heads, hd, n, M, seq, pos, rows, first, window
     ("bf16", 4, 1, 128, 1, 160, 896, [730], [160], [729], 0),
     ("bf16", 4, 2, 128, 300, 1, 640, [(37 * i) % 640 for i in range(300)], [1] * 300,
      [(11 * i) % 90 for i in range(300)], 0),
+    ("bf16", 32, 4, 128, 3, 40, 512, [100, 30, 400], [40, 33, 0], [120, 300, 0], 0),
+    ("bf16", 16, 2, 128, 2, 64, 1152, [1000, 5], [64, 50], [0, 20], 100),
+    ("bf16", 16, 2, 128, 5, 17, 832, [800, 1, 64, 127, 0], [17, 16, 1, 17, 17], [0, 0, 0, 5, 9], 0),
+    ("bf16", 129, 1, 128, 1, 1, 320, [319], [1], [0], 0),
+    ("bf16", 128, 1, 128, 2, 2, 192, [100, 63], [2, 1], [0, 0], 0),
 ]
 
 
@@ -269,6 +274,21 @@ def test_infinite_and_nan_queries_stay_in_their_rows():
     got = c.attention(q, _ints([100]))
     hit = torch.zeros(5, 8, dtype=torch.bool, device="cuda")
     hit[1, 3] = hit[2, 6] = True
+    assert bool(got[0][hit].isnan().all())
+    assert torch.equal(got[0][~hit], clean[0][~hit])
+
+
+@pytest.mark.parametrize("M", [9, 40, 75])
+def test_infinite_and_nan_queries_among_many_rows(M):
+    torch = _torch()
+    case = ("bf16", 8, 2, 128, 1, M, 512, [300], [M], [0], 0)
+    c, q, vals, clean = _attend(case, 12)
+    q = q.clone()
+    q[0, 1, 3, 5] = float("-inf")
+    q[0, M - 1, 6, 7] = float("nan")
+    got = c.attention(q, _ints([300]))
+    hit = torch.zeros(M, 8, dtype=torch.bool, device="cuda")
+    hit[1, 3] = hit[M - 1, 6] = True
     assert bool(got[0][hit].isnan().all())
     assert torch.equal(got[0][~hit], clean[0][~hit])
 
@@ -474,6 +494,47 @@ def test_other_stream_and_captured_replays():
     s.synchronize()
     assert torch.equal(got, alone[1])
     c.check()
+
+
+@pytest.mark.parametrize("M,seq", [(5, 4096), (12, 4096), (40, 1024), (40, 4096)])
+def test_captured_calls_of_every_kind(M, seq):
+    """Two captured attentions over two caches, replayed at once as their sequences grow, against
+    plain calls; then two calls at once on streams of the caller's."""
+    torch = _torch()
+    g = torch.Generator(device="cuda").manual_seed(15)
+    kvh, heads, hd = 2, 8, 128
+    caches, qs, poss, outs, graphs = [], [], [], [], []
+    for i in range(2):
+        c = _cache(kvh, hd, seq)
+        x = torch.randn(1, seq, 2 * kvh, hd, generator=g, device="cuda").bfloat16()
+        c.append(x[:, :, :kvh], x[:, :, kvh:], _ints([0]))
+        caches.append(c)
+        qs.append(torch.randn(1, M, heads, hd, generator=g, device="cuda").bfloat16())
+        poss.append(_ints([0]))
+        outs.append(torch.zeros_like(qs[i]))
+        c.attention(qs[i], poss[i], out=outs[i])
+    for c, q, p, o in zip(caches, qs, poss, outs):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            c.attention(q, p, out=o)
+        graphs.append(gr)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for step in (0, 1, 63, 64, 500, seq - M):
+        for i in range(2):
+            poss[i].fill_(max(step - 40 * i, 0))
+        want = [c.attention(q, p) for c, q, p in zip(caches, qs, poss)]
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for gr, s in zip(graphs, streams):
+                with torch.cuda.stream(s):
+                    gr.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, outs)), step
+        got = [c.attention(q, p, stream=s) for c, q, p, s in zip(caches, qs, poss, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got)), step
+    for c in caches:
+        c.check()
 
 
 def test_a_verification_over_the_8_bit_cache():
