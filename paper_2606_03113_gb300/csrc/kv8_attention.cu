@@ -87,7 +87,8 @@ struct RowsL {
     const int x = HD == 128 ? ((kk >> 1 & 3) << 1) ^ ((kk & 1) << 2) : kk >> 1 & 3;
     return (uint32_t)(kk * HD + ((ch ^ x) << 4));
   }
-  static_assert(kVWarps * kRT * kOPad * 4 <= kVWarps * kWarpBytes, "the exchange fits the ring");
+  static_assert(kVWarps * kRT * kOPad * 4 + kRT * HD * 4 <= kVWarps * kWarpBytes,
+                "the exchange and the part fit the ring");
 };
 
 __device__ __forceinline__ void load_query8(const float* p, float (&f)[8]) {
@@ -130,13 +131,13 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
   __shared__ float s_qs[kRT];  // scores = dot * s_qs * key scale
   __shared__ float s_m[kVWarps][kRT], s_l[kVWarps][kRT], s_ref[kVWarps][kRT];
   __shared__ float s_w[kVWarps][kRT], s_gm[kRT], s_sum[kRT];  // the warps' weights, the row's (max, sum)
-  __shared__ __align__(16) float s_part[kRT][HD];  // the block's part of a cluster's item
   __shared__ int s_nan;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int t = lane & 3, n8 = lane >> 2;
   unsigned char* const wring = smem + warp * L::kWarpBytes;
   unsigned char* const Qs = smem + L::kQOff;
   float* const Ox = reinterpret_cast<float*>(smem);
+  float* const part = Ox + kVWarps * kRT * L::kOPad;  // [kRT][HD]: the block's part of a cluster's item
 
   Kv8Cursor cur = kv8_plan<kRT, kKv8Block, kVThreads>(a, s_plan);
   pdl_launch_dependents();
@@ -490,7 +491,7 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
           }
         }
         if (a.split > 1) {
-          store_out8(&s_part[row][c8], acc);
+          store_out8(part + row * HD + c8, acc);
         } else if (whole) {
           if (p < lo) {  // sees no key
 #pragma unroll
@@ -532,7 +533,7 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
 #pragma unroll
       for (int y = 0; y < kSplitMax; ++y) {
         if (w[y] == 0.f) continue;
-        const uint32_t at = in_block(&s_part[row][c8], y);
+        const uint32_t at = in_block(part + row * HD + c8, y);
         const float4 u = ld_cluster_f32x4(at), v = ld_cluster_f32x4(at + 16);
         const float wt = part_weight(m[y], gm) * w[y];
         sum += wt;
@@ -570,15 +571,23 @@ namespace ssd {
 // takes parts w, w + WPR, ..; their sums are added in order.
 // Bound by round trips to L2: a part's place depends on the item alone, so the
 // first parts are on their way while the weights are worked out.  Few rows have many
-// parts and get a block a row; many rows have few and get a warp.  About 8 of
-// the 77 us of 512 rows of 32 heads over 7936 keys.
+// parts and get a block a row; many rows have few and get a warp.  About 6 of
+// the 75 us of 512 rows of 32 heads over 7936 keys.
 constexpr int kMWarps = 8;
-constexpr int kMRowBlocks = 8;  // blocks that share an item's rows, at most
+// Blocks that share an item's rows, at most; parts of a warp on their way; blocks of an SM.
+// A warp a row: 17 rows of 64 heads over 8 x 16000 keys, 512 of 32 over 8 x 7936: 33.8 and 77.3 us
+// as for few rows, 30.6 and 75.5 so; two warps a row 32.0 and 84.8.
+template <int WPR>
+constexpr int kMRowBlocks = WPR == kMWarps ? 8 : 32;
+template <int WPR>
+constexpr int kMBatch = WPR == kMWarps ? 6 : 4;
+template <int WPR>
+constexpr int kMBlocks = WPR == kMWarps ? 3 : 4;
 
 template <typename T, int HD, int RT, int WPR>
-__global__ void __launch_bounds__(kMWarps * 32, 3) k_kv8_merge(const Kv8Attn a) {
+__global__ void __launch_bounds__(kMWarps * 32, kMBlocks<WPR>) k_kv8_merge(const Kv8Attn a) {
   constexpr int kC = HD / 32;  // columns of a lane
-  constexpr int kBatch = 6;    // parts of a warp on their way
+  constexpr int kBatch = kMBatch<WPR>;
   constexpr int kRows = kMWarps / WPR;
   using Vec = typename std::conditional<HD == 128, float4, float2>::type;
   __shared__ float2 s_ml[kRows][kKv8MaxBlocks + 1];
@@ -766,7 +775,7 @@ cudaError_t merge_launch(const Kv8Attn& a, int P, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   constexpr int kWpr = RT == kRT ? kMWarps : 1;  // warps of a row
   const int ny = (a.part_rows * kWpr + kMWarps - 1) / kMWarps;
-  cfg.gridDim = dim3(P, ny < kMRowBlocks ? ny : kMRowBlocks);
+  cfg.gridDim = dim3(P, ny < kMRowBlocks<kWpr> ? ny : kMRowBlocks<kWpr>);
   cfg.blockDim = dim3(kMWarps * 32);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
