@@ -818,13 +818,17 @@ cudaError_t wide_launch(const Kv8Attn& a, int P, cudaStream_t st) {
 
 // The kernel of a call.  Tiles on tcgen05 where a KV head has more than 16 query rows,
 // the type is bf16 and head_dim 128, with one accumulator of 128 rows, or two where there
-// are more; tiles of 16 on mma.sync otherwise.  us a call, mma.sync / tcgen05, by rows of 8 KV
-// heads (of 32 in the last line):
+// are more; tiles of 16 on mma.sync otherwise, and where these form clusters (below) that
+// have room all at once.  us a call, mma.sync / tcgen05, by rows of 8 KV heads (of 32 in the
+// third line):
 //                     16           17           32           48          128
-//   500 keys      10.3/12.7    11.0/12.9    11.1/13.7    11.9/14.2    17.6/17.4
 //   16000         18.8/22.9    28.5/23.1    28.9/24.5    34.9/25.5    63.7/35.1
 //   100000        51.4/64.9    90.6/65.1    90.6/66.6     126/67.8     293/81.3
 //   16 x 1000     58.7/71.0    97.7/72.6    99.7/79.6     146/82.7     369/103
+// clusters / tcgen05 (one accumulator):
+//   240 keys                    8.7/12.8     9.2/13.5     9.4/13.7    11.2/14.5
+//   1000                       10.2/14.7    12.0/15.8    12.4/16.3    13.8/18.6
+//   2000                       11.9/17.3    13.9/18.2    14.1/19.0
 // and one / two accumulators, 8 KV heads:
 //                    129          256          300          512         1024
 //   500 keys      19.2/19.3    21.3/22.5    22.1/23.3    23.2/24.9    32.4/28.0
@@ -854,19 +858,25 @@ struct Kv8Plan {
 Kv8Plan plan_of(const ssd_kv8_cache* c, int dtype, int n_heads, int M) {
   Kv8Plan p;
   const long long rows = (long long)M * (n_heads / c->n_kv_heads);
-  const bool wide = dtype == SSD_DTYPE_BF16 && c->head_dim == kWHd && rows > kWideFrom;
-  p.wide = !wide ? 0 : rows > kWRows ? 2 : 1;
+  const long long heads = (long long)c->n_seq * c->n_kv_heads;
+  const long long small = (rows + kRT - 1) / kRT * heads;  // items of 16 rows
+  p.split = 1;
+  while (p.split < kSplitMax && c->max_seq > kSplitKeys * p.split &&
+         small * p.split * 2 <= kSplitBlocks)
+    p.split *= 2;
+  if (c->max_seq > kSplitSeq * p.split || c->max_seq > kSplitMost) p.split = 0;
+  p.wide = 0;
+  if (dtype == SSD_DTYPE_BF16 && c->head_dim == kWHd && rows > kWideFrom &&
+      !(p.split && small * p.split <= kSplitBlocks)) {
+    p.wide = rows > kWRows ? 2 : 1;
+    p.split = 0;
+  }
   p.rt = p.wide ? p.wide * kWRows : kRT;
   p.part_rows = rows < p.rt ? (int)rows : p.rt;
   p.ku = p.wide ? kWKeys : kKv8Block;
   p.n_rt = (rows + p.rt - 1) / p.rt;
-  p.units = p.n_rt * c->n_seq * c->n_kv_heads * ((c->max_seq + p.ku - 1) / p.ku + (p.wide == 2 ? kKv8ItemCost<256> : kKv8ItemCost<kRT>));
-  const long long items = p.n_rt * c->n_seq * c->n_kv_heads;
-  p.split = 1;
-  while (p.split < kSplitMax && c->max_seq > kSplitKeys * p.split &&
-         items * p.split * 2 <= kSplitBlocks)
-    p.split *= 2;
-  if (p.wide || c->max_seq > kSplitSeq * p.split || c->max_seq > kSplitMost) p.split = 0;
+  p.units = p.n_rt * heads * ((c->max_seq + p.ku - 1) / p.ku +
+                              (p.wide == 2 ? kKv8ItemCost<256> : kKv8ItemCost<kRT>));
   p.max_blocks = p.wide == 2 ? kKv8MaxBlocks / 2 : kKv8MaxBlocks;
   if (p.units < p.max_blocks) p.max_blocks = (int)p.units;
   return p;

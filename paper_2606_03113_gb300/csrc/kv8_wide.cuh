@@ -24,10 +24,10 @@
 // shared memory; 256 of code conversions (half with two accumulators), 256 of
 // exponentials; 700 of a scheduler's issue slots with two softmax warps there.  What it
 // takes is about 1050 (1200 with one accumulator), the rest waits of one role for another.
-// 512 rows of 32 heads over 8 KV heads x 7936 keys: 77 us = 867 TFLOP/s, of which 6 are
-// the start (the plan, the queries), 4 the last outputs and 8 the join; a floor of 34 at
+// 512 rows of 32 heads over 8 KV heads x 7936 keys: 76 us = 881 TFLOP/s, of which 6 are
+// the start (the plan, the queries), 4 the last outputs and 6 the join; a floor of 34 at
 // the library's bf16 rate.  17 rows of 64 heads over 8 x 16000
-// keys: 34 us.
+// keys: 31 us.
 #pragma once
 
 namespace ssd {
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
       }
   } else if (warp >= L::kSoft && warp < L::kQk) {
     // ------------------------------------------------------------ codes to f16
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");  // (64: spills, 88 us for 77)
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");  // (64: spills, 88 us for 77 then)
     const int ct = tid & 127;
     // the step that is loaded next: its first row in the cache, the keys (counted from
     // it) that some row sees, those that every row sees, steps left in the segment

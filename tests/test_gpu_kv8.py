@@ -279,9 +279,10 @@ def test_infinite_and_nan_queries_stay_in_their_rows():
 
 
 @pytest.mark.parametrize("M", [9, 40, 75])
-def test_infinite_and_nan_queries_among_many_rows(M):
+@pytest.mark.parametrize("seq", [512, 2560])
+def test_infinite_and_nan_queries_among_many_rows(M, seq):
     torch = _torch()
-    case = ("bf16", 8, 2, 128, 1, M, 512, [300], [M], [0], 0)
+    case = ("bf16", 8, 2, 128, 1, M, seq, [300], [M], [0], 0)
     c, q, vals, clean = _attend(case, 12)
     q = q.clone()
     q[0, 1, 3, 5] = float("-inf")
@@ -346,7 +347,7 @@ def test_large_values_behind_the_window_cost_nothing(dtype, M, window, seq):
 
 
 @pytest.mark.parametrize("dtype,heads,hd,n,M,seq", [("bf16", 8, 128, 2, 3, 320), ("bf16", 8, 128, 2, 40, 640),
-                                                    ("f32", 4, 64, 3, 7, 2048), ("bf16", 4, 128, 1, 5, 2560)])
+                                                    ("f32", 4, 64, 3, 7, 2048), ("bf16", 4, 128, 1, 5, 2560), ("bf16", 8, 128, 2, 40, 2560)])
 def test_output_over_the_queries_of_fused_rows(dtype, heads, hd, n, M, seq):
     """q, k and v read in place from a product's rows, the output written over q; what
     stands behind it in the rows stays."""
@@ -388,15 +389,15 @@ def test_a_padded_sequence_in_anothers_place():
 def test_attention_leaves_bad_sequences_alone():
     from paper_2606_03113_gb300 import ssd as S
     torch = _torch()
-    for seq in (128, 1024, 2560):
-        _bad_sequences(S, torch, seq)
+    for seq, M in ((128, 3), (1024, 3), (2560, 3), (2560, 40), (2560, 130)):
+        _bad_sequences(S, torch, seq, M)
 
 
-def _bad_sequences(S, torch, seq):
+def _bad_sequences(S, torch, seq, M):
     c = _cache(2, 128, seq, n=5)
-    out = torch.full((5, 3, 4, 128), 5.0, device="cuda", dtype=torch.bfloat16)
+    out = torch.full((5, M, 4, 128), 5.0, device="cuda", dtype=torch.bfloat16)
     q = torch.ones_like(out)
-    c.attention(q, _ints([-1, seq - 2, 0, 2 ** 31 - 1, 5]), rows=_ints([3, 3, 4, 1, 3]), out=out)
+    c.attention(q, _ints([-1, seq - 2, 0, 2 ** 31 - 1, 5]), rows=_ints([3, 3, M + 1, 1, M]), out=out)
     with pytest.raises(S.SsdError):
         c.check()
     assert bool((out[:4] == 5.0).all()) and not bool((out[4] == 5.0).any())
