@@ -114,11 +114,12 @@ __device__ __forceinline__ uint64_t ld_cluster_u64(uint32_t a) {
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(r) : "r"(a) : "memory");
   return r;
 }
-// Every thread of the cluster is here, and what they wrote before can be read.
+// Every thread of the cluster is here, and what they wrote before can be read (a warp's
+// lanes can come apart).
 __device__ __forceinline__ void cluster_sync() {
   asm volatile(
-      "barrier.cluster.arrive.release.aligned;\n\t"
-      "barrier.cluster.wait.acquire.aligned;" ::
+      "barrier.cluster.arrive.release;\n\t"
+      "barrier.cluster.wait.acquire;" ::
           : "memory");
 }
 

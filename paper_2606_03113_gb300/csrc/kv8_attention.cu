@@ -723,11 +723,8 @@ Kv8Device g_kv8_dev[64];
 
 template <typename T, int HD>
 cudaError_t prep_rows() {
-  const cudaError_t e =
-      cudaFuncSetAttribute(k_kv8_rows<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           (int)RowsL<HD>::template total<sizeof(T) == 4 ? 2 : 1>());
-  if (e != cudaSuccess) return e;  // (clusters of more than eight have to be allowed)
-  return cudaFuncSetAttribute(k_kv8_rows<T, HD>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  return cudaFuncSetAttribute(k_kv8_rows<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)RowsL<HD>::template total<sizeof(T) == 4 ? 2 : 1>());
 }
 
 template <int TILES>
