@@ -21,10 +21,11 @@
 // fragments read them, the same copies reach 4.9 TB/s and not 6.3), and waits for no
 // other warp until the end of an item.
 //
-// Bound by bytes for long caches, with issue slots close behind: 32 heads over 8 KV
-// heads x 131072 keys 54 us = 4.95 TB/s, 24 ragged sequences of 32 heads, 5 rows, window 2500,
-// 85 us = 4.4 TB/s.  Two blocks of four warps an SM, which the registers (244 a
-// thread) allow.
+// Bound by bytes for long caches, with the latencies of two warps a scheduler close
+// behind (issue slots 49 %, ALU 45 % in use): 32 heads over 8 KV heads x 131072 keys 54 us
+// = 4.95 TB/s, 24 ragged sequences of 32 heads, 5 rows, window 2500,
+// 85 us = 4.4 TB/s.  Two blocks of four warps an SM, 244 registers a thread; three
+// of 168 take 59 us for those 54.
 //
 // A key that some row of the tile does not see can hold anything: its scores are
 // dropped by position, and a NaN code of such a value row is zeroed before the
