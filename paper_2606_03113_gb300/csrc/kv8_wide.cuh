@@ -534,7 +534,9 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
           const int k0 = w_key0(sg, i);
           const bool full = k0 >= full_lo && k0 + kWKeys - 1 <= full_hi;
           const uint32_t at = tmS + (n & 1) * kWKeys;
-          const float c = qs * ks;
+          // (never 0, as it is for small queries over a block of zero keys: the -inf of a key
+          // out of sight stays -inf in a product with it)
+          const float c = fmaxf(qs * ks, pow2i(-126));
           uint32_t r[64];
           w_ld64(at, r);
           if (!full) {
