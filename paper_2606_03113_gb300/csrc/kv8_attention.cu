@@ -359,7 +359,8 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float top = mx[i] == -INFINITY ? 0.f : mx[i] - 15.f;
+          // (rounded up: no probability passes 2^15 where the maximum's unit is above 1)
+          const float top = mx[i] == -INFINITY ? 0.f : __fadd_ru(mx[i], -15.f);
           const float vrel = fminf(vs * rref[i], 1.f);  // (above 1: a row that sees no key here)
           const float x = exp2f(z[n][2 * i] - top), y = exp2f(z[n][2 * i + 1] - top);
           ls[i] += x + y;

@@ -73,3 +73,54 @@ def test_zero_keys_and_zero_queries(dtype, M, seq, how):
     q = q.to(torch.float32 if dtype == "f32" else torch.bfloat16)
     for pos, window in ((70, 0), (70, 50), (200, 0), (200, 70)):
         _check(c, vals, q, pos, window)
+
+
+def _direction(M, dtype, size):
+    """Queries along the first axis alone."""
+    torch = _torch()
+    q = torch.zeros(1, M, HEADS, HD, device="cuda")
+    q[..., 0] = size
+    return q.to(torch.float32 if dtype == "f32" else torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype,M,seq", SMALL)
+def test_large_scores_in_small_tiles(dtype, M, seq):
+    _large_scores(dtype, M, seq)
+
+
+def _large_scores(dtype, M, seq):
+    """Scores whose distance in fp32 is many powers of two: a softmax is a choice there, and its
+    outputs stay between the values.  Values that are the same for every key come out as they are
+    whatever the probabilities; and one key whose score stands out by half its size is taken alone,
+    from both signs, as the running maximum grows key by key."""
+    torch = _torch()
+    bf16 = dtype == "bf16"
+    g = torch.Generator(device="cuda").manual_seed(43)
+    k = torch.randn(400, KVH, HD, generator=g, device="cuda")
+    w = torch.randn(1, KVH, HD, generator=g, device="cuda").expand(400, KVH, HD)
+    same, (_, wv) = _appended(k, w, seq)
+    q0 = torch.randn(1, M, HEADS, HD, generator=g, device="cuda")
+    want = np.repeat(wv[0, :, 0], HEADS // KVH, 0)[None, None]
+    v = torch.randn(400, KVH, HD, generator=g, device="cuda")
+    pos = 390 - M - 50
+    for e in [*range(12, 34), 60, 90]:
+        q = (q0 * 2.0 ** e).to(torch.bfloat16 if bf16 else torch.float32)
+        out = _values(same.attention(q, _ints([pos])))
+        assert np.isfinite(out).all(), (e, np.argwhere(~np.isfinite(out))[:3])
+        # (the scores' errors move probabilities, but here not the output)
+        tol = R.attend_bound(want, np.abs(want), np.zeros(want.shape[:3]), HD, 400, bf16)
+        assert (np.abs(out - want) <= tol).all(), e
+    for sign in (1.0, -1.0):
+        keys = torch.zeros(400, KVH, HD, device="cuda")
+        keys[:, :, 0] = 1.0 if sign > 0 else -32.0
+        peaks = [10, 70, 129, 150, pos + M // 2]
+        for i, p in enumerate(peaks):
+            keys[p, :, 0] = 2.0 ** (i + 1) if sign > 0 else -(2.0 ** (4 - i))
+        c, vals = _appended(keys, v, seq)
+        for e in (14, 18, 22, 24, 25, 26, 27, 28, 31, 40):
+            out = _values(c.attention(_direction(M, dtype, 2.0 ** e), _ints([pos])))
+            for m in range(M):
+                at = peaks[-1] if pos + m >= peaks[-1] else peaks[-2]
+                ref = np.repeat(vals[1][0, :, at], HEADS // KVH, 0)
+                tol = R.attend_bound(ref, np.abs(ref), np.zeros(HEADS), HD, 400, bf16)
+                assert (np.abs(out[0, m] - ref) <= tol).all(), (sign, e, m)
