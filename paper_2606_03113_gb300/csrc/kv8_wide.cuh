@@ -24,7 +24,7 @@
 // shared memory; 256 of code conversions (half with two accumulators), 256 of
 // exponentials; 700 of a scheduler's issue slots with two softmax warps there.  What it
 // takes is about 1050 (1200 with one accumulator), the rest waits of one role for another.
-// 512 rows of 32 heads over 8 KV heads x 7936 keys: 76 us = 881 TFLOP/s, of which 6 are
+// 512 rows of 32 heads over 8 KV heads x 7936 keys: 76 us = 874 TFLOP/s, of which 6 are
 // the start (the plan, the queries), 4 the last outputs and 6 the join; a floor of 34 at
 // the library's bf16 rate.  17 rows of 64 heads over 8 x 16000
 // keys: 31 us.
@@ -53,6 +53,7 @@ struct WideL {
   static constexpr uint32_t kCols = 256 * TILES;  // tensor memory: S and P (2 x 64 each), O
 };
 constexpr float kWBase = 7.f, kWGrow = 8.f;
+constexpr float kWFar = 1048576.f;  // 2^20: half a unit there is 2^-4
 
 // Byte of 16-byte chunk ch (0..7, eight f16 each) of row r in 64 columns.
 __device__ __forceinline__ uint32_t w_place(int r, int ch) {
@@ -292,7 +293,7 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
   uint32_t n = 0;  // steps so far: the barriers' phases
   bool bad = false;
 
-  // registers: 128 x 120 + 128 x 72 + 64 x 96 = 320 x 96, what the block was launched with;
+  // registers: 128 x 112 + 128 x 80 + 64 x 96 = 320 x 96, what the block was launched with;
   // two accumulators: 256 x 136 + 256 x 72 + 128 x 64 = 640 x 96
   if (TILES == 2 && warp >= L::kQk) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
   if (warp >= L::kQk && warp < L::kPv) {
@@ -343,7 +344,10 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
       }
   } else if (warp >= L::kSoft && warp < L::kQk) {
     // ------------------------------------------------------------ codes to f16
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");  // (64: spills, 88 us for 77 then)
+    // (too few here spill: one accumulator 31 us with 72 for 26 over 16000 keys and 40 rows, two
+    // 88 us with 64 for 77)
+    if constexpr (TILES == 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     const int ct = tid & 127;
     // the step that is loaded next: its first row in the cache, the keys (counted from
     // it) that some row sees, those that every row sees, steps left in the segment
@@ -447,7 +451,7 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
     }
   } else if (warp < L::kSoft) {
     // ------------------------------------------------------------ softmax
-    if constexpr (TILES == 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 120;");
+    if constexpr (TILES == 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
     else asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
     const int t = TILES == 1 ? 0 : warp >> 2, ttid = tid & 127;  // the accumulator, its thread
     const int row = tid;  // of the tile
@@ -518,6 +522,10 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
       const int plo = row < it.nr ? kv8_row_lo(it, phi, a.window) : 0;
       float ref = -INFINITY, ls = 0.f;   // of the row
       float vref = pow2i(-126);          // the output's unit, as in k_kv8_rows
+      // Some row of the warp has a ref whose rounding is more than a small part of a power of two:
+      // the product in the exponent is not rounded, so such a row's scores are, beforehand, and
+      // taken from ref.
+      bool far = false;
       // (rows that see nothing have no block whose scale means something)
       const bool any = it.lo <= it.hi;
       float nks = any ? __ldg(ksp) : 0.f, nvs = any ? __ldg(vsp) : 0.f;
@@ -536,7 +544,7 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
           const uint32_t at = tmS + (n & 1) * kWKeys;
           // (never 0, as it is for small queries over a block of zero keys: the -inf of a key
           // out of sight stays -inf in a product with it)
-          const float c = fmaxf(qs * ks, pow2i(-126));
+          float c = fmaxf(qs * ks, pow2i(-126));
           uint32_t r[64];
           w_ld64(at, r);
           if (!full) {
@@ -553,7 +561,8 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
               m[y] = w_max3(m[y], __uint_as_float(r[x + 2 * y]), __uint_as_float(r[x + 2 * y + 1]));
           float mx = fmaxf(w_max3(m[0], m[1], m[2]), m[3]);
           if (mx > -INFINITY) mx *= c;
-          const bool grow = mx > ref + kWGrow || (ref == -INFINITY && mx > ref);
+          // (rounded down: what stays is not above ref + 8, whatever ref's unit is)
+          const bool grow = mx > __fadd_rd(ref, kWGrow) || (ref == -INFINITY && mx > ref);
           const bool up = vs > vref && mx > -INFINITY;
           if (__any_sync(0xffffffffu, grow || up)) {
             float f = 1.f;
@@ -562,6 +571,7 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
               ref = mx;
               ls *= f;
             }
+            far = __any_sync(0xffffffffu, ref > -INFINITY && fabsf(ref) >= kWFar);
             if (up) {
               f *= vref / vs;
               vref = vs;
@@ -580,7 +590,15 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
               }
             }
           }
-          const float top = ref == -INFINITY ? 0.f : ref - kWBase;
+          float top = ref == -INFINITY ? 0.f : ref - kWBase;
+          if (far) {
+            const bool own = ref > -INFINITY && fabsf(ref) >= kWFar;
+            const float by = own ? c : 1.f, off = own ? ref : 0.f;
+#pragma unroll
+            for (int x = 0; x < 64; ++x)
+              r[x] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(r[x]), by), off));
+            if (own) c = 1.f, top = -kWBase;
+          }
           const float rel = fminf(vs / vref, 1.f);  // (above 1: a row that sees no key here)
           const uint64_t c2 = pack2(c, c), t2 = pack2(-top, -top);
           uint64_t sum2 = 0;

@@ -88,6 +88,11 @@ def test_large_scores_in_small_tiles(dtype, M, seq):
     _large_scores(dtype, M, seq)
 
 
+@pytest.mark.parametrize("dtype,M,seq", WIDE)
+def test_large_scores_in_wide_tiles(dtype, M, seq):
+    _large_scores(dtype, M, seq)
+
+
 def _large_scores(dtype, M, seq):
     """Scores whose distance in fp32 is many powers of two: a softmax is a choice there, and its
     outputs stay between the values.  Values that are the same for every key come out as they are
