@@ -57,6 +57,11 @@ __device__ __forceinline__ uint32_t e4m3_nan_mask(uint32_t w) {
   return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
 }
 
+// Unit of a query row times a key scale: what a product of their codes is multiplied with to be a
+// score.  Exact where it is in range; past the largest number it is that number (rounded towards
+// zero), so that a product of 0 stays a score of 0.
+__device__ __forceinline__ float kv8_factor(float unit, float scale) { return __fmul_rz(unit, scale); }
+
 // 2^x, as close as the hardware's instruction (2 ulp; a result below 2^-126 is 0).
 __device__ __forceinline__ float ex2_approx(float x) {
   float r;

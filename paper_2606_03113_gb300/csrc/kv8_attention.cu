@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          z[n][x] = (sc[0][n][x] + sc[1][n][x]) * (qs[x >> 1] * ks);
+          z[n][x] = (sc[0][n][x] + sc[1][n][x]) * kv8_factor(qs[x >> 1], ks);
           if (!full) {
             const int key = k0 + 8 * n + 2 * t + (x & 1);
             if (key < plo[x >> 1] || key > phi[x >> 1]) z[n][x] = -INFINITY;

@@ -544,7 +544,7 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
           const uint32_t at = tmS + (n & 1) * kWKeys;
           // (never 0, as it is for small queries over a block of zero keys: the -inf of a key
           // out of sight stays -inf in a product with it)
-          float c = fmaxf(qs * ks, pow2i(-126));
+          float c = fmaxf(kv8_factor(qs, ks), pow2i(-126));
           uint32_t r[64];
           w_ld64(at, r);
           if (!full) {

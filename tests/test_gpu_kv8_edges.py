@@ -129,3 +129,20 @@ def _large_scores(dtype, M, seq):
                 ref = np.repeat(vals[1][0, :, at], HEADS // KVH, 0)
                 tol = R.attend_bound(ref, np.abs(ref), np.zeros(HEADS), HD, 400, bf16)
                 assert (np.abs(out[0, m] - ref) <= tol).all(), (sign, e, m)
+
+
+@pytest.mark.parametrize("dtype,M,seq", FORMS)
+def test_a_factor_beyond_fp32_leaves_zero_scores_zero(dtype, M, seq):
+    """Zero keys that share a block with huge ones behind a row, under huge queries: the row's
+    scores are zeros, although scale times unit is past the largest number."""
+    torch = _torch()
+    g = torch.Generator(device="cuda").manual_seed(47)
+    x = torch.randn(320, 2 * KVH, HD, generator=g, device="cuda")
+    last = 70 + M - 1
+    k, v = x[:, :KVH] * 2.0 ** 60, x[:, KVH:]
+    k[:last + 1] = 0
+    assert last % 64 != 63
+    c, vals = _appended(k, v, seq)
+    q = (torch.randn(1, M, HEADS, HD, generator=g, device="cuda") * 2.0 ** 100).to(
+        torch.float32 if dtype == "f32" else torch.bfloat16)
+    _check(c, vals, q, 70)
