@@ -116,13 +116,15 @@ ssd_status ssd_gemv_noalloc(const void* W, int32_t dtype, int32_t rows, int32_t 
  * capture.  Calls on different streams can run at the same time where they
  * share no output and no workspace; so can captured ones.  The returned
  * status covers the host-side checks and the launches, ssd_last_error(NULL) has
- * its message; what only the device can see sets bits (SSD error bits) in
- * *err_dev (device int32, may be NULL), which the caller clears. */
+ * its message; what only the device can see sets bits (SSD_DEV_ERR_*) in
+ * *err_dev (device int32; NULL: nothing tells of it), which the caller clears. */
 #define SSD_KV8_BLOCK 64       /* positions that share a scale */
 #define SSD_KV8_MAX_SEQS 4096
 #define SSD_DEV_ERR_TOKEN 1    /* a token id outside [0, vocab) */
 #define SSD_DEV_ERR_CAPACITY 2 /* positions outside the cache */
 #define SSD_DEV_ERR_CONTROL 4  /* a number of rows outside 0..M */
+#define SSD_DEV_ERR_TIMEOUT 16 /* ssd_kv8_attention: a wait inside a kernel gave up after some
+                                * seconds; none of that call's outputs mean anything */
 
 /* Cache of one layer for n_seq sequences (all memory the caller's, device).
  * k, v: e4m3 codes [n_seq][n_kv_heads][max_seq][head_dim], 16-byte aligned; k_scale,

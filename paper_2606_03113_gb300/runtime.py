@@ -302,8 +302,9 @@ class KV8Cache:
     Calls enqueue on `stream`, or on the current stream of the cache's device, and do not
     synchronise; the caller orders streams, and keeps tensors that another stream made alive
     (`Tensor.record_stream`).  They can be captured into CUDA graphs after a first call outside
-    of a capture.  What only the device can see (positions outside the cache, bad row numbers)
-    leaves the sequence alone and sets a bit in `err`, which `check` reads.
+    of a capture.  What only the device can see sets a bit in `err`, which `check` reads: positions
+    outside the cache and bad row numbers leave the sequence alone, a kernel whose wait gave up
+    after some seconds leaves the call's outputs undefined.
 
     A sequence that takes over another's place and begins inside of a block of 64 positions (a
     padded batch whose pads are not appended) has its `k_scale[b]` and `v_scale[b]` zeroed first:
@@ -425,13 +426,13 @@ class KV8Cache:
         return out
 
     def check(self):
-        """Waits for the device and raises SsdError if a call since the last check found bad
-        positions or row numbers there."""
+        """Waits for the device and raises SsdError, with what it was, if a call since the last
+        check set an error bit there."""
         torch.cuda.synchronize(self.device)
         bits = int(self.err.item())
         if bits:
             self.err.zero_()
-            raise S.SsdError(S.SSD_ERR_DEVICE_FLAG, "KV8Cache", f"device error bits {bits}")
+            raise S.SsdError(S.SSD_ERR_DEVICE_FLAG, "KV8Cache", S.dev_err_text(bits))
 
 
 class TokenLogprobs(NamedTuple):

@@ -97,7 +97,17 @@ class ssd_exit_stats(C.Structure):
 KV8_BLOCK = 64        # positions of the 8-bit cache that share a scale
 KV8_MAX_SEQS = 4096
 MAX_TOP = 32          # most probable tokens of ssd_token_logprobs
-DEV_ERR_TOKEN, DEV_ERR_CAPACITY, DEV_ERR_CONTROL = 1, 2, 4
+DEV_ERR_TOKEN, DEV_ERR_CAPACITY, DEV_ERR_CONTROL, DEV_ERR_TIMEOUT = 1, 2, 4, 16
+DEV_ERR_NAMES = {DEV_ERR_TOKEN: "a token id outside the vocabulary",
+                 DEV_ERR_CAPACITY: "positions outside the cache",
+                 DEV_ERR_CONTROL: "a number of rows outside 0..M",
+                 DEV_ERR_TIMEOUT: "a wait inside a kernel gave up: the call's outputs are undefined"}
+
+
+def dev_err_text(bits: int) -> str:
+    """What the bits of a device error word say."""
+    said = [name for bit, name in DEV_ERR_NAMES.items() if bits & bit]
+    return f"device error bits {bits}" + (f" ({'; '.join(said)})" if said else "")
 
 
 class ssd_kv8_cache(C.Structure):

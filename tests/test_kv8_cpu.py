@@ -226,3 +226,23 @@ def test_reference_rounding_is_the_type_s():
                                     (3.3e38, 111)])
 def test_reference_scale(amax, e):
     assert R.scale_of(amax) == 2.0 ** e
+
+
+def test_every_error_bit_of_the_kernels_is_named():
+    """The bits that the kernels set are those of the header and of the binding, each with words."""
+    import re
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    csrc = os.path.join(root, "paper_2606_03113_gb300", "csrc")
+    header = open(os.path.join(root, "include", "ssd_ops.h")).read()
+    named = {k: int(v) for k, v in re.findall(r"#define SSD_DEV_ERR_(\w+) (\d+)", header)}
+    enum = dict(re.findall(r"kErr(\w+) = (\d+)", open(os.path.join(csrc, "common.cuh")).read()))
+    used = set()
+    for f in ("kv8_append.cu", "kv8_attention.cu", "kv8_plan.cuh", "kv8_wide.cuh", "logprobs.cu"):
+        used |= set(re.findall(r"kErr([A-Z]\w+)", open(os.path.join(csrc, f)).read()))
+    assert used == {"Token", "Capacity", "Control", "Timeout"}
+    assert named == {u.upper(): int(enum[u]) for u in used}
+    assert named == {k[8:]: v for k, v in vars(S).items() if k.startswith("DEV_ERR_") and k != "DEV_ERR_NAMES"}
+    assert set(S.DEV_ERR_NAMES) == set(named.values())
+    assert "gave up" in S.dev_err_text(16) and "positions" not in S.dev_err_text(16)
+    both = S.dev_err_text(S.DEV_ERR_CAPACITY | S.DEV_ERR_CONTROL)
+    assert "6" in both and "positions" in both and "rows" in both
