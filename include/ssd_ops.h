@@ -147,7 +147,8 @@ typedef struct {
  * 0 leaves the sequence alone) go to positions pos[b] + m (pos: device [n_seq]).
  * k, v: device, dtype SSD_DTYPE_F32 or _BF16, row m of sequence b at element
  * (b M + m) row_stride, its heads one behind the other: a product's rows q | k | v
- * can be read in place; pointers and row_stride in multiples of 16 bytes.
+ * can be read in place; pointers and row_stride in multiples of 16 bytes.  M in 1 .. max_seq
+ * (SSD_ERR_CAPACITY above, whatever rows says).
  * Positions from pos[b] on in its block count as free (a rollback needs no call):
  * the block's scale is the larger of that of the positions in front of pos[b] and
  * the new rows' own.  Where it grows, the codes in front are rounded to it again
@@ -161,7 +162,8 @@ ssd_status ssd_kv8_append(const ssd_kv8_cache* cache, const void* k, const void*
                           int32_t* err_dev, void* stream);
 
 /* Bytes of device workspace that ssd_kv8_attention needs for these sizes,
- * whatever the lengths (0: invalid; 256: it uses none, and takes NULL). */
+ * whatever the lengths (256: it uses none, and takes NULL; 0: sizes that it refuses,
+ * ssd_last_error(NULL) says why). */
 size_t ssd_kv8_attention_bytes(const ssd_kv8_cache* cache, int32_t dtype, int32_t n_heads,
                                int32_t M);
 
@@ -181,8 +183,8 @@ size_t ssd_kv8_attention_bytes(const ssd_kv8_cache* cache, int32_t dtype, int32_
  * bits (fp32: 22) where its product with its value's scale is above 2^-20 (fp32: 2^-17) of
  * the row's largest probability times the largest value scale that the row sees.  Below
  * these they lose bits one by one.  Equal calls give equal bits.
- * Any M >= 1, any n_heads / n_kv_heads; SSD_ERR_CAPACITY where n_seq x M x max_seq is
- * so large that the work has more than 2^31 parts.  workspace: 256-byte aligned,
+ * Any M in 1 .. max_seq, any n_heads / n_kv_heads; SSD_ERR_CAPACITY for larger M, and where
+ * n_seq x M x max_seq is so large that the work has more than 2^31 parts.  workspace: 256-byte aligned,
  * used by this call until it has run. */
 ssd_status ssd_kv8_attention(const ssd_kv8_cache* cache, const void* q, int32_t dtype,
                              int32_t n_heads, int64_t q_stride, int32_t M, const int32_t* pos,

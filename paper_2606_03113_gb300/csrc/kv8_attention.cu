@@ -881,13 +881,20 @@ Kv8Plan plan_of(const ssd_kv8_cache* c, int dtype, int n_heads, int M) {
   return p;
 }
 
-// What both attention entry points check; null: fine.
-const char* check_attention(const ssd_kv8_cache* c, int32_t dtype, int32_t n_heads, int32_t M) {
+// What both attention entry points check of the sizes, and their plan; null: fine.
+const char* check_attention(const ssd_kv8_cache* c, int32_t dtype, int32_t n_heads, int32_t M,
+                            Kv8Plan* plan, ssd_status* status) {
+  *status = c && c->head_dim != 64 && c->head_dim != 128 ? SSD_ERR_UNSUPPORTED : SSD_ERR_INVALID_ARG;
   if (const char* why = check_kv8(c)) return why;
   if (dtype != SSD_DTYPE_F32 && dtype != SSD_DTYPE_BF16) return "dtype must be fp32 or bf16";
   if (n_heads < c->n_kv_heads || n_heads % c->n_kv_heads || n_heads > 65536)
     return "n_heads must be a multiple of the cache's n_kv_heads";
   if (M < 1) return "M must be at least 1";
+  *status = SSD_ERR_CAPACITY;
+  if (M > c->max_seq) return "more rows than the cache has positions";
+  *plan = plan_of(c, dtype, n_heads, M);
+  if (plan->units > 0x7fffffffll) return "n_seq x M x max_seq: more than 2^31 units of work";
+  *status = SSD_OK;
   return nullptr;
 }
 
@@ -897,11 +904,12 @@ const char* check_attention(const ssd_kv8_cache* c, int32_t dtype, int32_t n_hea
 extern "C" size_t ssd_kv8_attention_bytes(const ssd_kv8_cache* c, int32_t dtype, int32_t n_heads,
                                           int32_t M) {
   using namespace ssd;
-  if (const char* why = check_attention(c, dtype, n_heads, M)) {
-    fail_op(SSD_ERR_INVALID_ARG, why);
+  Kv8Plan p;
+  ssd_status status;
+  if (const char* why = check_attention(c, dtype, n_heads, M, &p, &status)) {
+    fail_op(status, why);
     return 0;
   }
-  const Kv8Plan p = plan_of(c, dtype, n_heads, M);
   return p.split ? 256 : kv8_work(p.max_blocks, p.part_rows, c->head_dim).total;
 }
 
@@ -912,9 +920,10 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
                                         int64_t out_stride, void* workspace,
                                         size_t workspace_bytes, int32_t* err_dev, void* stream) {
   using namespace ssd;
-  if (const char* why = check_attention(c, dtype, n_heads, M))
-    return fail_op(c && c->head_dim != 64 && c->head_dim != 128 ? SSD_ERR_UNSUPPORTED
-                                                                : SSD_ERR_INVALID_ARG, why);
+  Kv8Plan plan;
+  ssd_status status;
+  if (const char* why = check_attention(c, dtype, n_heads, M, &plan, &status))
+    return fail_op(status, why);
   const int elt = dtype == SSD_DTYPE_BF16 ? 2 : 4;
   const int64_t len = (int64_t)n_heads * c->head_dim;
   if (!q || !out || !pos || ((uintptr_t)q & 15u) || ((uintptr_t)out & 15u))
@@ -926,11 +935,7 @@ extern "C" ssd_status ssd_kv8_attention(const ssd_kv8_cache* c, const void* q, i
   if (out == q && out_stride != q_stride)
     return fail_op(SSD_ERR_INVALID_ARG, "out is q, but their strides differ");
   if (window < 0) return fail_op(SSD_ERR_INVALID_ARG, "window must be 0 (none) or positive");
-  if (M > c->max_seq) return fail_op(SSD_ERR_CAPACITY, "more rows than the cache has positions");
   const int G = n_heads / c->n_kv_heads;
-  const Kv8Plan plan = plan_of(c, dtype, n_heads, M);
-  if (plan.units > 0x7fffffffll)
-    return fail_op(SSD_ERR_CAPACITY, "n_seq x M x max_seq: more than 2^31 units of work");
   const Kv8Work lay = kv8_work(plan.max_blocks, plan.part_rows, c->head_dim);
   if (!plan.split) {
     if (!workspace || ((uintptr_t)workspace & 255u))

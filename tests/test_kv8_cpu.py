@@ -246,3 +246,19 @@ def test_every_error_bit_of_the_kernels_is_named():
     assert "gave up" in S.dev_err_text(16) and "positions" not in S.dev_err_text(16)
     both = S.dev_err_text(S.DEV_ERR_CAPACITY | S.DEV_ERR_CONTROL)
     assert "6" in both and "positions" in both and "rows" in both
+
+
+@pytest.mark.parametrize("kw,M", [(dict(max_seq=64), 65), (dict(max_seq=1024), 1 << 30),
+                                  (dict(max_seq=1 << 30, n_seq=4096), 64)])
+def test_sizes_that_attention_refuses_have_no_workspace(kw, M):
+    """The size query says 0, with the message of the call itself."""
+    c = cache(**kw)
+    with pytest.raises(S.SsdError) as e:
+        S.ssd_kv8_attention(c, BUF, S.SSD_DTYPE_BF16, 8, 1024, M, BUF, 0, 0, 0, BUF, 1024, BUF, 1 << 40)
+    assert e.value.status == S.SSD_ERR_CAPACITY
+    why = S.lib().ssd_last_error(None)
+    with pytest.raises(S.SsdError):  # another message in between
+        S.ssd_kv8_append(cache(n_seq=0), BUF, BUF, S.SSD_DTYPE_BF16, 512, 1, BUF)
+    assert S.ssd_kv8_attention_bytes(c, S.SSD_DTYPE_BF16, 8, M) == 0
+    assert S.lib().ssd_last_error(None) == why
+    assert S.ssd_kv8_attention_bytes(cache(max_seq=64), S.SSD_DTYPE_BF16, 8, 64) > 0
