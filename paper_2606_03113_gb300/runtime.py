@@ -278,8 +278,10 @@ def _per_seq(t, n_seq: int, device: torch.device, what: str) -> int:
     return t.data_ptr()
 
 
-# The address of a device's current stream (its index given), without a Stream object.
-_current_stream = torch._C._cuda_getCurrentRawStream
+# The address of a device's current stream (its index given), without a Stream object where this
+# PyTorch has that call: one built without CUDA has not, and imports this module all the same.
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _elsewhere(device: torch.device, stream):

@@ -4,6 +4,7 @@ the GPU tests compare with, pinned against torch's own e4m3 type."""
 import ctypes as C
 import os
 import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -262,3 +263,28 @@ def test_sizes_that_attention_refuses_have_no_workspace(kw, M):
     assert S.ssd_kv8_attention_bytes(c, S.SSD_DTYPE_BF16, 8, M) == 0
     assert S.lib().ssd_last_error(None) == why
     assert S.ssd_kv8_attention_bytes(cache(max_seq=64), S.SSD_DTYPE_BF16, 8, 64) > 0
+
+
+def test_the_module_imports_with_a_torch_without_cuda():
+    """A PyTorch that lacks CUDA's own calls: the module, its checks and its refusals are there."""
+    code = """
+import torch
+if hasattr(torch._C, "_cuda_getCurrentRawStream"):
+    del torch._C._cuda_getCurrentRawStream
+from paper_2606_03113_gb300 import runtime
+c = runtime.KV8Cache(2, 64, 64, device="cpu")
+try:
+    c.append(torch.zeros(1, 1, 2, 64), torch.zeros(1, 1, 2, 64), torch.zeros(1, dtype=torch.int32))
+except ValueError as e:
+    assert "CUDA" in str(e), e
+else:
+    raise SystemExit("not refused")
+class Stream:
+    cuda_stream = 77
+torch.cuda.current_stream = lambda index: Stream()
+assert runtime._current_stream(0) == 77
+print("fine")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    got = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
+    assert got.returncode == 0 and got.stdout.strip() == "fine", got.stderr
