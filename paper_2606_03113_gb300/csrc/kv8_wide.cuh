@@ -214,6 +214,7 @@ __device__ __forceinline__ float w_max3(float x, float y, float z) {
 template <int TILES>
 struct WideBars {
   uint64_t k_full[2], v_full[2], s_done[TILES][2], p_full[TILES][2], o_done[TILES][2], q_full[TILES];
+  uint64_t drained;  // after a wait that gave up: the products still in flight are done
 };
 
 // Keys of step i of a segment.
@@ -277,6 +278,7 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
       }
     }
     for (int t = 0; t < TILES; ++t) mbar_init(&bar.q_full[t], 128);
+    mbar_init(&bar.drained, 2 * TILES);
     mbar_init_fence();
     s_nan = s_fail = 0;
     a.desc[blockIdx.x].nr = 0;
@@ -693,7 +695,16 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (tid == 0 && s_fail && a.err) atomicOr(a.err, (int)kErrTimeout);
+  if (s_fail) {  // products may still be at work in this block's memory
+    if (tid == 0 && a.err) atomicOr(a.err, (int)kErrTimeout);
+    if (warp >= L::kQk) {  // the warps that issue them, 2 TILES
+      if (w_elect()) tc_commit(&bar.drained);
+      w_sleep(&bar.drained, 0);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+  }
   if (warp == L::kQk) tc_dealloc(tm, L::kCols);
 }
 
