@@ -129,9 +129,10 @@ ssd_status ssd_gemv_noalloc(const void* W, int32_t dtype, int32_t rows, int32_t 
 /* Cache of one layer for n_seq sequences (all memory the caller's, device).
  * k, v: e4m3 codes [n_seq][n_kv_heads][max_seq][head_dim], 16-byte aligned; k_scale,
  * v_scale: fp32 [n_seq][n_kv_heads][max_seq / 64].  A value is code * scale of
- * its block of 64 positions.  A scale is the smallest power of two, 2^-120 to
- * 2^111, that brings the block's largest magnitude to 448 or less (beyond
- * 448 * 2^111 values are cut to that).  max_seq: a multiple of 64; head_dim 64 or 128
+ * its block of 64 positions.  A scale is a power of two, 2^-120 to 2^111: the smallest that
+ * brings the largest magnitude of the rows to 448 or less (beyond 448 * 2^111 values are cut
+ * to that) where the block is written from its first position, growing with later rows
+ * that need a larger one.  max_seq: a multiple of 64; head_dim 64 or 128
  * (SSD_ERR_UNSUPPORTED otherwise).  Codes need no initial value.  Scales need one, 0,
  * only where a sequence begins inside of a block (a padded batch whose pads are not
  * appended): what stands there counts as the scale of the positions in front. */
@@ -149,14 +150,18 @@ typedef struct {
  * (b M + m) row_stride, its heads one behind the other: a product's rows q | k | v
  * can be read in place; pointers and row_stride in multiples of 16 bytes.  M in 1 .. max_seq
  * (SSD_ERR_CAPACITY above, whatever rows says).
- * Positions from pos[b] on in its block count as free (a rollback needs no call):
- * the block's scale is the larger of that of the positions in front of pos[b] and
- * the new rows' own.  Where it grows, the codes in front are rounded to it again
+ * Positions from pos[b] on in its block count as free (a rollback needs no call).  Where
+ * pos[b] is inside of a block, the larger of the scale that stands there and the new rows'
+ * own becomes the block's; where that grows, the codes in front are rounded to it again
  * (nothing but values below 2^-6 of the new scale can change).  Codes from
  * pos[b] + rows[b] on are not written, but stand under a new scale in that block.
+ * So rows that are rolled back leave a trace: the scale that they raised stays until the
+ * block is written from its first position again, and what the codes in front lost
+ * to it does not come back.
  * NaN and infinities are stored as NaN and take no part in a scale.
  * A sequence whose positions do not lie in 0 .. max_seq - 1, or whose rows[b] does
- * not in 0 .. M, is left alone, with its error bit. */
+ * not in 0 .. M, is left alone, with its error bit; pos[b] is in 0 .. max_seq where rows[b]
+ * is 0, too. */
 ssd_status ssd_kv8_append(const ssd_kv8_cache* cache, const void* k, const void* v, int32_t dtype,
                           int64_t row_stride, int32_t M, const int32_t* pos, const int32_t* rows,
                           int32_t* err_dev, void* stream);

@@ -3,8 +3,9 @@
 //
 // Codes are e4m3 (4 significant bits, largest value 448).  kKv8Block positions
 // of one KV head share one fp32 scale, K and V apart; a scale is the smallest
-// power of two 2^e, kKv8MinExp <= e <= kKv8MaxExp, that brings the block's largest
-// magnitude to 448 or less.  A power of two costs e4m3 nothing (the codes are
+// power of two 2^e, kKv8MinExp <= e <= kKv8MaxExp, that brings the largest
+// magnitude written there to 448 or less, and does not shrink until the block is written
+// from its first position again.  A power of two costs e4m3 nothing (the codes are
 // floating-point numbers already), and it makes a product of code and scale
 // exact, a change of scale a shift of exponents, and the scale itself free to
 // move between the factors of a product.

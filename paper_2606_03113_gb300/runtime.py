@@ -360,7 +360,8 @@ class KV8Cache:
     def append(self, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
                rows: torch.Tensor | None = None, stream=None):
         """Writes k[b, m], v[b, m] ([n_seq, M, n_kv_heads, head_dim]) for m < rows[b] (all M
-        without `rows`) to positions pos[b] + m.  Positions from pos[b] on count as free."""
+        without `rows`) to positions pos[b] + m.  Positions from pos[b] on count as free; a scale
+        that rows rolled back have raised stays until its block is written from the start."""
         code = _dtype_code(k, "k")
         if v.dtype != k.dtype:
             raise ValueError("k and v must have one type")

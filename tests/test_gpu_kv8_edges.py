@@ -146,3 +146,34 @@ def test_a_factor_beyond_fp32_leaves_zero_scores_zero(dtype, M, seq):
     q = (torch.randn(1, M, HEADS, HD, generator=g, device="cuda") * 2.0 ** 100).to(
         torch.float32 if dtype == "f32" else torch.bfloat16)
     _check(c, vals, q, 70)
+
+
+def test_rows_rolled_back_leave_their_scale():
+    """A rejected outlier raises its block's scale for good: the accepted codes in front are rounded
+    to it, the next rows stand under it, and only a block written from its start has its own again."""
+    torch = _torch()
+    c = _cache(KVH, HD, 128)
+    ref = [(np.zeros((1, KVH, 128, HD)), np.zeros((1, KVH, 2))) for _ in range(2)]
+    g = torch.Generator(device="cuda").manual_seed(53)
+    x = torch.randn(1, 70, 2 * KVH, HD, generator=g, device="cuda")
+
+    def append(rows, pos):
+        c.append(rows[:, :, :KVH], rows[:, :, KVH:], _ints([pos]))
+        for (codes, scale), y, t, s in zip(ref, (rows[:, :, :KVH], rows[:, :, KVH:]), (c.k, c.v),
+                                           (c.k_scale, c.v_scale)):
+            R.append(codes, scale, y.cpu().numpy(), [pos], [rows.shape[1]])
+            assert np.array_equal(_values(t), codes)
+            assert np.array_equal(s.cpu().numpy().astype(np.float64), scale)
+        return c.k_scale[0, :, 0].clone(), _values(c.k)[0, :, :10].copy()
+
+    first, codes0 = append(x[:, :10], 0)
+    raised, codes1 = append(x[:, 10:13] * 2.0 ** 12, 10)       # drafted
+    per = [t.cpu().numpy().astype(np.float64)[:, None, None] for t in (first, raised)]
+    assert bool((raised > first).all())
+    assert not np.array_equal(codes0 * per[0], codes1 * per[1])  # small values in front are coarser
+    kept, codes2 = append(x[:, 10:12], 10)                      # rejected: others in their place
+    assert torch.equal(kept, raised) and np.array_equal(codes1, codes2)
+    anew, codes3 = append(x[:, :12], 0)
+    assert bool((anew < raised).all()) and np.array_equal(
+        codes3, R.e4m3_round(x[0, :10, :KVH].permute(1, 0, 2).cpu().numpy().astype(np.float64)
+                             / anew.cpu().numpy()[:, None, None]))
