@@ -34,13 +34,19 @@ def _held(c):
             for t, s in ((c.k, c.k_scale), (c.v, c.v_scale))]
 
 
-def _check(c, vals, q, pos, window=0):
+def _check(c, vals, q, pos, window=0, unit=0.0):
+    """unit: the largest value scale in sight, where value scales are far apart.  A probability
+    times its value's scale over that unit is an f16 number, off by 2^-25 (half of the smallest
+    one's distance) where it is below 2^-14.  The row's largest probability stands there at 2^7 or
+    more, and so does their sum; a code is 448 at most: each key's part of the output is off by up
+    to 2^-25 448 unit / 2^7."""
     M = q.shape[1]
     got = c.attention(q, _ints([pos]), window=window)
     c.check()
     ref = np.zeros(got.shape)
     mass, size = R.attend(_values(q), vals[0], vals[1], [pos], [M], [0], window, ref)
     tol = R.attend_bound(ref, mass, size, HD, pos + M, got.dtype == _torch().bfloat16)
+    tol += (pos + M) * 2.0 ** -32 * 448 * unit
     out = _values(got)
     assert np.isfinite(out).all(), np.argwhere(~np.isfinite(out))[:5]
     assert (np.abs(out - ref) <= tol).all(), np.abs(out - ref).max()
@@ -177,3 +183,28 @@ def test_rows_rolled_back_leave_their_scale():
     assert bool((anew < raised).all()) and np.array_equal(
         codes3, R.e4m3_round(x[0, :10, :KVH].permute(1, 0, 2).cpu().numpy().astype(np.float64)
                              / anew.cpu().numpy()[:, None, None]))
+
+
+@pytest.mark.parametrize("dtype,M,seq", FORMS)
+def test_maxima_and_units_that_move(dtype, M, seq):
+    """Value scales 2^20 apart both ways, blocks of zero values, and single keys that outweigh all
+    others at places where the value scale falls or rises: the running maximum and the output's unit
+    move together and apart."""
+    torch = _torch()
+    g = torch.Generator(device="cuda").manual_seed(59)
+    x = torch.randn(400, 2 * KVH, HD, generator=g, device="cuda")
+    k, v = x[:, :KVH], x[:, KVH:]
+    v[64:128] = 0
+    v[128:192] *= 2.0 ** 20
+    v[192:256] *= 2.0 ** -20
+    q = torch.randn(1, M, HEADS, HD, generator=g, device="cuda").to(
+        torch.float32 if dtype == "f32" else torch.bfloat16)
+    unit = q[0].float() / q[0].float().norm(dim=-1, keepdim=True)
+    for at, m, h, size in ((3, 0, 0, 40), (100, M - 1, 3, 30), (150, M // 2, 1, 50), (210, 0, 2, 60),
+                           (257, M - 1, 0, 60)):
+        k[at, h // (HEADS // KVH)] = size * unit[m, h]
+    c, vals = _appended(k, v, seq)
+    for pos in (62, 140, 255, 399 - M):
+        for window in (0, 90):
+            seen = c.v_scale[..., max(pos - window, 0) // 64 if window else 0:(pos + M - 1) // 64 + 1]
+            _check(c, vals, q, pos, window, float(seen.max()))
