@@ -526,7 +526,8 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
       float vref = pow2i(-126);          // the output's unit, as in k_kv8_rows
       // Some row of the warp has a ref whose rounding is more than a small part of a power of two:
       // the product in the exponent is not rounded, so such a row's scores are, beforehand, and
-      // taken from ref.
+      // taken from ref (in the branch below, which every step then takes: a branch of its own
+      // costs the others 0.5 %).
       bool far = false;
       // (rows that see nothing have no block whose scale means something)
       const bool any = it.lo <= it.hi;
@@ -566,14 +567,14 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
           // (rounded down: what stays is not above ref + 8, whatever ref's unit is)
           const bool grow = mx > __fadd_rd(ref, kWGrow) || (ref == -INFINITY && mx > ref);
           const bool up = vs > vref && mx > -INFINITY;
-          if (__any_sync(0xffffffffu, grow || up)) {
+          float base = ref;  // what the exponents below are taken from
+          if (__any_sync(0xffffffffu, grow || up || far)) {
             float f = 1.f;
             if (grow) {
               f = ref == -INFINITY ? 0.f : exp2f(ref - mx);
               ref = mx;
               ls *= f;
             }
-            far = __any_sync(0xffffffffu, ref > -INFINITY && fabsf(ref) >= kWFar);
             if (up) {
               f *= vref / vs;
               vref = vs;
@@ -591,16 +592,18 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
                 w_st16(tmO + 16 * q, o);
               }
             }
-          }
-          float top = ref == -INFINITY ? 0.f : ref - kWBase;
-          if (far) {
+            base = ref;
             const bool own = ref > -INFINITY && fabsf(ref) >= kWFar;
-            const float by = own ? c : 1.f, off = own ? ref : 0.f;
+            far = __any_sync(0xffffffffu, own);
+            if (far) {
+              const float by = own ? c : 1.f, off = own ? ref : 0.f;
 #pragma unroll
-            for (int x = 0; x < 64; ++x)
-              r[x] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(r[x]), by), off));
-            if (own) c = 1.f, top = -kWBase;
+              for (int x = 0; x < 64; ++x)
+                r[x] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(r[x]), by), off));
+              if (own) c = 1.f, base = 0.f;
+            }
           }
+          const float top = base == -INFINITY ? 0.f : base - kWBase;
           const float rel = fminf(vs / vref, 1.f);  // (above 1: a row that sees no key here)
           const uint64_t c2 = pack2(c, c), t2 = pack2(-top, -top);
           uint64_t sum2 = 0;
@@ -695,7 +698,7 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (s_fail) {  // products may still be at work in this block's memory
+  if (__builtin_expect(s_fail, 0)) {  // products may still be at work in this block's memory
     if (tid == 0 && a.err) atomicOr(a.err, (int)kErrTimeout);
     if (warp >= L::kQk) {  // the warps that issue them, 2 TILES
       if (w_elect()) tc_commit(&bar.drained);
