@@ -189,8 +189,8 @@ size_t ssd_kv8_attention_bytes(const ssd_kv8_cache* cache, int32_t dtype, int32_
  * the row's largest probability times the largest value scale that the row sees.  Below
  * these they lose bits one by one.  Equal calls give equal bits.
  * Any M in 1 .. max_seq, any n_heads / n_kv_heads; SSD_ERR_CAPACITY for larger M, and where
- * n_seq x M x max_seq is so large that the work has more than 2^31 parts.  workspace: 256-byte aligned,
- * used by this call until it has run. */
+ * n_seq x M x max_seq is so large that the work has more than 2^31 parts.  workspace: 256-byte
+ * aligned, used by this call until it has run. */
 ssd_status ssd_kv8_attention(const ssd_kv8_cache* cache, const void* q, int32_t dtype,
                              int32_t n_heads, int64_t q_stride, int32_t M, const int32_t* pos,
                              const int32_t* rows, const int32_t* first, int32_t window, void* out,
@@ -199,14 +199,15 @@ ssd_status ssd_kv8_attention(const ssd_kv8_cache* cache, const void* q, int32_t 
 
 #define SSD_MAX_TOP 32 /* most probable tokens of a row, at most */
 
-/* Log-probabilities over rows of logits z at temperature t (0.001..1000): of
- * softmax(z / t), each row's lse = ln sum e^(z/t), entropy in nats, the n_tokens given
- * tokens' log-probabilities z/t - lse and the top_n (0..32) most probable tokens (lower
- * id first on ties) with theirs.  logits: device, dtype SSD_DTYPE_F32 or _BF16, row r
- * at element r row_stride (>= vocab; any alignment of an element).  tokens: device
- * [n_rows][n_tokens], logprob the same in fp32 (both may be NULL when n_tokens is 0); id
- * -1 marks a place without a token, its result is 0; any other id outside [0, vocab)
- * gives NaN and its error bit.  lse, entropy: device fp32 [n_rows], each may be NULL.
+/* Log-probabilities over rows of logits z at temperature t (0.001..1000; z / t is z times
+ * 1 / t, which is rounded to fp32 once): of softmax(z / t), each row's lse = ln sum e^(z/t),
+ * entropy in nats, the n_tokens given tokens' log-probabilities z/t - lse and the top_n (0..32)
+ * most probable tokens (lower id first on ties) with theirs.  logits: device, dtype
+ * SSD_DTYPE_F32 or _BF16, row r at element r row_stride (>= vocab; any alignment of an
+ * element).  tokens: device [n_rows][n_tokens], logprob the same in fp32 (both may be NULL
+ * when n_tokens is 0); id -1 marks a place without a token, its result is 0; any other id
+ * outside [0, vocab) gives NaN and its error bit.  lse, entropy: device fp32 [n_rows], each may
+ * be NULL.
  * top_id, top_logprob: device [n_rows][top_n], in descending order; where a row has
  * fewer than top_n logits above -inf, the places left are id -1, -inf.
  * A logit of -inf is a token of probability 0.  A row of nothing else has lse -inf,

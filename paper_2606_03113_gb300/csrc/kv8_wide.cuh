@@ -24,7 +24,7 @@
 // shared memory; 256 of code conversions (half with two accumulators), 256 of
 // exponentials; 700 of a scheduler's issue slots with two softmax warps there.  What it
 // takes is about 1050 (1200 with one accumulator), the rest waits of one role for another.
-// 512 rows of 32 heads over 8 KV heads x 7936 keys: 76 us = 874 TFLOP/s, of which 6 are
+// 512 rows of 32 heads over 8 KV heads x 7936 keys: 76 us = 876 TFLOP/s, of which 6 are
 // the start (the plan, the queries), 4 the last outputs and 6 the join; a floor of 34 at
 // the library's bf16 rate.  17 rows of 64 heads over 8 x 16000
 // keys: 31 us.
@@ -412,7 +412,9 @@ __global__ void __launch_bounds__(WideL<TILES>::kThreads, WideL<TILES>::kBlocks)
           w[x] &= ~((m >> 7) * 0xffu);
         }
       }
-      if (any) s_nan = 1;  // (published by the arrival that follows)
+      // (published by the arrival that follows; it stays set for the block's later tiles, which
+      // then look at the values of their own steps of this kind again, byte by byte)
+      if (any) s_nan = 1;
     };
     bool more = advance();
     if constexpr (TILES == 1) {  // keys and values in turn, a step ahead

@@ -425,7 +425,8 @@ class KV8Cache:
         # (256: none is used; others stay this call's until the launches)
         work = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes > 256 else None
         S.ssd_kv8_attention(self._c, qp, code, heads, row, M, pp, rp, fp, window, out.data_ptr(), orow,
-                            work.data_ptr() if work is not None else 0, nbytes, self._err_at, _current_stream(self.device.index))
+                            work.data_ptr() if work is not None else 0, nbytes, self._err_at,
+                            _current_stream(self.device.index))
         return out
 
     def check(self):
