@@ -531,14 +531,21 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
       for (int y = 0; y < kSplitMax; ++y)  // (a sum of 0: the row sees none of the part's keys)
         gm = fmaxf(gm, w[y] != 0.f ? m[y] : -INFINITY);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+      for (int y = 0; y < kSplitMax; ++y) {
+        if (w[y] != 0.f) w[y] *= part_weight(m[y], gm);
+        sum += w[y];
+      }
+      // (the parts are weighed by w / sum: w times a large value can be out of range; a row whose
+      // every score is -inf has no sum)
+      const float inv = 1.f / sum, none = sum == 0.f ? __uint_as_float(0x7fffffffu) : 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] = none;
 #pragma unroll
       for (int y = 0; y < kSplitMax; ++y) {
         if (w[y] == 0.f) continue;
         const uint32_t at = in_block(part + row * HD + c8, y);
         const float4 u = ld_cluster_f32x4(at), v = ld_cluster_f32x4(at + 16);
-        const float wt = part_weight(m[y], gm) * w[y];
-        sum += wt;
+        const float wt = w[y] * inv;
         acc[0] = fmaf(wt, u.x, acc[0]);
         acc[1] = fmaf(wt, u.y, acc[1]);
         acc[2] = fmaf(wt, u.z, acc[2]);
@@ -551,9 +558,8 @@ __global__ void __launch_bounds__(kVThreads, kVBlocks) k_kv8_rows(const Kv8Attn 
       const int r = it.r0 + row, mr = a.byG(r), h = g * a.G + r - mr * a.G;
       const int p = kv8_row_pos(a, it, r);
       const bool sees = kv8_row_lo(it, p, a.window) <= p;
-      const float inv = 1.f / sum;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] = sees ? acc[j] * inv : 0.f;
+      for (int j = 0; j < 8; ++j) acc[j] = sees ? acc[j] : 0.f;
       store_out8(static_cast<T*>(a.out) + ((int64_t)it.b * a.M + mr) * a.out_stride +
                      (int64_t)h * HD + c8,
                  acc);

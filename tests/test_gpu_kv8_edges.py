@@ -208,3 +208,19 @@ def test_maxima_and_units_that_move(dtype, M, seq):
         for window in (0, 90):
             seen = c.v_scale[..., max(pos - window, 0) // 64 if window else 0:(pos + M - 1) // 64 + 1]
             _check(c, vals, q, pos, window, float(seen.max()))
+
+
+@pytest.mark.parametrize("dtype,M,seq", FORMS)
+@pytest.mark.parametrize("e", [90, 104, 118])
+def test_values_near_the_largest(dtype, M, seq, e):
+    """Values of 2^90 to the largest that a cache holds: sums over them stay in range, in the order
+    that they are weighed and joined in."""
+    torch = _torch()
+    g = torch.Generator(device="cuda").manual_seed(61)
+    x = torch.randn(400, 2 * KVH, HD, generator=g, device="cuda")
+    v = x[:, KVH:].clamp(-2, 2) * 2.0 ** e
+    c, vals = _appended(x[:, :KVH], v, seq)
+    q = torch.randn(1, M, HEADS, HD, generator=g, device="cuda").to(
+        torch.float32 if dtype == "f32" else torch.bfloat16)
+    for pos in (0, 140, 399 - M):
+        _check(c, vals, q, pos)
