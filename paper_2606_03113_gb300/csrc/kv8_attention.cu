@@ -827,31 +827,31 @@ cudaError_t wide_launch(const Kv8Attn& a, int P, cudaStream_t st) {
 // have room all at once.  us a call, mma.sync / tcgen05, by rows of 8 KV heads (of 32 in the
 // third line):
 //                     16           17           32           48          128
-//   16000         18.8/22.9    28.5/23.1    28.9/24.5    34.9/25.5    63.7/35.1
-//   100000        51.4/64.9    90.6/65.1    90.6/66.6     126/67.8     293/81.3
-//   16 x 1000     58.7/71.0    97.7/72.6    99.7/79.6     146/82.7     369/103
+//   16000         19.6/23.8    24.4/24.4    25.7/25.0    33.2/25.8    63.3/29.9
+//   100000        51.1/66.2    81.8/66.8    82.7/67.4     121/68.5     281/75.9
+//   16 x 1000     60.6/62.6    86.9/64.0    97.8/69.0     130/71.9     304/90.8
 // clusters / tcgen05 (one accumulator):
-//   240 keys                    8.7/12.8     9.2/13.5     9.4/13.7    11.2/14.5
-//   1000                       10.2/14.7    12.0/15.8    12.4/16.3    13.8/18.6
-//   2000                       11.9/17.3    13.9/18.2    14.1/19.0
+//   240 keys                    8.9/13.0     8.9/13.7     8.9/13.9    11.0/14.6
+//   1000                        9.8/14.7    11.8/15.7    12.2/16.2    13.8/18.6
+//   2000                       11.5/17.3    13.6/18.1    13.9/18.9
 // and one / two accumulators, 8 KV heads:
 //                    129          256          300          512         1024
-//   500 keys      19.2/19.3    21.3/22.5    22.1/23.3    23.2/24.9    32.4/28.0
-//   16000         40.0/33.7    44.5/37.7    50.4/50.1    60.7/51.4    97.1/75.1
-//   100000         117/94.4     129/99.8     189/173      239/175      459/322
-//   16 x 1000     59.7/42.7    68.9/51.6    84.2/76.1     105/82.8     193/157
+//   500 keys      17.4/17.6    19.5/20.3    20.5/22.1    21.9/22.8    30.1/28.2
+//   16000         32.5/30.6    41.3/33.3    48.9/48.2    58.5/50.3    94.1/76.6
+//   100000         113/93.0     125/95.6     184/172      232/175      449/326
+//   16 x 1000     51.7/42.2    58.8/51.8    72.9/79.2    91.5/83.0     174/155
 constexpr int kWideFrom = 16;
 // Short caches: a cluster of blocks for each item, which joins its parts itself (mma.sync
 // kernel): of 1, 2, 4 or 8 blocks with 128 keys or more each, as long as there is room for
 // all, two on each of 152 SMs; up to 512 keys a block and 2048 in all.  us, line / clusters,
 // at full caches of 128, 512, 1024, 2048 and 4096 positions:
-//   1 sequence, 8 KV heads, 4 rows each     8.6/5.8   8.7/7.8   9.0/8.6   9.9/10.0  10.8/12.6
-//   1, 40 heads, 2 rows                     9.1/6.2  10.2/8.6  11.2/10.4 12.9/13.5  17.6/19.9
-//   4, 8 heads, 4 rows                      9.3/6.1  10.7/8.2  11.0/9.9  12.8/11.7  16.3/15.3
-//   16, 8 heads, 4 rows                    10.9/6.3  15.4/10.7 18.4/14.2 24.3/20.6  37.9/34.8
+//   1 sequence, 8 KV heads, 4 rows each     8.5/6.0   8.7/7.6   8.9/8.0   9.8/9.6   10.8/12.1
+//   1, 40 heads, 2 rows                     9.2/6.3  10.1/8.4  11.1/10.3 12.8/13.7  17.5/19.6
+//   4, 8 heads, 4 rows                      9.2/6.3  10.5/8.1  11.0/9.5  12.9/11.4  16.2/14.8
+//   16, 8 heads, 4 rows                    10.7/6.3  15.4/10.8 18.5/14.4 24.4/20.5  38.0/34.9
 // (sequences of one length, for which clusters are at their best), and a launch and a
 // workspace less, which the host takes 6 to 8 us for.  The capacity is what the host knows: 1 row of 32
-// heads over 8 KV heads x 1100 keys takes 9.1 us in a cache of 1216 positions and, on the line, 10.1 in one
+// heads over 8 KV heads x 1100 keys takes 8.7 us in a cache of 1216 positions and, on the line, 10.1 in one
 // of 2112 to 131072.
 constexpr int kSplitKeys = 128, kSplitBlocks = 304, kSplitSeq = 512, kSplitMost = 2048;
 
