@@ -219,6 +219,104 @@ ssd_status ssd_token_logprobs(const void* logits, int32_t dtype, int32_t n_rows,
                               float* entropy, int32_t* top_id, float* top_logprob,
                               int32_t* err_dev, void* stream);
 
+/* ------------------------------------------------------------------------
+ * A paged KV cache: a pool of pages that sequences share and give back, its
+ * pages forked, reserved and compacted, rows appended to them and attention
+ * over them (the paper has no counterpart: its one sequence has a contiguous cache).
+ * Several answers from one prompt keep the prompt's rows once, and a sequence
+ * takes memory as it grows.  Conventions as for the 8-bit cache above: no context, work
+ * enqueued on `stream`, no synchronisation, no allocation, graph-capturable after a first call
+ * outside of a capture, error bits in *err_dev.  All sequence state is read on the device.
+ * Calls that change pages or the table (reserve, fork, compact) are ordered by the caller
+ * against every other call on the same cache; appends and attentions that touch different
+ * rows or layers are not. */
+#define SSD_PAGED_ERR_PAGES 32 /* too few free pages: the call changed nothing */
+#define SSD_PAGED_ERR_TABLE 64 /* a page that the table does not name, or, for rows that are
+                                * written, one that other entries name too */
+
+/* The cache (all memory the caller's, device).
+ * pages: [n_pages][n_layers][2 (K, V)][n_kv_heads][page][head_dim] of dtype (SSD_DTYPE_F32 or
+ * _BF16), 16-byte aligned: `page` positions of a sequence, a power of two from 16 to 256
+ * (SSD_ERR_UNSUPPORTED otherwise, as head_dim other than 64 and 128).
+ * table: int32 [n_seq][max_pages], the pages of positions 0 .. page - 1, page .. 2 page - 1, ..
+ * of each sequence; -1: none.  Any other number outside 0 .. n_pages - 1 counts as none.
+ * refs: int32 [n_pages], 16-byte aligned: how many entries of the table name the page; 0: it is
+ * free.  An empty cache has a table of -1 and refs of 0.  A sequence holds up to
+ * max_pages x page positions, at most 2^30; a sequence names no page twice.  The calls
+ * keep refs; whoever writes the table otherwise keeps it too.
+ * A sequence's pages from some entry on may be missing, and so may any in front that no row
+ * will see again. */
+typedef struct {
+  int32_t n_layers, n_seq, n_kv_heads, head_dim, page, n_pages, max_pages, dtype;
+  void* pages;
+  int32_t* table;
+  int32_t* refs;
+} ssd_paged_cache;
+
+/* Bytes of device workspace that ssd_paged_reserve and ssd_paged_compact need (0: a cache that
+ * they refuse).  Calls that run one after the other can share it. */
+size_t ssd_paged_workspace_bytes(const ssd_paged_cache* cache);
+
+/* Pages for new rows: rows m < rows[b] of sequence b (rows: device [n_seq], NULL: M each; 0 leaves
+ * the sequence alone) will be written to positions pos[b] + m (pos: device [n_seq]).  Of the
+ * pages that hold these positions,
+ * - one that is missing becomes a free one;
+ * - one that other entries name too is left to them and becomes a free one, into which the
+ *   positions in front of pos[b] are copied, all layers and heads (copy on write);
+ *   where all who share a page ask for it in this call, it stays with the last of them;
+ * - any other stays.
+ * Free pages are taken lowest first, for the sequences in their order and each one's positions in
+ * theirs; the result is that of looking at the sequences one by one.  Positions from pos[b] + rows[b] on
+ * keep their pages.  Where the free pages do not suffice, nothing is changed, and the error bit
+ * SSD_PAGED_ERR_PAGES is set.  A sequence whose positions do not lie in the cache, or whose rows[b]
+ * does not in 0 .. M, is left alone, with its error bit. */
+ssd_status ssd_paged_reserve(const ssd_paged_cache* cache, const int32_t* pos, const int32_t* rows,
+                             int32_t M, void* workspace, size_t workspace_bytes, int32_t* err_dev,
+                             void* stream);
+
+/* Every sequence becomes the first length[b] positions of what sequence parent[b] was before the
+ * call: the pages that hold them are shared, the others of sequence b are given back (free where
+ * nobody else names them).  parent: device [n_seq], NULL: each its own; -1: the sequence is
+ * emptied.  length: device [n_seq], NULL: all positions.  So a fork, the reordering of a
+ * search's continuations, a truncation and the end of a sequence are one call.  No content is read
+ * or written.  Numbers outside -1 .. n_seq - 1 and negative lengths leave their sequence
+ * alone (SSD_DEV_ERR_CONTROL). */
+ssd_status ssd_paged_fork(const ssd_paged_cache* cache, const int32_t* parent, const int32_t* length,
+                          int32_t* err_dev, void* stream);
+
+/* Moves pages in use to the low end of the pool: with `used` pages in use, the k-th lowest of those at
+ * used and above goes to the k-th lowest free one below; the table and refs follow.  Free pages are
+ * then the pool's tail.  used: device int32, may be NULL. */
+ssd_status ssd_paged_compact(const ssd_paged_cache* cache, int32_t* used, void* workspace,
+                             size_t workspace_bytes, int32_t* err_dev, void* stream);
+
+/* Appends rows to the pages of layer `layer`: arguments as for ssd_kv8_append, k and v of the cache's
+ * dtype.  A row whose page is missing, or is named by more than one entry (reserve has not been
+ * called for it), is not written: SSD_PAGED_ERR_TABLE. */
+ssd_status ssd_paged_append(const ssd_paged_cache* cache, int32_t layer, const void* k,
+                            const void* v, int64_t row_stride, int32_t M, const int32_t* pos,
+                            const int32_t* rows, int32_t* err_dev, void* stream);
+
+/* Bytes of device workspace that ssd_paged_attention needs for these sizes, whatever the lengths
+ * (256: it uses none, and takes NULL; 0: sizes that it refuses). */
+size_t ssd_paged_attention_bytes(const ssd_paged_cache* cache, int32_t n_heads, int32_t M,
+                                 int32_t longest);
+
+/* Attention over the pages of layer `layer`, softmax scale 1/sqrt(head_dim): q, n_heads, q_stride, M,
+ * pos, rows, first, window, out, out_stride, workspace and the rows' sight as for ssd_kv8_attention;
+ * q and out of the cache's dtype.  longest: no sequence's pos[b] + rows[b] exceeds it (0: the
+ * cache's max_pages x page); it helps to deal out the work, and a sequence beyond it is left
+ * alone (SSD_DEV_ERR_CAPACITY).  A row that sees no key is zero.  Rows from rows[b] on are left as they
+ * were.  What stands in a key or value that a row does not see never reaches it; an infinity or NaN
+ * in one that it sees does.  A sequence some visible position of which has no page
+ * (SSD_PAGED_ERR_TABLE) has undefined rows.  Scores, sums and outputs are fp32.  Equal calls give
+ * equal bits. */
+ssd_status ssd_paged_attention(const ssd_paged_cache* cache, int32_t layer, const void* q,
+                               int32_t n_heads, int64_t q_stride, int32_t M, const int32_t* pos,
+                               const int32_t* rows, const int32_t* first, int32_t window,
+                               int32_t longest, void* out, int64_t out_stride, void* workspace,
+                               size_t workspace_bytes, int32_t* err_dev, void* stream);
+
 /* Test fixture: fills dst (device, n elements of dtype) with the seeded
  * synthetic weights of tensor `tid` (see synth/synth.h): element i is
  * synth_weight_f32(seed, tid, i, sigma), rounded to bf16 for SSD_DTYPE_BF16.

@@ -13,7 +13,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(BUILD_DIR, "libssd.so")
 SOURCES = ["gemv.cu", "fp32.cu", "tile.cu", "wide.cu", "head.cu", "attention.cu", "control.cu", "engine.cu",
-           "kv8_append.cu", "kv8_attention.cu", "logprobs.cu"]
+           "kv8_append.cu", "kv8_attention.cu", "logprobs.cu",
+           "paged_pages.cu", "paged_attention.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
               "-Xptxas", "-warn-spills"]

@@ -73,7 +73,9 @@ enum ErrBits : int32_t {
   kErrCapacity = 2,   // KV capacity would be exceeded
   kErrControl = 4,    // inconsistent round state (l*, k)
   kErrTraceFull = 8,  // more rounds than trace records
-  kErrTimeout = 16    // a pipeline wait gave up (see the streamed kernels)
+  kErrTimeout = 16,   // a pipeline wait gave up (see the streamed kernels)
+  kErrPages = 32,     // not enough free pages (paged caches)
+  kErrTable = 64      // a page that is missing, or shared where it is written (paged caches)
 };
 
 __device__ __forceinline__ void resolve_rows(const Ctl* c, const RowSel& s, int& pos0, int& M) {

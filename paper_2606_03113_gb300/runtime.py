@@ -5,7 +5,8 @@ GPU and fills them with the library's seeded synthetic-weight fixture (the
 same generator the CPU oracle reads).  `Engine` owns one ssd_ctx: workspace
 (KV cache, activations, control block) from PyTorch, work on a PyTorch stream.
 `KV8Cache` is a layer's KV cache held in 8 bits, with its append and attention;
-`token_logprobs` scores given tokens over rows of logits.
+`PagedKVCache` a decoder's KV cache in pages that sequences share; `token_logprobs`
+scores given tokens over rows of logits.
 """
 from __future__ import annotations
 
@@ -296,6 +297,20 @@ def _elsewhere(device: torch.device, stream):
     return None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
 
+def _rows_of(x: torch.Tensor, n: int, heads: int, hd: int, what: str) -> tuple[int, int]:
+    """(M, elements between rows) of x [n, M, heads, hd]."""
+    shape, strides = x.shape, x.stride()
+    if len(shape) != 4 or shape[0] != n or shape[2] != heads or shape[3] != hd or shape[1] < 1:
+        raise ValueError(f"{what} must be [{n}, M, {heads}, {hd}], not {list(shape)}")
+    s0, s1, s2, s3 = strides
+    M = shape[1]
+    row = s1 if M > 1 else (s0 if n > 1 else heads * hd)
+    if s3 != 1 or (s2 != hd and heads > 1) or (n > 1 and s0 != M * row):
+        raise ValueError(f"{what}: a row's heads must lie one behind the other, and the rows "
+                         f"of all sequences at one distance; strides are {strides}")
+    return M, row
+
+
 class KV8Cache:
     """The KV cache of one layer in 8 bits (ssd_kv8_cache, include/ssd_ops.h): e4m3 codes `k`, `v`
     [n_seq, n_kv_heads, max_seq, head_dim], one scale per 64 positions and KV head in `k_scale`,
@@ -345,17 +360,7 @@ class KV8Cache:
 
     def _rows(self, x: torch.Tensor, heads: int, what: str) -> tuple[int, int]:
         """(M, elements between rows) of x [n_seq, M, heads, head_dim]."""
-        shape, strides = x.shape, x.stride()
-        n, hd = self.n_seq, self.head_dim
-        if len(shape) != 4 or shape[0] != n or shape[2] != heads or shape[3] != hd or shape[1] < 1:
-            raise ValueError(f"{what} must be [{n}, M, {heads}, {hd}], not {list(shape)}")
-        s0, s1, s2, s3 = strides
-        M = shape[1]
-        row = s1 if M > 1 else (s0 if n > 1 else heads * hd)
-        if s3 != 1 or (s2 != hd and heads > 1) or (n > 1 and s0 != M * row):
-            raise ValueError(f"{what}: a row's heads must lie one behind the other, and the rows "
-                             f"of all sequences at one distance; strides are {strides}")
-        return M, row
+        return _rows_of(x, self.n_seq, heads, self.head_dim, what)
 
     def append(self, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
                rows: torch.Tensor | None = None, stream=None):
@@ -437,6 +442,216 @@ class KV8Cache:
         if bits:
             self.err.zero_()
             raise S.SsdError(S.SSD_ERR_DEVICE_FLAG, "KV8Cache", S.dev_err_text(bits))
+
+
+class PagedKVCache:
+    """A decoder's KV cache in pages that sequences share and give back (ssd_paged_cache,
+    include/ssd_ops.h): `pages` [n_pages, n_layers, 2 (K, V), n_kv_heads, page, head_dim], the pages
+    of each sequence in `table` [n_seq, max_seq / page] (-1: none), how many entries name each page in
+    `refs` [n_pages] (0: free).  `max_seq` is rounded up to a multiple of `page` (a power of
+    two from 16 to 256).
+
+    A step of decoding: `fork` where sequences branch, are cut back or end; `reserve` the places of the new
+    rows (a shared page is copied before it is written); for each layer `append` their K and V and
+    `attention` of their queries.  `compact` moves what is in use to the low end of the pool.
+
+    Calls enqueue on `stream`, or on the current stream of the cache's device, and do not
+    synchronise; the caller orders streams (`fork`, `reserve` and `compact` against every other
+    call on the cache), and keeps tensors that another stream made alive
+    (`Tensor.record_stream`).  They can be captured into CUDA graphs after a first call outside
+    of a capture.  What only the device can see sets a bit in `err`, which `check` reads: positions
+    outside the cache, bad row numbers and parents leave the sequence alone; a `reserve` for which the
+    free pages do not suffice changes nothing; rows whose page is missing or shared are not appended,
+    and a sequence that sees a missing page has undefined attention."""
+
+    # the tensors can be written, but not replaced: calls have their addresses
+    pages, table, refs, err = (property(operator.attrgetter(x))
+                               for x in ("_pages", "_table", "_refs", "_err"))
+
+    def __init__(self, n_layers: int, n_kv_heads: int, head_dim: int, n_pages: int, page: int = 64,
+                 n_seq: int = 1, max_seq: int | None = None, dtype: torch.dtype = torch.bfloat16,
+                 device: str | torch.device = "cuda:0"):
+        device = torch.device(device)
+        if device.type == "cuda" and device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        if head_dim not in (64, 128):
+            raise ValueError(f"head_dim must be 64 or 128, not {head_dim}")
+        if page not in S.PAGE_SIZES:
+            raise ValueError(f"page must be one of {S.PAGE_SIZES}, not {page}")
+        if dtype not in _CODES:
+            raise ValueError(f"dtype must be float32 or bfloat16, not {dtype}")
+        if n_layers < 1 or n_kv_heads < 1 or n_pages < 1 or not 1 <= n_seq <= S.KV8_MAX_SEQS:
+            raise ValueError("n_layers, n_kv_heads, n_pages and n_seq must be positive, "
+                             f"n_seq at most {S.KV8_MAX_SEQS}")
+        max_seq = n_pages * page if max_seq is None else max_seq
+        if not 1 <= max_seq <= 1 << 30:
+            raise ValueError(f"max_seq must be in 1..2^30, not {max_seq}")
+        self.device, self.dtype, self.page = device, dtype, page
+        self.n_layers, self.n_kv_heads, self.head_dim = n_layers, n_kv_heads, head_dim
+        self.n_seq, self.n_pages = n_seq, n_pages
+        self.max_pages = (max_seq + page - 1) // page
+        self.max_seq = self.max_pages * page
+        self._pages = torch.zeros((n_pages, n_layers, 2, n_kv_heads, page, head_dim), dtype=dtype,
+                                  device=device)
+        self._table = torch.full((n_seq, self.max_pages), -1, dtype=torch.int32, device=device)
+        self._refs = torch.zeros(n_pages, dtype=torch.int32, device=device)
+        self._err = torch.zeros(1, dtype=torch.int32, device=device)
+        self._c = S.ssd_paged_cache(n_layers, n_seq, n_kv_heads, head_dim, page, n_pages,
+                                    self.max_pages, _CODES[dtype], self._pages.data_ptr(),
+                                    self._table.data_ptr(), self._refs.data_ptr())
+        self._err_at = self._err.data_ptr()
+        # of the calls that change pages, which run one after the other
+        self._plan_bytes = S.ssd_paged_workspace_bytes(self._c) if device.type == "cuda" else 0
+        self._plan = torch.empty(self._plan_bytes, dtype=torch.uint8, device=device)
+        self._plan_at = self._plan.data_ptr()
+        self._work = {}  # (n_heads, M, longest) -> workspace bytes
+
+    def _rows(self, x: torch.Tensor, heads: int, what: str) -> tuple[int, int]:
+        """(M, elements between rows) of x [n_seq, M, heads, head_dim]."""
+        if x.dtype != self.dtype:
+            raise ValueError(f"{what} must be {self.dtype}, as the cache, not {x.dtype}")
+        return _rows_of(x, self.n_seq, heads, self.head_dim, what)
+
+    def _layer(self, layer: int) -> int:
+        if not 0 <= layer < self.n_layers:
+            raise ValueError(f"layer must be in 0..{self.n_layers - 1}, not {layer}")
+        return layer
+
+    def reserve(self, pos: torch.Tensor, rows: torch.Tensor | int = 1, stream=None):
+        """Pages for rows[b] new rows (or `rows` of each sequence) at positions pos[b] and up: missing
+        ones, and copies of shared ones up to pos[b], are taken lowest first.  Changes nothing where
+        too few pages are free (`check` raises)."""
+        if pos is None:
+            raise ValueError("pos is missing")
+        pp = _per_seq(pos, self.n_seq, self.device, "pos")
+        rp, M = 0, self.max_seq
+        if isinstance(rows, int):
+            M = rows
+            if not 1 <= M <= self.max_seq:
+                raise ValueError(f"rows must be in 1..{self.max_seq}, not {M}")
+        else:
+            rp = _per_seq(rows, self.n_seq, self.device, "rows")
+            if not rp:
+                raise ValueError("rows is missing")
+        there = _elsewhere(self.device, stream)
+        if there is not None:
+            with there:
+                return self.reserve(pos, rows)
+        S.ssd_paged_reserve(self._c, pp, rp, M, self._plan_at, self._plan_bytes, self._err_at,
+                            _current_stream(self.device.index))
+
+    def fork(self, parent: torch.Tensor | None, length: torch.Tensor | None = None, stream=None):
+        """Sequence b becomes the first length[b] positions (all without `length`) of what sequence
+        parent[b] was (-1: empty; without `parent`: of itself), sharing its pages."""
+        if parent is None and length is None:
+            raise ValueError("neither parent nor length")
+        pp = _per_seq(parent, self.n_seq, self.device, "parent")
+        lp = _per_seq(length, self.n_seq, self.device, "length")
+        there = _elsewhere(self.device, stream)
+        if there is not None:
+            with there:
+                return self.fork(parent, length)
+        S.ssd_paged_fork(self._c, pp, lp, self._err_at, _current_stream(self.device.index))
+
+    def truncate(self, length: torch.Tensor, stream=None):
+        """Sequence b keeps its first length[b] positions and gives the pages behind them back."""
+        if length is None:
+            raise ValueError("length is missing")
+        self.fork(None, length, stream)
+
+    def compact(self, stream=None) -> torch.Tensor:
+        """Moves the pages in use to the low end of the pool; the free ones are its tail then.
+        Returns how many are in use (int32 [1] on the device)."""
+        there = _elsewhere(self.device, stream)
+        if there is not None:
+            with there:
+                return self.compact()
+        used = torch.empty(1, dtype=torch.int32, device=self.device)
+        S.ssd_paged_compact(self._c, used.data_ptr(), self._plan_at, self._plan_bytes, self._err_at,
+                            _current_stream(self.device.index))
+        return used
+
+    def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
+               rows: torch.Tensor | None = None, stream=None):
+        """Writes k[b, m], v[b, m] ([n_seq, M, n_kv_heads, head_dim]) for m < rows[b] (all M
+        without `rows`) to positions pos[b] + m of a layer, which have been reserved."""
+        layer = self._layer(layer)
+        M, row = self._rows(k, self.n_kv_heads, "k")
+        if self._rows(v, self.n_kv_heads, "v") != (M, row):
+            raise ValueError("k and v must have the same rows and strides")
+        if pos is None:
+            raise ValueError("pos is missing")
+        kp, vp = _on(k, self.device, "k"), _on(v, self.device, "v")
+        pp = _per_seq(pos, self.n_seq, self.device, "pos")
+        rp = _per_seq(rows, self.n_seq, self.device, "rows")
+        there = _elsewhere(self.device, stream)
+        if there is not None:
+            with there:
+                return self.append(layer, k, v, pos, rows)
+        S.ssd_paged_append(self._c, layer, kp, vp, row, M, pp, rp, self._err_at,
+                           _current_stream(self.device.index))
+
+    def attention(self, layer: int, q: torch.Tensor, pos: torch.Tensor,
+                  rows: torch.Tensor | None = None, first: torch.Tensor | None = None,
+                  window: int = 0, longest: int = 0, out: torch.Tensor | None = None,
+                  stream=None) -> torch.Tensor:
+        """softmax(q k^T / sqrt(head_dim)) v over a layer's pages for q [n_seq, M, n_heads,
+        head_dim]: row m < rows[b] of sequence b sits at position pos[b] + m, whose key has been
+        appended, and sees the keys up to its own from first[b] on, at most `window` of them
+        (0: all).  A row that sees none is zero.  `longest`: no sequence's pos[b] + rows[b] exceeds
+        it (0: max_seq), which short sequences in a large table gain by.  Returns `out`, which keeps
+        its rows from rows[b] on; without it a new tensor, where those are zero (a sequence with
+        bad positions leaves its own unset)."""
+        layer = self._layer(layer)
+        heads = q.shape[2] if q.dim() == 4 else 0
+        M, row = self._rows(q, heads, "q")
+        if heads < 1 or heads % self.n_kv_heads:
+            raise ValueError(f"q has {heads} heads: not a multiple of {self.n_kv_heads}")
+        if pos is None:
+            raise ValueError("pos is missing")
+        qp = _on(q, self.device, "q")
+        pp = _per_seq(pos, self.n_seq, self.device, "pos")
+        rp = _per_seq(rows, self.n_seq, self.device, "rows")
+        fp = _per_seq(first, self.n_seq, self.device, "first")
+        if out is not None:
+            Mo, orow = self._rows(out, heads, "out")
+            if Mo != M:
+                raise ValueError("out must have q's rows")
+            if _on(out, self.device, "out") == qp and orow != row:
+                raise ValueError("out is q, but their strides differ")
+        if not 0 <= window < 1 << 31:
+            raise ValueError(f"window must be 0 (none) or a positive int32, not {window}")
+        if not 0 <= longest <= self.max_seq:
+            raise ValueError(f"longest must be in 0..{self.max_seq}, not {longest}")
+        key = (heads, M, longest)
+        nbytes = self._work.get(key)
+        if nbytes is None:
+            nbytes = S.ssd_paged_attention_bytes(self._c, heads, M, longest)
+            if len(self._work) < 4096:  # (a caller may pass another `longest` every step)
+                self._work[key] = nbytes
+        there = _elsewhere(self.device, stream)
+        if there is not None:
+            with there:
+                return self.attention(layer, q, pos, rows, first, window, longest, out)
+        if out is None:
+            make = torch.empty if rows is None else torch.zeros
+            out = make((self.n_seq, M, heads, self.head_dim), dtype=q.dtype, device=self.device)
+            orow = heads * self.head_dim
+        # (256: none is used; others stay this call's until the launches)
+        work = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes > 256 else None
+        S.ssd_paged_attention(self._c, layer, qp, heads, row, M, pp, rp, fp, window, longest,
+                              out.data_ptr(), orow, work.data_ptr() if work is not None else 0, nbytes,
+                              self._err_at, _current_stream(self.device.index))
+        return out
+
+    def check(self):
+        """Waits for the device and raises SsdError, with what it was, if a call since the last
+        check set an error bit there."""
+        torch.cuda.synchronize(self.device)
+        bits = int(self.err.item())
+        if bits:
+            self.err.zero_()
+            raise S.SsdError(S.SSD_ERR_DEVICE_FLAG, "PagedKVCache", S.dev_err_text(bits))
 
 
 class TokenLogprobs(NamedTuple):

@@ -96,17 +96,21 @@ class ssd_exit_stats(C.Structure):
 
 KV8_BLOCK = 64        # positions of the 8-bit cache that share a scale
 KV8_MAX_SEQS = 4096
+PAGE_SIZES = (16, 32, 64, 128, 256)  # positions of a page of the paged cache
 MAX_TOP = 32          # most probable tokens of ssd_token_logprobs
 DEV_ERR_TOKEN, DEV_ERR_CAPACITY, DEV_ERR_CONTROL, DEV_ERR_TIMEOUT = 1, 2, 4, 16
 DEV_ERR_NAMES = {DEV_ERR_TOKEN: "a token id outside the vocabulary",
                  DEV_ERR_CAPACITY: "positions outside the cache",
                  DEV_ERR_CONTROL: "a number of rows outside 0..M",
                  DEV_ERR_TIMEOUT: "a wait inside a kernel gave up: the call's outputs are undefined"}
+PAGED_ERR_PAGES, PAGED_ERR_TABLE = 32, 64  # of the paged cache, beside those
+PAGED_ERR_NAMES = {PAGED_ERR_PAGES: "too few free pages: nothing was reserved",
+                   PAGED_ERR_TABLE: "a page that is missing, or shared where rows are written"}
 
 
 def dev_err_text(bits: int) -> str:
     """What the bits of a device error word say."""
-    said = [name for bit, name in DEV_ERR_NAMES.items() if bits & bit]
+    said = [name for bit, name in (DEV_ERR_NAMES | PAGED_ERR_NAMES).items() if bits & bit]
     return f"device error bits {bits}" + (f" ({'; '.join(said)})" if said else "")
 
 
@@ -114,6 +118,13 @@ class ssd_kv8_cache(C.Structure):
     _fields_ = [("n_seq", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("max_seq", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
                 ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class ssd_paged_cache(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("n_seq", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("page", C.c_int32), ("n_pages", C.c_int32),
+                ("max_pages", C.c_int32), ("dtype", C.c_int32), ("pages", C.c_void_p),
+                ("table", C.c_void_p), ("refs", C.c_void_p)]
 
 
 # Every exported entry point with its ctypes signature (restype, argtypes).
@@ -146,6 +157,14 @@ SIGNATURES = {
                                     _SZ, _P, _P]),
     "ssd_token_logprobs": (C.c_int, [_P, _I32, _I32, _I32, _I64, _P, _I32, _F32, _I32, _P, _P, _P,
                                      _P, _P, _P, _P]),
+    "ssd_paged_workspace_bytes": (_SZ, [_P]),
+    "ssd_paged_reserve": (C.c_int, [_P, _P, _P, _I32, _P, _SZ, _P, _P]),
+    "ssd_paged_fork": (C.c_int, [_P, _P, _P, _P, _P]),
+    "ssd_paged_compact": (C.c_int, [_P, _P, _P, _SZ, _P, _P]),
+    "ssd_paged_append": (C.c_int, [_P, _I32, _P, _P, _I64, _I32, _P, _P, _P, _P]),
+    "ssd_paged_attention_bytes": (_SZ, [_P, _I32, _I32, _I32]),
+    "ssd_paged_attention": (C.c_int, [_P, _I32, _P, _I32, _I64, _I32, _P, _P, _P, _I32, _I32, _P, _I64,
+                                      _P, _SZ, _P, _P]),
     "ssd_synth_fill": (C.c_int, [_P, _I32, _U64, _U32, _U32, C.c_double, _P]),
     "ssd_read_probe": (C.c_int, [_P, _U64, _P, _P]),
 }
@@ -355,6 +374,62 @@ def ssd_token_logprobs(logits_ptr: int, dtype: int, n_rows: int, vocab: int, row
                                             stream_ptr)
     if st:
         _check(st, "ssd_token_logprobs")
+
+
+def ssd_paged_workspace_bytes(cache: ssd_paged_cache) -> int:
+    return lib().ssd_paged_workspace_bytes(C.addressof(cache))
+
+
+def ssd_paged_reserve(cache: ssd_paged_cache, pos_ptr: int, rows_ptr: int, M: int, workspace_ptr: int,
+                      workspace_bytes: int, err_ptr: int = 0, stream_ptr: int = 0):
+    """Pages for new rows of a paged cache, copied on write (see ssd_ops.h)."""
+    st = (_lib or lib()).ssd_paged_reserve(C.addressof(cache), pos_ptr, rows_ptr, M, workspace_ptr,
+                                           workspace_bytes, err_ptr, stream_ptr)
+    if st:
+        _check(st, "ssd_paged_reserve")
+
+
+def ssd_paged_fork(cache: ssd_paged_cache, parent_ptr: int, length_ptr: int = 0, err_ptr: int = 0,
+                   stream_ptr: int = 0):
+    """Sequences of a paged cache as prefixes of each other (see ssd_ops.h)."""
+    st = (_lib or lib()).ssd_paged_fork(C.addressof(cache), parent_ptr, length_ptr, err_ptr, stream_ptr)
+    if st:
+        _check(st, "ssd_paged_fork")
+
+
+def ssd_paged_compact(cache: ssd_paged_cache, used_ptr: int, workspace_ptr: int, workspace_bytes: int,
+                      err_ptr: int = 0, stream_ptr: int = 0):
+    """Pages in use to the low end of the pool (see ssd_ops.h)."""
+    st = (_lib or lib()).ssd_paged_compact(C.addressof(cache), used_ptr, workspace_ptr, workspace_bytes,
+                                           err_ptr, stream_ptr)
+    if st:
+        _check(st, "ssd_paged_compact")
+
+
+def ssd_paged_append(cache: ssd_paged_cache, layer: int, k_ptr: int, v_ptr: int, row_stride: int, M: int,
+                     pos_ptr: int, rows_ptr: int = 0, err_ptr: int = 0, stream_ptr: int = 0):
+    """Rows of K and V into a layer's pages (see ssd_ops.h)."""
+    st = (_lib or lib()).ssd_paged_append(C.addressof(cache), layer, k_ptr, v_ptr, row_stride, M, pos_ptr,
+                                          rows_ptr, err_ptr, stream_ptr)
+    if st:
+        _check(st, "ssd_paged_append")
+
+
+def ssd_paged_attention_bytes(cache: ssd_paged_cache, n_heads: int, M: int, longest: int = 0) -> int:
+    return lib().ssd_paged_attention_bytes(C.addressof(cache), n_heads, M, longest)
+
+
+def ssd_paged_attention(cache: ssd_paged_cache, layer: int, q_ptr: int, n_heads: int, q_stride: int,
+                        M: int, pos_ptr: int, rows_ptr: int, first_ptr: int, window: int,
+                        longest: int, out_ptr: int, out_stride: int, workspace_ptr: int,
+                        workspace_bytes: int, err_ptr: int = 0, stream_ptr: int = 0):
+    """Attention of new rows over a layer's pages (see ssd_ops.h)."""
+    st = (_lib or lib()).ssd_paged_attention(C.addressof(cache), layer, q_ptr, n_heads, q_stride, M,
+                                             pos_ptr, rows_ptr, first_ptr, window, longest, out_ptr,
+                                             out_stride, workspace_ptr, workspace_bytes, err_ptr,
+                                             stream_ptr)
+    if st:
+        _check(st, "ssd_paged_attention")
 
 
 def ssd_synth_fill(dst_ptr: int, dtype: int, n: int, seed: int, tid: int, sigma: float,
