@@ -1,4 +1,4 @@
-// kv8_plan.cuh -- how the attention over the 8-bit cache is dealt out.
+// kv8_plan.cuh -- how the attention over the 8-bit cache, or over pages, is dealt out.
 //
 // The query rows of one sequence and KV head are the M new rows times the G
 // query heads of the group, row r = m G + h, cut into tiles of RT rows.  An entry
@@ -38,10 +38,9 @@ struct Kv8Div {
 template <int RT>
 constexpr int kKv8ItemCost = RT > 128 ? 8 : 3;
 
-struct Kv8Attn {
+// What the plan, the join of parts and the kernels of both caches (8 bits, pages) share.
+struct AttnArgs {
   Kv8Div byG, byRt, byP;
-  const uint8_t *k, *v;
-  const float *ks, *vs;
   const void* q;
   void* out;
   const int32_t *pos, *rows, *first;
@@ -54,6 +53,11 @@ struct Kv8Attn {
   struct Kv8Desc* desc;
   float* part;  // [2 P][part_rows][hd] normalised partial outputs
   float2* ml;   // [2 P][part_rows] their (max, sum), max in powers of two
+};
+
+struct Kv8Attn : AttnArgs {
+  const uint8_t *k, *v;
+  const float *ks, *vs;
 };
 
 // What block i of the attention left to be joined: the item that begins in its
@@ -69,7 +73,7 @@ struct Kv8Item {
   int unit0, units;    // first unit of KU keys, number of them (0: no rows here)
 };
 
-__device__ __forceinline__ int kv8_row_pos(const Kv8Attn& a, const Kv8Item& it, int r) {
+__device__ __forceinline__ int kv8_row_pos(const AttnArgs& a, const Kv8Item& it, int r) {
   return it.pos + a.byG(r);
 }
 // First key that the row at position p sees.
@@ -78,7 +82,7 @@ __device__ __forceinline__ int kv8_row_lo(const Kv8Item& it, int p, int window) 
 }
 
 template <int RT, int KU>
-__device__ __forceinline__ Kv8Item kv8_entry(const Kv8Attn& a, int e) {
+__device__ __forceinline__ Kv8Item kv8_entry(const AttnArgs& a, int e) {
   Kv8Item it;
   it.b = a.byRt(e);
   it.rt = e - it.b * a.n_rt;
@@ -105,13 +109,13 @@ __device__ __forceinline__ Kv8Item kv8_entry(const Kv8Attn& a, int e) {
 // The line as the blocks share it: block i's stretch begins at i total / P.
 struct Kv8Line {
   int total, q, r;  // total = q P + r
-  __device__ __forceinline__ Kv8Line(const Kv8Attn& a, int t) : total(t) {
+  __device__ __forceinline__ Kv8Line(const AttnArgs& a, int t) : total(t) {
     q = a.byP(t);
     r = t - q * (int)a.byP.d;
   }
-  __device__ __forceinline__ int start(const Kv8Attn& a, int i) const { return i * q + a.byP(i * r); }
+  __device__ __forceinline__ int start(const AttnArgs& a, int i) const { return i * q + a.byP(i * r); }
   // The block whose stretch holds unit x.
-  __device__ __forceinline__ int block(const Kv8Attn& a, int x) const {
+  __device__ __forceinline__ int block(const AttnArgs& a, int x) const {
     int j = min((int)((float)x * (float)a.byP.d / (float)total), (int)a.byP.d - 1);
     while (j > 0 && start(a, j) > x) --j;
     while (start(a, j + 1) <= x) ++j;
@@ -144,7 +148,7 @@ struct Kv8PlanSmem {
 
 // Every thread of the block gets the block's stretch.
 template <int RT, int KU, int THREADS>
-__device__ __forceinline__ Kv8Cursor kv8_plan(const Kv8Attn& a, Kv8PlanSmem& sm) {
+__device__ __forceinline__ Kv8Cursor kv8_plan(const AttnArgs& a, Kv8PlanSmem& sm) {
   static_assert(THREADS / 32 <= 32, "a sum for each warp");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (a.split) {
@@ -195,7 +199,7 @@ __device__ __forceinline__ Kv8Cursor kv8_plan(const Kv8Attn& a, Kv8PlanSmem& sm)
 
 // The next segment of the block's stretch; false at its end.
 template <int RT, int KU>
-__device__ __forceinline__ bool kv8_next(const Kv8Attn& a, Kv8Cursor& c, Kv8Seg& s) {
+__device__ __forceinline__ bool kv8_next(const AttnArgs& a, Kv8Cursor& c, Kv8Seg& s) {
   while (c.w0 < c.w1) {
     s.it = kv8_entry<RT, KU>(a, c.e);
     const int len = kv8_len<RT, KU>(s.it);
@@ -222,7 +226,7 @@ __device__ __forceinline__ bool kv8_next(const Kv8Attn& a, Kv8Cursor& c, Kv8Seg&
 
 // The segment as the merge finds it, where it begins an item that goes on in
 // the next block.  c: the cursor behind the segment.
-__device__ __forceinline__ Kv8Desc kv8_desc(const Kv8Attn& a, const Kv8Cursor& c, const Kv8Seg& s) {
+__device__ __forceinline__ Kv8Desc kv8_desc(const AttnArgs& a, const Kv8Cursor& c, const Kv8Seg& s) {
   const int last = c.w0 - s.nu + s.it.units - 1;  // the item's last unit
   return Kv8Desc{s.it.nr, s.it.b, s.it.r0, s.g, Kv8Line(a, c.total).block(a, last), c.total,
                  s.it.pos, s.it.first};

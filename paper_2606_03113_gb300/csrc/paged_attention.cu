@@ -2,94 +2,597 @@
 //   o_r = sum_j p_rj v_j / sum_j p_rj,  p_rj = e^(q_r . k_j / sqrt(hd) - max),
 // over the keys j that row r sees: first .. its own position, at most `window`.
 //
-// k_paged_plain: a block a row and head, its warps take the keys in turn.
+// k_paged_rows: a block takes a stretch of the plan's units (kv8_plan.cuh), or, for short
+// sequences, a cluster of blocks an item. Stages of keys and values come by cp.async, kNst - 1 of
+// them on their way; a thread looks up the pages of a stage one stage ahead. Of an item's
+// R tiles of 16 query rows a warp has one, and of each stage the keys of its group; it keeps a
+// running maximum, sum and output of its own, and the block joins the groups once per item.
+// bf16: mma.sync on the rows as they are, probabilities in two bf16 parts (16 bits), so that the
+// output's own rounding is what remains. fp32: fused multiply-adds. Scores, sums and outputs are fp32.
+//
+// A key that some row of the tile does not see can hold anything: its scores are dropped by
+// position, and a value there that is no number is zeroed before the product. A row that sees one
+// gets it back at the end of the item: rows with such a value are summed again, key by key.
 #include <math.h>
 
+#include <mutex>
+#include <type_traits>
+
+#include "kv8_merge.cuh"
+#include "mma.cuh"
 #include "paged.cuh"
 
 namespace ssd {
 
 namespace {
 
-constexpr int kPlainWarps = 8;
+constexpr int kUnit = kKv8Block;  // keys of a unit of the plan
+constexpr int kTile = 16;         // query rows of a warp
+constexpr int kSplitMax = 8;      // blocks of a short sequence's item, a cluster, at most
 
-struct PagedAttn {
+struct PagedAttn : AttnArgs {
   PagedView c;
-  const char *k, *v;  // the layer's K and V of page 0
-  const void* q;
-  void* out;
-  const int32_t *pos, *rows, *first;
-  int32_t* err;
-  int64_t q_stride, out_stride;
-  int32_t G, M, longest, window;
-  float scale;  // log2(e) / sqrt(head_dim)
+  const char *k, *v;  // the layer's K and V in page 0
 };
+
+// Where things stand in a block's shared memory.
+template <typename T, int HD, int R, int NW>
+struct PL {
+  static constexpr int kRowBytes = HD * (int)sizeof(T);
+  static constexpr int kChunks = kRowBytes / 16;           // 16-byte chunks of a row
+  static constexpr int kKeys = kRowBytes > 256 ? 32 : 64;  // of a stage
+  static constexpr uint32_t kSide = kKeys * kRowBytes;
+  static constexpr uint32_t kStage = 2 * kSide;
+  static constexpr int kNst = (NW > 4 ? 192 : 96) * 1024 / (int)kStage;
+  static constexpr uint32_t kRing = kNst * kStage;
+  static constexpr int kGroups = NW / R;               // of warps, with keys of their own each
+  static constexpr int kGroupKeys = kKeys / kGroups;
+  static constexpr int kThreads = NW * 32;
+  static constexpr int kRows = R * kTile;
+  static constexpr int kOPad = HD + 4;  // floats of a row in the exchange
+  static constexpr uint32_t kQ = sizeof(T) == 4 ? kRows * kOPad * 4 : 0;  // fp32 queries
+  static constexpr uint32_t kSmem = kRing + kQ;
+  static constexpr uint32_t kExchange = kGroups * kRows * kOPad * 4;
+  static constexpr int kCopies = kKeys * kChunks / kThreads;  // of a thread, a stage and side
+  static constexpr int kLook = kKeys / 16;                     // pages of a stage, at most
+  static_assert(kExchange + kRows * HD * 4 <= kRing, "the exchange and the part fit the ring");
+  static_assert(kKeys * kChunks % kThreads == 0 && kThreads % kChunks == 0, "whole rows a pass");
+  // Chunk ch of row r: bf16 rows as ldmatrix wants them; fp32 rows such that eight lanes meet
+  // all banks, as two keys x four chunks and as four keys of one parity x two.
+  __device__ static __forceinline__ uint32_t place(int r, int ch) {
+    const int x = sizeof(T) == 2 ? r & 7 : (r & 6) ^ ((r & 1) << 2);
+    return (uint32_t)(r * kRowBytes + ((ch ^ x) << 4));
+  }
+};
+
+__device__ __forceinline__ bool no_number(float x) {
+  return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u;
+}
+// The bf16 pair without what is no number; `any` where there was one.
+__device__ __forceinline__ uint32_t numbers(uint32_t u, uint32_t& any) {
+  const uint32_t lo = (u & 0x7f80u) == 0x7f80u ? 0xffffu : 0u;
+  const uint32_t hi = (u & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+  any |= lo | hi;
+  return u & ~(lo | hi);
+}
+__device__ __forceinline__ float4 lds4(const unsigned char* p) {
+  return *reinterpret_cast<const float4*>(p);
+}
 
 }  // namespace
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(kPlainWarps * 32) k_paged_plain(const PagedAttn a) {
-  constexpr int C = HD / 32;
-  __shared__ float s_o[kPlainWarps][HD], s_m[kPlainWarps], s_l[kPlainWarps];
-  const int h = blockIdx.x, b = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int p0 = __ldg(a.pos + b), n = a.rows ? __ldg(a.rows + b) : a.M;
-  if (p0 < 0 || n < 0 || n > a.M || p0 > a.longest - n) {
-    if (threadIdx.x == 0 && h == 0 && blockIdx.y == 0 && a.err)
-      atomicOr(a.err, n < 0 || n > a.M ? (int)kErrControl : (int)kErrCapacity);
-    return;
+template <typename T, int HD, int R, int NW>
+__global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const PagedAttn a) {
+  using L = PL<T, HD, R, NW>;
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int NT = HD / 8;   // 8-column tiles of the output
+  constexpr int KS = HD / 16;  // 16-column steps of a score
+  extern __shared__ __align__(1024) unsigned char smem[];
+  __shared__ Kv8PlanSmem s_plan;
+  __shared__ float s_m[L::kGroups][L::kRows], s_l[L::kGroups][L::kRows], s_w[L::kGroups][L::kRows];
+  __shared__ float s_gm[L::kRows], s_sum[L::kRows];
+  __shared__ int s_bad;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int t = lane & 3, n8 = lane >> 2;
+  const int rt = warp % R, grp = warp / R;
+  float* const Ox = reinterpret_cast<float*>(smem);
+  float* const part = Ox + L::kExchange / 4;  // [rows][HD]: the block's part of a cluster's item
+  const int pmask = (1 << a.c.shift) - 1;
+
+  Kv8Cursor cur = kv8_plan<L::kRows, kUnit, L::kThreads>(a, s_plan);
+  pdl_launch_dependents();
+  if (tid == 0 && !a.split) a.desc[blockIdx.x].nr = 0;
+  if (tid < L::kRows) s_sum[tid] = 0.f, s_gm[tid] = -INFINITY;
+  Kv8Seg sg;
+  while (kv8_next<L::kRows, kUnit>(a, cur, sg)) {
+    const Kv8Item& it = sg.it;
+    const int g = sg.g;
+    const int seg0 = (it.unit0 + sg.u0) * kUnit;
+    const int kb = max(it.lo, seg0), ke = min(it.hi + 1, seg0 + sg.nu * kUnit);
+    const int nst = ke > kb ? (ke - seg0 + L::kKeys - 1) / L::kKeys : 0;
+    const int st0 = ke > kb ? (kb - seg0) / L::kKeys : 0;
+    const char* const kp = a.k + (size_t)g * a.c.slab;
+    const char* const vp = a.v + (size_t)g * a.c.slab;
+
+    // ---- stages: the pages of one are looked up while the one before is issued
+    const int ch = tid % L::kChunks, r0 = tid / L::kChunks;
+    int look[L::kLook];
+    auto look_up = [&](int s) {
+#pragma unroll
+      for (int j = 0; j < L::kLook; ++j) {
+        const int key = seg0 + s * L::kKeys + 16 * j;
+        const bool in = key < ke && key + 15 >= kb;
+        look[j] = in ? a.c.entry(it.b, min(key, ke - 1) >> a.c.shift) : 0;
+        if (look[j] < 0) {
+          look[j] = 0;
+          if (tid == 0 && a.err) atomicOr(a.err, (int)kErrTable);
+        }
+      }
+    };
+    auto issue = [&](int s) {
+      if (s < nst) {
+        const uint32_t dst = smem_u32(smem) + (uint32_t)(s % L::kNst) * L::kStage;
+#pragma unroll
+        for (int i = 0; i < L::kCopies; ++i) {
+          const int r = r0 + i * (L::kThreads / L::kChunks), key = seg0 + s * L::kKeys + r;
+          const bool in = key >= kb && key < ke;
+          const size_t off = (size_t)look[(i * (L::kThreads / L::kChunks)) / 16] * a.c.bytes +
+                             (size_t)(key & pmask) * L::kRowBytes + ch * 16;
+          const uint32_t at = dst + L::place(r, ch);
+          cp_async16(at, kp + (in ? off : 0), in);
+          cp_async16(at + L::kSide, vp + (in ? off : 0), in);
+        }
+        if (s + 1 < nst) look_up(s + 1);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if (st0 < nst) look_up(st0);
+#pragma unroll
+    for (int i = 0; i < L::kNst - 1; ++i) issue(st0 + i);
+
+    // ---- queries of the warp's tile
+    uint32_t qf[BF ? KS : 1][4];
+    float* const Qs = reinterpret_cast<float*>(smem + L::kRing);
+    if (tid == 0) s_bad = 0;
+    if constexpr (BF) {
+      const T* qp[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = rt * kTile + n8 + 8 * i, r = it.r0 + min(row, it.nr - 1);
+        const int m = a.byG(r), h = g * a.G + r - m * a.G;
+        qp[i] = static_cast<const T*>(a.q) + ((int64_t)it.b * a.M + m) * a.q_stride +
+                (int64_t)h * HD + 2 * t;
+      }
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          qf[k][x] = __ldg(reinterpret_cast<const uint32_t*>(qp[x & 1] + 16 * k + 8 * (x >> 1)));
+    } else {
+      for (int x = tid; x < L::kRows * (HD / 4); x += L::kThreads) {
+        const int row = x / (HD / 4), c4 = x % (HD / 4);
+        float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (row < it.nr) {
+          const int r = it.r0 + row, m = a.byG(r), h = g * a.G + r - m * a.G;
+          u = __ldg(reinterpret_cast<const float4*>(static_cast<const T*>(a.q) +
+                                                    ((int64_t)it.b * a.M + m) * a.q_stride +
+                                                    (int64_t)h * HD) +
+                    c4);
+        }
+        *reinterpret_cast<float4*>(Qs + row * L::kOPad + c4 * 4) = u;
+      }
+    }
+    int plo[2], phi[2];  // the lane's rows see keys plo .. phi
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = rt * kTile + n8 + 8 * i;
+      phi[i] = row < it.nr ? kv8_row_pos(a, it, it.r0 + row) : -1;  // no row here: sees none
+      plo[i] = row < it.nr ? kv8_row_lo(it, phi[i], a.window) : 0;
+    }
+    // every row of the item sees keys full_lo .. full_hi
+    const int full_lo = kv8_row_lo(it, it.hi, a.window);
+    const int full_hi = kv8_row_pos(a, it, it.r0);
+    const bool some = rt * kTile < it.nr;       // a tile without rows only helps to copy
+    const bool two = rt * kTile + 8 < it.nr;    // fp32: rows n8 + 8 are there
+
+    float o[NT][4], mx[2] = {-INFINITY, -INFINITY}, ls[2] = {0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[j][i] = 0.f;
+
+    for (int s = st0; s < nst; ++s) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(L::kNst - 2) : "memory");
+      __syncthreads();  // the stage is there, and everybody has read the one that is filled next
+      issue(s + L::kNst - 1);
+      const unsigned char* const sk = smem + (uint32_t)(s % L::kNst) * L::kStage;
+      const unsigned char* const sv = sk + L::kSide;
+#pragma unroll 1
+      for (int x0 = 0; x0 < L::kGroupKeys; x0 += 16) {
+        // the warp's 16 keys (fp32: 8 where a group has no more): lane n8, t has rows n8 and n8 + 8,
+        // keys 8 n + 2 t and 8 n + 2 t + 1
+        constexpr int kN = L::kGroupKeys < 16 ? 1 : 2;
+        const int kk0 = grp * L::kGroupKeys + x0, k0 = seg0 + s * L::kKeys + kk0;
+        if (!some || k0 >= ke || k0 + 8 * kN <= kb) continue;
+        float sc[2][4];
+        if constexpr (BF) {
+          float s2[2][2][4];
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) s2[i][n][x] = 0.f;
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            uint32_t b[4];
+            ldsm4(smem_u32(sk) + L::place(kk0 + (lane & 7) + ((lane >> 4) << 3), 2 * k + (lane >> 3 & 1)), b);
+            mma16816(s2[k & 1][0], qf[k], b[0], b[1]);
+            mma16816(s2[k & 1][1], qf[k], b[2], b[3]);
+          }
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) sc[n][x] = s2[0][n][x] + s2[1][n][x];
+        } else {
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) sc[n][x] = 0.f;
+#pragma unroll 4
+          for (int c4 = 0; c4 < L::kChunks; ++c4) {
+            float4 kq[kN][2];
+#pragma unroll
+            for (int n = 0; n < kN; ++n)
+#pragma unroll
+              for (int x = 0; x < 2; ++x) kq[n][x] = lds4(sk + L::place(kk0 + 8 * n + 2 * t + x, c4));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              if (i == 1 && !two) continue;
+              const float4 q = lds4(reinterpret_cast<const unsigned char*>(
+                  Qs + (rt * kTile + n8 + 8 * i) * L::kOPad + c4 * 4));
+#pragma unroll
+              for (int n = 0; n < kN; ++n)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                  float& d = sc[n][2 * i + x];
+                  d = fmaf(q.x, kq[n][x].x, d);
+                  d = fmaf(q.y, kq[n][x].y, d);
+                  d = fmaf(q.z, kq[n][x].z, d);
+                  d = fmaf(q.w, kq[n][x].w, d);
+                }
+            }
+          }
+        }
+        const bool full = k0 >= full_lo && k0 + 8 * kN - 1 <= full_hi;
+        float z[2][4], nm[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int n = 0; n < kN; ++n)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            z[n][x] = sc[n][x] * a.scale;
+            if (!full) {
+              const int key = k0 + 8 * n + 2 * t + (x & 1);
+              if (key < plo[x >> 1] || key > phi[x >> 1]) z[n][x] = -INFINITY;
+            }
+            nm[x >> 1] = fmaxf(nm[x >> 1], z[n][x]);
+          }
+        bool moved = false;
+        float f[2], top[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          nm[i] = fmaxf(nm[i], __shfl_xor_sync(0xffffffffu, nm[i], 1));
+          nm[i] = fmaxf(nm[i], __shfl_xor_sync(0xffffffffu, nm[i], 2));
+          nm[i] = fmaxf(nm[i], mx[i]);
+          top[i] = nm[i] == -INFINITY ? 0.f : nm[i];
+          f[i] = nm[i] == mx[i] ? 1.f : exp2f(mx[i] - nm[i]);
+          moved |= nm[i] != mx[i];
+          mx[i] = nm[i];
+          ls[i] *= f[i];
+        }
+        if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[j][x] *= f[x >> 1];
+        }
+        float p[2][4];
+#pragma unroll
+        for (int n = 0; n < kN; ++n)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            p[n][x] = exp2f(z[n][x] - top[x >> 1]);
+            ls[x >> 1] += p[n][x];
+          }
+        uint32_t any = 0;
+        if constexpr (BF) {
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              split2(p[n][2 * i], p[n][2 * i + 1], hi[2 * n + i], lo[2 * n + i]);
+#pragma unroll
+          for (int j = 0; j < NT; j += 2) {
+            uint32_t b[4];
+            ldsm4t(smem_u32(sv) + L::place(kk0 + (lane & 15), j + (lane >> 4)), b);
+            if (!full) {
+#pragma unroll
+              for (int x = 0; x < 4; ++x) b[x] = numbers(b[x], any);
+            }
+            mma16816(o[j], lo, b[0], b[1]);
+            mma16816(o[j + 1], lo, b[2], b[3]);
+            mma16816(o[j], hi, b[0], b[1]);
+            mma16816(o[j + 1], hi, b[2], b[3]);
+          }
+        } else {
+          // o[j][2 i + ..]: row n8 + 8 i; columns 16 (j / 2) + 4 t + 2 (j % 2) + ..
+#pragma unroll
+          for (int kk = 0; kk < 8 * kN; ++kk) {
+            float w[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              w[i] = __shfl_sync(0xffffffffu, p[kk >> 3][2 * i + (kk & 1)], (lane & 28) + (kk >> 1 & 3));
+#pragma unroll
+            for (int j = 0; j < NT; j += 2) {
+              float4 u = lds4(sv + L::place(kk0 + kk, 2 * j + t));
+              if (!full) {
+                float* e = &u.x;
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                  if (no_number(e[x])) e[x] = 0.f, any = 1;
+              }
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                if (i == 1 && !two) continue;
+                o[j][2 * i] = fmaf(w[i], u.x, o[j][2 * i]);
+                o[j][2 * i + 1] = fmaf(w[i], u.y, o[j][2 * i + 1]);
+                o[j + 1][2 * i] = fmaf(w[i], u.z, o[j + 1][2 * i]);
+                o[j + 1][2 * i + 1] = fmaf(w[i], u.w, o[j + 1][2 * i + 1]);
+              }
+            }
+          }
+        }
+        if (any) s_bad = 1;
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+
+    // ---- the groups' parts together
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 1);
+      ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 2);
+      if (t == 0) {
+        s_m[grp][rt * kTile + n8 + 8 * i] = mx[i];
+        s_l[grp][rt * kTile + n8 + 8 * i] = ls[i];
+      }
+    }
+    __syncthreads();  // nobody reads the ring any more
+    if (tid < L::kRows) {
+      float gm = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int x = 0; x < L::kGroups; ++x) gm = fmaxf(gm, s_m[x][tid]);
+#pragma unroll
+      for (int x = 0; x < L::kGroups; ++x) sum = fmaf(part_weight(s_m[x][tid], gm), s_l[x][tid], sum);
+#pragma unroll
+      for (int x = 0; x < L::kGroups; ++x)
+        s_w[x][tid] = sum != 0.f ? part_weight(s_m[x][tid], gm) / sum : 0.f;
+      s_gm[tid] = gm;
+      s_sum[tid] = sum;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = rt * kTile + n8 + 8 * i;
+      if (row < it.nr) {
+        float* p = Ox + (size_t)(grp * L::kRows + row) * L::kOPad;
+        if constexpr (BF) {
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            *reinterpret_cast<float2*>(p + 8 * j + 2 * t) = make_float2(o[j][2 * i], o[j][2 * i + 1]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < NT; j += 2)
+            *reinterpret_cast<float4*>(p + 8 * j + 4 * t) =
+                make_float4(o[j][2 * i], o[j][2 * i + 1], o[j + 1][2 * i], o[j + 1][2 * i + 1]);
+        }
+      }
+    }
+    __syncthreads();
+    const bool whole = sg.whole();
+    const int slot = 2 * blockIdx.x + (sg.u0 == 0);
+#pragma unroll 1
+    for (int x0 = 0; x0 < L::kRows * NT; x0 += L::kThreads) {
+      const int row = (x0 + tid) / NT, c8 = (tid % NT) * 8;
+      if (row < it.nr) {
+        const int r = it.r0 + row, m = a.byG(r), h = g * a.G + r - m * a.G;
+        const int p = kv8_row_pos(a, it, r), lo = kv8_row_lo(it, p, a.window);
+        const float gm = s_gm[row], Ls = s_sum[row];
+        float acc[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+        bool nan = false;
+#pragma unroll
+        for (int x = 0; x < L::kGroups; ++x) {
+          const float wt = s_w[x][row];
+          const float4* ox = reinterpret_cast<const float4*>(Ox + (size_t)(x * L::kRows + row) * L::kOPad + c8);
+          const float4 u = ox[0], w = ox[1];
+          acc[0] = fmaf(u.x, wt, acc[0]);
+          acc[1] = fmaf(u.y, wt, acc[1]);
+          acc[2] = fmaf(u.z, wt, acc[2]);
+          acc[3] = fmaf(u.w, wt, acc[3]);
+          acc[4] = fmaf(w.x, wt, acc[4]);
+          acc[5] = fmaf(w.y, wt, acc[5]);
+          acc[6] = fmaf(w.z, wt, acc[6]);
+          acc[7] = fmaf(w.w, wt, acc[7]);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) nan |= acc[j] != acc[j];
+        // values that are no numbers belong to the rows that see them (a part of a probability times
+        // infinity may have made NaN of one); where the scores are NaN, so is everything
+        if ((s_bad || nan) && Ls == Ls) {
+          float sum[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+          for (int key = max(kb, lo); key < min(ke, p + 1); ++key) {
+            const int e = max(a.c.entry(it.b, key >> a.c.shift), 0);
+            const T* v = reinterpret_cast<const T*>(vp + (size_t)e * a.c.bytes +
+                                                    (size_t)(key & pmask) * L::kRowBytes) + c8;
+            float f[8];
+            load_query8(v, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (no_number(f[j])) sum[j] += f[j];
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (sum[j] != 0.f) acc[j] = sum[j];
+        }
+        if (a.split > 1) {
+          store_out8(part + row * HD + c8, acc);
+        } else if (whole) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            acc[j] = p < lo ? 0.f : Ls == 0.f ? __uint_as_float(0x7fffffffu) : acc[j];
+          store_out8(static_cast<T*>(a.out) + ((int64_t)it.b * a.M + m) * a.out_stride +
+                         (int64_t)h * HD + c8,
+                     acc);
+        } else {
+          store_out8(a.part + ((size_t)slot * a.part_rows + row) * HD + c8, acc);
+          if (c8 == 0) a.ml[(size_t)slot * a.part_rows + row] = make_float2(gm, Ls);
+        }
+      }
+    }
+    if (!a.split && !whole && sg.u0 == 0 && tid == 0) a.desc[blockIdx.x] = kv8_desc(a, cur, sg);
+    __syncthreads();
   }
-  const int first = a.first ? max(__ldg(a.first + b), 0) : 0;
-  const size_t head = (size_t)(h / a.G) * a.c.slab;
-  const int mask = (1 << a.c.shift) - 1;
-  for (int m = blockIdx.y; m < n; m += gridDim.y) {
-    const int p = p0 + m, lo = a.window > 0 ? max(first, p - a.window + 1) : first;
-    const T* q = static_cast<const T*>(a.q) + ((int64_t)b * a.M + m) * a.q_stride + (int64_t)h * HD;
-    float fq[C], o[C], mx = -INFINITY, sum = 0.f;
+  if (a.split > 1) {  // the cluster's parts together, each block some of the columns
+    const int i = (int)blockIdx.x / a.split, rank = (int)blockIdx.x - i * a.split;
+    const int e = i / a.Hkv, g = i - e * a.Hkv;
+    const Kv8Item it = kv8_entry<L::kRows, kUnit>(a, e);
+    cluster_sync();
+    for (int x = rank * L::kThreads + tid; x < it.nr * NT; x += a.split * L::kThreads) {
+      const int row = x / NT, c8 = (x % NT) * 8;
+      float w[kSplitMax], m[kSplitMax], gm = -INFINITY, sum = 0.f, acc[8];
 #pragma unroll
-    for (int j = 0; j < C; ++j) fq[j] = Elem<T>::to_f(q[lane + 32 * j]) * a.scale, o[j] = 0.f;
-    for (int key = lo + warp; key <= p; key += kPlainWarps) {
-      const int e = a.c.entry(b, key >> a.c.shift);
-      if (e < 0) {
-        if (lane == 0 && a.err) atomicOr(a.err, (int)kErrTable);
-        continue;
+      for (int y = 0; y < kSplitMax; ++y) {
+        w[y] = y < a.split ? ld_cluster_f32(in_block(&s_sum[row], y)) : 0.f;
+        m[y] = y < a.split ? ld_cluster_f32(in_block(&s_gm[row], y)) : 0.f;
       }
-      const size_t at = e * a.c.bytes + head + (size_t)(key & mask) * HD * sizeof(T);
-      const T* kr = reinterpret_cast<const T*>(a.k + at);
-      const T* vr = reinterpret_cast<const T*>(a.v + at);
-      float s = 0.f;
 #pragma unroll
-      for (int j = 0; j < C; ++j) s = fmaf(fq[j], Elem<T>::to_f(kr[lane + 32 * j]), s);
-      s = warp_sum(s);
-      const float nm = fmaxf(mx, s), top = nm == -INFINITY ? 0.f : nm;
-      const float f = exp2f(mx - top), w = exp2f(s - top);
-      sum = sum * f + w;
+      for (int y = 0; y < kSplitMax; ++y)  // (a sum of 0: the row sees none of the part's keys)
+        gm = fmaxf(gm, w[y] != 0.f ? m[y] : -INFINITY);
 #pragma unroll
-      for (int j = 0; j < C; ++j) o[j] = fmaf(w, Elem<T>::to_f(vr[lane + 32 * j]), o[j] * f);
-      mx = nm;
-    }
-#pragma unroll
-    for (int j = 0; j < C; ++j) s_o[warp][lane + 32 * j] = o[j];
-    if (lane == 0) s_m[warp] = mx, s_l[warp] = sum;
-    __syncthreads();
-    if (threadIdx.x < HD) {
-      float gm = -INFINITY, L = 0.f, acc = 0.f;
-      for (int w = 0; w < kPlainWarps; ++w) gm = fmaxf(gm, s_m[w]);
-      for (int w = 0; w < kPlainWarps; ++w) {
-        const float f = exp2f(s_m[w] - (gm == -INFINITY ? 0.f : gm));
-        L = fmaf(f, s_l[w], L);
-        acc = fmaf(f, s_o[w][threadIdx.x], acc);
+      for (int y = 0; y < kSplitMax; ++y) {
+        if (w[y] != 0.f) w[y] *= part_weight(m[y], gm);
+        sum += w[y];
       }
-      static_cast<T*>(a.out)[((int64_t)b * a.M + m) * a.out_stride + (int64_t)h * HD + threadIdx.x] =
-          Elem<T>::from_f(lo <= p ? acc / L : 0.f);
+      // (the parts are weighed by w / sum: w times a large value can be out of range; a row whose
+      // every score is -inf has no sum)
+      const float inv = 1.f / sum, none = sum == 0.f ? __uint_as_float(0x7fffffffu) : 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] = none;
+#pragma unroll
+      for (int y = 0; y < kSplitMax; ++y) {
+        if (y >= a.split) continue;
+        const uint32_t at = in_block(part + row * HD + c8, y);
+        const float4 u = ld_cluster_f32x4(at), v = ld_cluster_f32x4(at + 16);
+        const float wt = w[y] * inv;
+        acc[0] = fmaf(wt, u.x, acc[0]);
+        acc[1] = fmaf(wt, u.y, acc[1]);
+        acc[2] = fmaf(wt, u.z, acc[2]);
+        acc[3] = fmaf(wt, u.w, acc[3]);
+        acc[4] = fmaf(wt, v.x, acc[4]);
+        acc[5] = fmaf(wt, v.y, acc[5]);
+        acc[6] = fmaf(wt, v.z, acc[6]);
+        acc[7] = fmaf(wt, v.w, acc[7]);
+      }
+      const int r = it.r0 + row, mr = a.byG(r), h = g * a.G + r - mr * a.G;
+      const int p = kv8_row_pos(a, it, r);
+      const bool sees = kv8_row_lo(it, p, a.window) <= p;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] = sees ? acc[j] : 0.f;
+      store_out8(static_cast<T*>(a.out) + ((int64_t)it.b * a.M + mr) * a.out_stride +
+                     (int64_t)h * HD + c8,
+                 acc);
     }
-    __syncthreads();
+    cluster_sync();  // everybody has read this block's part
   }
 }
 
+// ------------------------------------------------------------- host side
+
 namespace {
 
+struct PagedDevice {
+  bool ready = false;
+  int sms = 0;
+};
+std::mutex g_paged_mu;
+PagedDevice g_paged_dev[64];
+
+template <typename T, int HD, int R, int NW>
+cudaError_t prep() {
+  return cudaFuncSetAttribute(k_paged_rows<T, HD, R, NW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)PL<T, HD, R, NW>::kSmem);
+}
+template <int HD>
+cudaError_t prep_hd() {
+  cudaError_t e = prep<float, HD, 1, 4>();
+  if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 1, 4>();
+  if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 2, 4>();
+  if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 4, 4>();
+  return e;
+}
+
+// SMs of the current device; its kernels' limits of shared memory are set on the first call
+// there.
+cudaError_t paged_device(int* sms) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(g_paged_mu);
+  PagedDevice& d = g_paged_dev[dev];
+  if (!d.ready) {
+    if ((e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess ||
+        (e = prep_hd<64>()) != cudaSuccess || (e = prep_hd<128>()) != cudaSuccess)
+      return e;
+    d.ready = true;
+  }
+  *sms = d.sms;
+  return cudaSuccess;
+}
+
+// Short sequences: a cluster of blocks for each item, which joins its parts itself (no workspace, no
+// second launch): 1, 2, 4 or 8 blocks with 128 keys or more each, as long as there is room for all.
+constexpr int kSplitKeys = 128, kSplitBlocks = 304, kSplitSeq = 512, kSplitMost = 2048;
+
+struct PagedPlan {
+  int tiles;  // of 16 rows, of a block
+  int split;  // blocks of an item's own, 0: the line
+  int max_blocks, part_rows;
+  long long n_rt, units;  // tiles of a sequence; the line's places, at most
+};
+PagedPlan plan_of(const ssd_paged_cache* c, int n_heads, int M, int longest) {
+  PagedPlan p;
+  const long long rows = (long long)M * (n_heads / c->n_kv_heads);
+  const long long heads = (long long)c->n_seq * c->n_kv_heads;
+  p.tiles = c->dtype == SSD_DTYPE_F32 || rows <= kTile ? 1 : rows <= 2 * kTile ? 2 : 4;
+  p.n_rt = (rows + p.tiles * kTile - 1) / (p.tiles * kTile);
+  const long long items = p.n_rt * heads;
+  p.split = 1;
+  while (p.split < kSplitMax && longest > kSplitKeys * p.split && items * p.split * 2 <= kSplitBlocks)
+    p.split *= 2;
+  if (longest > kSplitSeq * p.split || longest > kSplitMost) p.split = 0;
+  p.part_rows = rows < p.tiles * kTile ? (int)rows : p.tiles * kTile;
+  p.units = items * ((longest + kUnit - 1) / kUnit + kKv8ItemCost<kTile>);
+  p.max_blocks = p.units < kKv8MaxBlocks ? (int)p.units : kKv8MaxBlocks;
+  return p;
+}
+
 const char* check_attention(const ssd_paged_cache* c, int32_t n_heads, int32_t M, int32_t longest,
-                            ssd_status* status) {
+                            PagedPlan* plan, ssd_status* status) {
   if (const char* why = check_paged(c, status)) return why;
   *status = SSD_ERR_INVALID_ARG;
   if (n_heads < c->n_kv_heads || n_heads % c->n_kv_heads || n_heads > 65536)
@@ -97,16 +600,39 @@ const char* check_attention(const ssd_paged_cache* c, int32_t n_heads, int32_t M
   if (M < 1) return "M must be at least 1";
   if (longest < 0) return "longest must be 0 (the cache's positions) or positive";
   *status = SSD_ERR_CAPACITY;
-  if (M > c->max_pages * c->page) return "more rows than the cache has positions";
-  if (longest > c->max_pages * c->page) return "longest: more than the cache has positions";
+  const int cap = c->max_pages * c->page;
+  if (M > cap) return "more rows than the cache has positions";
+  if (longest > cap) return "longest: more than the cache has positions";
+  *plan = plan_of(c, n_heads, M, longest ? longest : cap);
+  if (plan->units > 0x7fffffffll) return "n_seq x M x longest: more than 2^31 units of work";
   *status = SSD_OK;
   return nullptr;
 }
 
-template <typename T, int HD>
-cudaError_t plain_launch(const PagedAttn& a, int heads, int n_seq, cudaStream_t st) {
-  k_paged_plain<T, HD><<<dim3(heads, a.M < 65535 ? a.M : 65535, n_seq), kPlainWarps * 32, 0, st>>>(a);
-  return cudaGetLastError();
+template <typename T, int HD, int R, int NW>
+cudaError_t rows_launch(const PagedAttn& a, int P, cudaStream_t st) {
+  using L = PL<T, HD, R, NW>;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(P);
+  cfg.blockDim = dim3(L::kThreads);
+  cfg.dynamicSmemBytes = L::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = a.split > 1 ? a.split : 1;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.split > 1 ? 1 : 0;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_paged_rows<T, HD, R, NW>, a);
+  if (e != cudaSuccess || a.split) return e;
+  return R == 1 ? merge_launch<T, HD, kMWarps>(a, P, st) : merge_launch<T, HD, 1>(a, P, st);
+}
+template <int HD>
+cudaError_t rows_launch(const PagedAttn& a, int dtype, int tiles, int P, cudaStream_t st) {
+  if (dtype == SSD_DTYPE_F32) return rows_launch<float, HD, 1, 4>(a, P, st);
+  if (tiles == 1) return rows_launch<__nv_bfloat16, HD, 1, 4>(a, P, st);
+  if (tiles == 2) return rows_launch<__nv_bfloat16, HD, 2, 4>(a, P, st);
+  return rows_launch<__nv_bfloat16, HD, 4, 4>(a, P, st);
 }
 
 }  // namespace
@@ -116,11 +642,12 @@ extern "C" size_t ssd_paged_attention_bytes(const ssd_paged_cache* c, int32_t n_
                                             int32_t longest) {
   using namespace ssd;
   ssd_status status;
-  if (const char* why = check_attention(c, n_heads, M, longest, &status)) {
+  PagedPlan p;
+  if (const char* why = check_attention(c, n_heads, M, longest, &p, &status)) {
     fail_op(status, why);
     return 0;
   }
-  return 256;
+  return p.split ? 256 : kv8_work(p.max_blocks, p.part_rows, c->head_dim).total;
 }
 
 extern "C" ssd_status ssd_paged_attention(const ssd_paged_cache* c, int32_t layer, const void* q,
@@ -130,10 +657,10 @@ extern "C" ssd_status ssd_paged_attention(const ssd_paged_cache* c, int32_t laye
                                           void* out, int64_t out_stride, void* workspace,
                                           size_t workspace_bytes, int32_t* err_dev, void* stream) {
   using namespace ssd;
-  (void)workspace;
-  (void)workspace_bytes;
   ssd_status status;
-  if (const char* why = check_attention(c, n_heads, M, longest, &status)) return fail_op(status, why);
+  PagedPlan plan;
+  if (const char* why = check_attention(c, n_heads, M, longest, &plan, &status))
+    return fail_op(status, why);
   if (layer < 0 || layer >= c->n_layers)
     return fail_op(SSD_ERR_INVALID_ARG, "layer must be in 0..n_layers - 1");
   const int elt = c->dtype == SSD_DTYPE_BF16 ? 2 : 4;
@@ -147,6 +674,15 @@ extern "C" ssd_status ssd_paged_attention(const ssd_paged_cache* c, int32_t laye
   if (out == q && out_stride != q_stride)
     return fail_op(SSD_ERR_INVALID_ARG, "out is q, but their strides differ");
   if (window < 0) return fail_op(SSD_ERR_INVALID_ARG, "window must be 0 (none) or positive");
+  const Kv8Work lay = kv8_work(plan.max_blocks, plan.part_rows, c->head_dim);
+  if (!plan.split) {
+    if (!workspace || ((uintptr_t)workspace & 255u))
+      return fail_op(SSD_ERR_INVALID_ARG, "workspace must be non-NULL and 256-byte aligned");
+    if (workspace_bytes < lay.total) return fail_op(SSD_ERR_CAPACITY, "workspace too small");
+  }
+  int sms = 0;
+  cudaError_t e = paged_device(&sms);
+  if (e != cudaSuccess) return fail_op_cuda("ssd_paged_attention", e);
   PagedAttn a{};
   a.c = paged_view(c);
   a.k = a.c.pages + a.c.side(layer, 0);
@@ -159,19 +695,29 @@ extern "C" ssd_status ssd_paged_attention(const ssd_paged_cache* c, int32_t laye
   a.err = err_dev;
   a.q_stride = q_stride;
   a.out_stride = out_stride;
+  a.n_seq = c->n_seq;
+  a.Hkv = c->n_kv_heads;
   a.G = n_heads / c->n_kv_heads;
   a.M = M;
-  a.longest = longest ? longest : c->max_pages * c->page;
+  a.max_seq = longest ? longest : c->max_pages * c->page;
   a.window = window;
+  a.n_rt = (int)plan.n_rt;
+  a.entries = (int)plan.n_rt * c->n_seq;
   a.scale = (float)(1.4426950408889634 / sqrt((double)c->head_dim));
+  char* ws = static_cast<char*>(workspace);
+  a.desc = reinterpret_cast<Kv8Desc*>(ws);
+  a.ml = reinterpret_cast<float2*>(ws + lay.ml);
+  a.part = reinterpret_cast<float*>(ws + lay.part);
+  a.byG = Kv8Div::of((uint32_t)a.G);
+  a.byRt = Kv8Div::of((uint32_t)plan.n_rt);
+  int P = sms * 2;  // blocks of an SM
+  if (P > plan.max_blocks) P = plan.max_blocks;
+  a.part_rows = plan.part_rows;
+  a.split = plan.split;
+  if (plan.split) P = a.entries * a.Hkv * plan.split;
+  a.byP = Kv8Div::of((uint32_t)P);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const bool wide = c->head_dim == 128;
-  cudaError_t e;
-  if (c->dtype == SSD_DTYPE_BF16)
-    e = wide ? plain_launch<__nv_bfloat16, 128>(a, n_heads, c->n_seq, st)
-             : plain_launch<__nv_bfloat16, 64>(a, n_heads, c->n_seq, st);
-  else
-    e = wide ? plain_launch<float, 128>(a, n_heads, c->n_seq, st)
-             : plain_launch<float, 64>(a, n_heads, c->n_seq, st);
+  e = c->head_dim == 128 ? rows_launch<128>(a, c->dtype, plan.tiles, P, st)
+                         : rows_launch<64>(a, c->dtype, plan.tiles, P, st);
   return e == cudaSuccess ? SSD_OK : fail_op_cuda("ssd_paged_attention", e);
 }
