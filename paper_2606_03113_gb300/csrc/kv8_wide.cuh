@@ -30,16 +30,12 @@
 // keys: 31 us.
 #pragma once
 
+#include "attn_wide.cuh"
+
 namespace ssd {
 
 namespace {
 
-constexpr int kWRows = 128;   // query rows of an accumulator
-constexpr int kWKeys = kKv8Block;  // keys of a step: one scale
-constexpr int kWHd = 128;
-constexpr uint32_t kWQHalf = kWRows * 128;       // bytes of 64 f16 columns of the queries
-constexpr uint32_t kWKHalf = kWKeys * 128;       // of a step's keys or values
-constexpr uint32_t kWKTile = 2 * kWKHalf;
 // A block's tile of TILES accumulators.
 template <int TILES>
 struct WideL {
@@ -55,142 +51,10 @@ struct WideL {
 constexpr float kWBase = 7.f, kWGrow = 8.f;
 constexpr float kWFar = 1048576.f;  // 2^20: half a unit there is 2^-4
 
-// Byte of 16-byte chunk ch (0..7, eight f16 each) of row r in 64 columns.
-__device__ __forceinline__ uint32_t w_place(int r, int ch) {
-  return (uint32_t)(r * 128 + ((ch ^ (r & 7)) << 4));
-}
-
 // Instruction descriptors: f16 operands, fp32 accumulator, M = 128, N = the keys of a
 // step or the columns of the output; bit 16: B is MN-major.
 constexpr uint32_t kWIdesc = (1u << 4) | ((uint32_t)(kWKeys >> 3) << 17) | ((128u >> 4) << 24);
 constexpr uint32_t kWIdescV = (1u << 4) | (1u << 16) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
-
-// MN-major operand of 128-byte rows (64 columns) with the 128-byte swizzle: the
-// leading offset leads to the next 64 columns, the stride offset to the next 8 rows.
-__device__ __forceinline__ uint64_t w_desc_mn(uint32_t smem_addr) {
-  uint64_t d = 0;
-  d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)(kWKHalf >> 4) << 16;
-  d |= (uint64_t)(1024u >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
-}
-
-// A whole warp comes here, and the lane with `one` issues: where a branch leaves one lane
-// alone, the operands have to be brought into the warp's registers for each instruction,
-// and it took up to 125 cycles to issue what the tensor cores need 48 for.
-__device__ __forceinline__ void w_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc,
-                                      uint32_t one) {
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "setp.ne.b32 q, %5, 0;\n\t"
-      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc), "r"(one)
-      : "memory");
-}
-// A from tensor memory.
-__device__ __forceinline__ void w_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
-                                         bool acc, uint32_t one) {
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "setp.ne.b32 q, %5, 0;\n\t"
-      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc), "r"(one)
-      : "memory");
-}
-// 1 in one lane of the warp.
-__device__ __forceinline__ uint32_t w_elect() {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "elect.sync _|p, 0xffffffff;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(r));
-  return r;
-}
-
-// Columns of the thread's lane, there on return.
-__device__ __forceinline__ void w_ld16(uint32_t t, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
-      "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15"
-      "}, [%16];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
-        "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
-        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(t)
-      : "memory");
-}
-__device__ __forceinline__ void w_ld32(uint32_t t, uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
-      "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31"
-      "}, [%32];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
-        "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
-        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
-        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
-        "=r"(r[30]), "=r"(r[31])
-      : "r"(t)
-      : "memory");
-}
-__device__ __forceinline__ void w_ld64(uint32_t t, uint32_t (&r)[64]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
-      "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
-      "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
-      "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63"
-      "}, [%64];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
-        "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
-        "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
-        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
-        "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]),
-        "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]),
-        "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
-        "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]),
-        "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]),
-        "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
-      : "r"(t)
-      : "memory");
-}
-__device__ __forceinline__ void w_st16(uint32_t t, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(t),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-__device__ __forceinline__ void w_st32(uint32_t t, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(t),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
-      "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
-      "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
-      "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
-}
-__device__ __forceinline__ void w_st_wait() {
-  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-}
-// Writes of this thread to shared memory, for the tensor cores to read.
-__device__ __forceinline__ void w_smem_fence() {
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-}
 
 // Codes that are read once, a step ahead of their use (volatile: the load stays
 // where it is issued).
@@ -202,12 +66,6 @@ __device__ __forceinline__ uint4 w_load16(const void* p) {
   return r;
 }
 
-// The larger of three.
-__device__ __forceinline__ float w_max3(float x, float y, float z) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
-  return r;
-}
 // Barriers of the two buffers: keys and values stored, scores there (and the keys'
 // place free), probabilities there, output added (the values' and their place
 // free); queries of the segment stored.
@@ -222,23 +80,6 @@ __device__ __forceinline__ int w_key0(const Kv8Seg& s, int i) {
   return (s.it.unit0 + s.u0 + i) * kWKeys;
 }
 
-// Waits for a barrier's phase, asleep for up to a millisecond at a time (a
-// poll without that hint comes back at once, and the polls of nine waiting warps take
-// the issue slots of those at work); false after a few seconds.
-__device__ __forceinline__ bool w_sleep(uint64_t* b, uint32_t parity) {
-  for (int i = 0; i < 4096; ++i) {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done)
-        : "r"(smem_u32(b)), "r"(parity), "r"(1000000u)
-        : "memory");
-    if (done) return true;
-  }
-  return false;
-}
 // The phase that step n completes on its buffer's barrier; after a wait that gave
 // up, no thread of this role waits again: it runs through its steps, meets its
 // barriers and reports.

@@ -482,9 +482,13 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
 #pragma unroll
       for (int y = 0; y < kSplitMax; ++y)  // (a sum of 0: the row sees none of the part's keys)
         gm = fmaxf(gm, w[y] != 0.f ? m[y] : -INFINITY);
+      uint32_t has = 0;  // parts whose keys the row sees (of the others there may be nothing to read)
 #pragma unroll
       for (int y = 0; y < kSplitMax; ++y) {
-        if (w[y] != 0.f) w[y] *= part_weight(m[y], gm);
+        if (w[y] != 0.f) {
+          has |= 1u << y;
+          w[y] *= part_weight(m[y], gm);
+        }
         sum += w[y];
       }
       // (the parts are weighed by w / sum: w times a large value can be out of range; a row whose
@@ -494,7 +498,7 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
       for (int j = 0; j < 8; ++j) acc[j] = none;
 #pragma unroll
       for (int y = 0; y < kSplitMax; ++y) {
-        if (y >= a.split) continue;
+        if (!(has >> y & 1)) continue;
         const uint32_t at = in_block(part + row * HD + c8, y);
         const float4 u = ld_cluster_f32x4(at), v = ld_cluster_f32x4(at + 16);
         const float wt = w[y] * inv;
@@ -520,6 +524,12 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
   }
 }
 
+}  // namespace ssd
+
+#include "paged_wide.cuh"
+
+namespace ssd {
+
 // ------------------------------------------------------------- host side
 
 namespace {
@@ -535,6 +545,11 @@ template <typename T, int HD, int R, int NW>
 cudaError_t prep() {
   return cudaFuncSetAttribute(k_paged_rows<T, HD, R, NW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               (int)PL<T, HD, R, NW>::kSmem);
+}
+template <int TILES>
+cudaError_t prep_wide() {
+  return cudaFuncSetAttribute(k_paged_wide<TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)PWideL<TILES>::kSmem);
 }
 template <int HD>
 cudaError_t prep_hd() {
@@ -556,7 +571,8 @@ cudaError_t paged_device(int* sms) {
   PagedDevice& d = g_paged_dev[dev];
   if (!d.ready) {
     if ((e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess ||
-        (e = prep_hd<64>()) != cudaSuccess || (e = prep_hd<128>()) != cudaSuccess)
+        (e = prep_hd<64>()) != cudaSuccess || (e = prep_hd<128>()) != cudaSuccess ||
+        (e = prep_wide<1>()) != cudaSuccess || (e = prep_wide<2>()) != cudaSuccess)
       return e;
     d.ready = true;
   }
@@ -568,7 +584,13 @@ cudaError_t paged_device(int* sms) {
 // second launch): 1, 2, 4 or 8 blocks with 128 keys or more each, as long as there is room for all.
 constexpr int kSplitKeys = 128, kSplitBlocks = 304, kSplitSeq = 512, kSplitMost = 2048;
 
+#ifndef PWIDE_FROM
+#define PWIDE_FROM 64
+#endif
+constexpr int kWideFrom = PWIDE_FROM;
+
 struct PagedPlan {
+  int wide;   // accumulators of a tile on tcgen05, 0: mma.sync
   int tiles;  // of 16 rows, of a block
   int split;  // blocks of an item's own, 0: the line
   int max_blocks, part_rows;
@@ -579,15 +601,27 @@ PagedPlan plan_of(const ssd_paged_cache* c, int n_heads, int M, int longest) {
   const long long rows = (long long)M * (n_heads / c->n_kv_heads);
   const long long heads = (long long)c->n_seq * c->n_kv_heads;
   p.tiles = c->dtype == SSD_DTYPE_F32 || rows <= kTile ? 1 : rows <= 2 * kTile ? 2 : 4;
-  p.n_rt = (rows + p.tiles * kTile - 1) / (p.tiles * kTile);
-  const long long items = p.n_rt * heads;
+  int rt = p.tiles * kTile;
+  p.n_rt = (rows + rt - 1) / rt;
+  long long items = p.n_rt * heads;
   p.split = 1;
   while (p.split < kSplitMax && longest > kSplitKeys * p.split && items * p.split * 2 <= kSplitBlocks)
     p.split *= 2;
   if (longest > kSplitSeq * p.split || longest > kSplitMost) p.split = 0;
-  p.part_rows = rows < p.tiles * kTile ? (int)rows : p.tiles * kTile;
-  p.units = items * ((longest + kUnit - 1) / kUnit + kKv8ItemCost<kTile>);
-  p.max_blocks = p.units < kKv8MaxBlocks ? (int)p.units : kKv8MaxBlocks;
+  p.wide = 0;
+  if (c->dtype == SSD_DTYPE_BF16 && c->head_dim == kWHd && rows > kWideFrom &&
+      !(p.split && items * p.split <= kSplitBlocks)) {
+    p.wide = rows > kWRows ? 2 : 1;
+    p.split = 0;
+    rt = p.wide * kWRows;
+    p.n_rt = (rows + rt - 1) / rt;
+    items = p.n_rt * heads;
+  }
+  p.part_rows = rows < rt ? (int)rows : rt;
+  p.units = items * ((longest + kUnit - 1) / kUnit +
+                     (p.wide == 2 ? kKv8ItemCost<256> : kKv8ItemCost<kTile>));
+  p.max_blocks = p.wide ? kKv8MaxBlocks / 2 : kKv8MaxBlocks;
+  if (p.units < p.max_blocks) p.max_blocks = (int)p.units;
   return p;
 }
 
@@ -626,6 +660,13 @@ cudaError_t rows_launch(const PagedAttn& a, int P, cudaStream_t st) {
   const cudaError_t e = cudaLaunchKernelEx(&cfg, k_paged_rows<T, HD, R, NW>, a);
   if (e != cudaSuccess || a.split) return e;
   return R == 1 ? merge_launch<T, HD, kMWarps>(a, P, st) : merge_launch<T, HD, 1>(a, P, st);
+}
+template <int TILES>
+cudaError_t wide_launch(const PagedAttn& a, int P, cudaStream_t st) {
+  using L = PWideL<TILES>;
+  k_paged_wide<TILES><<<P, L::kThreads, L::kSmem, st>>>(a);
+  const cudaError_t e = cudaGetLastError();
+  return e != cudaSuccess ? e : merge_launch<__nv_bfloat16, kWHd, 1>(a, P, st);
 }
 template <int HD>
 cudaError_t rows_launch(const PagedAttn& a, int dtype, int tiles, int P, cudaStream_t st) {
@@ -710,14 +751,17 @@ extern "C" ssd_status ssd_paged_attention(const ssd_paged_cache* c, int32_t laye
   a.part = reinterpret_cast<float*>(ws + lay.part);
   a.byG = Kv8Div::of((uint32_t)a.G);
   a.byRt = Kv8Div::of((uint32_t)plan.n_rt);
-  int P = sms * 2;  // blocks of an SM
+  int P = sms * (plan.wide ? 1 : 2);  // blocks of an SM
   if (P > plan.max_blocks) P = plan.max_blocks;
   a.part_rows = plan.part_rows;
   a.split = plan.split;
   if (plan.split) P = a.entries * a.Hkv * plan.split;
   a.byP = Kv8Div::of((uint32_t)P);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  e = c->head_dim == 128 ? rows_launch<128>(a, c->dtype, plan.tiles, P, st)
-                         : rows_launch<64>(a, c->dtype, plan.tiles, P, st);
+  if (plan.wide)
+    e = plan.wide == 2 ? wide_launch<2>(a, P, st) : wide_launch<1>(a, P, st);
+  else
+    e = c->head_dim == 128 ? rows_launch<128>(a, c->dtype, plan.tiles, P, st)
+                           : rows_launch<64>(a, c->dtype, plan.tiles, P, st);
   return e == cudaSuccess ? SSD_OK : fail_op_cuda("ssd_paged_attention", e);
 }

@@ -1,0 +1,457 @@
+// paged_wide.cuh -- attention over pages for many query rows a KV head (wide verifications, grouped
+// queries, prompt chunks; bf16, head_dim 128), on the 5th-generation tensor cores. Included by
+// paged_attention.cu.
+//
+// A tile (the plan's items) has one or two accumulators of 128 query rows each; a block, one an SM,
+// walks its keys 64 at a time. Its warps work side by side:
+//  - four copy keys and values as they are (cp.async) to a ring of steps in shared memory, rows of
+//    128 bytes with the 128-byte swizzle; keys are a K-major operand, values, whose columns lie one
+//    behind the other, an MN-major one;
+//  - one an accumulator issues S = Q K^T (tcgen05.mma, 128 x 64 x 128, fp32 in tensor memory, two
+//    buffers) for a step while the softmax of the step before is at work, another one O += P V,
+//    P read from tensor memory, as soon as a softmax is done;
+//  - four an accumulator do the softmax, a thread per row: the row's 64 scores into registers, their
+//    maximum, p = 2^(s - ref) as bf16, which takes the place of S. ref is the row's maximum as of the
+//    last time it grew by more than 8 (in powers of two), so O is rescaled in tensor memory only
+//    then.
+// A probability keeps bf16's 8 bits here (an error of the size of the output's own rounding at most: a
+// second part would take half as many products again, and these tiles are close to bound by them).
+#pragma once
+
+#include "attn_wide.cuh"
+
+namespace ssd {
+
+namespace {
+
+// A block's tile of TILES accumulators.
+template <int TILES>
+struct PWideL {
+  static constexpr int kRows = TILES * kWRows;
+  // warps: 4 TILES softmax, 4 copies, then the accumulators' scores and outputs
+  static constexpr int kSoft = 4 * TILES, kQk = kSoft + 4, kPv = kQk + TILES;
+  static constexpr int kThreads = (kPv + TILES) * 32;
+  static constexpr int kNst = 6 - TILES;  // steps of the ring
+  static constexpr uint32_t kStep = 2 * kWKTile;
+  static constexpr uint32_t kSmem = 2 * TILES * kWQHalf + kNst * kStep + 1024;  // queries, ring; alignment
+  static constexpr uint32_t kCols = 256 * TILES;  // tensor memory: S and P (2 x 64 each), O
+};
+constexpr float kPGrow = 8.f;
+
+// Instruction descriptors: bf16 operands, fp32 accumulator, M = 128; values are MN-major (bit 16).
+constexpr uint32_t kPIdesc = idesc_bf16_f32(128, kWKeys);
+constexpr uint32_t kPIdescV = idesc_bf16_f32(128, kWHd) | 1u << 16;
+
+// Barriers: a ring step's keys and values stored, and free again; of the two buffers of S: scores
+// there, probabilities there, output added; queries of the segment stored.
+template <int TILES>
+struct PWideBars {
+  uint64_t k_full[5], v_full[5], k_free[5], v_free[5];
+  uint64_t s_done[TILES][2], p_full[TILES][2], o_done[TILES][2], q_full[TILES];
+  uint64_t drained;  // after a wait that gave up: the products still in flight are done
+};
+
+// Step n's place in the ring and its phase there.
+template <int NST>
+struct Ring {
+  uint32_t at = 0, phase = 0;
+  __device__ __forceinline__ void next() {
+    if (++at == NST) at = 0, phase ^= 1;
+  }
+};
+
+// The phase that step n completes on its buffer's barrier; after a wait that gave up, no thread of
+// this role waits again: it runs through its steps, meets its barriers and reports.
+__device__ __forceinline__ void p_wait2(uint64_t (&b)[2], uint32_t n, bool& bad) {
+  if (!bad) bad = !w_sleep(&b[n & 1], (n >> 1) & 1);
+}
+__device__ __forceinline__ void p_wait(uint64_t* b, uint32_t phase, bool& bad) {
+  if (!bad) bad = !w_sleep(b, phase);
+}
+
+// Arrives when this thread's copies so far are there (one of the arrivals that the barrier counts). They
+// are writes of the generic proxy: who waits for them makes them visible to the tensor cores.
+__device__ __forceinline__ void p_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
+}  // namespace
+
+template <int TILES>
+__global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const PagedAttn a) {
+  using L = PWideL<TILES>;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ Kv8PlanSmem s_plan;
+  __shared__ PWideBars<TILES> bar;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_bad, s_fail, s_more[TILES];
+  __shared__ Kv8Cursor s_cur[TILES];  // of the softmax warps
+  __shared__ Kv8Seg s_seg[TILES];
+  unsigned char* const smem =
+      reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  unsigned char* const Qs = smem;
+  unsigned char* const Ks = Qs + 2 * TILES * kWQHalf;  // [kNst] keys, then values
+  const int tid = threadIdx.x, warp = tid >> 5;
+  const int pmask = (1 << a.c.shift) - 1;
+
+  if (tid == 0) {
+    for (int i = 0; i < L::kNst; ++i) {
+      mbar_init(&bar.k_full[i], 128);
+      mbar_init(&bar.v_full[i], 128);
+      mbar_init(&bar.k_free[i], TILES);
+      mbar_init(&bar.v_free[i], TILES);
+    }
+    for (int t = 0; t < TILES; ++t) {
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&bar.p_full[t][i], 128);
+        mbar_init(&bar.s_done[t][i], 1);
+        mbar_init(&bar.o_done[t][i], 1);
+      }
+      mbar_init(&bar.q_full[t], 128);
+    }
+    mbar_init(&bar.drained, 2 * TILES);
+    mbar_init_fence();
+    s_bad = s_fail = 0;
+    a.desc[blockIdx.x].nr = 0;
+  }
+  if (warp == L::kQk) tc_alloc(&s_tmem, L::kCols);
+  tc_fence_before();
+  Kv8Cursor cur = kv8_plan<L::kRows, kWKeys, L::kThreads>(a, s_plan);  // (with block barriers)
+  tc_fence_after();
+  pdl_launch_dependents();
+  // tensor memory: the accumulators' scores, two buffers each, then their outputs
+  const uint32_t tm = s_tmem;
+  constexpr uint32_t kS = 2 * kWKeys, kO = TILES * kS;
+  if (warp < L::kSoft && (tid & 127) == 0) s_cur[tid >> 7] = cur;
+  uint32_t n = 0;  // steps so far: the phases of the two buffers
+  Ring<L::kNst> ring;
+  bool bad = false;
+
+  if (warp >= L::kQk && warp < L::kPv) {
+    // ------------------------------------------------------------ scores
+    Kv8Seg sg;
+    const uint32_t one = w_elect();
+    const int t = warp - L::kQk;
+    const uint32_t tmS = tm + t * kS;
+    const uint64_t dq = sdesc_k128(smem_u32(Qs)) + (2 * t * kWQHalf >> 4);
+    const uint64_t dk = sdesc_k128(smem_u32(Ks));
+    for (uint32_t seg = 0; kv8_next<L::kRows, kWKeys>(a, cur, sg); ++seg) {
+      p_wait(&bar.q_full[t], seg & 1, bad);
+      for (int i = 0; i < sg.nu; ++i, ++n, ring.next()) {
+        p_wait(&bar.k_full[ring.at], ring.phase, bad);
+        if (n >= 2) p_wait2(bar.o_done[t], n - 2, bad);  // P of that step was read there
+        w_smem_fence();
+        __syncwarp();
+        tc_fence_after();
+        const uint32_t buf = n & 1;
+        if (t == 0 || sg.it.nr > t * kWRows)
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            w_mma(tmS + buf * kWKeys, dq + (((k >> 2) * kWQHalf + (k & 3) * 32) >> 4),
+                  dk + ((ring.at * L::kStep + (k >> 2) * kWKHalf + (k & 3) * 32) >> 4), kPIdesc, k > 0,
+                  one);
+        if (one) {
+          tc_commit(&bar.s_done[t][buf]);
+          tc_commit(&bar.k_free[ring.at]);
+        }
+      }
+    }
+  } else if (warp >= L::kPv) {
+    // ------------------------------------------------------------ outputs
+    Kv8Seg sg;
+    const uint32_t one = w_elect();
+    const int t = warp - L::kPv;
+    const uint32_t tmS = tm + t * kS, tmO = tm + kO + t * kWHd;
+    const uint64_t dv = w_desc_mn(smem_u32(Ks + kWKTile));
+    while (kv8_next<L::kRows, kWKeys>(a, cur, sg))
+      for (int i = 0; i < sg.nu; ++i, ++n, ring.next()) {
+        p_wait(&bar.v_full[ring.at], ring.phase, bad);
+        p_wait2(bar.p_full[t], n, bad);
+        w_smem_fence();
+        __syncwarp();
+        tc_fence_after();
+        const uint32_t buf = n & 1;
+        if (t == 0 || sg.it.nr > t * kWRows)
+#pragma unroll
+          for (int k = 0; k < kWKeys / 16; ++k)  // 16 keys: 8 words of P, two 8-row groups of V
+            w_mma_ts(tmO, tmS + buf * kWKeys + 8 * k, dv + ((ring.at * L::kStep + k * 2048) >> 4),
+                     kPIdescV, i > 0 || k > 0, one);
+        if (one) {
+          tc_commit(&bar.o_done[t][buf]);
+          tc_commit(&bar.v_free[ring.at]);
+        }
+      }
+  } else if (warp >= L::kSoft) {
+    // ------------------------------------------------------------ copies
+    const int ct = tid - L::kSoft * 32;
+    const int ch = ct & 15, r0 = ct >> 4;  // chunk of rows r0 + 8 j
+    const uint32_t to = (ch >> 3) * kWKHalf;
+    // values that are no numbers to zero, in a step that not every row sees whole (each thread in the
+    // chunks that it copied)
+    auto clean = [&]() {
+      unsigned char* const st = Ks + ring.at * L::kStep + kWKTile + to;
+      uint32_t any = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        uint4* p = reinterpret_cast<uint4*>(st + w_place(r0 + 8 * j, ch & 7));
+        uint4 u = *p;
+        u.x = numbers(u.x, any), u.y = numbers(u.y, any);
+        u.z = numbers(u.z, any), u.w = numbers(u.w, any);
+        *p = u;
+      }
+      // (published by the arrival that follows; it stays set for the block's later tiles)
+      if (any) s_bad = 1;
+    };
+    Kv8Seg sg;
+    while (kv8_next<L::kRows, kWKeys>(a, cur, sg)) {
+      const Kv8Item& it = sg.it;
+      const int k00 = (it.unit0 + sg.u0) * kWKeys;
+      const int full_lo = kv8_row_lo(it, it.hi, a.window), full_hi = kv8_row_pos(a, it, it.r0);
+      const char* const kp = a.k + (size_t)sg.g * a.c.slab + ch * 16;
+      const char* const vp = a.v + (size_t)sg.g * a.c.slab + ch * 16;
+      int look[4];  // pages of the step that is issued next
+      auto look_up = [&](int k0) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int key = k0 + 16 * j;
+          const bool in = key <= it.hi && key + 15 >= it.lo && it.lo <= it.hi;
+          look[j] = in ? a.c.entry(it.b, min(key, it.hi) >> a.c.shift) : 0;
+          if (look[j] < 0) {
+            look[j] = 0;
+            if (ct == 0 && a.err) atomicOr(a.err, (int)kErrTable);
+          }
+        }
+      };
+      look_up(k00);
+      for (int i = 0; i < sg.nu; ++i, ++n, ring.next()) {
+        const int k0 = k00 + i * kWKeys;
+        const uint32_t dst = smem_u32(Ks) + ring.at * L::kStep + to;
+        auto copy = [&](const char* base, uint32_t at) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int r = r0 + 8 * j, key = k0 + r;
+            const bool in = key >= it.lo && key <= it.hi;
+            const size_t off = (size_t)look[j >> 1] * a.c.bytes + (size_t)(key & pmask) * (kWHd * 2);
+            cp_async16(at + w_place(r, ch & 7), base + (in ? off : 0), in);
+          }
+        };
+        if (n >= (uint32_t)L::kNst) p_wait(&bar.k_free[ring.at], ring.phase ^ 1, bad);
+        copy(kp, dst);
+        p_arrive(&bar.k_full[ring.at]);
+        if (n >= (uint32_t)L::kNst) p_wait(&bar.v_free[ring.at], ring.phase ^ 1, bad);
+        copy(vp, dst + kWKTile);
+        if (k0 >= full_lo && k0 + kWKeys - 1 <= full_hi) {
+          p_arrive(&bar.v_full[ring.at]);
+        } else {
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          clean();
+          mbar_arrive(&bar.v_full[ring.at]);
+        }
+        if (i + 1 < sg.nu) look_up(k0 + kWKeys);
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else {
+    // ------------------------------------------------------------ softmax
+    const int t = TILES == 1 ? 0 : warp >> 2, ttid = tid & 127;  // the accumulator, its thread
+    const int row = tid;  // of the tile
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t tmS = tm + t * kS + lanes, tmO = tm + kO + t * kWHd + lanes;
+    for (;;) {
+      // the segment stands in shared memory: the steps need the registers
+      if (ttid == 0) s_more[t] = kv8_next<L::kRows, kWKeys>(a, s_cur[t], s_seg[t]);
+      named_sync(1 + t, 128);
+      if (!s_more[t]) break;
+      const Kv8Seg& sg = s_seg[t];
+      const Kv8Item& it = sg.it;
+      // queries, sixteen lanes a row (rows past the last: the last one's, not used); the products
+      // of the segment before are done with theirs
+      {
+        const int ch = tid % 16;
+        const __nv_bfloat16* const q0 = static_cast<const __nv_bfloat16*>(a.q) + ch * 8 +
+                                        (int64_t)it.b * a.M * a.q_stride + (int64_t)sg.g * a.G * kWHd;
+        unsigned char* const own = Qs + (2 * t + (ch >> 3)) * kWQHalf;
+        uint4 u[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int r = it.r0 + min(t * kWRows + j * 8 + ttid / 16, it.nr - 1), m = a.byG(r);
+          u[j] = __ldg(reinterpret_cast<const uint4*>(q0 + m * a.q_stride + (r - m * a.G) * kWHd));
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          *reinterpret_cast<uint4*>(own + w_place(j * 8 + ttid / 16, ch & 7)) = u[j];
+      }
+      w_smem_fence();
+      tc_fence_before();
+      mbar_arrive(&bar.q_full[t]);
+      const bool live = warp * 32 < it.nr;  // the warp has rows
+      const int k00 = (it.unit0 + sg.u0) * kWKeys;
+      const int full_lo = kv8_row_lo(it, it.hi, a.window);
+      const int full_hi = kv8_row_pos(a, it, it.r0);
+      const int phi = row < it.nr ? kv8_row_pos(a, it, it.r0 + row) : -1;
+      const int plo = row < it.nr ? kv8_row_lo(it, phi, a.window) : 0;
+      float ref = -INFINITY, ls = 0.f;  // of the row
+      for (int i = 0; i < sg.nu; ++i, ++n) {
+        p_wait2(bar.s_done[t], n, bad);
+        __syncwarp();
+        tc_fence_after();
+        if (live) {
+          const int k0 = k00 + i * kWKeys;
+          const bool full = k0 >= full_lo && k0 + kWKeys - 1 <= full_hi;
+          const uint32_t at = tmS + (n & 1) * kWKeys;
+          uint32_t r[64];
+          w_ld64(at, r);
+          if (!full) {
+            const int lo = plo - k0, hi = phi - k0;
+#pragma unroll
+            for (int x = 0; x < 64; ++x)
+              if (x < lo || x > hi) r[x] = 0xff800000u;  // -inf
+          }
+          float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int x = 0; x < 64; x += 8)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              m[y] = w_max3(m[y], __uint_as_float(r[x + 2 * y]), __uint_as_float(r[x + 2 * y + 1]));
+          const float mx = fmaxf(w_max3(m[0], m[1], m[2]), m[3]) * a.scale;
+          const bool grow = mx > ref + kPGrow || (ref == -INFINITY && mx > ref);
+          if (__any_sync(0xffffffffu, grow)) {
+            float f = 1.f;
+            if (grow) {
+              f = ref == -INFINITY ? 0.f : exp2f(ref - mx);
+              ref = mx;
+              ls *= f;
+            }
+            if (i > 0) {
+              p_wait2(bar.o_done[t], n - 1, bad);
+              __syncwarp();
+              tc_fence_after();
+#pragma unroll 1
+              for (int q = 0; q < 8; ++q) {
+                uint32_t o[16];
+                w_ld16(tmO + 16 * q, o);
+#pragma unroll
+                for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+                w_st16(tmO + 16 * q, o);
+              }
+            }
+          }
+          // (scores are rounded before ref is taken from them, as the maximum was: however large
+          // they are, none passes it by more than it may)
+          const float top = ref == -INFINITY ? 0.f : ref;
+          const uint64_t c2 = pack2(a.scale, a.scale), t2 = pack2(-top, -top);
+          uint64_t sum2 = 0;
+#pragma unroll
+          for (int x = 0; x < 64; x += 2) {
+            const float2 z = unpack2(
+                add2(mul2(pack2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), c2), t2));
+            const float e0 = ex2_approx(z.x), e1 = ex2_approx(z.y);
+            sum2 = add2(sum2, pack2(e0, e1));
+            const __nv_bfloat162 h = __floats2bfloat162_rn(e0, e1);
+            r[x / 2] = *reinterpret_cast<const uint32_t*>(&h);
+          }
+          const float2 sum = unpack2(sum2);
+          ls += sum.x + sum.y;
+          w_st32(at, r);
+          w_st_wait();
+        }
+        tc_fence_before();
+        mbar_arrive(&bar.p_full[t][n & 1]);
+      }
+      p_wait2(bar.o_done[t], n - 1, bad);
+      __syncwarp();
+      tc_fence_after();
+      // ---- the rows' outputs, or the block's part of them
+      if (live) {
+        const bool whole = sg.whole(), odd = *(volatile int*)&s_bad;
+        const int slot = 2 * blockIdx.x + (sg.u0 == 0);
+        const bool in = row < it.nr, sees = plo <= phi;
+        const float unit = ls == 0.f ? 0.f : 1.f / ls;
+        // 64 columns at a time through the warp's part of the queries' place, which is free now, so
+        // that a row is stored in one piece
+        unsigned char* const xs = Qs + warp * 8192;
+        const int lane = tid & 31, c4 = lane & 15;
+#pragma unroll 1
+        for (int q = 0; q < 4; ++q) {
+          uint32_t o[32];
+          w_ld32(tmO + 32 * q, o);
+          float f[32];
+          bool nan = false;
+#pragma unroll
+          for (int x = 0; x < 32; ++x) {
+            f[x] = ls == 0.f ? 0.f : __uint_as_float(o[x]) * unit;
+            nan |= f[x] != f[x];
+          }
+          if ((odd || nan) && in && ls == ls) {  // as in k_paged_rows
+            uint32_t seen = 0;  // columns with such a value: their sum takes the column's place
+            const int kb = max(k00, plo), ke = min(k00 + sg.nu * kWKeys - 1, phi);
+            for (int key = kb; key <= ke; ++key) {
+              const int e = max(a.c.entry(it.b, key >> a.c.shift), 0);
+              const char* v = a.v + (size_t)sg.g * a.c.slab + (size_t)e * a.c.bytes +
+                              (size_t)(key & pmask) * (kWHd * 2) + 64 * q;
+#pragma unroll 1
+              for (int x = 0; x < 32; ++x) {
+                const float y = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(v)[x]);
+                if (!no_number(y)) continue;
+#pragma unroll
+                for (int z = 0; z < 32; ++z)
+                  if (z == x) f[z] = seen >> x & 1 ? f[z] + y : y;
+                seen |= 1u << x;
+              }
+            }
+          }
+          if (whole && (!sees || ls == 0.f)) {
+#pragma unroll
+            for (int x = 0; x < 32; ++x) f[x] = sees ? __uint_as_float(0x7fffffffu) : 0.f;
+          }
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+            *reinterpret_cast<float4*>(xs + lane * 256 + ((((q & 1) * 8 + x) ^ (lane & 15)) << 4)) =
+                make_float4(f[4 * x], f[4 * x + 1], f[4 * x + 2], f[4 * x + 3]);
+          if (!(q & 1)) continue;
+          __syncwarp();
+          const int rows = min(32, it.nr - warp * 32);
+          for (int y = lane >> 4; y < rows; y += 2) {
+            const float4 v = *reinterpret_cast<const float4*>(xs + y * 256 + ((c4 ^ (y & 15)) << 4));
+            const int col = (q >> 1) * 64 + c4 * 4;
+            if (whole) {
+              const int r = it.r0 + warp * 32 + y, m = a.byG(r), h = sg.g * a.G + r - m * a.G;
+              const __nv_bfloat162 b0 = __floats2bfloat162_rn(v.x, v.y);
+              const __nv_bfloat162 b1 = __floats2bfloat162_rn(v.z, v.w);
+              *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) +
+                                        ((int64_t)it.b * a.M + m) * a.out_stride +
+                                        (int64_t)h * kWHd + col) =
+                  make_uint2(*reinterpret_cast<const uint32_t*>(&b0),
+                             *reinterpret_cast<const uint32_t*>(&b1));
+            } else {
+              *reinterpret_cast<float4*>(
+                  a.part + ((size_t)slot * a.part_rows + warp * 32 + y) * kWHd + col) = v;
+            }
+          }
+          __syncwarp();
+        }
+        if (in && !whole) a.ml[(size_t)slot * a.part_rows + row] = make_float2(ref, ls);
+      }
+      if (row == 0 && !sg.whole() && sg.u0 == 0) a.desc[blockIdx.x] = kv8_desc(a, s_cur[0], sg);
+      named_sync(1 + t, 128);  // the next segment's queries go where outputs were exchanged
+      tc_fence_before();  // the next segment's products overwrite O, behind its p_full
+    }
+  }
+  if (bad) s_fail = 1;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (__builtin_expect(s_fail, 0)) {  // products may still be at work in this block's memory
+    if (tid == 0 && a.err) atomicOr(a.err, (int)kErrTimeout);
+    if (warp >= L::kQk) {  // the warps that issue them, 2 TILES
+      if (w_elect()) tc_commit(&bar.drained);
+      w_sleep(&bar.drained, 0);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+  }
+  if (warp == L::kQk) tc_dealloc(tm, L::kCols);
+}
+
+}  // namespace ssd

@@ -265,15 +265,16 @@ def test_append_reads_rows_in_place():
 
 # ------------------------------------------------------------------ attention
 
-def _filled(dtype, layers, heads, hd, page, n, width, seed, extra=3):
-    """A cache whose sequences hold every position, in scattered pages of random contents."""
+def _filled(dtype, layers, heads, hd, page, n, width, seed, extra=3, room=0):
+    """A cache whose sequences hold the first `width` pages' positions, in scattered pages of random
+    contents, of `room` pages more that their tables have room for."""
     torch = _torch()
     pool = n * width + extra
-    c = _cache(dtype, layers, heads, hd, pool, page, n, width)
+    c = _cache(dtype, layers, heads, hd, pool, page, n, width + room)
     g = torch.Generator(device="cuda").manual_seed(seed)
     c.pages.normal_(generator=g)
     ids = torch.randperm(pool, generator=g, device="cuda")[:n * width].int()
-    c.table.copy_(ids.view(n, width))
+    c.table[:, :width] = ids.view(n, width)
     c.refs[ids.long()] = 1
     return c, g
 
@@ -319,16 +320,25 @@ ATTEND = [  # dtype, layers, heads, kv heads, hd, page, sequences of (pos, rows)
     ("bf16", 1, 8, 2, 128, 16, [(0, 300)], 300, None, 0, 0),
     ("f32", 1, 6, 2, 64, 16, [(3, 130)], 130, None, 50, 0),
     ("bf16", 1, 4, 4, 128, 16, [(5, 1)] * 61, 1, None, 0, 0),
+    ("bf16", 1, 16, 1, 128, 64, [(150, 8), (64, 1), (0, 8)], 8, [0, 60, 0], 0, 0),
+    ("bf16", 1, 64, 2, 128, 32, [(500, 6), (190, 5)], 6, [0, 300], 90, 0),
+    ("bf16", 1, 12, 1, 128, 256, [(63, 65), (1, 64)], 65, None, 0, 0),
+    ("bf16", 1, 16, 8, 128, 16, [(1, 140)], 140, None, 64, 0),
 ]
 
+# positions that the table has room for behind what a case needs: 0 deals short sequences out by clusters,
+# more than 2048 by the line of units and, for many rows, to the tcgen05 tiles
+ROOM = [0, 2100]
 
+
+@pytest.mark.parametrize("room", ROOM)
 @pytest.mark.parametrize("dtype,layers,heads,kvh,hd,page,seqs,M,first,window,longest", ATTEND)
-def test_attention(dtype, layers, heads, kvh, hd, page, seqs, M, first, window, longest):
+def test_attention(dtype, layers, heads, kvh, hd, page, seqs, M, first, window, longest, room):
     torch = _torch()
     n = len(seqs)
     pos, rows = [p for p, _ in seqs], [m for _, m in seqs]
     width = max(p + M for p in pos) // page + 2
-    c, g = _filled(dtype, layers, kvh, hd, page, n, width, seed=heads + page)
+    c, g = _filled(dtype, layers, kvh, hd, page, n, width, seed=heads + page, room=room // page)
     q = (1.5 * torch.randn(n, M, heads, hd, generator=g, device="cuda")).to(_dtype(dtype))
     a = _check_attention(c, layers - 1, q, pos, rows, first, window, longest)
     assert torch.equal(a, _check_attention(c, layers - 1, q, pos, rows, first, window, longest))
@@ -355,14 +365,16 @@ def _check_attention_inplace(c, layer, q, want, pos, rows, first, window, longes
 
 @pytest.mark.parametrize("dtype,hd,heads,kvh,M", [("bf16", 128, 8, 2, 1), ("bf16", 64, 8, 2, 6),
                                                  ("bf16", 128, 16, 1, 5), ("f32", 64, 4, 4, 5),
-                                                 ("f32", 128, 4, 1, 2), ("bf16", 128, 64, 4, 9)])
+                                                 ("f32", 128, 4, 1, 2), ("bf16", 128, 64, 4, 9),
+                                                 ("bf16", 128, 64, 8, 40)])
+@pytest.mark.parametrize("room", ROOM)
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_what_is_out_of_sight_does_not_matter(dtype, hd, heads, kvh, M, bad):
+def test_what_is_out_of_sight_does_not_matter(dtype, hd, heads, kvh, M, room, bad):
     """NaN and infinities in positions that no row sees, and in those that some rows see: in front of `first`,
     behind the window, behind the last row, in a row's future, in pages of others."""
     torch = _torch()
     n, page, width = 3, 16, 16
-    c, g = _filled(dtype, 1, kvh, hd, page, n, width, seed=M)
+    c, g = _filled(dtype, 1, kvh, hd, page, n, width, seed=M, room=room // page)
     pos, rows, first, window = [100, 7, 180], [M, M, M - 1 if M > 1 else 1], [30, 0, 200], 60
     pages = c.pages.view(-1, 1, 2, kvh, page, hd)
     table = c.table.tolist()
@@ -390,6 +402,38 @@ def test_what_is_out_of_sight_does_not_matter(dtype, hd, heads, kvh, M, bad):
         keep = torch.ones(hd, dtype=torch.bool, device="cuda")
         keep[3] = False
         assert same[0, rows[0] - 1, :G][:, keep].all()
+    # a value in the middle that every row sees, in a step that is seen whole
+    at = 64
+    pages[table[0][at // page], 0, 1, kvh - 1, at % page, 5] = bad
+    z = c.attention(0, q, _ints(pos), rows=_ints(rows), first=_ints(first), window=window)
+    sees = [p + m - window < at <= p + m and at >= f for p, f in zip(pos, first) for m in range(1)]
+    col = z[0, :rows[0], heads - heads // kvh:, 5].float()
+    live = torch.tensor([pos[0] + m - window < at for m in range(rows[0])], device="cuda")
+    assert sees[0] and (torch.isnan(col) if bad != bad else col == bad)[live].all()
+    assert torch.isfinite(col[~live]).all() and torch.isfinite(z[1:].float()).all()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dtype,heads,kvh,M,cap", [("bf16", 8, 2, 1, 640), ("bf16", 8, 2, 1, 4096),
+                                                  ("bf16", 64, 4, 10, 4096), ("f32", 4, 2, 3, 4096),
+                                                  ("bf16", 8, 1, 4, 4096)])
+def test_a_value_that_all_rows_see_reaches_them(dtype, heads, kvh, M, cap, bad):
+    """NaN and infinity far from any mask's edge, with weights of many sizes, through every form."""
+    torch = _torch()
+    c, g = _filled(dtype, 1, kvh, 128, 64, 1, 9, seed=12, room=cap // 64 - 9)
+    q = torch.randn(1, M, heads, 128, generator=g, device="cuda").to(_dtype(dtype))
+    want = c.attention(0, q, _ints([500]))
+    for at in (0, 70, 200, 499):
+        e = int(c.table[0, at // 64])
+        was = c.pages[e, 0, 1, 0, at % 64, 9].clone()
+        c.pages[e, 0, 1, 0, at % 64, 9] = bad
+        z = c.attention(0, q, _ints([500])).float()
+        hit = z[0, :, :heads // kvh, 9]
+        assert (torch.isnan(hit) if bad != bad else hit == bad).all(), at
+        z[0, :, :heads // kvh, 9] = want[0, :, :heads // kvh, 9].float()
+        assert torch.equal(z, want.float())
+        c.pages[e, 0, 1, 0, at % 64, 9] = was
+    c.check()
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
