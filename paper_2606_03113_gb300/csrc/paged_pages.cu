@@ -20,6 +20,7 @@ constexpr int kPlanThreads = 1024;
 constexpr int kPlanWarps = kPlanThreads / 32;
 constexpr int kScan = 16;                        // counts of a thread in a pass over refs
 constexpr int kScanStep = kPlanThreads * kScan;  // counts of a pass
+constexpr int kHeld = 2 * kPlanThreads;  // entries of a reserve that stay in registers
 constexpr int kClaim = 1 << 16;  // refs while a reserve looks: entries below, claims above
 constexpr int kCopyThreads = 256;
 constexpr int kForkCols = 8;     // entries of a sequence that a fork's block looks at: a sector
@@ -99,10 +100,11 @@ __device__ __forceinline__ void load_refs(const PagedView& c, int id0, int (&r)[
 //    who else has claimed does not matter for who is sharing);
 //  2 where all names claim, the largest sequence is found, which keeps the page;
 //  3 the entries that need a page are counted and as many free pages found, lowest first;
-//  4 (too few: the claims are taken back) entries get theirs by rank, the list of copies is written;
-//  5 the counts follow.
-// One block. Bound by about five dependent round trips where nothing is needed, by the pass over
-// refs for pools of 10^5 pages.
+//  4 (too few: the claims are taken back) entries get theirs by rank, the list of copies is written,
+//    the counts follow.
+// One block, bound by round trips to L2: four where no page is shared (positions, entries, counts, a
+// pass over 16384 counts, which is on its way from the start), two more for shared ones. Up to kHeld wanted
+// entries, as a decode step has them, stay in registers from step to step; more are looked at again in each.
 __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView c, const PlanWork w,
                                                                 const int32_t* pos,
                                                                 const int32_t* rows, int M,
@@ -110,6 +112,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
   __shared__ PlanSmem sm;
   __shared__ int s_pre[SSD_KV8_MAX_SEQS + 1];  // wanted entries of the sequences before
   __shared__ int s_pos[SSD_KV8_MAX_SEQS];
+  __shared__ int s_fresh[kHeld];
   __shared__ int s_copies;
   pdl_launch_dependents();
   const int tid = threadIdx.x;
@@ -130,6 +133,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
     }
     sum += cnt[j];
   }
+  int ahead[kScan];  // the first counts: which are 0 no step changes before pages are given out
+  load_refs(c, tid * kScan, ahead);
   if (tid == 0) s_copies = 0;
   int E;
   int at = before_me(sum, sm, E);
@@ -156,6 +161,98 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
     const int e = __ldcg(c.table + (size_t)b * c.max_pages + i);
     return (unsigned)e < (unsigned)c.n_pages ? e : -1;
   };
+  auto all_claim = [&](int v) { return (v >> 16) == (v & (kClaim - 1)); };
+  // as many free pages as are needed, lowest first; how many were found
+  auto find_free = [&](int need, int32_t* fresh) {
+    int found = 0;
+    for (int id0 = 0; id0 < c.n_pages && found < need; id0 += kScanStep) {
+      int r[kScan], n = 0, total;
+      if (id0) load_refs(c, id0 + tid * kScan, r);
+      else
+#pragma unroll
+        for (int j = 0; j < kScan; ++j) r[j] = ahead[j];
+#pragma unroll
+      for (int j = 0; j < kScan; ++j) n += r[j] == 0;
+      int rank = found + before_me(n, sm, total);
+#pragma unroll
+      for (int j = 0; j < kScan; ++j)
+        if (r[j] == 0) {
+          if (rank < need) fresh[rank] = id0 + tid * kScan + j;
+          ++rank;
+        }
+      found += total;
+    }
+    __syncthreads();
+    return found;
+  };
+  // entry i of sequence b gets page `to`; the page that it leaves is `from` (-1: none)
+  auto give = [&](int b, int i, int from, int to) {
+    c.table[(size_t)b * c.max_pages + i] = to;
+    const int kept = s_pos[b] - (i << c.shift);  // positive in a sequence's first entry alone
+    if (from >= 0 && kept > 0) w.list[atomicAdd(&s_copies, 1)] = Copy{from, to, kept, 0};
+  };
+
+  if (E <= kHeld) {
+    constexpr int K = kHeld / kPlanThreads;
+    int eb[K], ei[K], ee[K];
+    bool shared[K], all[K];
+    int claims = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      eb[k] = ei[k] = 0, ee[k] = -1;
+      if (tid * K + k < E) {
+        find(tid * K + k, eb[k], ei[k]);
+        ee[k] = entry(eb[k], ei[k]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      shared[k] = ee[k] >= 0 && (__ldcg(c.refs + ee[k]) & (kClaim - 1)) > 1;
+      all[k] = false;
+      if (shared[k]) {
+        atomicAdd(c.refs + ee[k], kClaim);
+        w.a[ee[k]] = 0;
+        claims = 1;
+      }
+    }
+    if (__syncthreads_or(claims)) {
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (shared[k]) {
+          all[k] = all_claim(__ldcg(c.refs + ee[k]));
+          if (all[k]) atomicMax(w.a + ee[k], eb[k] + 1);
+        }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < K; ++k)  // whether the entry keeps a page that all claim
+        all[k] = all[k] && __ldcg(w.a + ee[k]) == eb[k] + 1;
+    }
+    int mine = 0, need;
+    bool needs[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      needs[k] = tid * K + k < E && (ee[k] < 0 || (shared[k] && !all[k]));
+      mine += needs[k];
+    }
+    int rank = before_me(mine, sm, need);
+    const bool enough = need == 0 || find_free(need, s_fresh) >= need;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (enough && needs[k]) {
+        const int to = s_fresh[rank++];
+        give(eb[k], ei[k], shared[k] ? ee[k] : -1, to);
+        c.refs[to] = 1;
+      }
+      if (shared[k]) atomicSub(c.refs + ee[k], kClaim + (enough && needs[k]));
+    }
+    __syncthreads();
+    if (tid == 0) {
+      w.head->copies = s_copies;
+      if (!enough && err) atomicOr(err, (int)kErrPages);
+    }
+    return;
+  }
+
   int claims = 0;
   for (int x = tid; x < E; x += kPlanThreads) {
     int b, i;
@@ -168,7 +265,6 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
     }
   }
   const bool any = __syncthreads_or(claims);
-  auto all_claim = [&](int v) { return (v >> 16) == (v & (kClaim - 1)); };
   if (any) {
     for (int x = tid; x < E; x += kPlanThreads) {
       int b, i;
@@ -201,23 +297,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
     }
     need += __syncthreads_count(mine);
   }
-  int found = 0;
-  for (int id0 = 0; id0 < c.n_pages && found < need; id0 += kScanStep) {
-    int r[kScan], n = 0, total;
-    load_refs(c, id0 + tid * kScan, r);
-#pragma unroll
-    for (int j = 0; j < kScan; ++j) n += r[j] == 0;
-    int rank = found + before_me(n, sm, total);
-#pragma unroll
-    for (int j = 0; j < kScan; ++j)
-      if (r[j] == 0) {
-        if (rank < need) w.fresh[rank] = id0 + tid * kScan + j;
-        ++rank;
-      }
-    found += total;
-  }
-  __syncthreads();
-  if (found < need) {
+  if (find_free(need, w.fresh) < need) {
     for (int x = tid; x < E; x += kPlanThreads) {
       int b, i;
       find(x, b, i);
@@ -242,11 +322,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
     const int rank = base + before_me(mine, sm, total);
     base += total;
     if (mine) {
-      const int to = __ldcg(w.fresh + rank), p = s_pos[b];
-      c.table[(size_t)b * c.max_pages + i] = to;
+      give(b, i, from, __ldcg(w.fresh + rank));
       w.old[rank] = from;
-      const int kept = p - (i << c.shift);  // positive in a sequence's first entry alone
-      if (from >= 0 && kept > 0) w.list[atomicAdd(&s_copies, 1)] = Copy{from, to, kept, 0};
     }
   }
   __syncthreads();
@@ -267,18 +344,30 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
   if (tid == 0) w.head->copies = s_copies;
 }
 
-// Carries out a list of copies: a warp a slab, so that all SMs have many lines on their way.
+// Carries out a list of copies: a warp a slab, so that all SMs have many lines on their way; the next
+// slab's entry of the list is looked up beside the copy.
 __device__ __forceinline__ void copy_pages(const PagedView& c, const PlanWork& w, int copies) {
   const int lane = threadIdx.x & 31;
   const int64_t units = (int64_t)copies * c.slabs;
   const int64_t step = (int64_t)gridDim.x * (kCopyThreads / 32);
   const int row_shift = 31 - __clz(c.slab) - c.shift - 4;  // 16-byte chunks of a row
-  for (int64_t u = (int64_t)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); u < units;
-       u += step) {
-    const int k = (int)(u / c.slabs), s = (int)(u - (int64_t)k * c.slabs);
-    const int4 d = __ldcg(reinterpret_cast<const int4*>(w.list + k));
+  int64_t u = (int64_t)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5);
+  int s = 0;
+  int4 next = make_int4(0, 0, 0, 0);
+  auto look = [&]() {
+    if (u < units) {
+      const int k = units <= 0x7fffffff ? (int)((uint32_t)u / (uint32_t)c.slabs) : (int)(u / c.slabs);
+      s = (int)(u - (int64_t)k * c.slabs);
+      next = __ldcg(reinterpret_cast<const int4*>(w.list + k));
+    }
+  };
+  look();
+  while (u < units) {
+    const int4 d = next;
     const uint4* src = reinterpret_cast<const uint4*>(c.pages + d.x * c.bytes + (size_t)s * c.slab);
     uint4* dst = reinterpret_cast<uint4*>(c.pages + d.y * c.bytes + (size_t)s * c.slab);
+    u += step;
+    look();
     const int n = d.z << row_shift;
     for (int x0 = lane; x0 < n; x0 += 8 * 32) {
       uint4 v[8];
@@ -304,9 +393,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_compact(const PagedView 
   __shared__ PlanSmem sm;
   pdl_launch_dependents();
   const int tid = threadIdx.x;
-  int n = 0, low;
+  int n = 0, low, r[kScan];
   for (int id0 = 0; id0 < c.n_pages; id0 += kScanStep) {
-    int r[kScan];
     load_refs(c, id0 + tid * kScan, r);
 #pragma unroll
     for (int j = 0; j < kScan; ++j) n += r[j] != 0 && id0 + tid * kScan + j < c.n_pages;
@@ -314,9 +402,9 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_compact(const PagedView 
   before_me(n, sm, low);
   int holes = 0, moved = 0;
   for (int id0 = 0; id0 < c.n_pages; id0 += kScanStep) {
-    int r[kScan], mine = 0, total;
+    int mine = 0, total;
     const int first = id0 + tid * kScan;
-    load_refs(c, first, r);
+    if (c.n_pages > kScanStep) load_refs(c, first, r);  // (one pass: they are here)
 #pragma unroll
     for (int j = 0; j < kScan; ++j) {
       const bool in = first + j < c.n_pages, below = first + j < low;
@@ -402,6 +490,7 @@ __global__ void __launch_bounds__(kCopyThreads) k_paged_fork(const PagedView c,
 namespace {
 
 constexpr int kRowThreads = 128;
+constexpr int kRowBatch = 5;  // 16-byte chunks of K and of V that a thread has on their way
 
 struct PagedAppend {
   PagedView c;
@@ -417,35 +506,52 @@ struct PagedAppend {
 
 }  // namespace
 
-// A block a row. Bound by bytes for prompts, for a few rows by the launch and three round trips:
-// position, table entry, the page's count (a row is not written to a page that others name).
+// A block a row: its K and V are on their way while the table entry and the page's count are looked up,
+// one after the other (a row is not written to a page that others name).
 __global__ void __launch_bounds__(kRowThreads) k_paged_append(const PagedAppend a) {
   const int m = blockIdx.x, b = blockIdx.y;
-  const char* xk = a.k + ((int64_t)b * a.M + m) * a.stride;
-  const char* xv = a.v + ((int64_t)b * a.M + m) * a.stride;
+  const uint4* xk = reinterpret_cast<const uint4*>(a.k + ((int64_t)b * a.M + m) * a.stride);
+  const uint4* xv = reinterpret_cast<const uint4*>(a.v + ((int64_t)b * a.M + m) * a.stride);
   const int p0 = __ldg(a.pos + b), n = a.rows ? __ldg(a.rows + b) : a.M;
+  uint4 uk[kRowBatch], uv[kRowBatch];
+  auto load = [&](int x0) {
+#pragma unroll
+    for (int j = 0; j < kRowBatch; ++j) {
+      const int x = x0 + j * kRowThreads;
+      if (x < a.chunks) {
+        uk[j] = __ldcs(xk + x);
+        uv[j] = __ldcs(xv + x);
+      }
+    }
+  };
   if (p0 < 0 || n < 0 || n > a.M || p0 > a.c.cap() - n) {
     if (threadIdx.x == 0 && m == 0 && a.err)
       atomicOr(a.err, n < 0 || n > a.M ? (int)kErrControl : (int)kErrCapacity);
     return;
   }
   if (m >= n) return;
+  load(threadIdx.x);
   const int p = p0 + m, e = a.c.entry(b, p >> a.c.shift);
   if (e < 0 || __ldg(a.c.refs + e) > 1) {
     if (threadIdx.x == 0 && a.err) atomicOr(a.err, (int)kErrTable);
     return;
   }
   const int slot = p & ((1 << a.c.shift) - 1);
-  char* page = a.c.pages + e * a.c.bytes;
-#pragma unroll 4
-  for (int x = threadIdx.x; x < a.chunks; x += kRowThreads) {
-    const uint4 uk = __ldg(reinterpret_cast<const uint4*>(xk) + x);
-    const uint4 uv = __ldg(reinterpret_cast<const uint4*>(xv) + x);
-    const int h = x >> a.head_shift;
-    const size_t off = (size_t)h * a.c.slab +
-                       ((size_t)((slot << a.head_shift) + (x - (h << a.head_shift))) << 4);
-    *reinterpret_cast<uint4*>(page + a.to_k + off) = uk;
-    *reinterpret_cast<uint4*>(page + a.to_v + off) = uv;
+  char* const page = a.c.pages + e * a.c.bytes;
+  for (int x0 = threadIdx.x;;) {
+#pragma unroll
+    for (int j = 0; j < kRowBatch; ++j) {
+      const int x = x0 + j * kRowThreads, h = x >> a.head_shift;
+      if (x < a.chunks) {
+        const size_t off = (size_t)h * a.c.slab +
+                           ((size_t)((slot << a.head_shift) + (x - (h << a.head_shift))) << 4);
+        *reinterpret_cast<uint4*>(page + a.to_k + off) = uk[j];
+        *reinterpret_cast<uint4*>(page + a.to_v + off) = uv[j];
+      }
+    }
+    x0 += kRowBatch * kRowThreads;
+    if (x0 >= a.chunks) break;
+    load(x0);
   }
 }
 
