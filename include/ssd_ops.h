@@ -235,7 +235,7 @@ ssd_status ssd_token_logprobs(const void* logits, int32_t dtype, int32_t n_rows,
                                 * written, one that other entries name too */
 
 /* The cache (all memory the caller's, device).
- * pages: [n_pages][n_layers][2 (K, V)][n_kv_heads][page][head_dim] of dtype (SSD_DTYPE_F32 or
+ * pages: [n_pages][n_layers][n_kv_heads][2 (K, V)][page][head_dim] of dtype (SSD_DTYPE_F32 or
  * _BF16), 16-byte aligned: `page` positions of a sequence, a power of two from 16 to 256
  * (SSD_ERR_UNSUPPORTED otherwise, as head_dim other than 64 and 128).
  * table: int32 [n_seq][max_pages], the pages of positions 0 .. page - 1, page .. 2 page - 1, ..

@@ -170,5 +170,25 @@ __device__ __forceinline__ bool w_sleep(uint64_t* b, uint32_t parity) {
   }
   return false;
 }
+// Step n's place in the ring and its phase there.
+template <int NST>
+struct Ring {
+  uint32_t at = 0, phase = 0;
+  __device__ __forceinline__ void next() {
+    if (++at == NST) at = 0, phase ^= 1;
+  }
+};
+
+// Waits for a phase of a barrier; after a wait that gave up, no thread of this role waits again.
+__device__ __forceinline__ void p_wait(uint64_t* b, uint32_t phase, bool& bad) {
+  if (!bad) bad = !w_sleep(b, phase);
+}
+
+// Arrives when this thread's copies so far are there (one of the arrivals that the barrier counts). They
+// are writes of the generic proxy: who waits for them makes them visible to the tensor cores.
+__device__ __forceinline__ void p_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
 }  // namespace
 }  // namespace ssd

@@ -1,8 +1,9 @@
 // paged.cuh -- the paged KV cache of the kernel-level entry points: where things stand in it.
 //
-// pages [n_pages][n_layers][2][n_kv_heads][page][head_dim]: a page is one piece of memory, so that
-// copying or moving one is a single long copy, and the rows of a layer, side and head
-// in a page (a slab) are another, so that an attention reads whole lines.
+// pages [n_pages][n_layers][n_kv_heads][2][page][head_dim]: a page is one piece of memory, so that
+// copying or moving one is a single long copy. What an attention reads of a page, a head's keys (a slab)
+// and its values, lies in one piece, too: memory far apart costs it, 1 row of 32 heads over 8 KV heads x 524288
+// keys in scattered pages of 16, 64 and 256 reads 5.6, 6.4 and 6.7 TB/s with all keys in front of all values.
 #pragma once
 
 #include "kv8.cuh"
@@ -22,10 +23,11 @@ struct PagedView {
     const int e = __ldg(table + (size_t)b * max_pages + i);
     return (unsigned)e < (unsigned)n_pages ? e : -1;
   }
-  // Layer `layer`, side 0 (K) or 1 (V) of page 0, head 0.
+  // Layer `layer`, side 0 (K) or 1 (V) of page 0, head 0; bytes to the next head.
   __host__ __device__ __forceinline__ size_t side(int layer, int side) const {
-    return (size_t)(layer * 2 + side) * n_kv_heads * slab;
+    return ((size_t)layer * n_kv_heads * 2 + side) * slab;
   }
+  __host__ __device__ __forceinline__ size_t head() const { return (size_t)2 * slab; }
 };
 
 // Checks of a cache that every entry point makes; null: fine.

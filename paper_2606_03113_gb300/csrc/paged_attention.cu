@@ -79,6 +79,195 @@ __device__ __forceinline__ float4 lds4(const unsigned char* p) {
   return *reinterpret_cast<const float4*>(p);
 }
 
+// What a warp holds of its 16 query rows: lane n8, t has rows n8 and n8 + 8.
+template <int HD>
+struct RowTile {
+  float o[HD / 8][4], mx[2], ls[2];  // outputs, running maxima (in powers of two) and sums
+  int plo[2], phi[2];                // the rows see keys plo .. phi
+  __device__ __forceinline__ void start(const AttnArgs& a, const Kv8Item& it, int row0) {
+    const int n8 = (threadIdx.x & 31) >> 2;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = row0 + n8 + 8 * i;
+      phi[i] = row < it.nr ? kv8_row_pos(a, it, it.r0 + row) : -1;  // no row here: sees none
+      plo[i] = row < it.nr ? kv8_row_lo(it, phi[i], a.window) : 0;
+      mx[i] = -INFINITY;
+      ls[i] = 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < HD / 8; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[j][i] = 0.f;
+  }
+  // Scores sc of 8 N keys from k0 on (lane: keys 8 n + 2 t and 8 n + 2 t + 1) become
+  // probabilities; maxima, sums and outputs follow.
+  template <int N>
+  __device__ __forceinline__ void weigh(float (&sc)[2][4], int k0, bool full, float scale) {
+    const int t = threadIdx.x & 3;
+    float nm[2] = {-INFINITY, -INFINITY}, f[2], top[2];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        sc[n][x] *= scale;
+        if (!full) {
+          const int key = k0 + 8 * n + 2 * t + (x & 1);
+          if (key < plo[x >> 1] || key > phi[x >> 1]) sc[n][x] = -INFINITY;
+        }
+        nm[x >> 1] = fmaxf(nm[x >> 1], sc[n][x]);
+      }
+    bool moved = false;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      nm[i] = fmaxf(nm[i], __shfl_xor_sync(0xffffffffu, nm[i], 1));
+      nm[i] = fmaxf(nm[i], __shfl_xor_sync(0xffffffffu, nm[i], 2));
+      nm[i] = fmaxf(nm[i], mx[i]);
+      top[i] = nm[i] == -INFINITY ? 0.f : nm[i];
+      f[i] = nm[i] == mx[i] ? 1.f : exp2f(mx[i] - nm[i]);
+      moved |= nm[i] != mx[i];
+      mx[i] = nm[i];
+      ls[i] *= f[i];
+    }
+    if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+      for (int j = 0; j < HD / 8; ++j)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[j][x] *= f[x >> 1];
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        sc[n][x] = exp2f(sc[n][x] - top[x >> 1]);
+        ls[x >> 1] += sc[n][x];
+      }
+  }
+};
+
+// 16 keys from row kk0 of a stage on, bf16: keys at sk, values at sv (shared memory), places by L.
+// Nonzero where a value that is no number was zeroed.
+template <typename L, int HD>
+__device__ __forceinline__ uint32_t bf16_step(RowTile<HD>& w, const uint32_t (&qf)[HD / 16][4],
+                                              uint32_t sk, uint32_t sv, int kk0, int k0, bool full,
+                                              float scale) {
+  const int lane = threadIdx.x & 31;
+  float s2[2][2][4];  // even and odd 16-column steps summed apart
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) s2[i][n][x] = 0.f;
+#pragma unroll
+  for (int k = 0; k < HD / 16; ++k) {
+    uint32_t b[4];
+    ldsm4(sk + L::place(kk0 + (lane & 7) + ((lane >> 4) << 3), 2 * k + (lane >> 3 & 1)), b);
+    mma16816(s2[k & 1][0], qf[k], b[0], b[1]);
+    mma16816(s2[k & 1][1], qf[k], b[2], b[3]);
+  }
+  float p[2][4];
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) p[n][x] = s2[0][n][x] + s2[1][n][x];
+  w.template weigh<2>(p, k0, full, scale);
+  uint32_t any = 0, hi[4], lo[4];
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) split2(p[n][2 * i], p[n][2 * i + 1], hi[2 * n + i], lo[2 * n + i]);
+#pragma unroll
+  for (int j = 0; j < HD / 8; j += 2) {
+    uint32_t b[4];
+    ldsm4t(sv + L::place(kk0 + (lane & 15), j + (lane >> 4)), b);
+    if (!full) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) b[x] = numbers(b[x], any);
+    }
+    mma16816(w.o[j], lo, b[0], b[1]);
+    mma16816(w.o[j + 1], lo, b[2], b[3]);
+    mma16816(w.o[j], hi, b[0], b[1]);
+    mma16816(w.o[j + 1], hi, b[2], b[3]);
+  }
+  return any;
+}
+
+// The rows of a block's part of an item, from what GROUPS groups of warps left: outputs in Ox
+// [GROUPS][ROWS][HD + 4], weights s_w (NULL: 1), the rows' maxima and sums. Of keys kb .. ke - 1. To `part` in shared
+// memory for a cluster's join, to the output, or to the workspace.
+template <typename T, int HD, int GROUPS, int ROWS, int THREADS>
+__device__ __forceinline__ void finish_rows(const PagedAttn& a, const Kv8Seg& sg, int kb, int ke,
+                                            const float* Ox, const float (*s_w)[ROWS],
+                                            const float* s_gm, const float* s_sum, bool bad,
+                                            float* part, int tid) {
+  constexpr int NT = HD / 8, kOPad = HD + 4;
+  const Kv8Item& it = sg.it;
+  const bool whole = sg.whole();
+  const int slot = 2 * blockIdx.x + (sg.u0 == 0), g = sg.g, pmask = (1 << a.c.shift) - 1;
+  const char* const vp = a.v + g * a.c.head();
+#pragma unroll 1
+  for (int x0 = 0; x0 < ROWS * NT; x0 += THREADS) {
+    const int row = (x0 + tid) / NT, c8 = (tid % NT) * 8;
+    if (row >= it.nr) continue;
+    const int r = it.r0 + row, m = a.byG(r), h = g * a.G + r - m * a.G;
+    const int p = kv8_row_pos(a, it, r), lo = kv8_row_lo(it, p, a.window);
+    const float gm = s_gm[row], Ls = s_sum[row];
+    float acc[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+    bool nan = false;
+#pragma unroll
+    for (int x = 0; x < GROUPS; ++x) {
+      const float wt = s_w ? s_w[x][row] : 1.f;
+      const float4* ox = reinterpret_cast<const float4*>(Ox + (size_t)(x * ROWS + row) * kOPad + c8);
+      const float4 u = ox[0], w = ox[1];
+      acc[0] = fmaf(u.x, wt, acc[0]);
+      acc[1] = fmaf(u.y, wt, acc[1]);
+      acc[2] = fmaf(u.z, wt, acc[2]);
+      acc[3] = fmaf(u.w, wt, acc[3]);
+      acc[4] = fmaf(w.x, wt, acc[4]);
+      acc[5] = fmaf(w.y, wt, acc[5]);
+      acc[6] = fmaf(w.z, wt, acc[6]);
+      acc[7] = fmaf(w.w, wt, acc[7]);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) nan |= acc[j] != acc[j];
+    // values that are no numbers belong to the rows that see them (a part of a probability times
+    // infinity may have made NaN of one); where the scores are NaN, so is everything
+    if ((bad || nan) && Ls == Ls) {
+      float sum[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+      for (int key = max(kb, lo); key < min(ke, p + 1); ++key) {
+        const int e = max(a.c.entry(it.b, key >> a.c.shift), 0);
+        const T* v = reinterpret_cast<const T*>(vp + (size_t)e * a.c.bytes) +
+                     (size_t)(key & pmask) * HD + c8;
+        float f[8];
+        load_query8(v, f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (no_number(f[j])) sum[j] += f[j];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (sum[j] != 0.f) acc[j] = sum[j];
+    }
+    if (a.split > 1) {
+      store_out8(part + row * HD + c8, acc);
+    } else if (whole) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        acc[j] = p < lo ? 0.f : Ls == 0.f ? __uint_as_float(0x7fffffffu) : acc[j];
+      store_out8(static_cast<T*>(a.out) + ((int64_t)it.b * a.M + m) * a.out_stride + (int64_t)h * HD +
+                     c8,
+                 acc);
+    } else {
+      store_out8(a.part + ((size_t)slot * a.part_rows + row) * HD + c8, acc);
+      if (c8 == 0) a.ml[(size_t)slot * a.part_rows + row] = make_float2(gm, Ls);
+    }
+  }
+}
+
 }  // namespace
 
 template <typename T, int HD, int R, int NW>
@@ -111,8 +300,8 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
     const int kb = max(it.lo, seg0), ke = min(it.hi + 1, seg0 + sg.nu * kUnit);
     const int nst = ke > kb ? (ke - seg0 + L::kKeys - 1) / L::kKeys : 0;
     const int st0 = ke > kb ? (kb - seg0) / L::kKeys : 0;
-    const char* const kp = a.k + (size_t)g * a.c.slab;
-    const char* const vp = a.v + (size_t)g * a.c.slab;
+    const char* const kp = a.k + g * a.c.head();
+    const char* const vp = a.v + g * a.c.head();
 
     // ---- stages: the pages of one are looked up while the one before is issued
     const int ch = tid % L::kChunks, r0 = tid / L::kChunks;
@@ -182,24 +371,13 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
         *reinterpret_cast<float4*>(Qs + row * L::kOPad + c4 * 4) = u;
       }
     }
-    int plo[2], phi[2];  // the lane's rows see keys plo .. phi
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int row = rt * kTile + n8 + 8 * i;
-      phi[i] = row < it.nr ? kv8_row_pos(a, it, it.r0 + row) : -1;  // no row here: sees none
-      plo[i] = row < it.nr ? kv8_row_lo(it, phi[i], a.window) : 0;
-    }
+    RowTile<HD> w;
+    w.start(a, it, rt * kTile);
     // every row of the item sees keys full_lo .. full_hi
     const int full_lo = kv8_row_lo(it, it.hi, a.window);
     const int full_hi = kv8_row_pos(a, it, it.r0);
     const bool some = rt * kTile < it.nr;       // a tile without rows only helps to copy
     const bool two = rt * kTile + 8 < it.nr;    // fp32: rows n8 + 8 are there
-
-    float o[NT][4], mx[2] = {-INFINITY, -INFINITY}, ls[2] = {0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[j][i] = 0.f;
 
     for (int s = st0; s < nst; ++s) {
       asm volatile("cp.async.wait_group %0;" ::"n"(L::kNst - 2) : "memory");
@@ -214,31 +392,16 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
         constexpr int kN = L::kGroupKeys < 16 ? 1 : 2;
         const int kk0 = grp * L::kGroupKeys + x0, k0 = seg0 + s * L::kKeys + kk0;
         if (!some || k0 >= ke || k0 + 8 * kN <= kb) continue;
-        float sc[2][4];
+        const bool full = k0 >= full_lo && k0 + 8 * kN - 1 <= full_hi;
+        uint32_t any = 0;
         if constexpr (BF) {
-          float s2[2][2][4];
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-              for (int x = 0; x < 4; ++x) s2[i][n][x] = 0.f;
-#pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            uint32_t b[4];
-            ldsm4(smem_u32(sk) + L::place(kk0 + (lane & 7) + ((lane >> 4) << 3), 2 * k + (lane >> 3 & 1)), b);
-            mma16816(s2[k & 1][0], qf[k], b[0], b[1]);
-            mma16816(s2[k & 1][1], qf[k], b[2], b[3]);
-          }
-#pragma unroll
-          for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) sc[n][x] = s2[0][n][x] + s2[1][n][x];
+          any = bf16_step<L, HD>(w, qf, smem_u32(sk), smem_u32(sv), kk0, k0, full, a.scale);
         } else {
+          float p[2][4];
 #pragma unroll
           for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) sc[n][x] = 0.f;
+            for (int x = 0; x < 4; ++x) p[n][x] = 0.f;
 #pragma unroll 4
           for (int c4 = 0; c4 < L::kChunks; ++c4) {
             float4 kq[kN][2];
@@ -255,7 +418,7 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
               for (int n = 0; n < kN; ++n)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                  float& d = sc[n][2 * i + x];
+                  float& d = p[n][2 * i + x];
                   d = fmaf(q.x, kq[n][x].x, d);
                   d = fmaf(q.y, kq[n][x].y, d);
                   d = fmaf(q.z, kq[n][x].z, d);
@@ -263,76 +426,14 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
                 }
             }
           }
-        }
-        const bool full = k0 >= full_lo && k0 + 8 * kN - 1 <= full_hi;
-        float z[2][4], nm[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-        for (int n = 0; n < kN; ++n)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            z[n][x] = sc[n][x] * a.scale;
-            if (!full) {
-              const int key = k0 + 8 * n + 2 * t + (x & 1);
-              if (key < plo[x >> 1] || key > phi[x >> 1]) z[n][x] = -INFINITY;
-            }
-            nm[x >> 1] = fmaxf(nm[x >> 1], z[n][x]);
-          }
-        bool moved = false;
-        float f[2], top[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          nm[i] = fmaxf(nm[i], __shfl_xor_sync(0xffffffffu, nm[i], 1));
-          nm[i] = fmaxf(nm[i], __shfl_xor_sync(0xffffffffu, nm[i], 2));
-          nm[i] = fmaxf(nm[i], mx[i]);
-          top[i] = nm[i] == -INFINITY ? 0.f : nm[i];
-          f[i] = nm[i] == mx[i] ? 1.f : exp2f(mx[i] - nm[i]);
-          moved |= nm[i] != mx[i];
-          mx[i] = nm[i];
-          ls[i] *= f[i];
-        }
-        if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) o[j][x] *= f[x >> 1];
-        }
-        float p[2][4];
-#pragma unroll
-        for (int n = 0; n < kN; ++n)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            p[n][x] = exp2f(z[n][x] - top[x >> 1]);
-            ls[x >> 1] += p[n][x];
-          }
-        uint32_t any = 0;
-        if constexpr (BF) {
-          uint32_t hi[4], lo[4];
-#pragma unroll
-          for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-              split2(p[n][2 * i], p[n][2 * i + 1], hi[2 * n + i], lo[2 * n + i]);
-#pragma unroll
-          for (int j = 0; j < NT; j += 2) {
-            uint32_t b[4];
-            ldsm4t(smem_u32(sv) + L::place(kk0 + (lane & 15), j + (lane >> 4)), b);
-            if (!full) {
-#pragma unroll
-              for (int x = 0; x < 4; ++x) b[x] = numbers(b[x], any);
-            }
-            mma16816(o[j], lo, b[0], b[1]);
-            mma16816(o[j + 1], lo, b[2], b[3]);
-            mma16816(o[j], hi, b[0], b[1]);
-            mma16816(o[j + 1], hi, b[2], b[3]);
-          }
-        } else {
+          w.template weigh<kN>(p, k0, full, a.scale);
           // o[j][2 i + ..]: row n8 + 8 i; columns 16 (j / 2) + 4 t + 2 (j % 2) + ..
 #pragma unroll
           for (int kk = 0; kk < 8 * kN; ++kk) {
-            float w[2];
+            float pw[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-              w[i] = __shfl_sync(0xffffffffu, p[kk >> 3][2 * i + (kk & 1)], (lane & 28) + (kk >> 1 & 3));
+              pw[i] = __shfl_sync(0xffffffffu, p[kk >> 3][2 * i + (kk & 1)], (lane & 28) + (kk >> 1 & 3));
 #pragma unroll
             for (int j = 0; j < NT; j += 2) {
               float4 u = lds4(sv + L::place(kk0 + kk, 2 * j + t));
@@ -345,10 +446,10 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
                 if (i == 1 && !two) continue;
-                o[j][2 * i] = fmaf(w[i], u.x, o[j][2 * i]);
-                o[j][2 * i + 1] = fmaf(w[i], u.y, o[j][2 * i + 1]);
-                o[j + 1][2 * i] = fmaf(w[i], u.z, o[j + 1][2 * i]);
-                o[j + 1][2 * i + 1] = fmaf(w[i], u.w, o[j + 1][2 * i + 1]);
+                w.o[j][2 * i] = fmaf(pw[i], u.x, w.o[j][2 * i]);
+                w.o[j][2 * i + 1] = fmaf(pw[i], u.y, w.o[j][2 * i + 1]);
+                w.o[j + 1][2 * i] = fmaf(pw[i], u.z, w.o[j + 1][2 * i]);
+                w.o[j + 1][2 * i + 1] = fmaf(pw[i], u.w, w.o[j + 1][2 * i + 1]);
               }
             }
           }
@@ -361,11 +462,11 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
     // ---- the groups' parts together
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 1);
-      ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 2);
+      w.ls[i] += __shfl_xor_sync(0xffffffffu, w.ls[i], 1);
+      w.ls[i] += __shfl_xor_sync(0xffffffffu, w.ls[i], 2);
       if (t == 0) {
-        s_m[grp][rt * kTile + n8 + 8 * i] = mx[i];
-        s_l[grp][rt * kTile + n8 + 8 * i] = ls[i];
+        s_m[grp][rt * kTile + n8 + 8 * i] = w.mx[i];
+        s_l[grp][rt * kTile + n8 + 8 * i] = w.ls[i];
       }
     }
     __syncthreads();  // nobody reads the ring any more
@@ -389,81 +490,19 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
         if constexpr (BF) {
 #pragma unroll
           for (int j = 0; j < NT; ++j)
-            *reinterpret_cast<float2*>(p + 8 * j + 2 * t) = make_float2(o[j][2 * i], o[j][2 * i + 1]);
+            *reinterpret_cast<float2*>(p + 8 * j + 2 * t) = make_float2(w.o[j][2 * i], w.o[j][2 * i + 1]);
         } else {
 #pragma unroll
           for (int j = 0; j < NT; j += 2)
             *reinterpret_cast<float4*>(p + 8 * j + 4 * t) =
-                make_float4(o[j][2 * i], o[j][2 * i + 1], o[j + 1][2 * i], o[j + 1][2 * i + 1]);
+                make_float4(w.o[j][2 * i], w.o[j][2 * i + 1], w.o[j + 1][2 * i], w.o[j + 1][2 * i + 1]);
         }
       }
     }
     __syncthreads();
-    const bool whole = sg.whole();
-    const int slot = 2 * blockIdx.x + (sg.u0 == 0);
-#pragma unroll 1
-    for (int x0 = 0; x0 < L::kRows * NT; x0 += L::kThreads) {
-      const int row = (x0 + tid) / NT, c8 = (tid % NT) * 8;
-      if (row < it.nr) {
-        const int r = it.r0 + row, m = a.byG(r), h = g * a.G + r - m * a.G;
-        const int p = kv8_row_pos(a, it, r), lo = kv8_row_lo(it, p, a.window);
-        const float gm = s_gm[row], Ls = s_sum[row];
-        float acc[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-        bool nan = false;
-#pragma unroll
-        for (int x = 0; x < L::kGroups; ++x) {
-          const float wt = s_w[x][row];
-          const float4* ox = reinterpret_cast<const float4*>(Ox + (size_t)(x * L::kRows + row) * L::kOPad + c8);
-          const float4 u = ox[0], w = ox[1];
-          acc[0] = fmaf(u.x, wt, acc[0]);
-          acc[1] = fmaf(u.y, wt, acc[1]);
-          acc[2] = fmaf(u.z, wt, acc[2]);
-          acc[3] = fmaf(u.w, wt, acc[3]);
-          acc[4] = fmaf(w.x, wt, acc[4]);
-          acc[5] = fmaf(w.y, wt, acc[5]);
-          acc[6] = fmaf(w.z, wt, acc[6]);
-          acc[7] = fmaf(w.w, wt, acc[7]);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) nan |= acc[j] != acc[j];
-        // values that are no numbers belong to the rows that see them (a part of a probability times
-        // infinity may have made NaN of one); where the scores are NaN, so is everything
-        if ((s_bad || nan) && Ls == Ls) {
-          float sum[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) sum[j] = 0.f;
-          for (int key = max(kb, lo); key < min(ke, p + 1); ++key) {
-            const int e = max(a.c.entry(it.b, key >> a.c.shift), 0);
-            const T* v = reinterpret_cast<const T*>(vp + (size_t)e * a.c.bytes +
-                                                    (size_t)(key & pmask) * L::kRowBytes) + c8;
-            float f[8];
-            load_query8(v, f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (no_number(f[j])) sum[j] += f[j];
-          }
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (sum[j] != 0.f) acc[j] = sum[j];
-        }
-        if (a.split > 1) {
-          store_out8(part + row * HD + c8, acc);
-        } else if (whole) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            acc[j] = p < lo ? 0.f : Ls == 0.f ? __uint_as_float(0x7fffffffu) : acc[j];
-          store_out8(static_cast<T*>(a.out) + ((int64_t)it.b * a.M + m) * a.out_stride +
-                         (int64_t)h * HD + c8,
-                     acc);
-        } else {
-          store_out8(a.part + ((size_t)slot * a.part_rows + row) * HD + c8, acc);
-          if (c8 == 0) a.ml[(size_t)slot * a.part_rows + row] = make_float2(gm, Ls);
-        }
-      }
-    }
-    if (!a.split && !whole && sg.u0 == 0 && tid == 0) a.desc[blockIdx.x] = kv8_desc(a, cur, sg);
+    finish_rows<T, HD, L::kGroups, L::kRows, L::kThreads>(a, sg, kb, ke, Ox, s_w, s_gm, s_sum, s_bad,
+                                                           part, tid);
+    if (!a.split && !sg.whole() && sg.u0 == 0 && tid == 0) a.desc[blockIdx.x] = kv8_desc(a, cur, sg);
     __syncthreads();
   }
   if (a.split > 1) {  // the cluster's parts together, each block some of the columns
@@ -526,6 +565,7 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
 
 }  // namespace ssd
 
+#include "paged_stream.cuh"
 #include "paged_wide.cuh"
 
 namespace ssd {
@@ -552,6 +592,11 @@ cudaError_t prep_wide() {
                               (int)PWideL<TILES>::kSmem);
 }
 template <int HD>
+cudaError_t prep_stream() {
+  return cudaFuncSetAttribute(k_paged_stream<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)SL<HD>::kSmem);
+}
+template <int HD>
 cudaError_t prep_hd() {
   cudaError_t e = prep<float, HD, 1, 4>();
   if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 1, 4>();
@@ -572,6 +617,7 @@ cudaError_t paged_device(int* sms) {
   if (!d.ready) {
     if ((e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess ||
         (e = prep_hd<64>()) != cudaSuccess || (e = prep_hd<128>()) != cudaSuccess ||
+        (e = prep_stream<64>()) != cudaSuccess || (e = prep_stream<128>()) != cudaSuccess ||
         (e = prep_wide<1>()) != cudaSuccess || (e = prep_wide<2>()) != cudaSuccess)
       return e;
     d.ready = true;
@@ -591,6 +637,7 @@ constexpr int kWideFrom = PWIDE_FROM;
 
 struct PagedPlan {
   int wide;   // accumulators of a tile on tcgen05, 0: mma.sync
+  bool stream;  // k_paged_stream
   int tiles;  // of 16 rows, of a block
   int split;  // blocks of an item's own, 0: the line
   int max_blocks, part_rows;
@@ -617,10 +664,11 @@ PagedPlan plan_of(const ssd_paged_cache* c, int n_heads, int M, int longest) {
     p.n_rt = (rows + rt - 1) / rt;
     items = p.n_rt * heads;
   }
+  p.stream = !p.wide && !p.split && c->dtype == SSD_DTYPE_BF16 && rows <= kTile;
   p.part_rows = rows < rt ? (int)rows : rt;
   p.units = items * ((longest + kUnit - 1) / kUnit +
                      (p.wide == 2 ? kKv8ItemCost<256> : kKv8ItemCost<kTile>));
-  p.max_blocks = p.wide ? kKv8MaxBlocks / 2 : kKv8MaxBlocks;
+  p.max_blocks = p.wide || p.stream ? kKv8MaxBlocks / 2 : kKv8MaxBlocks;
   if (p.units < p.max_blocks) p.max_blocks = (int)p.units;
   return p;
 }
@@ -667,6 +715,13 @@ cudaError_t wide_launch(const PagedAttn& a, int P, cudaStream_t st) {
   k_paged_wide<TILES><<<P, L::kThreads, L::kSmem, st>>>(a);
   const cudaError_t e = cudaGetLastError();
   return e != cudaSuccess ? e : merge_launch<__nv_bfloat16, kWHd, 1>(a, P, st);
+}
+template <int HD>
+cudaError_t stream_launch(const PagedAttn& a, int P, cudaStream_t st) {
+  using L = SL<HD>;
+  k_paged_stream<HD><<<P, L::kThreads, L::kSmem, st>>>(a);
+  const cudaError_t e = cudaGetLastError();
+  return e != cudaSuccess ? e : merge_launch<__nv_bfloat16, HD, kMWarps>(a, P, st);
 }
 template <int HD>
 cudaError_t rows_launch(const PagedAttn& a, int dtype, int tiles, int P, cudaStream_t st) {
@@ -751,7 +806,7 @@ extern "C" ssd_status ssd_paged_attention(const ssd_paged_cache* c, int32_t laye
   a.part = reinterpret_cast<float*>(ws + lay.part);
   a.byG = Kv8Div::of((uint32_t)a.G);
   a.byRt = Kv8Div::of((uint32_t)plan.n_rt);
-  int P = sms * (plan.wide ? 1 : 2);  // blocks of an SM
+  int P = sms * (plan.wide || plan.stream ? 1 : 2);  // blocks of an SM
   if (P > plan.max_blocks) P = plan.max_blocks;
   a.part_rows = plan.part_rows;
   a.split = plan.split;
@@ -760,6 +815,8 @@ extern "C" ssd_status ssd_paged_attention(const ssd_paged_cache* c, int32_t laye
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (plan.wide)
     e = plan.wide == 2 ? wide_launch<2>(a, P, st) : wide_launch<1>(a, P, st);
+  else if (plan.stream)
+    e = c->head_dim == 128 ? stream_launch<128>(a, P, st) : stream_launch<64>(a, P, st);
   else
     e = c->head_dim == 128 ? rows_launch<128>(a, c->dtype, plan.tiles, P, st)
                            : rows_launch<64>(a, c->dtype, plan.tiles, P, st);

@@ -543,7 +543,7 @@ __global__ void __launch_bounds__(kRowThreads) k_paged_append(const PagedAppend 
     for (int j = 0; j < kRowBatch; ++j) {
       const int x = x0 + j * kRowThreads, h = x >> a.head_shift;
       if (x < a.chunks) {
-        const size_t off = (size_t)h * a.c.slab +
+        const size_t off = h * a.c.head() +
                            ((size_t)((slot << a.head_shift) + (x - (h << a.head_shift))) << 4);
         *reinterpret_cast<uint4*>(page + a.to_k + off) = uk[j];
         *reinterpret_cast<uint4*>(page + a.to_v + off) = uv[j];

@@ -51,30 +51,11 @@ struct PWideBars {
   uint64_t drained;  // after a wait that gave up: the products still in flight are done
 };
 
-// Step n's place in the ring and its phase there.
-template <int NST>
-struct Ring {
-  uint32_t at = 0, phase = 0;
-  __device__ __forceinline__ void next() {
-    if (++at == NST) at = 0, phase ^= 1;
-  }
-};
-
 // The phase that step n completes on its buffer's barrier; after a wait that gave up, no thread of
 // this role waits again: it runs through its steps, meets its barriers and reports.
 __device__ __forceinline__ void p_wait2(uint64_t (&b)[2], uint32_t n, bool& bad) {
   if (!bad) bad = !w_sleep(&b[n & 1], (n >> 1) & 1);
 }
-__device__ __forceinline__ void p_wait(uint64_t* b, uint32_t phase, bool& bad) {
-  if (!bad) bad = !w_sleep(b, phase);
-}
-
-// Arrives when this thread's copies so far are there (one of the arrivals that the barrier counts). They
-// are writes of the generic proxy: who waits for them makes them visible to the tensor cores.
-__device__ __forceinline__ void p_arrive(uint64_t* bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-
 }  // namespace
 
 template <int TILES>
@@ -207,8 +188,8 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
       const Kv8Item& it = sg.it;
       const int k00 = (it.unit0 + sg.u0) * kWKeys;
       const int full_lo = kv8_row_lo(it, it.hi, a.window), full_hi = kv8_row_pos(a, it, it.r0);
-      const char* const kp = a.k + (size_t)sg.g * a.c.slab + ch * 16;
-      const char* const vp = a.v + (size_t)sg.g * a.c.slab + ch * 16;
+      const char* const kp = a.k + sg.g * a.c.head() + ch * 16;
+      const char* const vp = a.v + sg.g * a.c.head() + ch * 16;
       int look[4];  // pages of the step that is issued next
       auto look_up = [&](int k0) {
 #pragma unroll
@@ -387,7 +368,7 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
             const int kb = max(k00, plo), ke = min(k00 + sg.nu * kWKeys - 1, phi);
             for (int key = kb; key <= ke; ++key) {
               const int e = max(a.c.entry(it.b, key >> a.c.shift), 0);
-              const char* v = a.v + (size_t)sg.g * a.c.slab + (size_t)e * a.c.bytes +
+              const char* v = a.v + sg.g * a.c.head() + (size_t)e * a.c.bytes +
                               (size_t)(key & pmask) * (kWHd * 2) + 64 * q;
 #pragma unroll 1
               for (int x = 0; x < 32; ++x) {

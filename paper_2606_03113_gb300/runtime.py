@@ -446,8 +446,8 @@ class KV8Cache:
 
 class PagedKVCache:
     """A decoder's KV cache in pages that sequences share and give back (ssd_paged_cache,
-    include/ssd_ops.h): `pages` [n_pages, n_layers, 2 (K, V), n_kv_heads, page, head_dim], the pages
-    of each sequence in `table` [n_seq, max_seq / page] (-1: none), how many entries name each page in
+    include/ssd_ops.h): `pages` [n_pages, n_layers, 2 (K, V), n_kv_heads, page, head_dim] (a view: in
+    memory the heads stand in front of K and V), the pages of each sequence in `table` [n_seq, max_seq / page] (-1: none), how many entries name each page in
     `refs` [n_pages] (0: free).  `max_seq` is rounded up to a multiple of `page` (a power of
     two from 16 to 256).
 
@@ -491,8 +491,9 @@ class PagedKVCache:
         self.n_seq, self.n_pages = n_seq, n_pages
         self.max_pages = (max_seq + page - 1) // page
         self.max_seq = self.max_pages * page
-        self._pages = torch.zeros((n_pages, n_layers, 2, n_kv_heads, page, head_dim), dtype=dtype,
-                                  device=device)
+        # a head's keys and values in a page lie side by side
+        self._pages = torch.zeros((n_pages, n_layers, n_kv_heads, 2, page, head_dim), dtype=dtype,
+                                  device=device).transpose(2, 3)
         self._table = torch.full((n_seq, self.max_pages), -1, dtype=torch.int32, device=device)
         self._refs = torch.zeros(n_pages, dtype=torch.int32, device=device)
         self._err = torch.zeros(1, dtype=torch.int32, device=device)
