@@ -4,7 +4,7 @@
 //
 // k_paged_rows: a block takes a stretch of the plan's units (kv8_plan.cuh), or, for short
 // sequences, a cluster of blocks an item. Stages of keys and values come by cp.async, kNst - 1 of
-// them on their way; a thread looks up the pages of a stage one stage ahead. Of an item's
+// them on their way. Of an item's
 // R tiles of 16 query rows a warp has one, and of each stage the keys of its group; it keeps a
 // running maximum, sum and output of its own, and the block joins the groups once per item.
 // bf16: mma.sync on the rows as they are, probabilities in two bf16 parts (16 bits), so that the
@@ -303,24 +303,15 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
     const char* const kp = a.k + g * a.c.head();
     const char* const vp = a.v + g * a.c.head();
 
-    // ---- stages: the pages of one are looked up while the one before is issued
+    // ---- stages
     const int ch = tid % L::kChunks, r0 = tid / L::kChunks;
-    int look[L::kLook];
-    auto look_up = [&](int s) {
-#pragma unroll
-      for (int j = 0; j < L::kLook; ++j) {
-        const int key = seg0 + s * L::kKeys + 16 * j;
-        const bool in = key < ke && key + 15 >= kb;
-        look[j] = in ? a.c.entry(it.b, min(key, ke - 1) >> a.c.shift) : 0;
-        if (look[j] < 0) {
-          look[j] = 0;
-          if (tid == 0 && a.err) atomicOr(a.err, (int)kErrTable);
-        }
-      }
-    };
+    PageWalk walk(a.c, a.err);
     auto issue = [&](int s) {
       if (s < nst) {
         const uint32_t dst = smem_u32(smem) + (uint32_t)(s % L::kNst) * L::kStage;
+        int look[L::kLook];
+#pragma unroll
+        for (int j = 0; j < L::kLook; ++j) look[j] = walk.page(seg0 + s * L::kKeys + 16 * j);
 #pragma unroll
         for (int i = 0; i < L::kCopies; ++i) {
           const int r = r0 + i * (L::kThreads / L::kChunks), key = seg0 + s * L::kKeys + r;
@@ -331,11 +322,10 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
           cp_async16(at, kp + (in ? off : 0), in);
           cp_async16(at + L::kSide, vp + (in ? off : 0), in);
         }
-        if (s + 1 < nst) look_up(s + 1);
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    if (st0 < nst) look_up(st0);
+    walk.start(it.b, seg0 + st0 * L::kKeys, kb, ke);
 #pragma unroll
     for (int i = 0; i < L::kNst - 1; ++i) issue(st0 + i);
 

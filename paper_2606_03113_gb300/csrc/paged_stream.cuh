@@ -86,20 +86,8 @@ __global__ void __launch_bounds__(SL<HD>::kThreads, 1) k_paged_stream(const Page
     for (uint32_t i = 0; kv8_next<kTile, kUnit>(a, cur, sg); ++i) {
       const Kv8Item& it = sg.it;
       stages();
-      int look[L::kKeys / 16];  // pages of the stage that is issued next
-      auto look_up = [&](int s) {
-#pragma unroll
-        for (int j = 0; j < L::kKeys / 16; ++j) {
-          const int key = seg0 + s * L::kKeys + 16 * j;
-          const bool in = key < ke && key + 15 >= kb;
-          look[j] = in ? a.c.entry(it.b, min(key, ke - 1) >> a.c.shift) : 0;
-          if (look[j] < 0) {
-            look[j] = 0;
-            if (ct == 0 && a.err) atomicOr(a.err, (int)kErrTable);
-          }
-        }
-      };
-      if (first < last) look_up(first);
+      PageWalk walk(a.c, a.err);
+      walk.start(it.b, seg0 + first * L::kKeys, kb, ke);
       if (i >= 2) p_wait(&bar.q_free[i & 1], ((i >> 1) - 1) & 1, bad);
       for (int x = ct; x < kTile * L::kChunks; x += L::kCopy * 32) {
         const int row = x / L::kChunks, r = it.r0 + min(row, it.nr - 1), m = a.byG(r);
@@ -114,6 +102,9 @@ __global__ void __launch_bounds__(SL<HD>::kThreads, 1) k_paged_stream(const Page
       for (int s = first; s < last; ++s, ++n, ring.next()) {
         if (n >= (uint32_t)L::kNst) p_wait(&bar.empty[ring.at], ring.phase ^ 1, bad);
         const uint32_t dst = smem_u32(smem) + ring.at * L::kStage;
+        int look[L::kKeys / 16];
+#pragma unroll
+        for (int j = 0; j < L::kKeys / 16; ++j) look[j] = walk.page(seg0 + s * L::kKeys + 16 * j);
 #pragma unroll
         for (int j = 0; j < L::kKeys / kPass; ++j) {
           const int r = r0 + j * kPass, key = seg0 + s * L::kKeys + r;
@@ -125,7 +116,6 @@ __global__ void __launch_bounds__(SL<HD>::kThreads, 1) k_paged_stream(const Page
           cp_async16(at + L::kSide, vp + (in ? off : 0), in);
         }
         p_arrive(&bar.full[ring.at]);
-        if (s + 1 < last) look_up(s + 1);
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");

@@ -190,23 +190,14 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
       const int full_lo = kv8_row_lo(it, it.hi, a.window), full_hi = kv8_row_pos(a, it, it.r0);
       const char* const kp = a.k + sg.g * a.c.head() + ch * 16;
       const char* const vp = a.v + sg.g * a.c.head() + ch * 16;
-      int look[4];  // pages of the step that is issued next
-      auto look_up = [&](int k0) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int key = k0 + 16 * j;
-          const bool in = key <= it.hi && key + 15 >= it.lo && it.lo <= it.hi;
-          look[j] = in ? a.c.entry(it.b, min(key, it.hi) >> a.c.shift) : 0;
-          if (look[j] < 0) {
-            look[j] = 0;
-            if (ct == 0 && a.err) atomicOr(a.err, (int)kErrTable);
-          }
-        }
-      };
-      look_up(k00);
+      PageWalk walk(a.c, a.err);
+      walk.start(it.b, k00, max(k00, it.lo), min(k00 + sg.nu * kWKeys, it.hi + 1));
       for (int i = 0; i < sg.nu; ++i, ++n, ring.next()) {
         const int k0 = k00 + i * kWKeys;
         const uint32_t dst = smem_u32(Ks) + ring.at * L::kStep + to;
+        int look[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) look[j] = walk.page(k0 + 16 * j);
         auto copy = [&](const char* base, uint32_t at) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -228,7 +219,6 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
           clean();
           mbar_arrive(&bar.v_full[ring.at]);
         }
-        if (i + 1 < sg.nu) look_up(k0 + kWKeys);
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
