@@ -34,26 +34,27 @@ struct PagedView {
 // 32 entries, and the next 32 are on their way meanwhile. (Looked up a stage of 64 keys ahead, an entry that had
 // to come from memory held the copies up: pages of 16, 64 and 256 positions read 5.6, 6.4 and 6.7 TB/s.)
 struct PageWalk {
-  const PagedView& c;
+  const PagedView* view;
   int32_t* err;
   int b, from, to, base, now, then;  // entries from .. to are there; `now` are those from base on
-  __device__ __forceinline__ PageWalk(const PagedView& v, int32_t* e) : c(v), err(e) {}
+  __device__ __forceinline__ PageWalk(const PagedView& v, int32_t* e)
+      : view(&v), err(e), b(0), from(0), to(-1), base(0), now(0), then(0) {}
   __device__ __forceinline__ int load(int i) const {
     i += threadIdx.x & 31;
-    return i < from || i > to ? 0 : c.entry(b, i);
+    return i < from || i > to ? 0 : view->entry(b, i);
   }
   // key0: where the walk begins, kb or in front of it
   __device__ __forceinline__ void start(int seq, int key0, int kb, int ke) {
     b = seq;
-    from = kb >> c.shift;
-    to = kb < ke ? (ke - 1) >> c.shift : -1;
-    base = key0 >> c.shift;
+    from = kb >> view->shift;
+    to = kb < ke ? (ke - 1) >> view->shift : -1;
+    base = key0 >> view->shift;
     now = load(base);
     then = load(base + 32);
   }
   // The page of the entry that holds `key` (one for the whole warp, none in front of the last one's).
   __device__ __forceinline__ int page(int key) {
-    const int i = key >> c.shift;
+    const int i = key >> view->shift;
     if (i >= base + 32) {
       base += 32;
       now = then;

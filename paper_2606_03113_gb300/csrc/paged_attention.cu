@@ -27,7 +27,7 @@ namespace ssd {
 namespace {
 
 constexpr int kUnit = kKv8Block;  // keys of a unit of the plan
-constexpr int kTile = 16;         // query rows of a warp
+constexpr int kTile = 16;         // query rows of a warp, at most
 constexpr int kSplitMax = 8;      // blocks of a short sequence's item, a cluster, at most
 
 struct PagedAttn : AttnArgs {
@@ -36,19 +36,20 @@ struct PagedAttn : AttnArgs {
 };
 
 // Where things stand in a block's shared memory.
-template <typename T, int HD, int R, int NW>
+template <typename T, int HD, int R, int NB>
 struct PL {
+  static constexpr int NW = 4;
   static constexpr int kRowBytes = HD * (int)sizeof(T);
   static constexpr int kChunks = kRowBytes / 16;           // 16-byte chunks of a row
   static constexpr int kKeys = kRowBytes > 256 ? 32 : 64;  // of a stage
   static constexpr uint32_t kSide = kKeys * kRowBytes;
   static constexpr uint32_t kStage = 2 * kSide;
-  static constexpr int kNst = (NW > 4 ? 192 : 96) * 1024 / (int)kStage;
+  static constexpr int kNst = 96 * 1024 / (int)kStage;
   static constexpr uint32_t kRing = kNst * kStage;
   static constexpr int kGroups = NW / R;               // of warps, with keys of their own each
   static constexpr int kGroupKeys = kKeys / kGroups;
   static constexpr int kThreads = NW * 32;
-  static constexpr int kRows = R * kTile;
+  static constexpr int kWarpRows = 8 * NB, kRows = R * kWarpRows;
   static constexpr int kOPad = HD + 4;  // floats of a row in the exchange
   static constexpr uint32_t kQ = sizeof(T) == 4 ? kRows * kOPad * 4 : 0;  // fp32 queries
   static constexpr uint32_t kSmem = kRing + kQ;
@@ -79,7 +80,7 @@ __device__ __forceinline__ float4 lds4(const unsigned char* p) {
   return *reinterpret_cast<const float4*>(p);
 }
 
-// What a warp holds of its 16 query rows: lane n8, t has rows n8 and n8 + 8.
+// What a warp holds of 16 query rows, fp32: lane n8, t has rows n8 and n8 + 8.
 template <int HD>
 struct RowTile {
   float o[HD / 8][4], mx[2], ls[2];  // outputs, running maxima (in powers of two) and sums
@@ -142,55 +143,142 @@ struct RowTile {
         ls[x >> 1] += sc[n][x];
       }
   }
+  // The rows' sums, of all lanes.
+  __device__ __forceinline__ void sum_up() {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 1);
+      ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 2);
+    }
+  }
 };
 
-// 16 keys from row kk0 of a stage on, bf16: keys at sk, values at sv (shared memory), places by L.
-// Nonzero where a value that is no number was zeroed.
-template <typename L, int HD>
-__device__ __forceinline__ uint32_t bf16_step(RowTile<HD>& w, const uint32_t (&qf)[HD / 16][4],
-                                              uint32_t sk, uint32_t sv, int kk0, int k0, bool full,
-                                              float scale) {
-  const int lane = threadIdx.x & 31;
-  float s2[2][2][4];  // even and odd 16-column steps summed apart
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) s2[i][n][x] = 0.f;
-#pragma unroll
-  for (int k = 0; k < HD / 16; ++k) {
-    uint32_t b[4];
-    ldsm4(sk + L::place(kk0 + (lane & 7) + ((lane >> 4) << 3), 2 * k + (lane >> 3 & 1)), b);
-    mma16816(s2[k & 1][0], qf[k], b[0], b[1]);
-    mma16816(s2[k & 1][1], qf[k], b[2], b[3]);
-  }
-  float p[2][4];
-#pragma unroll
-  for (int n = 0; n < 2; ++n)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) p[n][x] = s2[0][n][x] + s2[1][n][x];
-  w.template weigh<2>(p, k0, full, scale);
-  uint32_t any = 0, hi[4], lo[4];
-#pragma unroll
-  for (int n = 0; n < 2; ++n)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) split2(p[n][2 * i], p[n][2 * i + 1], hi[2 * n + i], lo[2 * n + i]);
-#pragma unroll
-  for (int j = 0; j < HD / 8; j += 2) {
-    uint32_t b[4];
-    ldsm4t(sv + L::place(kk0 + (lane & 15), j + (lane >> 4)), b);
-    if (!full) {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) b[x] = numbers(b[x], any);
-    }
-    mma16816(w.o[j], lo, b[0], b[1]);
-    mma16816(w.o[j + 1], lo, b[2], b[3]);
-    mma16816(w.o[j], hi, b[0], b[1]);
-    mma16816(w.o[j + 1], hi, b[2], b[3]);
-  }
-  return any;
+// The rows and columns of an 8 x 8 matrix of 16-bit values, two a lane, exchanged.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
 }
+
+// What a warp holds of 8 NB query rows, bf16. Keys are the matrix rows of its products (S^T = K Q^T, 16 keys
+// x 8 query rows an instruction, and O^T = V^T P^T), so that the few rows of a decode step take half of
+// the instructions that a tile of 16 would: mma.sync is what a step of 16 keys takes longest for (24 of them for 8
+// rows, 48 for 16; about 19 cycles each of a quarter of an SM). Lane n8, t has keys n8 and n8 + 8, rows
+// 8 b + 2 t and + 1.
+template <int HD, int NB>
+struct ColTile {
+  float o[HD / 16][NB][4], mx[NB][2], ls[NB][2];  // outputs (columns 16 j + n8, + 8), maxima, sums
+  int plo[NB][2], phi[NB][2];                     // the rows see keys plo .. phi
+  __device__ __forceinline__ void start(const AttnArgs& a, const Kv8Item& it, int row0) {
+    const int t = threadIdx.x & 3;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = row0 + 8 * b + 2 * t + i;
+        phi[b][i] = row < it.nr ? kv8_row_pos(a, it, it.r0 + row) : -1;  // no row here: sees none
+        plo[b][i] = row < it.nr ? kv8_row_lo(it, phi[b][i], a.window) : 0;
+        mx[b][i] = -INFINITY;
+        ls[b][i] = 0.f;
+      }
+#pragma unroll
+    for (int j = 0; j < HD / 16; ++j)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[j][b][x] = 0.f;
+  }
+  // 16 keys from row kk0 of a stage on: keys at sk, values at sv (shared memory), places by L. qf: the rows
+  // as an operand. Nonzero where a value that is no number was zeroed.
+  template <typename L>
+  __device__ __forceinline__ uint32_t step(const uint32_t (&qf)[HD / 16][NB][2], uint32_t sk, uint32_t sv,
+                                           int kk0, int k0, bool full, float scale) {
+    const int lane = threadIdx.x & 31, n8 = lane >> 2;
+    float s2[2][NB][4];  // even and odd 16-column steps summed apart
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s2[i][b][x] = 0.f;
+#pragma unroll
+    for (int k = 0; k < HD / 16; ++k) {
+      uint32_t u[4];
+      ldsm4(sk + L::place(kk0 + (lane & 15), 2 * k + (lane >> 4)), u);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) mma16816(s2[k & 1][b], u, qf[k][b][0], qf[k][b][1]);
+    }
+    float z[NB][4], f[NB][2], top[NB][2];
+    bool moved = false;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      float nm[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        z[b][x] = (s2[0][b][x] + s2[1][b][x]) * scale;
+        if (!full) {
+          const int key = k0 + n8 + 8 * (x >> 1);
+          if (key < plo[b][x & 1] || key > phi[b][x & 1]) z[b][x] = -INFINITY;
+        }
+        nm[x & 1] = fmaxf(nm[x & 1], z[b][x]);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int y = 4; y < 32; y <<= 1) nm[i] = fmaxf(nm[i], __shfl_xor_sync(0xffffffffu, nm[i], y));
+        nm[i] = fmaxf(nm[i], mx[b][i]);
+        top[b][i] = nm[i] == -INFINITY ? 0.f : nm[i];
+        f[b][i] = nm[i] == mx[b][i] ? 1.f : exp2f(mx[b][i] - nm[i]);
+        moved |= nm[i] != mx[b][i];
+        mx[b][i] = nm[i];
+        ls[b][i] *= f[b][i];
+      }
+    }
+    if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+      for (int j = 0; j < HD / 16; ++j)
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[j][b][x] *= f[b][x & 1];
+    }
+    uint32_t any = 0, hi[NB][2], lo[NB][2];  // probabilities in two parts, keys n8 and n8 + 8
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float p0 = exp2f(z[b][2 * h] - top[b][0]), p1 = exp2f(z[b][2 * h + 1] - top[b][1]);
+        ls[b][0] += p0;
+        ls[b][1] += p1;
+        split2(p0, p1, hi[b][h], lo[b][h]);
+        hi[b][h] = transpose8(hi[b][h]);
+        lo[b][h] = transpose8(lo[b][h]);
+      }
+#pragma unroll
+    for (int j = 0; j < HD / 16; ++j) {
+      uint32_t u[4];
+      ldsm4t(sv + L::place(kk0 + (lane & 7) + ((lane >> 4) << 3), 2 * j + (lane >> 3 & 1)), u);
+      if (!full) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) u[x] = numbers(u[x], any);
+      }
+#pragma unroll
+      for (int b = 0; b < NB; ++b) mma16816(o[j][b], u, lo[b][0], lo[b][1]);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) mma16816(o[j][b], u, hi[b][0], hi[b][1]);
+    }
+    return any;
+  }
+  // The rows' sums, of all lanes.
+  __device__ __forceinline__ void sum_up() {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int y = 4; y < 32; y <<= 1) ls[b][i] += __shfl_xor_sync(0xffffffffu, ls[b][i], y);
+  }
+};
 
 // The rows of a block's part of an item, from what GROUPS groups of warps left: outputs in Ox
 // [GROUPS][ROWS][HD + 4], weights s_w (NULL: 1), the rows' maxima and sums. Of keys kb .. ke - 1. To `part` in shared
@@ -270,9 +358,10 @@ __device__ __forceinline__ void finish_rows(const PagedAttn& a, const Kv8Seg& sg
 
 }  // namespace
 
-template <typename T, int HD, int R, int NW>
-__global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const PagedAttn a) {
-  using L = PL<T, HD, R, NW>;
+template <typename T, int HD, int R, int NB>
+__global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(const PagedAttn a) {
+  using L = PL<T, HD, R, NB>;
+  static_assert(sizeof(T) == 2 || NB == 2, "fp32 rows are held by sixteens");
   constexpr bool BF = sizeof(T) == 2;
   constexpr int NT = HD / 8;   // 8-column tiles of the output
   constexpr int KS = HD / 16;  // 16-column steps of a score
@@ -330,23 +419,25 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
     for (int i = 0; i < L::kNst - 1; ++i) issue(st0 + i);
 
     // ---- queries of the warp's tile
-    uint32_t qf[BF ? KS : 1][4];
+    uint32_t qf[BF ? KS : 1][NB][2];
     float* const Qs = reinterpret_cast<float*>(smem + L::kRing);
     if (tid == 0) s_bad = 0;
     if constexpr (BF) {
-      const T* qp[2];
+      const T* qp[NB];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int row = rt * kTile + n8 + 8 * i, r = it.r0 + min(row, it.nr - 1);
+      for (int b = 0; b < NB; ++b) {
+        const int r = it.r0 + min(rt * L::kWarpRows + 8 * b + n8, it.nr - 1);
         const int m = a.byG(r), h = g * a.G + r - m * a.G;
-        qp[i] = static_cast<const T*>(a.q) + ((int64_t)it.b * a.M + m) * a.q_stride +
+        qp[b] = static_cast<const T*>(a.q) + ((int64_t)it.b * a.M + m) * a.q_stride +
                 (int64_t)h * HD + 2 * t;
       }
 #pragma unroll
       for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          qf[k][x] = __ldg(reinterpret_cast<const uint32_t*>(qp[x & 1] + 16 * k + 8 * (x >> 1)));
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            qf[k][b][x] = __ldg(reinterpret_cast<const uint32_t*>(qp[b] + 16 * k + 8 * x));
     } else {
       for (int x = tid; x < L::kRows * (HD / 4); x += L::kThreads) {
         const int row = x / (HD / 4), c4 = x % (HD / 4);
@@ -361,13 +452,13 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
         *reinterpret_cast<float4*>(Qs + row * L::kOPad + c4 * 4) = u;
       }
     }
-    RowTile<HD> w;
-    w.start(a, it, rt * kTile);
+    typename std::conditional<BF, ColTile<HD, NB>, RowTile<HD>>::type w;
+    w.start(a, it, rt * L::kWarpRows);
     // every row of the item sees keys full_lo .. full_hi
     const int full_lo = kv8_row_lo(it, it.hi, a.window);
     const int full_hi = kv8_row_pos(a, it, it.r0);
-    const bool some = rt * kTile < it.nr;       // a tile without rows only helps to copy
-    const bool two = rt * kTile + 8 < it.nr;    // fp32: rows n8 + 8 are there
+    const bool some = rt * L::kWarpRows < it.nr;  // a tile without rows only helps to copy
+    const bool two = rt * kTile + 8 < it.nr;      // fp32: rows n8 + 8 are there
 
     for (int s = st0; s < nst; ++s) {
       asm volatile("cp.async.wait_group %0;" ::"n"(L::kNst - 2) : "memory");
@@ -385,7 +476,7 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
         const bool full = k0 >= full_lo && k0 + 8 * kN - 1 <= full_hi;
         uint32_t any = 0;
         if constexpr (BF) {
-          any = bf16_step<L, HD>(w, qf, smem_u32(sk), smem_u32(sv), kk0, k0, full, a.scale);
+          any = w.template step<L>(qf, smem_u32(sk), smem_u32(sv), kk0, k0, full, a.scale);
         } else {
           float p[2][4];
 #pragma unroll
@@ -450,14 +541,23 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
     asm volatile("cp.async.wait_all;" ::: "memory");
 
     // ---- the groups' parts together
+    w.sum_up();
+    if constexpr (BF) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      w.ls[i] += __shfl_xor_sync(0xffffffffu, w.ls[i], 1);
-      w.ls[i] += __shfl_xor_sync(0xffffffffu, w.ls[i], 2);
-      if (t == 0) {
-        s_m[grp][rt * kTile + n8 + 8 * i] = w.mx[i];
-        s_l[grp][rt * kTile + n8 + 8 * i] = w.ls[i];
-      }
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (n8 == 0) {
+            s_m[grp][rt * L::kWarpRows + 8 * b + 2 * t + i] = w.mx[b][i];
+            s_l[grp][rt * L::kWarpRows + 8 * b + 2 * t + i] = w.ls[b][i];
+          }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (t == 0) {
+          s_m[grp][rt * kTile + n8 + 8 * i] = w.mx[i];
+          s_l[grp][rt * kTile + n8 + 8 * i] = w.ls[i];
+        }
     }
     __syncthreads();  // nobody reads the ring any more
     if (tid < L::kRows) {
@@ -472,21 +572,30 @@ __global__ void __launch_bounds__(NW * 32, NW > 4 ? 1 : 2) k_paged_rows(const Pa
       s_gm[tid] = gm;
       s_sum[tid] = sum;
     }
+    if constexpr (BF) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int row = rt * kTile + n8 + 8 * i;
-      if (row < it.nr) {
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = rt * L::kWarpRows + 8 * b + 2 * t + i;
+          float* p = Ox + (size_t)(grp * L::kRows + row) * L::kOPad + n8;
+          if (row < it.nr)
+#pragma unroll
+            for (int j = 0; j < HD / 16; ++j) {
+              p[16 * j] = w.o[j][b][i];
+              p[16 * j + 8] = w.o[j][b][2 + i];
+            }
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = rt * kTile + n8 + 8 * i;
         float* p = Ox + (size_t)(grp * L::kRows + row) * L::kOPad;
-        if constexpr (BF) {
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-            *reinterpret_cast<float2*>(p + 8 * j + 2 * t) = make_float2(w.o[j][2 * i], w.o[j][2 * i + 1]);
-        } else {
+        if (row < it.nr)
 #pragma unroll
           for (int j = 0; j < NT; j += 2)
             *reinterpret_cast<float4*>(p + 8 * j + 4 * t) =
                 make_float4(w.o[j][2 * i], w.o[j][2 * i + 1], w.o[j + 1][2 * i], w.o[j + 1][2 * i + 1]);
-        }
       }
     }
     __syncthreads();
@@ -571,27 +680,30 @@ struct PagedDevice {
 std::mutex g_paged_mu;
 PagedDevice g_paged_dev[64];
 
-template <typename T, int HD, int R, int NW>
+template <typename T, int HD, int R, int NB>
 cudaError_t prep() {
-  return cudaFuncSetAttribute(k_paged_rows<T, HD, R, NW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)PL<T, HD, R, NW>::kSmem);
+  return cudaFuncSetAttribute(k_paged_rows<T, HD, R, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)PL<T, HD, R, NB>::kSmem);
 }
 template <int TILES>
 cudaError_t prep_wide() {
   return cudaFuncSetAttribute(k_paged_wide<TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               (int)PWideL<TILES>::kSmem);
 }
-template <int HD>
+template <int HD, int NB>
 cudaError_t prep_stream() {
-  return cudaFuncSetAttribute(k_paged_stream<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)SL<HD>::kSmem);
+  return cudaFuncSetAttribute(k_paged_stream<HD, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)SL<HD, NB>::kSmem);
 }
 template <int HD>
 cudaError_t prep_hd() {
-  cudaError_t e = prep<float, HD, 1, 4>();
-  if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 1, 4>();
-  if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 2, 4>();
-  if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 4, 4>();
+  cudaError_t e = prep<float, HD, 1, 2>();
+  if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 1, 1>();
+  if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 1, 2>();
+  if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 2, 2>();
+  if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 4, 2>();
+  if (e == cudaSuccess) e = prep_stream<HD, 1>();
+  if (e == cudaSuccess) e = prep_stream<HD, 2>();
   return e;
 }
 
@@ -607,7 +719,6 @@ cudaError_t paged_device(int* sms) {
   if (!d.ready) {
     if ((e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess ||
         (e = prep_hd<64>()) != cudaSuccess || (e = prep_hd<128>()) != cudaSuccess ||
-        (e = prep_stream<64>()) != cudaSuccess || (e = prep_stream<128>()) != cudaSuccess ||
         (e = prep_wide<1>()) != cudaSuccess || (e = prep_wide<2>()) != cudaSuccess)
       return e;
     d.ready = true;
@@ -628,7 +739,8 @@ constexpr int kWideFrom = PWIDE_FROM;
 struct PagedPlan {
   int wide;   // accumulators of a tile on tcgen05, 0: mma.sync
   bool stream;  // k_paged_stream
-  int tiles;  // of 16 rows, of a block
+  int tiles;  // warps of a block that have rows of their own each
+  int eights;  // a warp's rows by eights
   int split;  // blocks of an item's own, 0: the line
   int max_blocks, part_rows;
   long long n_rt, units;  // tiles of a sequence; the line's places, at most
@@ -638,7 +750,8 @@ PagedPlan plan_of(const ssd_paged_cache* c, int n_heads, int M, int longest) {
   const long long rows = (long long)M * (n_heads / c->n_kv_heads);
   const long long heads = (long long)c->n_seq * c->n_kv_heads;
   p.tiles = c->dtype == SSD_DTYPE_F32 || rows <= kTile ? 1 : rows <= 2 * kTile ? 2 : 4;
-  int rt = p.tiles * kTile;
+  p.eights = c->dtype == SSD_DTYPE_F32 || rows > 8 ? 2 : 1;
+  int rt = p.tiles * p.eights * 8;
   p.n_rt = (rows + rt - 1) / rt;
   long long items = p.n_rt * heads;
   p.split = 1;
@@ -681,9 +794,9 @@ const char* check_attention(const ssd_paged_cache* c, int32_t n_heads, int32_t M
   return nullptr;
 }
 
-template <typename T, int HD, int R, int NW>
+template <typename T, int HD, int R, int NB>
 cudaError_t rows_launch(const PagedAttn& a, int P, cudaStream_t st) {
-  using L = PL<T, HD, R, NW>;
+  using L = PL<T, HD, R, NB>;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(P);
   cfg.blockDim = dim3(L::kThreads);
@@ -695,9 +808,16 @@ cudaError_t rows_launch(const PagedAttn& a, int P, cudaStream_t st) {
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = a.split > 1 ? 1 : 0;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_paged_rows<T, HD, R, NW>, a);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_paged_rows<T, HD, R, NB>, a);
   if (e != cudaSuccess || a.split) return e;
   return R == 1 ? merge_launch<T, HD, kMWarps>(a, P, st) : merge_launch<T, HD, 1>(a, P, st);
+}
+template <int HD, int NB>
+cudaError_t stream_launch(const PagedAttn& a, int P, cudaStream_t st) {
+  using L = SL<HD, NB>;
+  k_paged_stream<HD, NB><<<P, L::kThreads, L::kSmem, st>>>(a);
+  const cudaError_t e = cudaGetLastError();
+  return e != cudaSuccess ? e : merge_launch<__nv_bfloat16, HD, kMWarps>(a, P, st);
 }
 template <int TILES>
 cudaError_t wide_launch(const PagedAttn& a, int P, cudaStream_t st) {
@@ -707,18 +827,14 @@ cudaError_t wide_launch(const PagedAttn& a, int P, cudaStream_t st) {
   return e != cudaSuccess ? e : merge_launch<__nv_bfloat16, kWHd, 1>(a, P, st);
 }
 template <int HD>
-cudaError_t stream_launch(const PagedAttn& a, int P, cudaStream_t st) {
-  using L = SL<HD>;
-  k_paged_stream<HD><<<P, L::kThreads, L::kSmem, st>>>(a);
-  const cudaError_t e = cudaGetLastError();
-  return e != cudaSuccess ? e : merge_launch<__nv_bfloat16, HD, kMWarps>(a, P, st);
-}
-template <int HD>
-cudaError_t rows_launch(const PagedAttn& a, int dtype, int tiles, int P, cudaStream_t st) {
-  if (dtype == SSD_DTYPE_F32) return rows_launch<float, HD, 1, 4>(a, P, st);
-  if (tiles == 1) return rows_launch<__nv_bfloat16, HD, 1, 4>(a, P, st);
-  if (tiles == 2) return rows_launch<__nv_bfloat16, HD, 2, 4>(a, P, st);
-  return rows_launch<__nv_bfloat16, HD, 4, 4>(a, P, st);
+cudaError_t launch(const PagedAttn& a, int dtype, const PagedPlan& p, int P, cudaStream_t st) {
+  using B = __nv_bfloat16;
+  if (dtype == SSD_DTYPE_F32) return rows_launch<float, HD, 1, 2>(a, P, st);
+  if (p.wide) return p.wide == 2 ? wide_launch<2>(a, P, st) : wide_launch<1>(a, P, st);
+  if (p.stream) return p.eights == 1 ? stream_launch<HD, 1>(a, P, st) : stream_launch<HD, 2>(a, P, st);
+  if (p.eights == 1) return rows_launch<B, HD, 1, 1>(a, P, st);
+  if (p.tiles == 1) return rows_launch<B, HD, 1, 2>(a, P, st);
+  return p.tiles == 2 ? rows_launch<B, HD, 2, 2>(a, P, st) : rows_launch<B, HD, 4, 2>(a, P, st);
 }
 
 }  // namespace
@@ -803,12 +919,6 @@ extern "C" ssd_status ssd_paged_attention(const ssd_paged_cache* c, int32_t laye
   if (plan.split) P = a.entries * a.Hkv * plan.split;
   a.byP = Kv8Div::of((uint32_t)P);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (plan.wide)
-    e = plan.wide == 2 ? wide_launch<2>(a, P, st) : wide_launch<1>(a, P, st);
-  else if (plan.stream)
-    e = c->head_dim == 128 ? stream_launch<128>(a, P, st) : stream_launch<64>(a, P, st);
-  else
-    e = c->head_dim == 128 ? rows_launch<128>(a, c->dtype, plan.tiles, P, st)
-                           : rows_launch<64>(a, c->dtype, plan.tiles, P, st);
+  e = c->head_dim == 128 ? launch<128>(a, c->dtype, plan, P, st) : launch<64>(a, c->dtype, plan, P, st);
   return e == cudaSuccess ? SSD_OK : fail_op_cuda("ssd_paged_attention", e);
 }

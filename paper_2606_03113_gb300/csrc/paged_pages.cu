@@ -16,11 +16,8 @@ namespace ssd {
 
 namespace {
 
-constexpr int kPlanThreads = 1024;
-constexpr int kPlanWarps = kPlanThreads / 32;
-constexpr int kScan = 16;                        // counts of a thread in a pass over refs
-constexpr int kScanStep = kPlanThreads * kScan;  // counts of a pass
-constexpr int kHeld = 2 * kPlanThreads;  // entries of a reserve that stay in registers
+constexpr int kScan = 16;    // counts of a thread in a pass over refs
+constexpr int kHeld = 2048;  // entries of a reserve that stay in registers
 constexpr int kClaim = 1 << 16;  // refs while a reserve looks: entries below, claims above
 constexpr int kCopyThreads = 256;
 constexpr int kForkCols = 8;     // entries of a sequence that a fork's block looks at: a sector
@@ -51,10 +48,11 @@ PlanWork plan_work(void* p, int n_pages) {
 }
 
 struct PlanSmem {
-  int warp[kPlanWarps];
+  int warp[32];
 };
 
-// Sum of v over the threads before this one; `total` of all. Two barriers.
+// Sum of v over the threads before this one, of WARPS warps; `total` of all. Two barriers.
+template <int WARPS>
 __device__ __forceinline__ int before_me(int v, PlanSmem& sm, int& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int inc = v;
@@ -68,7 +66,7 @@ __device__ __forceinline__ int before_me(int v, PlanSmem& sm, int& total) {
   __syncthreads();
   int base = 0, all = 0;
 #pragma unroll
-  for (int w = 0; w < kPlanWarps; ++w) {
+  for (int w = 0; w < WARPS; ++w) {
     const int s = sm.warp[w];
     base += w < warp ? s : 0;
     all += s;
@@ -102,13 +100,14 @@ __device__ __forceinline__ void load_refs(const PagedView& c, int id0, int (&r)[
 //  3 the entries that need a page are counted and as many free pages found, lowest first;
 //  4 (too few: the claims are taken back) entries get theirs by rank, the list of copies is written,
 //    the counts follow.
-// One block, bound by round trips to L2: four where no page is shared (positions, entries, counts, a
-// pass over 16384 counts, which is on its way from the start), two more for shared ones. Up to kHeld wanted
-// entries, as a decode step has them, stay in registers from step to step; more are looked at again in each.
-__global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView c, const PlanWork w,
-                                                                const int32_t* pos,
-                                                                const int32_t* rows, int M,
-                                                                int32_t* err) {
+// One block, bound by round trips to L2: three where nothing is needed (positions, entries, counts), a pass
+// over the counts for free pages, two more for shared ones. Up to kHeld wanted entries, as a decode step
+// has them, stay in registers from step to step; more are looked at again in each.
+template <int TH>
+__global__ void __launch_bounds__(TH, 1) k_paged_reserve(const PagedView c, const PlanWork w,
+                                                      const int32_t* pos, const int32_t* rows, int M,
+                                                      int32_t* err) {
+  constexpr int kWarps = TH / 32, kScanStep = TH * kScan;  // counts of a pass
   __shared__ PlanSmem sm;
   __shared__ int s_pre[SSD_KV8_MAX_SEQS + 1];  // wanted entries of the sequences before
   __shared__ int s_pos[SSD_KV8_MAX_SEQS];
@@ -116,34 +115,27 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
   __shared__ int s_copies;
   pdl_launch_dependents();
   const int tid = threadIdx.x;
-  const int per = (c.n_seq + kPlanThreads - 1) / kPlanThreads;
-  int cnt[SSD_KV8_MAX_SEQS / kPlanThreads], sum = 0;
-#pragma unroll
-  for (int j = 0; j < SSD_KV8_MAX_SEQS / kPlanThreads; ++j) {
+  // sequences tid per .. (tid + 1) per - 1 are this thread's
+  const int per = (c.n_seq + TH - 1) / TH;
+  int sum = 0;
+  for (int j = 0; j < per; ++j) {
     const int b = tid * per + j;
-    cnt[j] = 0;
-    if (j < per && b < c.n_seq) {
-      const int p = __ldg(pos + b), n = rows ? __ldg(rows + b) : M;
-      if (p < 0 || n < 0 || n > M || p > c.cap() - n) {
-        if (err) atomicOr(err, n < 0 || n > M ? (int)kErrControl : (int)kErrCapacity);
-      } else if (n > 0) {
-        cnt[j] = ((p + n - 1) >> c.shift) - (p >> c.shift) + 1;
-      }
-      s_pos[b] = p;
+    if (b >= c.n_seq) break;
+    const int p = __ldg(pos + b), n = rows ? __ldg(rows + b) : M;
+    int cnt = 0;
+    if (p < 0 || n < 0 || n > M || p > c.cap() - n) {
+      if (err) atomicOr(err, n < 0 || n > M ? (int)kErrControl : (int)kErrCapacity);
+    } else if (n > 0) {
+      cnt = ((p + n - 1) >> c.shift) - (p >> c.shift) + 1;
     }
-    sum += cnt[j];
+    s_pos[b] = p;
+    s_pre[b] = sum;  // (of this thread's, for now)
+    sum += cnt;
   }
-  int ahead[kScan];  // the first counts: which are 0 no step changes before pages are given out
-  load_refs(c, tid * kScan, ahead);
   if (tid == 0) s_copies = 0;
   int E;
-  int at = before_me(sum, sm, E);
-#pragma unroll
-  for (int j = 0; j < SSD_KV8_MAX_SEQS / kPlanThreads; ++j) {
-    const int b = tid * per + j;
-    if (j < per && b < c.n_seq) s_pre[b] = at;
-    at += cnt[j];
-  }
+  const int at = before_me<kWarps>(sum, sm, E);
+  for (int j = 0; j < per && tid * per + j < c.n_seq; ++j) s_pre[tid * per + j] += at;
   if (tid == 0) s_pre[c.n_seq] = E;
   __syncthreads();
   // wanted entry x: its sequence and place in the table
@@ -167,13 +159,10 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
     int found = 0;
     for (int id0 = 0; id0 < c.n_pages && found < need; id0 += kScanStep) {
       int r[kScan], n = 0, total;
-      if (id0) load_refs(c, id0 + tid * kScan, r);
-      else
-#pragma unroll
-        for (int j = 0; j < kScan; ++j) r[j] = ahead[j];
+      load_refs(c, id0 + tid * kScan, r);
 #pragma unroll
       for (int j = 0; j < kScan; ++j) n += r[j] == 0;
-      int rank = found + before_me(n, sm, total);
+      int rank = found + before_me<kWarps>(n, sm, total);
 #pragma unroll
       for (int j = 0; j < kScan; ++j)
         if (r[j] == 0) {
@@ -193,17 +182,23 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
   };
 
   if (E <= kHeld) {
-    constexpr int K = kHeld / kPlanThreads;
+    constexpr int K = kHeld / TH;
     int eb[K], ei[K], ee[K];
     bool shared[K], all[K];
     int claims = 0;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
+      const int x = tid * K + k;
       eb[k] = ei[k] = 0, ee[k] = -1;
-      if (tid * K + k < E) {
-        find(tid * K + k, eb[k], ei[k]);
-        ee[k] = entry(eb[k], ei[k]);
+      if (x >= E) continue;
+      if (k == 0) {
+        find(x, eb[0], ei[0]);
+      } else {
+        eb[k] = eb[k - 1];
+        while (s_pre[eb[k] + 1] <= x) ++eb[k];
+        ei[k] = (s_pos[eb[k]] >> c.shift) + x - s_pre[eb[k]];
       }
+      ee[k] = entry(eb[k], ei[k]);
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -234,7 +229,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
       needs[k] = tid * K + k < E && (ee[k] < 0 || (shared[k] && !all[k]));
       mine += needs[k];
     }
-    int rank = before_me(mine, sm, need);
+    int rank = before_me<kWarps>(mine, sm, need);
     const bool enough = need == 0 || find_free(need, s_fresh) >= need;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -254,7 +249,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
   }
 
   int claims = 0;
-  for (int x = tid; x < E; x += kPlanThreads) {
+  for (int x = tid; x < E; x += TH) {
     int b, i;
     find(x, b, i);
     const int e = entry(b, i);
@@ -266,7 +261,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
   }
   const bool any = __syncthreads_or(claims);
   if (any) {
-    for (int x = tid; x < E; x += kPlanThreads) {
+    for (int x = tid; x < E; x += TH) {
       int b, i;
       find(x, b, i);
       const int e = entry(b, i);
@@ -288,7 +283,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
     return true;
   };
   int need = 0;
-  for (int x0 = 0; x0 < E; x0 += kPlanThreads) {
+  for (int x0 = 0; x0 < E; x0 += TH) {
     int mine = 0;
     if (x0 + tid < E) {
       int b, i, from;
@@ -298,7 +293,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
     need += __syncthreads_count(mine);
   }
   if (find_free(need, w.fresh) < need) {
-    for (int x = tid; x < E; x += kPlanThreads) {
+    for (int x = tid; x < E; x += TH) {
       int b, i;
       find(x, b, i);
       const int e = entry(b, i);
@@ -312,14 +307,14 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
     return;
   }
   int base = 0;
-  for (int x0 = 0; x0 < E && need > 0; x0 += kPlanThreads) {
+  for (int x0 = 0; x0 < E && need > 0; x0 += TH) {
     int b = 0, i = 0, from = -1, total;
     bool mine = false;
     if (x0 + tid < E) {
       find(x0 + tid, b, i);
       mine = needs(b, entry(b, i), from);
     }
-    const int rank = base + before_me(mine, sm, total);
+    const int rank = base + before_me<kWarps>(mine, sm, total);
     base += total;
     if (mine) {
       give(b, i, from, __ldcg(w.fresh + rank));
@@ -327,14 +322,14 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_reserve(const PagedView 
     }
   }
   __syncthreads();
-  for (int k = tid; k < need; k += kPlanThreads) {
+  for (int k = tid; k < need; k += TH) {
     c.refs[__ldcg(w.fresh + k)] = 1;
     const int from = __ldcg(w.old + k);
     if (from >= 0) atomicSub(c.refs + from, kClaim + 1);
   }
   if (any) {  // the claims of those who keep a page, which their entries still name
     __syncthreads();
-    for (int x = tid; x < E; x += kPlanThreads) {
+    for (int x = tid; x < E; x += TH) {
       int b, i;
       find(x, b, i);
       const int e = entry(b, i);
@@ -388,8 +383,10 @@ __global__ void __launch_bounds__(kCopyThreads) k_paged_copy(const PagedView c, 
 
 // One block: pages in use are counted, then holes below that number and pages above it are
 // listed in the order of their ids.
-__global__ void __launch_bounds__(kPlanThreads) k_paged_compact(const PagedView c, const PlanWork w,
+template <int TH>
+__global__ void __launch_bounds__(TH, 1) k_paged_compact(const PagedView c, const PlanWork w,
                                                                 int32_t* used) {
+  constexpr int kWarps = TH / 32, kScanStep = TH * kScan;
   __shared__ PlanSmem sm;
   pdl_launch_dependents();
   const int tid = threadIdx.x;
@@ -399,7 +396,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_compact(const PagedView 
 #pragma unroll
     for (int j = 0; j < kScan; ++j) n += r[j] != 0 && id0 + tid * kScan + j < c.n_pages;
   }
-  before_me(n, sm, low);
+  before_me<kWarps>(n, sm, low);
   int holes = 0, moved = 0;
   for (int id0 = 0; id0 < c.n_pages; id0 += kScanStep) {
     int mine = 0, total;
@@ -411,7 +408,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_compact(const PagedView 
       mine += in && below && r[j] == 0 ? 1 : 0;
       mine += in && !below && r[j] != 0 ? 1 << 16 : 0;
     }
-    const int rank = before_me(mine, sm, total);  // (at most kScanStep of each: 15 bits)
+    const int rank = before_me<kWarps>(mine, sm, total);  // (at most kScanStep of each: 15 bits)
     int h = holes + (rank & 0xffff), m = moved + (rank >> 16);
 #pragma unroll
     for (int j = 0; j < kScan; ++j) {
@@ -426,7 +423,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_compact(const PagedView 
     moved += total >> 16;
   }
   __syncthreads();
-  for (int k = tid; k < moved; k += kPlanThreads) {
+  for (int k = tid; k < moved; k += TH) {
     const int from = __ldcg(w.old + k), to = __ldcg(w.fresh + k);
     w.a[from] = to;
     w.list[k] = Copy{from, to, 1 << c.shift, 0};
@@ -611,6 +608,13 @@ const char* check_work(const ssd_paged_cache* c, const void* workspace, size_t b
   return nullptr;
 }
 
+// Pools for which the planning block has 256 threads, whose barriers cost less, and above which 1024, which
+// look at more counts at once.
+#ifndef SMALL_POOL
+#define SMALL_POOL 8192
+#endif
+constexpr int kSmallPool = SMALL_POOL;
+
 // The launch that carries a plan out: up to four blocks an SM.
 template <typename Kern>
 cudaError_t carry_out(Kern k, const PagedView& v, const PlanWork& w, int most, int64_t more,
@@ -658,7 +662,8 @@ extern "C" ssd_status ssd_paged_reserve(const ssd_paged_cache* c, const int32_t*
   const PagedView v = paged_view(c);
   const PlanWork w = plan_work(workspace, c->n_pages);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  k_paged_reserve<<<1, kPlanThreads, 0, st>>>(v, w, pos, rows, M, err_dev);
+  if (c->n_pages <= kSmallPool) k_paged_reserve<256><<<1, 256, 0, st>>>(v, w, pos, rows, M, err_dev);
+  else k_paged_reserve<1024><<<1, 1024, 0, st>>>(v, w, pos, rows, M, err_dev);
   cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess)
     e = carry_out(k_paged_copy, v, w, c->n_seq < c->n_pages ? c->n_seq : c->n_pages, 1, st);
@@ -696,7 +701,8 @@ extern "C" ssd_status ssd_paged_compact(const ssd_paged_cache* c, int32_t* used,
   const PagedView v = paged_view(c);
   const PlanWork w = plan_work(workspace, c->n_pages);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  k_paged_compact<<<1, kPlanThreads, 0, st>>>(v, w, used);
+  if (c->n_pages <= kSmallPool) k_paged_compact<256><<<1, 256, 0, st>>>(v, w, used);
+  else k_paged_compact<1024><<<1, 1024, 0, st>>>(v, w, used);
   cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess)
     e = carry_out(k_paged_move, v, w, c->n_pages / 2,
