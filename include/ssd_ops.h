@@ -300,7 +300,7 @@ ssd_status ssd_paged_append(const ssd_paged_cache* cache, int32_t layer, const v
 /* Bytes of device workspace that ssd_paged_attention needs for these sizes, whatever the lengths
  * (256: it uses none, and takes NULL; 0: sizes that it refuses). */
 size_t ssd_paged_attention_bytes(const ssd_paged_cache* cache, int32_t n_heads, int32_t M,
-                                 int32_t longest);
+                                 int32_t window, int32_t longest);
 
 /* Attention over the pages of layer `layer`, softmax scale 1/sqrt(head_dim): q, n_heads, q_stride, M,
  * pos, rows, first, window, out, out_stride, workspace and the rows' sight as for ssd_kv8_attention;

@@ -38,7 +38,7 @@ struct PagedAttn : AttnArgs {
 // Where things stand in a block's shared memory.
 template <typename T, int HD, int R, int NB>
 struct PL {
-  static constexpr int NW = 4;
+  static constexpr int NW = sizeof(T) == 4 && NB == 1 ? 8 : 4;  // warps
   static constexpr int kRowBytes = HD * (int)sizeof(T);
   static constexpr int kChunks = kRowBytes / 16;           // 16-byte chunks of a row
   static constexpr int kKeys = kRowBytes > 256 ? 32 : 64;  // of a stage
@@ -79,6 +79,101 @@ __device__ __forceinline__ uint32_t numbers(uint32_t u, uint32_t& any) {
 __device__ __forceinline__ float4 lds4(const unsigned char* p) {
   return *reinterpret_cast<const float4*>(p);
 }
+
+// What a warp holds of up to 8 query rows, fp32: every lane has all rows, HD / 32 columns of each; a step is of
+// KEYS keys, a key's score the sum of 32 / KEYS lanes.
+template <int HD, int KEYS>
+struct FewTile {
+  static constexpr int kRows = 8, C = HD / 32, SUB = 32 / KEYS;
+  float o[kRows][C], mx[kRows], ls[kRows];
+  __device__ __forceinline__ void start(const AttnArgs&, const Kv8Item&, int) {
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      mx[r] = -INFINITY;
+      ls[r] = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) o[r][c] = 0.f;
+    }
+  }
+  // Keys kk0 .. kk0 + KEYS - 1 of a stage, of them key k0 the first.
+  template <typename L>
+  __device__ __forceinline__ uint32_t step(const AttnArgs& a, const Kv8Item& it, const float* Qs,
+                                           const unsigned char* sk, const unsigned char* sv, int kk0,
+                                           int k0, bool full) {
+    const int lane = threadIdx.x & 31, kk = lane / SUB, q = lane % SUB;
+    float4 k4[L::kChunks / SUB];
+#pragma unroll
+    for (int i = 0; i < L::kChunks / SUB; ++i) k4[i] = lds4(sk + L::place(kk0 + kk, i * SUB + q));
+    float p[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      p[r] = 0.f;
+      if (r >= it.nr) continue;
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < L::kChunks / SUB; ++i) {
+        const float4 u = *reinterpret_cast<const float4*>(Qs + r * L::kOPad + (i * SUB + q) * 4);
+        s = fmaf(u.x, k4[i].x, s);
+        s = fmaf(u.y, k4[i].y, s);
+        s = fmaf(u.z, k4[i].z, s);
+        s = fmaf(u.w, k4[i].w, s);
+      }
+#pragma unroll
+      for (int y = 1; y < SUB; y <<= 1) s += __shfl_xor_sync(0xffffffffu, s, y);
+      float z = s * a.scale;
+      if (!full) {
+        const int at = kv8_row_pos(a, it, it.r0 + r);
+        if (k0 + kk > at || k0 + kk < kv8_row_lo(it, at, a.window)) z = -INFINITY;
+      }
+      float nm = z;
+#pragma unroll
+      for (int y = SUB; y < 32; y <<= 1) nm = fmaxf(nm, __shfl_xor_sync(0xffffffffu, nm, y));
+      nm = fmaxf(nm, mx[r]);
+      if (nm != mx[r]) {  // (the same in all lanes)
+        const float f = exp2f(mx[r] - nm);
+        ls[r] *= f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[r][c] *= f;
+        mx[r] = nm;
+      }
+      p[r] = exp2f(z - (nm == -INFINITY ? 0.f : nm));
+      ls[r] += p[r];
+    }
+    uint32_t any = 0;
+#pragma unroll
+    for (int x = 0; x < KEYS; ++x) {
+      const unsigned char* const at = sv + L::place(kk0 + x, lane * C / 4) + (lane * C % 4) * 4;
+      float v[C];
+      if constexpr (C == 4) {
+        const float4 u = *reinterpret_cast<const float4*>(at);
+        v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
+      } else {
+        const float2 u = *reinterpret_cast<const float2*>(at);
+        v[0] = u.x, v[1] = u.y;
+      }
+      if (!full) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          if (no_number(v[c])) v[c] = 0.f, any = 1;
+      }
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        if (r >= it.nr) continue;
+        const float w = __shfl_sync(0xffffffffu, p[r], x * SUB);
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[r][c] = fmaf(w, v[c], o[r][c]);
+      }
+    }
+    return any;
+  }
+  // The rows' sums, of all lanes.
+  __device__ __forceinline__ void sum_up() {
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int y = SUB; y < 32; y <<= 1) ls[r] += __shfl_xor_sync(0xffffffffu, ls[r], y);
+  }
+};
 
 // What a warp holds of 16 query rows, fp32: lane n8, t has rows n8 and n8 + 8.
 template <int HD>
@@ -361,8 +456,7 @@ __device__ __forceinline__ void finish_rows(const PagedAttn& a, const Kv8Seg& sg
 template <typename T, int HD, int R, int NB>
 __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(const PagedAttn a) {
   using L = PL<T, HD, R, NB>;
-  static_assert(sizeof(T) == 2 || NB == 2, "fp32 rows are held by sixteens");
-  constexpr bool BF = sizeof(T) == 2;
+  constexpr bool BF = sizeof(T) == 2, FEW = !BF && NB == 1;
   constexpr int NT = HD / 8;   // 8-column tiles of the output
   constexpr int KS = HD / 16;  // 16-column steps of a score
   extern __shared__ __align__(1024) unsigned char smem[];
@@ -452,7 +546,9 @@ __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(co
         *reinterpret_cast<float4*>(Qs + row * L::kOPad + c4 * 4) = u;
       }
     }
-    typename std::conditional<BF, ColTile<HD, NB>, RowTile<HD>>::type w;
+    typename std::conditional<
+        BF, ColTile<HD, NB>,
+        typename std::conditional<FEW, FewTile<HD, L::kGroupKeys>, RowTile<HD>>::type>::type w;
     w.start(a, it, rt * L::kWarpRows);
     // every row of the item sees keys full_lo .. full_hi
     const int full_lo = kv8_row_lo(it, it.hi, a.window);
@@ -468,17 +564,18 @@ __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(co
       const unsigned char* const sv = sk + L::kSide;
 #pragma unroll 1
       for (int x0 = 0; x0 < L::kGroupKeys; x0 += 16) {
-        // the warp's 16 keys (fp32: 8 where a group has no more): lane n8, t has rows n8 and n8 + 8,
-        // keys 8 n + 2 t and 8 n + 2 t + 1
-        constexpr int kN = L::kGroupKeys < 16 ? 1 : 2;
+        // the warp's 16 keys, or 8 kN, or as many as its group has
+        constexpr int kN = L::kGroupKeys < 16 ? 1 : 2, kStep = FEW ? L::kGroupKeys : 8 * kN;
         const int kk0 = grp * L::kGroupKeys + x0, k0 = seg0 + s * L::kKeys + kk0;
-        if (!some || k0 >= ke || k0 + 8 * kN <= kb) continue;
-        const bool full = k0 >= full_lo && k0 + 8 * kN - 1 <= full_hi;
+        if (!some || k0 >= ke || k0 + kStep <= kb) continue;
+        const bool full = k0 >= full_lo && k0 + kStep - 1 <= full_hi;
         uint32_t any = 0;
         if constexpr (BF) {
           any = w.template step<L>(qf, smem_u32(sk), smem_u32(sv), kk0, k0, full, a.scale);
+        } else if constexpr (FEW) {
+          any = w.template step<L>(a, it, Qs, sk, sv, kk0, k0, full);
         } else {
-          float p[2][4];
+          float p[2][4];  // lane n8, t: rows n8 and n8 + 8, keys 8 n + 2 t and 8 n + 2 t + 1
 #pragma unroll
           for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -551,6 +648,13 @@ __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(co
             s_m[grp][rt * L::kWarpRows + 8 * b + 2 * t + i] = w.mx[b][i];
             s_l[grp][rt * L::kWarpRows + 8 * b + 2 * t + i] = w.ls[b][i];
           }
+    } else if constexpr (FEW) {
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+        if (lane == 0) {
+          s_m[grp][r] = w.mx[r];
+          s_l[grp][r] = w.ls[r];
+        }
     } else {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -586,6 +690,13 @@ __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(co
               p[16 * j + 8] = w.o[j][b][2 + i];
             }
         }
+    } else if constexpr (FEW) {
+      constexpr int C = HD / 32;
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+        if (r < it.nr)
+#pragma unroll
+          for (int c = 0; c < C; ++c) Ox[(size_t)(grp * L::kRows + r) * L::kOPad + lane * C + c] = w.o[r][c];
     } else {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -697,11 +808,13 @@ cudaError_t prep_stream() {
 }
 template <int HD>
 cudaError_t prep_hd() {
-  cudaError_t e = prep<float, HD, 1, 2>();
+  cudaError_t e = prep<float, HD, 1, 1>();
+  if (e == cudaSuccess) e = prep<float, HD, 1, 2>();
   if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 1, 1>();
   if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 1, 2>();
   if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 2, 2>();
-  if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 4, 2>();
+  if constexpr (HD == 64)
+    if (e == cudaSuccess) e = prep<__nv_bfloat16, HD, 4, 2>();
   if (e == cudaSuccess) e = prep_stream<HD, 1>();
   if (e == cudaSuccess) e = prep_stream<HD, 2>();
   return e;
@@ -731,11 +844,6 @@ cudaError_t paged_device(int* sms) {
 // second launch): 1, 2, 4 or 8 blocks with 128 keys or more each, as long as there is room for all.
 constexpr int kSplitKeys = 128, kSplitBlocks = 304, kSplitSeq = 512, kSplitMost = 2048;
 
-#ifndef PWIDE_FROM
-#define PWIDE_FROM 64
-#endif
-constexpr int kWideFrom = PWIDE_FROM;
-
 struct PagedPlan {
   int wide;   // accumulators of a tile on tcgen05, 0: mma.sync
   bool stream;  // k_paged_stream
@@ -745,22 +853,23 @@ struct PagedPlan {
   int max_blocks, part_rows;
   long long n_rt, units;  // tiles of a sequence; the line's places, at most
 };
-PagedPlan plan_of(const ssd_paged_cache* c, int n_heads, int M, int longest) {
+PagedPlan plan_of(const ssd_paged_cache* c, int n_heads, int M, int longest, int window) {
   PagedPlan p;
   const long long rows = (long long)M * (n_heads / c->n_kv_heads);
   const long long heads = (long long)c->n_seq * c->n_kv_heads;
   p.tiles = c->dtype == SSD_DTYPE_F32 || rows <= kTile ? 1 : rows <= 2 * kTile ? 2 : 4;
-  p.eights = c->dtype == SSD_DTYPE_F32 || rows > 8 ? 2 : 1;
+  p.eights = rows > 8 ? 2 : 1;
   int rt = p.tiles * p.eights * 8;
   p.n_rt = (rows + rt - 1) / rt;
   long long items = p.n_rt * heads;
+  // keys that an item's rows see, at most
+  const int span = window > 0 && window < longest - M ? window + M : longest;
   p.split = 1;
-  while (p.split < kSplitMax && longest > kSplitKeys * p.split && items * p.split * 2 <= kSplitBlocks)
+  while (p.split < kSplitMax && span > kSplitKeys * p.split && items * p.split * 2 <= kSplitBlocks)
     p.split *= 2;
-  if (longest > kSplitSeq * p.split || longest > kSplitMost) p.split = 0;
+  if (span > kSplitSeq * p.split || span > kSplitMost) p.split = 0;
   p.wide = 0;
-  if (c->dtype == SSD_DTYPE_BF16 && c->head_dim == kWHd && rows > kWideFrom &&
-      !(p.split && items * p.split <= kSplitBlocks)) {
+  if (c->dtype == SSD_DTYPE_BF16 && c->head_dim == kWHd && rows > (p.split ? 2 * kTile : kTile)) {
     p.wide = rows > kWRows ? 2 : 1;
     p.split = 0;
     rt = p.wide * kWRows;
@@ -769,26 +878,27 @@ PagedPlan plan_of(const ssd_paged_cache* c, int n_heads, int M, int longest) {
   }
   p.stream = !p.wide && !p.split && c->dtype == SSD_DTYPE_BF16 && rows <= kTile;
   p.part_rows = rows < rt ? (int)rows : rt;
-  p.units = items * ((longest + kUnit - 1) / kUnit +
+  p.units = items * ((span + 2 * kUnit - 2) / kUnit +
                      (p.wide == 2 ? kKv8ItemCost<256> : kKv8ItemCost<kTile>));
   p.max_blocks = p.wide || p.stream ? kKv8MaxBlocks / 2 : kKv8MaxBlocks;
   if (p.units < p.max_blocks) p.max_blocks = (int)p.units;
   return p;
 }
 
-const char* check_attention(const ssd_paged_cache* c, int32_t n_heads, int32_t M, int32_t longest,
-                            PagedPlan* plan, ssd_status* status) {
+const char* check_attention(const ssd_paged_cache* c, int32_t n_heads, int32_t M, int32_t window,
+                            int32_t longest, PagedPlan* plan, ssd_status* status) {
   if (const char* why = check_paged(c, status)) return why;
   *status = SSD_ERR_INVALID_ARG;
   if (n_heads < c->n_kv_heads || n_heads % c->n_kv_heads || n_heads > 65536)
     return "n_heads must be a multiple of the cache's n_kv_heads";
   if (M < 1) return "M must be at least 1";
+  if (window < 0) return "window must be 0 (none) or positive";
   if (longest < 0) return "longest must be 0 (the cache's positions) or positive";
   *status = SSD_ERR_CAPACITY;
   const int cap = c->max_pages * c->page;
   if (M > cap) return "more rows than the cache has positions";
   if (longest > cap) return "longest: more than the cache has positions";
-  *plan = plan_of(c, n_heads, M, longest ? longest : cap);
+  *plan = plan_of(c, n_heads, M, longest ? longest : cap, window);
   if (plan->units > 0x7fffffffll) return "n_seq x M x longest: more than 2^31 units of work";
   *status = SSD_OK;
   return nullptr;
@@ -829,23 +939,26 @@ cudaError_t wide_launch(const PagedAttn& a, int P, cudaStream_t st) {
 template <int HD>
 cudaError_t launch(const PagedAttn& a, int dtype, const PagedPlan& p, int P, cudaStream_t st) {
   using B = __nv_bfloat16;
-  if (dtype == SSD_DTYPE_F32) return rows_launch<float, HD, 1, 2>(a, P, st);
+  if (dtype == SSD_DTYPE_F32)
+    return p.eights == 1 ? rows_launch<float, HD, 1, 1>(a, P, st) : rows_launch<float, HD, 1, 2>(a, P, st);
   if (p.wide) return p.wide == 2 ? wide_launch<2>(a, P, st) : wide_launch<1>(a, P, st);
   if (p.stream) return p.eights == 1 ? stream_launch<HD, 1>(a, P, st) : stream_launch<HD, 2>(a, P, st);
   if (p.eights == 1) return rows_launch<B, HD, 1, 1>(a, P, st);
   if (p.tiles == 1) return rows_launch<B, HD, 1, 2>(a, P, st);
-  return p.tiles == 2 ? rows_launch<B, HD, 2, 2>(a, P, st) : rows_launch<B, HD, 4, 2>(a, P, st);
+  if constexpr (HD == 64)
+    if (p.tiles == 4) return rows_launch<B, HD, 4, 2>(a, P, st);
+  return rows_launch<B, HD, 2, 2>(a, P, st);
 }
 
 }  // namespace
 }  // namespace ssd
 
 extern "C" size_t ssd_paged_attention_bytes(const ssd_paged_cache* c, int32_t n_heads, int32_t M,
-                                            int32_t longest) {
+                                            int32_t window, int32_t longest) {
   using namespace ssd;
   ssd_status status;
   PagedPlan p;
-  if (const char* why = check_attention(c, n_heads, M, longest, &p, &status)) {
+  if (const char* why = check_attention(c, n_heads, M, window, longest, &p, &status)) {
     fail_op(status, why);
     return 0;
   }
@@ -861,7 +974,7 @@ extern "C" ssd_status ssd_paged_attention(const ssd_paged_cache* c, int32_t laye
   using namespace ssd;
   ssd_status status;
   PagedPlan plan;
-  if (const char* why = check_attention(c, n_heads, M, longest, &plan, &status))
+  if (const char* why = check_attention(c, n_heads, M, window, longest, &plan, &status))
     return fail_op(status, why);
   if (layer < 0 || layer >= c->n_layers)
     return fail_op(SSD_ERR_INVALID_ARG, "layer must be in 0..n_layers - 1");
@@ -875,7 +988,6 @@ extern "C" ssd_status ssd_paged_attention(const ssd_paged_cache* c, int32_t laye
                    "q_stride or out_stride: below a row's length, or not a multiple of 16 bytes");
   if (out == q && out_stride != q_stride)
     return fail_op(SSD_ERR_INVALID_ARG, "out is q, but their strides differ");
-  if (window < 0) return fail_op(SSD_ERR_INVALID_ARG, "window must be 0 (none) or positive");
   const Kv8Work lay = kv8_work(plan.max_blocks, plan.part_rows, c->head_dim);
   if (!plan.split) {
     if (!workspace || ((uintptr_t)workspace & 255u))

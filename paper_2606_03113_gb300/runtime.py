@@ -505,7 +505,7 @@ class PagedKVCache:
         self._plan_bytes = S.ssd_paged_workspace_bytes(self._c) if device.type == "cuda" else 0
         self._plan = torch.empty(self._plan_bytes, dtype=torch.uint8, device=device)
         self._plan_at = self._plan.data_ptr()
-        self._work = {}  # (n_heads, M, longest) -> workspace bytes
+        self._work = {}  # (n_heads, M, window, longest) -> workspace bytes
 
     def _rows(self, x: torch.Tensor, heads: int, what: str) -> tuple[int, int]:
         """(M, elements between rows) of x [n_seq, M, heads, head_dim]."""
@@ -624,10 +624,10 @@ class PagedKVCache:
             raise ValueError(f"window must be 0 (none) or a positive int32, not {window}")
         if not 0 <= longest <= self.max_seq:
             raise ValueError(f"longest must be in 0..{self.max_seq}, not {longest}")
-        key = (heads, M, longest)
+        key = (heads, M, window, longest)
         nbytes = self._work.get(key)
         if nbytes is None:
-            nbytes = S.ssd_paged_attention_bytes(self._c, heads, M, longest)
+            nbytes = S.ssd_paged_attention_bytes(self._c, heads, M, window, longest)
             if len(self._work) < 4096:  # (a caller may pass another `longest` every step)
                 self._work[key] = nbytes
         there = _elsewhere(self.device, stream)

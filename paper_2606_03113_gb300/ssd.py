@@ -162,7 +162,7 @@ SIGNATURES = {
     "ssd_paged_fork": (C.c_int, [_P, _P, _P, _P, _P]),
     "ssd_paged_compact": (C.c_int, [_P, _P, _P, _SZ, _P, _P]),
     "ssd_paged_append": (C.c_int, [_P, _I32, _P, _P, _I64, _I32, _P, _P, _P, _P]),
-    "ssd_paged_attention_bytes": (_SZ, [_P, _I32, _I32, _I32]),
+    "ssd_paged_attention_bytes": (_SZ, [_P, _I32, _I32, _I32, _I32]),
     "ssd_paged_attention": (C.c_int, [_P, _I32, _P, _I32, _I64, _I32, _P, _P, _P, _I32, _I32, _P, _I64,
                                       _P, _SZ, _P, _P]),
     "ssd_synth_fill": (C.c_int, [_P, _I32, _U64, _U32, _U32, C.c_double, _P]),
@@ -415,8 +415,9 @@ def ssd_paged_append(cache: ssd_paged_cache, layer: int, k_ptr: int, v_ptr: int,
         _check(st, "ssd_paged_append")
 
 
-def ssd_paged_attention_bytes(cache: ssd_paged_cache, n_heads: int, M: int, longest: int = 0) -> int:
-    return lib().ssd_paged_attention_bytes(C.addressof(cache), n_heads, M, longest)
+def ssd_paged_attention_bytes(cache: ssd_paged_cache, n_heads: int, M: int, window: int = 0,
+                              longest: int = 0) -> int:
+    return lib().ssd_paged_attention_bytes(C.addressof(cache), n_heads, M, window, longest)
 
 
 def ssd_paged_attention(cache: ssd_paged_cache, layer: int, q_ptr: int, n_heads: int, q_stride: int,
