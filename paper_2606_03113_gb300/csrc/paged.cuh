@@ -7,6 +7,7 @@
 #pragma once
 
 #include "kv8.cuh"
+#include "mma.cuh"
 
 namespace ssd {
 
@@ -65,6 +66,29 @@ struct PageWalk {
     return max(e, 0);
   }
 };
+
+// Copies keys k0 .. k0 + KEYS - 1 and their values to shared memory, zeros for those outside of kb .. ke - 1, as
+// one of the threads that hold PASS rows at a time: kp, vp at its chunk of its row (r0, below PASS) of position 0 of
+// page 0, to(r) where that chunk of row r of the keys goes, `side` bytes in front of the values'.
+template <int KEYS, int ROW_BYTES, int PASS, typename To>
+__device__ __forceinline__ void copy_keys(PageWalk& walk, const char* kp, const char* vp, int r0, int k0,
+                                          int kb, int ke, uint32_t side, To to) {
+  static_assert(16 % PASS == 0, "sixteen positions lie in one page");
+  const bool all = k0 >= kb && k0 + KEYS <= ke;
+#pragma unroll
+  for (int j = 0; j < KEYS; j += 16) {
+    const size_t off = (size_t)walk.page(k0 + j) * walk.view->bytes +
+                       (size_t)((k0 + j) & ((1 << walk.view->shift) - 1)) * ROW_BYTES;
+#pragma unroll
+    for (int i = 0; i < 16; i += PASS) {
+      const int key = k0 + j + i + r0;
+      const bool in = all || (key >= kb && key < ke);
+      const uint32_t at = to(j + i);
+      cp_async16(at, kp + off + i * ROW_BYTES, in);
+      cp_async16(at + side, vp + off + i * ROW_BYTES, in);
+    }
+  }
+}
 
 // Checks of a cache that every entry point makes; null: fine.
 const char* check_paged(const ssd_paged_cache* c, ssd_status* status) noexcept;

@@ -30,6 +30,22 @@ constexpr int kUnit = kKv8Block;  // keys of a unit of the plan
 constexpr int kTile = 16;         // query rows of a warp, at most
 constexpr int kSplitMax = 8;      // blocks of a short sequence's item, a cluster, at most
 
+// The cluster's barrier in two halves (a warp's lanes can come apart), and writes to another block's shared memory.
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ void st_cluster_f32x2(uint32_t at, float2 v) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(v.x), "f"(v.y) : "memory");
+}
+__device__ __forceinline__ void st_cluster_f32x4(uint32_t at, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(v.x), "f"(v.y), "f"(v.z),
+               "f"(v.w)
+               : "memory");
+}
+
 struct PagedAttn : AttnArgs {
   PagedView c;
   const char *k, *v;  // the layer's K and V in page 0
@@ -57,12 +73,19 @@ struct PL {
   static constexpr int kCopies = kKeys * kChunks / kThreads;  // of a thread, a stage and side
   static constexpr int kLook = kKeys / 16;                     // pages of a stage, at most
   static_assert(kExchange + kRows * HD * 4 <= kRing, "the exchange and the part fit the ring");
+  static_assert(kRows % kSplitMax == 0, "a cluster's blocks have as many rows each");
   static_assert(kKeys * kChunks % kThreads == 0 && kThreads % kChunks == 0, "whole rows a pass");
   // Chunk ch of row r: bf16 rows as ldmatrix wants them; fp32 rows such that eight lanes meet
   // all banks, as two keys x four chunks and as four keys of one parity x two.
   __device__ static __forceinline__ uint32_t place(int r, int ch) {
     const int x = sizeof(T) == 2 ? r & 7 : (r & 6) ^ ((r & 1) << 2);
     return (uint32_t)(r * kRowBytes + ((ch ^ x) << 4));
+  }
+  // The same for row r0 + r, with at0 = place(r0, ch), r a multiple of PASS and r0 below it.
+  template <int PASS>
+  __device__ static __forceinline__ uint32_t place_from(uint32_t at0, int r) {
+    return PASS % 8 == 0 ? at0 + (uint32_t)(r * kRowBytes)
+                         : (at0 ^ (uint32_t)((r & 4) << 4)) + (uint32_t)(r * kRowBytes);
   }
 };
 
@@ -108,7 +131,7 @@ struct FewTile {
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
       p[r] = 0.f;
-      if (r >= it.nr) continue;
+      if (r >= it.nr) break;
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < L::kChunks / SUB; ++i) {
@@ -140,28 +163,31 @@ struct FewTile {
       ls[r] += p[r];
     }
     uint32_t any = 0;
+    float v[KEYS][C];
 #pragma unroll
     for (int x = 0; x < KEYS; ++x) {
       const unsigned char* const at = sv + L::place(kk0 + x, lane * C / 4) + (lane * C % 4) * 4;
-      float v[C];
       if constexpr (C == 4) {
         const float4 u = *reinterpret_cast<const float4*>(at);
-        v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
+        v[x][0] = u.x, v[x][1] = u.y, v[x][2] = u.z, v[x][3] = u.w;
       } else {
         const float2 u = *reinterpret_cast<const float2*>(at);
-        v[0] = u.x, v[1] = u.y;
+        v[x][0] = u.x, v[x][1] = u.y;
       }
       if (!full) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
-          if (no_number(v[c])) v[c] = 0.f, any = 1;
+          if (no_number(v[x][c])) v[x][c] = 0.f, any = 1;
       }
+    }
 #pragma unroll
-      for (int r = 0; r < kRows; ++r) {
-        if (r >= it.nr) continue;
+    for (int r = 0; r < kRows; ++r) {
+      if (r >= it.nr) break;
+#pragma unroll
+      for (int x = 0; x < KEYS; ++x) {
         const float w = __shfl_sync(0xffffffffu, p[r], x * SUB);
 #pragma unroll
-        for (int c = 0; c < C; ++c) o[r][c] = fmaf(w, v[c], o[r][c]);
+        for (int c = 0; c < C; ++c) o[r][c] = fmaf(w, v[x][c], o[r][c]);
       }
     }
     return any;
@@ -376,13 +402,13 @@ struct ColTile {
 };
 
 // The rows of a block's part of an item, from what GROUPS groups of warps left: outputs in Ox
-// [GROUPS][ROWS][HD + 4], weights s_w (NULL: 1), the rows' maxima and sums. Of keys kb .. ke - 1. To `part` in shared
-// memory for a cluster's join, to the output, or to the workspace.
-template <typename T, int HD, int GROUPS, int ROWS, int THREADS>
+// [GROUPS][ROWS][HD + 4], weights s_w (NULL: 1), the rows' maxima and sums. Of keys kb .. ke - 1. To the output,
+// to the workspace, or, for a cluster's join, where `put` says.
+template <typename T, int HD, int GROUPS, int ROWS, int THREADS, typename Put>
 __device__ __forceinline__ void finish_rows(const PagedAttn& a, const Kv8Seg& sg, int kb, int ke,
                                             const float* Ox, const float (*s_w)[ROWS],
-                                            const float* s_gm, const float* s_sum, bool bad,
-                                            float* part, int tid) {
+                                            const float* s_gm, const float* s_sum, bool bad, int tid,
+                                            Put put) {
   constexpr int NT = HD / 8, kOPad = HD + 4;
   const Kv8Item& it = sg.it;
   const bool whole = sg.whole();
@@ -436,7 +462,7 @@ __device__ __forceinline__ void finish_rows(const PagedAttn& a, const Kv8Seg& sg
         if (sum[j] != 0.f) acc[j] = sum[j];
     }
     if (a.split > 1) {
-      store_out8(part + row * HD + c8, acc);
+      put(row, c8, acc);
     } else if (whole) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
@@ -463,48 +489,53 @@ __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(co
   __shared__ Kv8PlanSmem s_plan;
   __shared__ float s_m[L::kGroups][L::kRows], s_l[L::kGroups][L::kRows], s_w[L::kGroups][L::kRows];
   __shared__ float s_gm[L::kRows], s_sum[L::kRows];
+  __shared__ float2 s_in[kSplitMax][L::kRows];  // of a cluster's join: (max, sum) of the blocks' parts
   __shared__ int s_bad;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int t = lane & 3, n8 = lane >> 2;
   const int rt = warp % R, grp = warp / R;
   float* const Ox = reinterpret_cast<float*>(smem);
-  float* const part = Ox + L::kExchange / 4;  // [rows][HD]: the block's part of a cluster's item
-  const int pmask = (1 << a.c.shift) - 1;
+  // a cluster's join: block `row % split` takes the row, [its rows][HD] of each block's part
+  float* const parts = Ox + L::kExchange / 4;
+  constexpr int kPass = L::kThreads / L::kChunks;  // rows of a pass of copies
+  const int ch = tid % L::kChunks, r0 = tid / L::kChunks;
+  const uint32_t at0 = L::place(r0, ch);
 
-  Kv8Cursor cur = kv8_plan<L::kRows, kUnit, L::kThreads>(a, s_plan);
-  pdl_launch_dependents();
-  if (tid == 0 && !a.split) a.desc[blockIdx.x].nr = 0;
-  if (tid < L::kRows) s_sum[tid] = 0.f, s_gm[tid] = -INFINITY;
+  Kv8Cursor cur;
   Kv8Seg sg;
-  while (kv8_next<L::kRows, kUnit>(a, cur, sg)) {
+  bool more;
+  const int rank = a.split > 1 ? (int)blockIdx.x % a.split : 0;
+  if (a.split) {  // the block's share of its cluster's item
+    const int i = (int)blockIdx.x / a.split, e = i / a.Hkv;
+    sg.it = kv8_entry<L::kRows, kUnit>(a, e);
+    sg.g = i - e * a.Hkv;
+    sg.u0 = sg.it.units * rank / a.split;
+    sg.nu = sg.it.units * (rank + 1) / a.split - sg.u0;
+    more = sg.nu > 0;
+  } else {
+    cur = kv8_plan<L::kRows, kUnit, L::kThreads>(a, s_plan);
+    pdl_launch_dependents();
+    if (tid == 0) a.desc[blockIdx.x].nr = 0;
+    more = kv8_next<L::kRows, kUnit>(a, cur, sg);
+  }
+  while (more) {
     const Kv8Item& it = sg.it;
     const int g = sg.g;
     const int seg0 = (it.unit0 + sg.u0) * kUnit;
     const int kb = max(it.lo, seg0), ke = min(it.hi + 1, seg0 + sg.nu * kUnit);
     const int nst = ke > kb ? (ke - seg0 + L::kKeys - 1) / L::kKeys : 0;
     const int st0 = ke > kb ? (kb - seg0) / L::kKeys : 0;
-    const char* const kp = a.k + g * a.c.head();
-    const char* const vp = a.v + g * a.c.head();
+    const char* const kp = a.k + g * a.c.head() + r0 * L::kRowBytes + ch * 16;
+    const char* const vp = kp + (a.v - a.k);
 
     // ---- stages
-    const int ch = tid % L::kChunks, r0 = tid / L::kChunks;
     PageWalk walk(a.c, a.err);
     auto issue = [&](int s) {
       if (s < nst) {
-        const uint32_t dst = smem_u32(smem) + (uint32_t)(s % L::kNst) * L::kStage;
-        int look[L::kLook];
-#pragma unroll
-        for (int j = 0; j < L::kLook; ++j) look[j] = walk.page(seg0 + s * L::kKeys + 16 * j);
-#pragma unroll
-        for (int i = 0; i < L::kCopies; ++i) {
-          const int r = r0 + i * (L::kThreads / L::kChunks), key = seg0 + s * L::kKeys + r;
-          const bool in = key >= kb && key < ke;
-          const size_t off = (size_t)look[(i * (L::kThreads / L::kChunks)) / 16] * a.c.bytes +
-                             (size_t)(key & pmask) * L::kRowBytes + ch * 16;
-          const uint32_t at = dst + L::place(r, ch);
-          cp_async16(at, kp + (in ? off : 0), in);
-          cp_async16(at + L::kSide, vp + (in ? off : 0), in);
-        }
+        const uint32_t dst = smem_u32(smem) + (uint32_t)(s % L::kNst) * L::kStage + at0;
+        copy_keys<L::kKeys, L::kRowBytes, kPass>(
+            walk, kp, vp, r0, seg0 + s * L::kKeys, kb, ke, L::kSide,
+            [&](int r) { return L::template place_from<kPass>(dst, r); });
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -664,6 +695,7 @@ __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(co
         }
     }
     __syncthreads();  // nobody reads the ring any more
+    if (a.split > 1) cluster_arrive();
     if (tid < L::kRows) {
       float gm = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -710,36 +742,55 @@ __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(co
       }
     }
     __syncthreads();
-    finish_rows<T, HD, L::kGroups, L::kRows, L::kThreads>(a, sg, kb, ke, Ox, s_w, s_gm, s_sum, s_bad,
-                                                           part, tid);
-    if (!a.split && !sg.whole() && sg.u0 == 0 && tid == 0) a.desc[blockIdx.x] = kv8_desc(a, cur, sg);
-    __syncthreads();
-  }
-  if (a.split > 1) {  // the cluster's parts together, each block some of the columns
-    const int i = (int)blockIdx.x / a.split, rank = (int)blockIdx.x - i * a.split;
-    const int e = i / a.Hkv, g = i - e * a.Hkv;
-    const Kv8Item it = kv8_entry<L::kRows, kUnit>(a, e);
-    cluster_sync();
-    for (int x = rank * L::kThreads + tid; x < it.nr * NT; x += a.split * L::kThreads) {
-      const int row = x / NT, c8 = (x % NT) * 8;
-      float w[kSplitMax], m[kSplitMax], gm = -INFINITY, sum = 0.f, acc[8];
-#pragma unroll
-      for (int y = 0; y < kSplitMax; ++y) {
-        w[y] = y < a.split ? ld_cluster_f32(in_block(&s_sum[row], y)) : 0.f;
-        m[y] = y < a.split ? ld_cluster_f32(in_block(&s_gm[row], y)) : 0.f;
+    if (a.split > 1) {
+      cluster_wait();  // nobody reads its ring any more
+      if (tid < it.nr) {
+        const float2 v = make_float2(s_gm[tid], s_sum[tid]);
+        st_cluster_f32x2(in_block(&s_in[rank][tid], tid % a.split), v);
       }
-#pragma unroll
-      for (int y = 0; y < kSplitMax; ++y)  // (a sum of 0: the row sees none of the part's keys)
-        gm = fmaxf(gm, w[y] != 0.f ? m[y] : -INFINITY);
+    }
+    finish_rows<T, HD, L::kGroups, L::kRows, L::kThreads>(
+        a, sg, kb, ke, Ox, s_w, s_gm, s_sum, s_bad, tid, [&](int row, int c8, const float (&acc)[8]) {
+          float* const p = parts + ((size_t)rank * (L::kRows / a.split) + row / a.split) * HD + c8;
+          const uint32_t at = in_block(p, row % a.split);
+          st_cluster_f32x4(at, make_float4(acc[0], acc[1], acc[2], acc[3]));
+          st_cluster_f32x4(at + 16, make_float4(acc[4], acc[5], acc[6], acc[7]));
+        });
+    if (a.split) break;
+    if (!sg.whole() && sg.u0 == 0 && tid == 0) a.desc[blockIdx.x] = kv8_desc(a, cur, sg);
+    __syncthreads();
+    more = kv8_next<L::kRows, kUnit>(a, cur, sg);
+  }
+  if (a.split > 1) {
+    const Kv8Item& it = sg.it;
+    if (!more) {  // no keys for this block: a sum of 0
+      cluster_arrive();
+      cluster_wait();
+      if (tid < it.nr)
+        st_cluster_f32x2(in_block(&s_in[rank][tid], tid % a.split), make_float2(-INFINITY, 0.f));
+    }
+    cluster_arrive();
+    cluster_wait();  // every block's parts of this one's rows are here
+    for (int x = tid; x < (it.nr + a.split - 1 - rank) / a.split * NT; x += L::kThreads) {
+      const int mine = x / NT, row = mine * a.split + rank, c8 = (x % NT) * 8;
+      float w[kSplitMax], gm = -INFINITY, sum = 0.f, acc[8];
       uint32_t has = 0;  // parts whose keys the row sees (of the others there may be nothing to read)
 #pragma unroll
       for (int y = 0; y < kSplitMax; ++y) {
-        if (w[y] != 0.f) {
+        if (y >= a.split) break;
+        const float2 v = s_in[y][row];
+        w[y] = v.y;
+        if (v.y != 0.f) {
           has |= 1u << y;
-          w[y] *= part_weight(m[y], gm);
+          gm = fmaxf(gm, v.x);
         }
-        sum += w[y];
       }
+#pragma unroll
+      for (int y = 0; y < kSplitMax; ++y)
+        if (has >> y & 1) {
+          w[y] *= part_weight(s_in[y][row].x, gm);
+          sum += w[y];
+        }
       // (the parts are weighed by w / sum: w times a large value can be out of range; a row whose
       // every score is -inf has no sum)
       const float inv = 1.f / sum, none = sum == 0.f ? __uint_as_float(0x7fffffffu) : 0.f;
@@ -748,19 +799,20 @@ __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(co
 #pragma unroll
       for (int y = 0; y < kSplitMax; ++y) {
         if (!(has >> y & 1)) continue;
-        const uint32_t at = in_block(part + row * HD + c8, y);
-        const float4 u = ld_cluster_f32x4(at), v = ld_cluster_f32x4(at + 16);
+        const float4* u = reinterpret_cast<const float4*>(
+            parts + ((size_t)y * (L::kRows / a.split) + mine) * HD + c8);
+        const float4 lo = u[0], hi = u[1];
         const float wt = w[y] * inv;
-        acc[0] = fmaf(wt, u.x, acc[0]);
-        acc[1] = fmaf(wt, u.y, acc[1]);
-        acc[2] = fmaf(wt, u.z, acc[2]);
-        acc[3] = fmaf(wt, u.w, acc[3]);
-        acc[4] = fmaf(wt, v.x, acc[4]);
-        acc[5] = fmaf(wt, v.y, acc[5]);
-        acc[6] = fmaf(wt, v.z, acc[6]);
-        acc[7] = fmaf(wt, v.w, acc[7]);
+        acc[0] = fmaf(wt, lo.x, acc[0]);
+        acc[1] = fmaf(wt, lo.y, acc[1]);
+        acc[2] = fmaf(wt, lo.z, acc[2]);
+        acc[3] = fmaf(wt, lo.w, acc[3]);
+        acc[4] = fmaf(wt, hi.x, acc[4]);
+        acc[5] = fmaf(wt, hi.y, acc[5]);
+        acc[6] = fmaf(wt, hi.z, acc[6]);
+        acc[7] = fmaf(wt, hi.w, acc[7]);
       }
-      const int r = it.r0 + row, mr = a.byG(r), h = g * a.G + r - mr * a.G;
+      const int r = it.r0 + row, mr = a.byG(r), h = sg.g * a.G + r - mr * a.G;
       const int p = kv8_row_pos(a, it, r);
       const bool sees = kv8_row_lo(it, p, a.window) <= p;
 #pragma unroll
@@ -769,7 +821,6 @@ __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(co
                      (int64_t)h * HD + c8,
                  acc);
     }
-    cluster_sync();  // everybody has read this block's part
   }
 }
 

@@ -68,7 +68,6 @@ __global__ void __launch_bounds__(SL<HD, NB>::kThreads, 1) k_paged_stream(const 
   __shared__ Kv8Seg s_seg[2];  // the items under way, as the copying warps hand them on
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int t = lane & 3, n8 = lane >> 2;
-  const int pmask = (1 << a.c.shift) - 1;
   if (tid == 0) {
     for (int i = 0; i < L::kNst; ++i) {
       mbar_init(&bar.full[i], L::kCopy * 32);
@@ -104,6 +103,7 @@ __global__ void __launch_bounds__(SL<HD, NB>::kThreads, 1) k_paged_stream(const 
     const int ct = tid - L::kUse * 32;
     const int ch = ct % L::kChunks, r0 = ct / L::kChunks;
     constexpr int kPass = L::kCopy * 32 / L::kChunks;  // rows of a pass
+    const uint32_t at0 = L::P::place(r0, ch);
     // the next segment is found, and its first pages are looked up, while the last stage of the one
     // before waits for its place
     Kv8Seg next;
@@ -141,25 +141,15 @@ __global__ void __launch_bounds__(SL<HD, NB>::kThreads, 1) k_paged_stream(const 
       const int seg0 = sp.seg0, kb = sp.kb, ke = sp.ke, last = sp.last;
       PageWalk walk = ahead;
       if (sp.first >= last) more = look();
-      const char* const kp = a.k + sg.g * a.c.head() + ch * 16;
-      const char* const vp = a.v + sg.g * a.c.head() + ch * 16;
+      const char* const kp = a.k + sg.g * a.c.head() + r0 * HD * 2 + ch * 16;
+      const char* const vp = kp + (a.v - a.k);
       for (int s = sp.first; s < last; ++s, ++n, ring.next()) {
         if (s == last - 1) more = look();
         if (n >= (uint32_t)L::kNst) p_wait(&bar.empty[ring.at], ring.phase ^ 1, bad);
-        const uint32_t dst = smem_u32(smem) + ring.at * L::kStage;
-        int page[L::kKeys / 16];
-#pragma unroll
-        for (int j = 0; j < L::kKeys / 16; ++j) page[j] = walk.page(seg0 + s * L::kKeys + 16 * j);
-#pragma unroll
-        for (int j = 0; j < L::kKeys / kPass; ++j) {
-          const int r = r0 + j * kPass, key = seg0 + s * L::kKeys + r;
-          const bool in = key >= kb && key < ke;
-          const size_t off =
-              (size_t)page[j * kPass / 16] * a.c.bytes + (size_t)(key & pmask) * (HD * 2);
-          const uint32_t at = dst + L::P::place(r, ch);
-          cp_async16(at, kp + (in ? off : 0), in);
-          cp_async16(at + L::kSide, vp + (in ? off : 0), in);
-        }
+        const uint32_t dst = smem_u32(smem) + ring.at * L::kStage + at0;
+        copy_keys<L::kKeys, HD * 2, kPass>(
+            walk, kp, vp, r0, seg0 + s * L::kKeys, kb, ke, L::kSide,
+            [&](int r) { return L::P::template place_from<kPass>(dst, r); });
         p_arrive(&bar.full[ring.at]);
       }
     }
@@ -253,7 +243,7 @@ __global__ void __launch_bounds__(SL<HD, NB>::kThreads, 1) k_paged_stream(const 
       if (tid == 0) s_bad[(i + 1) & 1] = 0;
       named_sync(1, L::kUse * 32);
       finish_rows<T, HD, 4, kRows, L::kUse * 32>(a, sg, kb, ke, Ox, nullptr, s_gm, s_sum, s_bad[i & 1],
-                                                 nullptr, tid);
+                                                 tid, [](int, int, const float (&)[8]) {});
       named_sync(1, L::kUse * 32);  // the exchange is read
     }
   }

@@ -188,30 +188,20 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
       const Kv8Item& it = sg.it;
       const int k00 = (it.unit0 + sg.u0) * kWKeys;
       const int full_lo = kv8_row_lo(it, it.hi, a.window), full_hi = kv8_row_pos(a, it, it.r0);
-      const char* const kp = a.k + sg.g * a.c.head() + ch * 16;
-      const char* const vp = a.v + sg.g * a.c.head() + ch * 16;
+      const char* const kp = a.k + sg.g * a.c.head() + r0 * kWHd * 2 + ch * 16;
+      const char* const vp = kp + (a.v - a.k);
       PageWalk walk(a.c, a.err);
       walk.start(it.b, k00, max(k00, it.lo), min(k00 + sg.nu * kWKeys, it.hi + 1));
       for (int i = 0; i < sg.nu; ++i, ++n, ring.next()) {
         const int k0 = k00 + i * kWKeys;
-        const uint32_t dst = smem_u32(Ks) + ring.at * L::kStep + to;
-        int look[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) look[j] = walk.page(k0 + 16 * j);
-        auto copy = [&](const char* base, uint32_t at) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int r = r0 + 8 * j, key = k0 + r;
-            const bool in = key >= it.lo && key <= it.hi;
-            const size_t off = (size_t)look[j >> 1] * a.c.bytes + (size_t)(key & pmask) * (kWHd * 2);
-            cp_async16(at + w_place(r, ch & 7), base + (in ? off : 0), in);
-          }
-        };
-        if (n >= (uint32_t)L::kNst) p_wait(&bar.k_free[ring.at], ring.phase ^ 1, bad);
-        copy(kp, dst);
+        const uint32_t dst = smem_u32(Ks) + ring.at * L::kStep + to + w_place(r0, ch & 7);
+        if (n >= (uint32_t)L::kNst) {
+          p_wait(&bar.k_free[ring.at], ring.phase ^ 1, bad);
+          p_wait(&bar.v_free[ring.at], ring.phase ^ 1, bad);
+        }
+        copy_keys<kWKeys, kWHd * 2, 8>(walk, kp, vp, r0, k0, it.lo, it.hi + 1, kWKTile,
+                                       [&](int r) { return dst + (uint32_t)(r * 128); });
         p_arrive(&bar.k_full[ring.at]);
-        if (n >= (uint32_t)L::kNst) p_wait(&bar.v_free[ring.at], ring.phase ^ 1, bad);
-        copy(vp, dst + kWKTile);
         if (k0 >= full_lo && k0 + kWKeys - 1 <= full_hi) {
           p_arrive(&bar.v_full[ring.at]);
         } else {
