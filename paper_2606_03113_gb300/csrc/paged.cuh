@@ -90,6 +90,31 @@ __device__ __forceinline__ void copy_keys(PageWalk& walk, const char* kp, const 
   }
 }
 
+// Launches a call's first kernel, which begins with pdl_wait(): its blocks take their places while the kernel before
+// it in the stream ends (about 2 us of each call; not while a graph is captured, where what comes before
+// need not be a kernel). cluster: blocks of a cluster, or 1.
+template <typename Kern, typename... Args>
+cudaError_t launch_first(Kern k, dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st,
+                         Args... args) {
+  cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+  const bool early = g_pdl_enabled && cudaStreamIsCapturing(st, &capturing) == cudaSuccess &&
+                     capturing == cudaStreamCaptureStatusNone;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = early ? 1 : 0;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, k, args...);
+}
+
 // Checks of a cache that every entry point makes; null: fine.
 const char* check_paged(const ssd_paged_cache* c, ssd_status* status) noexcept;
 PagedView paged_view(const ssd_paged_cache* c) noexcept;

@@ -70,8 +70,6 @@ struct PL {
   static constexpr uint32_t kQ = sizeof(T) == 4 ? kRows * kOPad * 4 : 0;  // fp32 queries
   static constexpr uint32_t kSmem = kRing + kQ;
   static constexpr uint32_t kExchange = kGroups * kRows * kOPad * 4;
-  static constexpr int kCopies = kKeys * kChunks / kThreads;  // of a thread, a stage and side
-  static constexpr int kLook = kKeys / 16;                     // pages of a stage, at most
   static_assert(kExchange + kRows * HD * 4 <= kRing, "the exchange and the part fit the ring");
   static_assert(kRows % kSplitMax == 0, "a cluster's blocks have as many rows each");
   static_assert(kKeys * kChunks % kThreads == 0 && kThreads % kChunks == 0, "whole rows a pass");
@@ -501,6 +499,7 @@ __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(co
   const int ch = tid % L::kChunks, r0 = tid / L::kChunks;
   const uint32_t at0 = L::place(r0, ch);
 
+  pdl_wait();
   Kv8Cursor cur;
   Kv8Seg sg;
   bool more;
@@ -958,33 +957,21 @@ const char* check_attention(const ssd_paged_cache* c, int32_t n_heads, int32_t M
 template <typename T, int HD, int R, int NB>
 cudaError_t rows_launch(const PagedAttn& a, int P, cudaStream_t st) {
   using L = PL<T, HD, R, NB>;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(P);
-  cfg.blockDim = dim3(L::kThreads);
-  cfg.dynamicSmemBytes = L::kSmem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = a.split > 1 ? a.split : 1;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = a.split > 1 ? 1 : 0;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_paged_rows<T, HD, R, NB>, a);
+  const cudaError_t e = launch_first(k_paged_rows<T, HD, R, NB>, dim3(P), L::kThreads, L::kSmem,
+                                     a.split > 1 ? a.split : 1, st, a);
   if (e != cudaSuccess || a.split) return e;
   return R == 1 ? merge_launch<T, HD, kMWarps>(a, P, st) : merge_launch<T, HD, 1>(a, P, st);
 }
 template <int HD, int NB>
 cudaError_t stream_launch(const PagedAttn& a, int P, cudaStream_t st) {
   using L = SL<HD, NB>;
-  k_paged_stream<HD, NB><<<P, L::kThreads, L::kSmem, st>>>(a);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_first(k_paged_stream<HD, NB>, dim3(P), L::kThreads, L::kSmem, 1, st, a);
   return e != cudaSuccess ? e : merge_launch<__nv_bfloat16, HD, kMWarps>(a, P, st);
 }
 template <int TILES>
 cudaError_t wide_launch(const PagedAttn& a, int P, cudaStream_t st) {
   using L = PWideL<TILES>;
-  k_paged_wide<TILES><<<P, L::kThreads, L::kSmem, st>>>(a);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_first(k_paged_wide<TILES>, dim3(P), L::kThreads, L::kSmem, 1, st, a);
   return e != cudaSuccess ? e : merge_launch<__nv_bfloat16, kWHd, 1>(a, P, st);
 }
 template <int HD>

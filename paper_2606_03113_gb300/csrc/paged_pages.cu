@@ -113,6 +113,7 @@ __global__ void __launch_bounds__(TH, 1) k_paged_reserve(const PagedView c, cons
   __shared__ int s_pos[SSD_KV8_MAX_SEQS];
   __shared__ int s_fresh[kHeld];
   __shared__ int s_copies;
+  pdl_wait();
   pdl_launch_dependents();
   const int tid = threadIdx.x;
   // sequences tid per .. (tid + 1) per - 1 are this thread's
@@ -388,6 +389,7 @@ __global__ void __launch_bounds__(TH, 1) k_paged_compact(const PagedView c, cons
                                                                 int32_t* used) {
   constexpr int kWarps = TH / 32, kScanStep = TH * kScan;
   __shared__ PlanSmem sm;
+  pdl_wait();
   pdl_launch_dependents();
   const int tid = threadIdx.x;
   int n = 0, low, r[kScan];
@@ -458,6 +460,7 @@ __global__ void __launch_bounds__(kCopyThreads) k_paged_fork(const PagedView c,
                                                              const int32_t* parent,
                                                              const int32_t* length, int32_t* err) {
   extern __shared__ int s_old[];  // [n_seq][kForkCols]
+  pdl_wait();
   const int c0 = blockIdx.x * kForkCols;
   for (int x = threadIdx.x; x < c.n_seq * kForkCols; x += kCopyThreads) {
     const int b = x / kForkCols, i = c0 + x % kForkCols;
@@ -506,6 +509,7 @@ struct PagedAppend {
 // A block a row: its K and V are on their way while the table entry and the page's count are looked up,
 // one after the other (a row is not written to a page that others name).
 __global__ void __launch_bounds__(kRowThreads) k_paged_append(const PagedAppend a) {
+  pdl_wait();
   const int m = blockIdx.x, b = blockIdx.y;
   const uint4* xk = reinterpret_cast<const uint4*>(a.k + ((int64_t)b * a.M + m) * a.stride);
   const uint4* xv = reinterpret_cast<const uint4*>(a.v + ((int64_t)b * a.M + m) * a.stride);
@@ -662,9 +666,9 @@ extern "C" ssd_status ssd_paged_reserve(const ssd_paged_cache* c, const int32_t*
   const PagedView v = paged_view(c);
   const PlanWork w = plan_work(workspace, c->n_pages);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (c->n_pages <= kSmallPool) k_paged_reserve<256><<<1, 256, 0, st>>>(v, w, pos, rows, M, err_dev);
-  else k_paged_reserve<1024><<<1, 1024, 0, st>>>(v, w, pos, rows, M, err_dev);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = c->n_pages <= kSmallPool
+                      ? launch_first(k_paged_reserve<256>, dim3(1), 256, 0, 1, st, v, w, pos, rows, M, err_dev)
+                      : launch_first(k_paged_reserve<1024>, dim3(1), 1024, 0, 1, st, v, w, pos, rows, M, err_dev);
   if (e == cudaSuccess)
     e = carry_out(k_paged_copy, v, w, c->n_seq < c->n_pages ? c->n_seq : c->n_pages, 1, st);
   return e == cudaSuccess ? SSD_OK : fail_op_cuda("ssd_paged_reserve", e);
@@ -682,11 +686,9 @@ extern "C" ssd_status ssd_paged_fork(const ssd_paged_cache* c, const int32_t* pa
   if (smem > 48 * 1024)
     e = cudaFuncSetAttribute(k_paged_fork, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              SSD_KV8_MAX_SEQS * kForkCols * (int)sizeof(int));
-  if (e == cudaSuccess) {
-    k_paged_fork<<<(c->max_pages + kForkCols - 1) / kForkCols, kCopyThreads, smem,
-                   static_cast<cudaStream_t>(stream)>>>(v, parent, length, err_dev);
-    e = cudaGetLastError();
-  }
+  if (e == cudaSuccess)
+    e = launch_first(k_paged_fork, dim3((c->max_pages + kForkCols - 1) / kForkCols), kCopyThreads, smem, 1,
+                     static_cast<cudaStream_t>(stream), v, parent, length, err_dev);
   return e == cudaSuccess ? SSD_OK : fail_op_cuda("ssd_paged_fork", e);
 }
 
@@ -701,9 +703,9 @@ extern "C" ssd_status ssd_paged_compact(const ssd_paged_cache* c, int32_t* used,
   const PagedView v = paged_view(c);
   const PlanWork w = plan_work(workspace, c->n_pages);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (c->n_pages <= kSmallPool) k_paged_compact<256><<<1, 256, 0, st>>>(v, w, used);
-  else k_paged_compact<1024><<<1, 1024, 0, st>>>(v, w, used);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = c->n_pages <= kSmallPool
+                      ? launch_first(k_paged_compact<256>, dim3(1), 256, 0, 1, st, v, w, used)
+                      : launch_first(k_paged_compact<1024>, dim3(1), 1024, 0, 1, st, v, w, used);
   if (e == cudaSuccess)
     e = carry_out(k_paged_move, v, w, c->n_pages / 2,
                   ((int64_t)c->n_seq * c->max_pages + kCopyThreads - 1) / kCopyThreads, st);
@@ -742,7 +744,7 @@ extern "C" ssd_status ssd_paged_append(const ssd_paged_cache* c, int32_t layer, 
   a.rows = rows;
   a.err = err_dev;
   a.M = M;
-  k_paged_append<<<dim3(M, c->n_seq), kRowThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_first(k_paged_append, dim3(M, c->n_seq), kRowThreads, 0, 1,
+                                     static_cast<cudaStream_t>(stream), a);
   return e == cudaSuccess ? SSD_OK : fail_op_cuda("ssd_paged_append", e);
 }

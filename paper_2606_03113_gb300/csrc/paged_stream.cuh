@@ -68,6 +68,7 @@ __global__ void __launch_bounds__(SL<HD, NB>::kThreads, 1) k_paged_stream(const 
   __shared__ Kv8Seg s_seg[2];  // the items under way, as the copying warps hand them on
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int t = lane & 3, n8 = lane >> 2;
+  pdl_wait();
   if (tid == 0) {
     for (int i = 0; i < L::kNst; ++i) {
       mbar_init(&bar.full[i], L::kCopy * 32);

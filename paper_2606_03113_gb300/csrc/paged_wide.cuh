@@ -75,6 +75,7 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
   const int tid = threadIdx.x, warp = tid >> 5;
   const int pmask = (1 << a.c.shift) - 1;
 
+  pdl_wait();
   if (tid == 0) {
     for (int i = 0; i < L::kNst; ++i) {
       mbar_init(&bar.k_full[i], 128);
