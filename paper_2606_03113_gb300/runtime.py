@@ -283,6 +283,7 @@ def _per_seq(t, n_seq: int, device: torch.device, what: str) -> int:
 # PyTorch has that call: one built without CUDA has not, and imports this module all the same.
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _elsewhere(device: torch.device, stream):
@@ -506,12 +507,34 @@ class PagedKVCache:
         self._plan = torch.empty(self._plan_bytes, dtype=torch.uint8, device=device)
         self._plan_at = self._plan.data_ptr()
         self._work = {}  # (n_heads, M, window, longest) -> workspace bytes
+        # what every call looks at (the calls of a decode step are as short as their launches: they
+        # look at each tensor once, and leave the words of a refusal to the slower checks)
+        self._at = C.addressof(self._c)
+        self._lib = S.lib()
+        self._seqs = torch.Size((n_seq,))
+        self._index = device.index if device.type == "cuda" else -1
 
-    def _rows(self, x: torch.Tensor, heads: int, what: str) -> tuple[int, int]:
-        """(M, elements between rows) of x [n_seq, M, heads, head_dim]."""
-        if x.dtype != self.dtype:
+    def _ints(self, t, what: str) -> int:
+        """The address of an int32 [n_seq] tensor, or 0 for None."""
+        if t is None:
+            return 0
+        if t.dtype is not torch.int32 or t.shape != self._seqs or not t.is_contiguous() or \
+                t.get_device() != self._index:
+            return _per_seq(t, self.n_seq, self.device, what)
+        return t.data_ptr()
+
+    def _rows(self, x: torch.Tensor, heads: int, what: str) -> tuple[int, int, int]:
+        """(address, M, elements between rows) of x [n_seq, M, heads, head_dim]."""
+        if x.dtype is not self.dtype:
             raise ValueError(f"{what} must be {self.dtype}, as the cache, not {x.dtype}")
-        return _rows_of(x, self.n_seq, heads, self.head_dim, what)
+        M, row = _rows_of(x, self.n_seq, heads, self.head_dim, what)
+        at = x.data_ptr() if x.get_device() == self._index and not x.requires_grad else \
+            _on(x, self.device, what)
+        return at, M, row
+
+    def _here(self, stream) -> bool:
+        """Whether a call's work belongs on the current stream of the current device."""
+        return stream is None and self._index >= 0 and _current_device() == self._index
 
     def _layer(self, layer: int) -> int:
         if not 0 <= layer < self.n_layers:
@@ -524,35 +547,40 @@ class PagedKVCache:
         too few pages are free (`check` raises)."""
         if pos is None:
             raise ValueError("pos is missing")
-        pp = _per_seq(pos, self.n_seq, self.device, "pos")
+        pp = self._ints(pos, "pos")
         rp, M = 0, self.max_seq
         if isinstance(rows, int):
             M = rows
             if not 1 <= M <= self.max_seq:
                 raise ValueError(f"rows must be in 1..{self.max_seq}, not {M}")
         else:
-            rp = _per_seq(rows, self.n_seq, self.device, "rows")
+            rp = self._ints(rows, "rows")
             if not rp:
                 raise ValueError("rows is missing")
-        there = _elsewhere(self.device, stream)
-        if there is not None:
-            with there:
-                return self.reserve(pos, rows)
-        S.ssd_paged_reserve(self._c, pp, rp, M, self._plan_at, self._plan_bytes, self._err_at,
-                            _current_stream(self.device.index))
+        if not self._here(stream):
+            there = _elsewhere(self.device, stream)
+            if there is not None:
+                with there:
+                    return self.reserve(pos, rows)
+        st = self._lib.ssd_paged_reserve(self._at, pp, rp, M, self._plan_at, self._plan_bytes,
+                                         self._err_at, _current_stream(self._index))
+        if st:
+            S._check(st, "ssd_paged_reserve")
 
     def fork(self, parent: torch.Tensor | None, length: torch.Tensor | None = None, stream=None):
         """Sequence b becomes the first length[b] positions (all without `length`) of what sequence
         parent[b] was (-1: empty; without `parent`: of itself), sharing its pages."""
         if parent is None and length is None:
             raise ValueError("neither parent nor length")
-        pp = _per_seq(parent, self.n_seq, self.device, "parent")
-        lp = _per_seq(length, self.n_seq, self.device, "length")
-        there = _elsewhere(self.device, stream)
-        if there is not None:
-            with there:
-                return self.fork(parent, length)
-        S.ssd_paged_fork(self._c, pp, lp, self._err_at, _current_stream(self.device.index))
+        pp, lp = self._ints(parent, "parent"), self._ints(length, "length")
+        if not self._here(stream):
+            there = _elsewhere(self.device, stream)
+            if there is not None:
+                with there:
+                    return self.fork(parent, length)
+        st = self._lib.ssd_paged_fork(self._at, pp, lp, self._err_at, _current_stream(self._index))
+        if st:
+            S._check(st, "ssd_paged_fork")
 
     def truncate(self, length: torch.Tensor, stream=None):
         """Sequence b keeps its first length[b] positions and gives the pages behind them back."""
@@ -563,13 +591,16 @@ class PagedKVCache:
     def compact(self, stream=None) -> torch.Tensor:
         """Moves the pages in use to the low end of the pool; the free ones are its tail then.
         Returns how many are in use (int32 [1] on the device)."""
-        there = _elsewhere(self.device, stream)
-        if there is not None:
-            with there:
-                return self.compact()
+        if not self._here(stream):
+            there = _elsewhere(self.device, stream)
+            if there is not None:
+                with there:
+                    return self.compact()
         used = torch.empty(1, dtype=torch.int32, device=self.device)
-        S.ssd_paged_compact(self._c, used.data_ptr(), self._plan_at, self._plan_bytes, self._err_at,
-                            _current_stream(self.device.index))
+        st = self._lib.ssd_paged_compact(self._at, used.data_ptr(), self._plan_at, self._plan_bytes,
+                                         self._err_at, _current_stream(self._index))
+        if st:
+            S._check(st, "ssd_paged_compact")
         return used
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor,
@@ -577,20 +608,22 @@ class PagedKVCache:
         """Writes k[b, m], v[b, m] ([n_seq, M, n_kv_heads, head_dim]) for m < rows[b] (all M
         without `rows`) to positions pos[b] + m of a layer, which have been reserved."""
         layer = self._layer(layer)
-        M, row = self._rows(k, self.n_kv_heads, "k")
-        if self._rows(v, self.n_kv_heads, "v") != (M, row):
+        kp, M, row = self._rows(k, self.n_kv_heads, "k")
+        vp, Mv, vrow = self._rows(v, self.n_kv_heads, "v")
+        if Mv != M or vrow != row:
             raise ValueError("k and v must have the same rows and strides")
         if pos is None:
             raise ValueError("pos is missing")
-        kp, vp = _on(k, self.device, "k"), _on(v, self.device, "v")
-        pp = _per_seq(pos, self.n_seq, self.device, "pos")
-        rp = _per_seq(rows, self.n_seq, self.device, "rows")
-        there = _elsewhere(self.device, stream)
-        if there is not None:
-            with there:
-                return self.append(layer, k, v, pos, rows)
-        S.ssd_paged_append(self._c, layer, kp, vp, row, M, pp, rp, self._err_at,
-                           _current_stream(self.device.index))
+        pp, rp = self._ints(pos, "pos"), self._ints(rows, "rows")
+        if not self._here(stream):
+            there = _elsewhere(self.device, stream)
+            if there is not None:
+                with there:
+                    return self.append(layer, k, v, pos, rows)
+        st = self._lib.ssd_paged_append(self._at, layer, kp, vp, row, M, pp, rp, self._err_at,
+                                        _current_stream(self._index))
+        if st:
+            S._check(st, "ssd_paged_append")
 
     def attention(self, layer: int, q: torch.Tensor, pos: torch.Tensor,
                   rows: torch.Tensor | None = None, first: torch.Tensor | None = None,
@@ -604,21 +637,19 @@ class PagedKVCache:
         its rows from rows[b] on; without it a new tensor, where those are zero (a sequence with
         bad positions leaves its own unset)."""
         layer = self._layer(layer)
-        heads = q.shape[2] if q.dim() == 4 else 0
-        M, row = self._rows(q, heads, "q")
+        shape = q.shape
+        heads = shape[2] if len(shape) == 4 else 0
+        qp, M, row = self._rows(q, heads, "q")
         if heads < 1 or heads % self.n_kv_heads:
             raise ValueError(f"q has {heads} heads: not a multiple of {self.n_kv_heads}")
         if pos is None:
             raise ValueError("pos is missing")
-        qp = _on(q, self.device, "q")
-        pp = _per_seq(pos, self.n_seq, self.device, "pos")
-        rp = _per_seq(rows, self.n_seq, self.device, "rows")
-        fp = _per_seq(first, self.n_seq, self.device, "first")
+        pp, rp, fp = self._ints(pos, "pos"), self._ints(rows, "rows"), self._ints(first, "first")
         if out is not None:
-            Mo, orow = self._rows(out, heads, "out")
+            op, Mo, orow = self._rows(out, heads, "out")
             if Mo != M:
                 raise ValueError("out must have q's rows")
-            if _on(out, self.device, "out") == qp and orow != row:
+            if op == qp and orow != row:
                 raise ValueError("out is q, but their strides differ")
         if not 0 <= window < 1 << 31:
             raise ValueError(f"window must be 0 (none) or a positive int32, not {window}")
@@ -630,19 +661,22 @@ class PagedKVCache:
             nbytes = S.ssd_paged_attention_bytes(self._c, heads, M, window, longest)
             if len(self._work) < 4096:  # (a caller may pass another `longest` every step)
                 self._work[key] = nbytes
-        there = _elsewhere(self.device, stream)
-        if there is not None:
-            with there:
-                return self.attention(layer, q, pos, rows, first, window, longest, out)
+        if not self._here(stream):
+            there = _elsewhere(self.device, stream)
+            if there is not None:
+                with there:
+                    return self.attention(layer, q, pos, rows, first, window, longest, out)
         if out is None:
             make = torch.empty if rows is None else torch.zeros
             out = make((self.n_seq, M, heads, self.head_dim), dtype=q.dtype, device=self.device)
-            orow = heads * self.head_dim
+            op, orow = out.data_ptr(), heads * self.head_dim
         # (256: none is used; others stay this call's until the launches)
         work = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes > 256 else None
-        S.ssd_paged_attention(self._c, layer, qp, heads, row, M, pp, rp, fp, window, longest,
-                              out.data_ptr(), orow, work.data_ptr() if work is not None else 0, nbytes,
-                              self._err_at, _current_stream(self.device.index))
+        st = self._lib.ssd_paged_attention(self._at, layer, qp, heads, row, M, pp, rp, fp, window, longest,
+                                           op, orow, work.data_ptr() if work is not None else 0, nbytes,
+                                           self._err_at, _current_stream(self._index))
+        if st:
+            S._check(st, "ssd_paged_attention")
         return out
 
     def check(self):
