@@ -64,15 +64,15 @@ __device__ __forceinline__ int before_me(int v, PlanSmem& sm, int& total) {
   __syncthreads();  // the sums of the call before have been read
   if (lane == 31) sm.warp[warp] = inc;
   __syncthreads();
-  int base = 0, all = 0;
+  int sums = lane < WARPS ? sm.warp[lane] : 0;  // every warp adds up the warps' sums
 #pragma unroll
-  for (int w = 0; w < WARPS; ++w) {
-    const int s = sm.warp[w];
-    base += w < warp ? s : 0;
-    all += s;
+  for (int o = 1; o < WARPS; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, sums, o);
+    if (lane >= o) sums += u;
   }
-  total = all;
-  return base + inc - v;
+  total = __shfl_sync(0xffffffffu, sums, WARPS - 1);
+  const int base = __shfl_sync(0xffffffffu, sums, warp > 0 ? warp - 1 : 0);
+  return (warp > 0 ? base : 0) + inc - v;
 }
 
 // The kScan counts from id0 on (1 behind the pool's end: not free).
@@ -184,14 +184,16 @@ __global__ void __launch_bounds__(TH, 1) k_paged_reserve(const PagedView c, cons
 
   if (E <= kHeld) {
     constexpr int K = kHeld / TH;
+    const int each = (E + TH - 1) / TH;  // entries tid each .. are this thread's
     int eb[K], ei[K], ee[K];
-    bool shared[K], all[K];
+    bool wanted[K], shared[K], all[K];
     int claims = 0;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int x = tid * K + k;
+      const int x = tid * each + k;
       eb[k] = ei[k] = 0, ee[k] = -1;
-      if (x >= E) continue;
+      wanted[k] = k < each && x < E;
+      if (!wanted[k]) continue;
       if (k == 0) {
         find(x, eb[0], ei[0]);
       } else {
@@ -227,7 +229,7 @@ __global__ void __launch_bounds__(TH, 1) k_paged_reserve(const PagedView c, cons
     bool needs[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      needs[k] = tid * K + k < E && (ee[k] < 0 || (shared[k] && !all[k]));
+      needs[k] = wanted[k] && (ee[k] < 0 || (shared[k] && !all[k]));
       mine += needs[k];
     }
     int rank = before_me<kWarps>(mine, sm, need);
