@@ -86,9 +86,9 @@ __device__ __forceinline__ Kv8Item kv8_entry(const AttnArgs& a, int e) {
   Kv8Item it;
   it.b = a.byRt(e);
   it.rt = e - it.b * a.n_rt;
-  it.pos = __ldg(a.pos + it.b);
-  const int n = a.rows ? __ldg(a.rows + it.b) : a.M;
-  it.first = a.first ? max(__ldg(a.first + it.b), 0) : 0;
+  it.pos = a.pos[it.b];
+  const int n = a.rows ? a.rows[it.b] : a.M;
+  it.first = a.first ? max(a.first[it.b], 0) : 0;
   it.r0 = it.rt * RT;
   it.nr = 0;
   it.units = it.unit0 = it.lo = it.hi = 0;
@@ -124,9 +124,9 @@ struct Kv8Line {
 };
 
 // The line's places that an item takes.
-template <int RT, int KU, int COST = kKv8ItemCost<RT>>
+template <int RT, int KU>
 __device__ __forceinline__ int kv8_len(const Kv8Item& it) {
-  return it.units ? it.units + COST : 0;
+  return it.units ? it.units + kKv8ItemCost<RT> : 0;
 }
 
 // The block's part of an item: units u0 .. u0 + nu - 1.
@@ -147,7 +147,7 @@ struct Kv8PlanSmem {
 };
 
 // Every thread of the block gets the block's stretch.
-template <int RT, int KU, int THREADS, int COST = kKv8ItemCost<RT>>
+template <int RT, int KU, int THREADS>
 __device__ __forceinline__ Kv8Cursor kv8_plan(const AttnArgs& a, Kv8PlanSmem& sm) {
   static_assert(THREADS / 32 <= 32, "a sum for each warp");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -156,7 +156,7 @@ __device__ __forceinline__ Kv8Cursor kv8_plan(const AttnArgs& a, Kv8PlanSmem& sm
     const int e = i / a.Hkv, g = i - e * a.Hkv;
     const Kv8Item own = kv8_entry<RT, KU>(a, e);
     const int w0 = own.units * rank / a.split, w1 = own.units * (rank + 1) / a.split;
-    return Kv8Cursor{w0, w1, 0, e, g * kv8_len<RT, KU, COST>(own) + w0};
+    return Kv8Cursor{w0, w1, 0, e, g * kv8_len<RT, KU>(own) + w0};
   }
   const int per = (a.entries + THREADS - 1) / THREADS;
   const int e0 = min(tid * per, a.entries), e1 = min(e0 + per, a.entries);
@@ -164,7 +164,7 @@ __device__ __forceinline__ Kv8Cursor kv8_plan(const AttnArgs& a, Kv8PlanSmem& sm
   Kv8Item it;
   for (int e = e0; e < e1; ++e) {
     it = kv8_entry<RT, KU>(a, e);
-    sum += kv8_len<RT, KU, COST>(it) * a.Hkv;
+    sum += kv8_len<RT, KU>(it) * a.Hkv;
   }
   int inc = sum;
 #pragma unroll
@@ -187,7 +187,7 @@ __device__ __forceinline__ Kv8Cursor kv8_plan(const AttnArgs& a, Kv8PlanSmem& sm
     int off = w0 - before, e = e0;
     for (;; ++e) {
       if (per > 1) it = kv8_entry<RT, KU>(a, e);
-      const int u = kv8_len<RT, KU, COST>(it) * a.Hkv;
+      const int u = kv8_len<RT, KU>(it) * a.Hkv;
       if (off < u) break;
       off -= u;
     }
@@ -198,11 +198,11 @@ __device__ __forceinline__ Kv8Cursor kv8_plan(const AttnArgs& a, Kv8PlanSmem& sm
 }
 
 // The next segment of the block's stretch; false at its end.
-template <int RT, int KU, int COST = kKv8ItemCost<RT>>
+template <int RT, int KU>
 __device__ __forceinline__ bool kv8_next(const AttnArgs& a, Kv8Cursor& c, Kv8Seg& s) {
   while (c.w0 < c.w1) {
     s.it = kv8_entry<RT, KU>(a, c.e);
-    const int len = kv8_len<RT, KU, COST>(s.it);
+    const int len = kv8_len<RT, KU>(s.it);
     if (c.off >= len * a.Hkv) {
       c.off = 0;
       ++c.e;

@@ -21,7 +21,7 @@ struct PagedView {
   __host__ __device__ __forceinline__ int cap() const { return max_pages << shift; }
   // The page of entry i of sequence b, or -1.
   __device__ __forceinline__ int entry(int b, int i) const {
-    const int e = __ldg(table + (size_t)b * max_pages + i);
+    const int e = table[(size_t)b * max_pages + i];
     return (unsigned)e < (unsigned)n_pages ? e : -1;
   }
   // Layer `layer`, side 0 (K) or 1 (V) of page 0, head 0; bytes to the next head.
@@ -67,32 +67,33 @@ struct PageWalk {
   }
 };
 
-// Copies keys k0 .. k0 + KEYS - 1 and their values to shared memory, zeros for those outside of kb .. ke - 1, as
-// one of the threads that hold PASS rows at a time: kp, vp at its chunk of its row (r0, below PASS) of position 0 of
-// page 0, to(r) where that chunk of row r of the keys goes, `side` bytes in front of the values'.
+// Where keys k0 .. k0 + KEYS - 1 stand, by sixteens, which lie in one page each: bytes from position 0 of page 0.
+template <int KEYS, int ROW_BYTES>
+__device__ __forceinline__ void find_keys(PageWalk& walk, int k0, size_t (&off)[KEYS / 16]) {
+#pragma unroll
+  for (int j = 0; j < KEYS / 16; ++j)
+    off[j] = (size_t)walk.page(k0 + 16 * j) * walk.view->bytes +
+             (size_t)((k0 + 16 * j) & ((1 << walk.view->shift) - 1)) * ROW_BYTES;
+}
+// Copies them (or their values) to shared memory, zeros for those outside of kb .. ke - 1, as one of the
+// threads that hold PASS rows at a time: p at its chunk of its row (r0, below PASS) of position 0 of page 0, to(r)
+// where that chunk of row r0 + r goes.
 template <int KEYS, int ROW_BYTES, int PASS, typename To>
-__device__ __forceinline__ void copy_keys(PageWalk& walk, const char* kp, const char* vp, int r0, int k0,
-                                          int kb, int ke, uint32_t side, To to) {
-  static_assert(16 % PASS == 0, "sixteen positions lie in one page");
+__device__ __forceinline__ void copy_keys(const size_t (&off)[KEYS / 16], const char* p, int r0, int k0,
+                                          int kb, int ke, To to) {
+  static_assert(16 % PASS == 0, "whole passes of sixteen rows");
   const bool all = k0 >= kb && k0 + KEYS <= ke;
 #pragma unroll
-  for (int j = 0; j < KEYS; j += 16) {
-    const size_t off = (size_t)walk.page(k0 + j) * walk.view->bytes +
-                       (size_t)((k0 + j) & ((1 << walk.view->shift) - 1)) * ROW_BYTES;
-#pragma unroll
-    for (int i = 0; i < 16; i += PASS) {
-      const int key = k0 + j + i + r0;
-      const bool in = all || (key >= kb && key < ke);
-      const uint32_t at = to(j + i);
-      cp_async16(at, kp + off + i * ROW_BYTES, in);
-      cp_async16(at + side, vp + off + i * ROW_BYTES, in);
-    }
+  for (int j = 0; j < KEYS; j += PASS) {
+    const int key = k0 + j + r0;
+    cp_async16(to(j), p + off[j / 16] + j % 16 * ROW_BYTES, all || (key >= kb && key < ke));
   }
 }
 
 // Launches a call's first kernel, which begins with pdl_wait(): its blocks take their places while the kernel before
-// it in the stream ends (about 2 us of each call; not while a graph is captured, where what comes before
-// need not be a kernel). cluster: blocks of a cluster, or 1.
+// it in the stream ends (a call of 9 us takes 12 otherwise; not while a graph is captured, where what comes before
+// need not be a kernel). What that kernel may have written is read by plain loads, not as read-only data, which
+// has to be constant while a kernel is resident. cluster: blocks of a cluster, or 1.
 template <typename Kern, typename... Args>
 cudaError_t launch_first(Kern k, dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st,
                          Args... args) {

@@ -450,7 +450,8 @@ __device__ __forceinline__ void finish_rows(const PagedAttn& a, const Kv8Seg& sg
         const T* v = reinterpret_cast<const T*>(vp + (size_t)e * a.c.bytes) +
                      (size_t)(key & pmask) * HD + c8;
         float f[8];
-        load_query8(v, f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = Elem<T>::to_f(v[j]);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
           if (no_number(f[j])) sum[j] += f[j];
@@ -532,9 +533,14 @@ __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(co
     auto issue = [&](int s) {
       if (s < nst) {
         const uint32_t dst = smem_u32(smem) + (uint32_t)(s % L::kNst) * L::kStage + at0;
+        const int k0 = seg0 + s * L::kKeys;
+        size_t off[L::kKeys / 16];
+        find_keys<L::kKeys, L::kRowBytes>(walk, k0, off);
         copy_keys<L::kKeys, L::kRowBytes, kPass>(
-            walk, kp, vp, r0, seg0 + s * L::kKeys, kb, ke, L::kSide,
-            [&](int r) { return L::template place_from<kPass>(dst, r); });
+            off, kp, r0, k0, kb, ke, [&](int r) { return L::template place_from<kPass>(dst, r); });
+        copy_keys<L::kKeys, L::kRowBytes, kPass>(off, vp, r0, k0, kb, ke, [&](int r) {
+          return L::template place_from<kPass>(dst, r) + L::kSide;
+        });
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -561,17 +567,17 @@ __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(co
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int x = 0; x < 2; ++x)
-            qf[k][b][x] = __ldg(reinterpret_cast<const uint32_t*>(qp[b] + 16 * k + 8 * x));
+            qf[k][b][x] = *reinterpret_cast<const uint32_t*>(qp[b] + 16 * k + 8 * x);
     } else {
       for (int x = tid; x < L::kRows * (HD / 4); x += L::kThreads) {
         const int row = x / (HD / 4), c4 = x % (HD / 4);
         float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
         if (row < it.nr) {
           const int r = it.r0 + row, m = a.byG(r), h = g * a.G + r - m * a.G;
-          u = __ldg(reinterpret_cast<const float4*>(static_cast<const T*>(a.q) +
-                                                    ((int64_t)it.b * a.M + m) * a.q_stride +
-                                                    (int64_t)h * HD) +
-                    c4);
+          u = *(reinterpret_cast<const float4*>(static_cast<const T*>(a.q) +
+                                                ((int64_t)it.b * a.M + m) * a.q_stride +
+                                                (int64_t)h * HD) +
+                c4);
         }
         *reinterpret_cast<float4*>(Qs + row * L::kOPad + c4 * 4) = u;
       }

@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(TH, 1) k_paged_reserve(const PagedView c, cons
   for (int j = 0; j < per; ++j) {
     const int b = tid * per + j;
     if (b >= c.n_seq) break;
-    const int p = __ldg(pos + b), n = rows ? __ldg(rows + b) : M;
+    const int p = pos[b], n = rows ? rows[b] : M;
     int cnt = 0;
     if (p < 0 || n < 0 || n > M || p > c.cap() - n) {
       if (err) atomicOr(err, n < 0 || n > M ? (int)kErrControl : (int)kErrCapacity);
@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(kCopyThreads) k_paged_fork(const PagedView c,
   for (int x = threadIdx.x; x < c.n_seq * kForkCols; x += kCopyThreads) {
     const int b = x / kForkCols, i = c0 + x % kForkCols;
     if (i >= c.max_pages) continue;
-    const int p = parent ? __ldg(parent + b) : b, n = length ? __ldg(length + b) : 0x7fffffff;
+    const int p = parent ? parent[b] : b, n = length ? length[b] : 0x7fffffff;
     if (p < -1 || p >= c.n_seq || n < 0) {
       if (i == 0 && err) atomicOr(err, (int)kErrControl);
       continue;
@@ -515,7 +515,7 @@ __global__ void __launch_bounds__(kRowThreads) k_paged_append(const PagedAppend 
   const int m = blockIdx.x, b = blockIdx.y;
   const uint4* xk = reinterpret_cast<const uint4*>(a.k + ((int64_t)b * a.M + m) * a.stride);
   const uint4* xv = reinterpret_cast<const uint4*>(a.v + ((int64_t)b * a.M + m) * a.stride);
-  const int p0 = __ldg(a.pos + b), n = a.rows ? __ldg(a.rows + b) : a.M;
+  const int p0 = a.pos[b], n = a.rows ? a.rows[b] : a.M;
   uint4 uk[kRowBatch], uv[kRowBatch];
   auto load = [&](int x0) {
 #pragma unroll
@@ -535,7 +535,7 @@ __global__ void __launch_bounds__(kRowThreads) k_paged_append(const PagedAppend 
   if (m >= n) return;
   load(threadIdx.x);
   const int p = p0 + m, e = a.c.entry(b, p >> a.c.shift);
-  if (e < 0 || __ldg(a.c.refs + e) > 1) {
+  if (e < 0 || a.c.refs[e] > 1) {
     if (threadIdx.x == 0 && a.err) atomicOr(a.err, (int)kErrTable);
     return;
   }
@@ -616,10 +616,7 @@ const char* check_work(const ssd_paged_cache* c, const void* workspace, size_t b
 
 // Pools for which the planning block has 256 threads, whose barriers cost less, and above which 1024, which
 // look at more counts at once.
-#ifndef SMALL_POOL
-#define SMALL_POOL 8192
-#endif
-constexpr int kSmallPool = SMALL_POOL;
+constexpr int kSmallPool = 8192;
 
 // The launch that carries a plan out: up to four blocks an SM.
 template <typename Kern>

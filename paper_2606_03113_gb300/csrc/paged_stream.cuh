@@ -13,11 +13,6 @@ namespace ssd {
 
 namespace {
 
-#ifndef PSTREAM_COST
-#define PSTREAM_COST 3
-#endif
-constexpr int kStreamCost = PSTREAM_COST;
-
 template <int HD, int NB>
 struct SL {
   using P = PL<__nv_bfloat16, HD, 1, NB>;  // its stages and places
@@ -82,7 +77,7 @@ __global__ void __launch_bounds__(SL<HD, NB>::kThreads, 1) k_paged_stream(const 
     s_bad[0] = s_bad[1] = s_fail = 0;
     a.desc[blockIdx.x].nr = 0;
   }
-  Kv8Cursor cur = kv8_plan<kRows, kUnit, L::kThreads, kStreamCost>(a, s_plan);  // (with block barriers)
+  Kv8Cursor cur = kv8_plan<kRows, kUnit, L::kThreads>(a, s_plan);  // (with block barriers)
   pdl_launch_dependents();
   uint32_t n = 0;  // stages so far
   Ring<L::kNst> ring;
@@ -110,7 +105,7 @@ __global__ void __launch_bounds__(SL<HD, NB>::kThreads, 1) k_paged_stream(const 
     Kv8Seg next;
     PageWalk ahead(a.c, a.err);
     auto look = [&]() -> bool {
-      if (!kv8_next<kRows, kUnit, kStreamCost>(a, cur, next)) return false;
+      if (!kv8_next<kRows, kUnit>(a, cur, next)) return false;
       const Span n(next);
       ahead.start(next.it.b, n.seg0 + n.first * L::kKeys, n.kb, n.ke);
       if (ct == 0 && !next.whole() && next.u0 == 0) a.desc[blockIdx.x] = kv8_desc(a, cur, next);
@@ -146,11 +141,16 @@ __global__ void __launch_bounds__(SL<HD, NB>::kThreads, 1) k_paged_stream(const 
       const char* const vp = kp + (a.v - a.k);
       for (int s = sp.first; s < last; ++s, ++n, ring.next()) {
         if (s == last - 1) more = look();
+        const int k0 = seg0 + s * L::kKeys;
+        size_t off[L::kKeys / 16];
+        find_keys<L::kKeys, HD * 2>(walk, k0, off);
         if (n >= (uint32_t)L::kNst) p_wait(&bar.empty[ring.at], ring.phase ^ 1, bad);
         const uint32_t dst = smem_u32(smem) + ring.at * L::kStage + at0;
         copy_keys<L::kKeys, HD * 2, kPass>(
-            walk, kp, vp, r0, seg0 + s * L::kKeys, kb, ke, L::kSide,
-            [&](int r) { return L::P::template place_from<kPass>(dst, r); });
+            off, kp, r0, k0, kb, ke, [&](int r) { return L::P::template place_from<kPass>(dst, r); });
+        copy_keys<L::kKeys, HD * 2, kPass>(off, vp, r0, k0, kb, ke, [&](int r) {
+          return L::P::template place_from<kPass>(dst, r) + L::kSide;
+        });
         p_arrive(&bar.full[ring.at]);
       }
     }

@@ -31,7 +31,7 @@ struct PWideL {
   // warps: 4 TILES softmax, 4 copies, then the accumulators' scores and outputs
   static constexpr int kSoft = 4 * TILES, kQk = kSoft + 4, kPv = kQk + TILES;
   static constexpr int kThreads = (kPv + TILES) * 32;
-  static constexpr int kNst = 6 - TILES;  // steps of the ring
+  static constexpr int kNst = 6 - TILES;  // steps of the ring (five for two accumulators: no faster)
   static constexpr uint32_t kStep = 2 * kWKTile;
   static constexpr uint32_t kSmem = 2 * TILES * kWQHalf + kNst * kStep + 1024;  // queries, ring; alignment
   static constexpr uint32_t kCols = 256 * TILES;  // tensor memory: S and P (2 x 64 each), O
@@ -196,13 +196,15 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
       for (int i = 0; i < sg.nu; ++i, ++n, ring.next()) {
         const int k0 = k00 + i * kWKeys;
         const uint32_t dst = smem_u32(Ks) + ring.at * L::kStep + to + w_place(r0, ch & 7);
-        if (n >= (uint32_t)L::kNst) {
-          p_wait(&bar.k_free[ring.at], ring.phase ^ 1, bad);
-          p_wait(&bar.v_free[ring.at], ring.phase ^ 1, bad);
-        }
-        copy_keys<kWKeys, kWHd * 2, 8>(walk, kp, vp, r0, k0, it.lo, it.hi + 1, kWKTile,
+        size_t off[kWKeys / 16];
+        find_keys<kWKeys, kWHd * 2>(walk, k0, off);
+        if (n >= (uint32_t)L::kNst) p_wait(&bar.k_free[ring.at], ring.phase ^ 1, bad);
+        copy_keys<kWKeys, kWHd * 2, 8>(off, kp, r0, k0, it.lo, it.hi + 1,
                                        [&](int r) { return dst + (uint32_t)(r * 128); });
         p_arrive(&bar.k_full[ring.at]);
+        if (n >= (uint32_t)L::kNst) p_wait(&bar.v_free[ring.at], ring.phase ^ 1, bad);
+        copy_keys<kWKeys, kWHd * 2, 8>(off, vp, r0, k0, it.lo, it.hi + 1,
+                                       [&](int r) { return dst + kWKTile + (uint32_t)(r * 128); });
         if (k0 >= full_lo && k0 + kWKeys - 1 <= full_hi) {
           p_arrive(&bar.v_full[ring.at]);
         } else {
@@ -237,7 +239,7 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           const int r = it.r0 + min(t * kWRows + j * 8 + ttid / 16, it.nr - 1), m = a.byG(r);
-          u[j] = __ldg(reinterpret_cast<const uint4*>(q0 + m * a.q_stride + (r - m * a.G) * kWHd));
+          u[j] = *reinterpret_cast<const uint4*>(q0 + m * a.q_stride + (r - m * a.G) * kWHd);
         }
 #pragma unroll
         for (int j = 0; j < 16; ++j)
