@@ -141,7 +141,7 @@ struct FewTile {
       }
 #pragma unroll
       for (int y = 1; y < SUB; y <<= 1) s += __shfl_xor_sync(0xffffffffu, s, y);
-      float z = s * a.scale;
+      float z = __fmul_rn(s, a.scale);  // (not contracted: the maximum is one of these)
       if (!full) {
         const int at = kv8_row_pos(a, it, it.r0 + r);
         if (k0 + kk > at || k0 + kk < kv8_row_lo(it, at, a.window)) z = -INFINITY;
@@ -229,7 +229,7 @@ struct RowTile {
     for (int n = 0; n < N; ++n)
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        sc[n][x] *= scale;
+        sc[n][x] = __fmul_rn(sc[n][x], scale);  // (not contracted: the maximum is one of these)
         if (!full) {
           const int key = k0 + 8 * n + 2 * t + (x & 1);
           if (key < plo[x >> 1] || key > phi[x >> 1]) sc[n][x] = -INFINITY;
@@ -334,7 +334,8 @@ struct ColTile {
       float nm[2] = {-INFINITY, -INFINITY};
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        z[b][x] = (s2[0][b][x] + s2[1][b][x]) * scale;
+        // (not contracted with what follows: the maximum is one of these)
+        z[b][x] = __fmul_rn(s2[0][b][x] + s2[1][b][x], scale);
         if (!full) {
           const int key = k0 + n8 + 8 * (x >> 1);
           if (key < plo[b][x & 1] || key > phi[b][x & 1]) z[b][x] = -INFINITY;

@@ -37,6 +37,7 @@ struct PWideL {
   static constexpr uint32_t kCols = 256 * TILES;  // tensor memory: S and P (2 x 64 each), O
 };
 constexpr float kPGrow = 8.f;
+constexpr float kPFar = 1048576.f;  // 2^20: half a unit there is 2^-4
 
 // Instruction descriptors: bf16 operands, fp32 accumulator, M = 128; values are MN-major (bit 16).
 constexpr uint32_t kPIdesc = idesc_bf16_f32(128, kWKeys);
@@ -255,6 +256,10 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
       const int phi = row < it.nr ? kv8_row_pos(a, it, it.r0 + row) : -1;
       const int plo = row < it.nr ? kv8_row_lo(it, phi, a.window) : 0;
       float ref = -INFINITY, ls = 0.f;  // of the row
+      // Some row of the warp has a ref whose rounding is more than a small part of a power of two: the
+      // product in the exponent is not rounded, so such a row's scores are, beforehand, and taken from
+      // ref (in the branch below, which every step then takes).
+      bool far = false;
       for (int i = 0; i < sg.nu; ++i, ++n) {
         p_wait2(bar.s_done[t], n, bad);
         __syncwarp();
@@ -278,8 +283,10 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
             for (int y = 0; y < 4; ++y)
               m[y] = w_max3(m[y], __uint_as_float(r[x + 2 * y]), __uint_as_float(r[x + 2 * y + 1]));
           const float mx = fmaxf(w_max3(m[0], m[1], m[2]), m[3]) * a.scale;
-          const bool grow = mx > ref + kPGrow || (ref == -INFINITY && mx > ref);
-          if (__any_sync(0xffffffffu, grow)) {
+          // (rounded down: what stays is not above ref + 8, whatever ref's unit is)
+          const bool grow = mx > __fadd_rd(ref, kPGrow) || (ref == -INFINITY && mx > ref);
+          float c = a.scale, base = ref;  // what the exponents below are taken from
+          if (__any_sync(0xffffffffu, grow || far)) {
             float f = 1.f;
             if (grow) {
               f = ref == -INFINITY ? 0.f : exp2f(ref - mx);
@@ -290,29 +297,40 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
               p_wait2(bar.o_done[t], n - 1, bad);
               __syncwarp();
               tc_fence_after();
+              if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll 1
-              for (int q = 0; q < 8; ++q) {
-                uint32_t o[16];
-                w_ld16(tmO + 16 * q, o);
+                for (int q = 0; q < 8; ++q) {
+                  uint32_t o[16];
+                  w_ld16(tmO + 16 * q, o);
 #pragma unroll
-                for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
-                w_st16(tmO + 16 * q, o);
+                  for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+                  w_st16(tmO + 16 * q, o);
+                }
               }
             }
+            base = ref;
+            const bool own = ref > -INFINITY && fabsf(ref) >= kPFar;
+            far = __any_sync(0xffffffffu, own);
+            if (far) {
+              const float by = own ? c : 1.f, off = own ? ref : 0.f;
+#pragma unroll
+              for (int x = 0; x < 64; ++x)
+                r[x] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(r[x]), by), off));
+              if (own) c = 1.f, base = 0.f;
+            }
           }
-          // (scores are rounded before ref is taken from them, as the maximum was: however large
-          // they are, none passes it by more than it may)
-          const float top = ref == -INFINITY ? 0.f : ref;
-          const uint64_t c2 = pack2(a.scale, a.scale), t2 = pack2(-top, -top);
+          // A probability's rounding to 8 bits is in the sum, too: the weights add up to one.
+          const float top = base == -INFINITY ? 0.f : base;
+          const uint64_t c2 = pack2(c, c), t2 = pack2(-top, -top);
           uint64_t sum2 = 0;
 #pragma unroll
           for (int x = 0; x < 64; x += 2) {
-            const float2 z = unpack2(
-                add2(mul2(pack2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), c2), t2));
-            const float e0 = ex2_approx(z.x), e1 = ex2_approx(z.y);
-            sum2 = add2(sum2, pack2(e0, e1));
-            const __nv_bfloat162 h = __floats2bfloat162_rn(e0, e1);
-            r[x / 2] = *reinterpret_cast<const uint32_t*>(&h);
+            const float2 z =
+                unpack2(fma2(pack2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), c2, t2));
+            const __nv_bfloat162 h = __floats2bfloat162_rn(ex2_approx(z.x), ex2_approx(z.y));
+            const uint32_t u = *reinterpret_cast<const uint32_t*>(&h);
+            sum2 = add2(sum2, pack2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)));
+            r[x / 2] = u;
           }
           const float2 sum = unpack2(sum2);
           ls += sum.x + sum.y;

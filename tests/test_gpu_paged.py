@@ -324,6 +324,12 @@ ATTEND = [  # dtype, layers, heads, kv heads, hd, page, sequences of (pos, rows)
     ("bf16", 1, 64, 2, 128, 32, [(500, 6), (190, 5)], 6, [0, 300], 90, 0),
     ("bf16", 1, 12, 1, 128, 256, [(63, 65), (1, 64)], 65, None, 0, 0),
     ("bf16", 1, 16, 8, 128, 16, [(1, 140)], 140, None, 64, 0),
+    ("bf16", 1, 8, 4, 128, 16, [(5000, 1), (4999, 1), (100, 1)], 1, None, 100, 0),
+    ("bf16", 1, 8, 4, 64, 32, [(3000, 4), (2047, 1)], 4, [0, 2040], 0, 0),
+    ("bf16", 1, 8, 2, 128, 16, [(3 * b % 70, 1 + b % 2) for b in range(150)], 2, None, 0, 0),
+    ("f32", 1, 2, 1, 64, 16, [(5 * b % 90, 1) for b in range(70)], 1, None, 0, 0),
+    ("f32", 1, 16, 2, 128, 64, [(700, 3), (1, 1)], 3, None, 0, 0),
+    ("bf16", 1, 24, 8, 64, 64, [(150, 9), (600, 2)], 9, None, 0, 0),
 ]
 
 # positions that the table has room for behind what a case needs: 0 deals short sequences out by clusters,
@@ -406,10 +412,9 @@ def test_what_is_out_of_sight_does_not_matter(dtype, hd, heads, kvh, M, room, ba
     at = 64
     pages[table[0][at // page], 0, 1, kvh - 1, at % page, 5] = bad
     z = c.attention(0, q, _ints(pos), rows=_ints(rows), first=_ints(first), window=window)
-    sees = [p + m - window < at <= p + m and at >= f for p, f in zip(pos, first) for m in range(1)]
     col = z[0, :rows[0], heads - heads // kvh:, 5].float()
     live = torch.tensor([pos[0] + m - window < at for m in range(rows[0])], device="cuda")
-    assert sees[0] and (torch.isnan(col) if bad != bad else col == bad)[live].all()
+    assert live[0] and (torch.isnan(col) if bad != bad else col == bad)[live].all()
     assert torch.isfinite(col[~live]).all() and torch.isfinite(z[1:].float()).all()
 
 
@@ -456,31 +461,65 @@ def test_a_missing_page_is_told(dtype):
     c.check()
 
 
-def test_bad_positions_leave_the_output():
+@pytest.mark.parametrize("dtype,heads,room", [("bf16", 4, 0), ("bf16", 4, 2100), ("bf16", 64, 2100),
+                                              ("f32", 4, 2100)])
+def test_bad_positions_leave_the_output(dtype, heads, room):
     torch = _torch()
-    c, g = _filled("bf16", 1, 2, 128, 16, 5, 4, seed=2)
-    q = torch.randn(5, 3, 4, 128, generator=g, device="cuda").bfloat16()
+    c, g = _filled(dtype, 1, 2, 128, 16, 5, 4, seed=2, room=room // 16)
+    q = torch.randn(5, 3, heads, 128, generator=g, device="cuda").to(_dtype(dtype))
     out = torch.full_like(q, 3.0)
-    pos, rows = [62, -1, 5, 5, 30], [3, 1, 4, -1, 3]
+    pos, rows = [c.max_seq - 2, -1, 5, 5, 30], [3, 1, 4, -1, 3]
     c.attention(0, q, _ints(pos), rows=_ints(rows), out=out)
     assert (out[:4] == 3.0).all() and (out[4] != 3.0).any() and _err(c) == R.CAPACITY | R.CONTROL
     out.fill_(3.0)
+    pos, rows = [2 ** 31 - 1, -2 ** 31, 1 << 30, 0, 0], [1, 1, 1, 2 ** 31 - 1, -2 ** 31]
+    c.attention(0, q, _ints(pos), rows=_ints(rows), out=out)
+    assert (out == 3.0).all() and _err(c) == R.CAPACITY | R.CONTROL
     c.attention(0, q, _ints([30, 30, 30, 30, 30]), rows=_ints([3] * 5), out=out, longest=32)
     assert (out == 3.0).all() and _err(c) == R.CAPACITY
 
 
-def test_scores_of_every_size():
-    """Scores up to 1e4 and queries of zero: one key takes it all, or all share alike."""
+@pytest.mark.parametrize("dtype,hd,heads,room", [("f32", 64, 8, 0), ("f32", 128, 4, 2100), ("bf16", 64, 8, 0),
+                                                 ("bf16", 128, 8, 2100), ("bf16", 128, 64, 2100)])
+def test_scores_of_every_size(dtype, hd, heads, room):
+    """Scores from zero to 1e4, where one key takes it all, and up to 1e32, where rounding decides which."""
     torch = _torch()
-    for dtype in ("f32", "bf16"):
-        c, g = _filled(dtype, 1, 2, 64, 32, 2, 10, seed=3)
-        q = torch.randn(2, 3, 8, 64, generator=g, device="cuda")
-        q[0, 0] *= 1000.0
-        q[0, 1] = 0.0
-        q[1, 0] *= 1e-20
-        q = q.to(_dtype(dtype))
-        _check_attention(c, 0, q, [200, 290], [3, 3])
-        c.check()
+    c, g = _filled(dtype, 1, 2, hd, 32, 2, 10, seed=3, room=room // 32)
+    q = torch.randn(2, 3, heads, hd, generator=g, device="cuda")
+    q[0, 0] *= 1000.0
+    q[0, 1] = 0.0
+    q[1, 0] *= 1e-20
+    q = q.to(_dtype(dtype))
+    _check_attention(c, 0, q, [200, 290], [3, 3])
+    for scale in (1e7, 1e30):  # rows with scores far apart in one tile
+        mixed = q.clone()
+        mixed[:, 1, ::3] = scale
+        got = c.attention(0, mixed, _ints([200, 290]))
+        want = c.attention(0, q, _ints([200, 290]))
+        same = torch.ones(heads, dtype=torch.bool, device="cuda")
+        same[::3] = False
+        off = (got.float() - want.float()).abs()[:, 1][:, same]
+        assert torch.isfinite(got.float()).all() and off.max() <= 2.0 ** -6 * want.float().abs().max()
+    _check_attention(c, 0, mixed[:, ::2].contiguous(), [200, 290], [2, 2])
+    held = c.table[0, :10].long()
+    one, slot = c.table[0, 130 // 32].long(), 130 % 32
+    for scale in (1e6, 1e9, 1e13, 1e30):
+        # all keys alike but for one, whose score is twice as large: its value is the answer
+        c.pages[held, 0, 0] = 0.5
+        c.pages[one, 0, 0, :, slot] = 1.0
+        big = torch.full_like(q, scale)
+        got = c.attention(0, big, _ints([200, 290]))
+        want = c.pages[one, 0, 1, :, slot]
+        assert torch.equal(got[0], want.repeat_interleave(heads // 2, 0).expand(3, heads, hd))
+        # all alike: the mean of 201 values. A sum of 201 terms in fp32, its parts' weights and the
+        # division: below 2^-16 of the mean magnitude
+        c.pages[one, 0, 0, :, slot] = 0.5
+        got = c.attention(0, big, _ints([200, 290]))[0, 0].double()
+        v = c.pages[held, 0, 1].double().permute(1, 0, 2, 3).reshape(2, -1, hd)[:, :201]
+        mean, off = v.mean(1)[:, None], v.abs().mean(1)[:, None] * 2.0 ** -16
+        half = 2.0 ** -24 if dtype == "f32" else 2.0 ** -8
+        assert ((got.view(2, heads // 2, hd) - mean).abs() <= off + half * (mean.abs() + off)).all()
+    c.check()
 
 
 def test_long_cache_beyond_32_bits():
@@ -596,6 +635,59 @@ def test_a_search_in_a_graph():
         _agree(captured, ref)
     eager.check()
     captured.check()
+
+
+def test_calls_in_a_row_without_a_wait():
+    """A call's first kernel is resident before the kernel in front of it has ended: steps whose positions, parents,
+    rows and queries are made by kernels right in front of the calls that read them, against the same
+    steps with a wait behind everything."""
+    torch = _torch()
+
+    def run(wait):
+        c = _cache("bf16", 1, 2, 128, 60, 16, 6, 9)
+        g = torch.Generator(device="cuda").manual_seed(21)
+        pos = torch.zeros(6, dtype=torch.int32, device="cuda")
+        parent = torch.arange(6, dtype=torch.int32, device="cuda")
+        kv = torch.randn(6, 1, 4, 128, generator=g, device="cuda").bfloat16()
+        q = torch.randn(6, 1, 8, 128, generator=g, device="cuda").bfloat16()
+        mix = torch.randn(8, 8, generator=g, device="cuda").bfloat16()
+        outs = []
+
+        def then():
+            if wait:
+                torch.cuda.synchronize()
+        for step in range(120):
+            parent.add_(step % 3).remainder_(6)
+            then()
+            c.fork(parent)
+            then()
+            pos = pos[parent.long()]
+            then()
+            c.reserve(pos, 1)
+            then()
+            c.append(0, kv[:, :, :2], kv[:, :, 2:], pos)
+            then()
+            o = c.attention(0, q, pos, longest=144 if step % 2 else 0)
+            then()
+            q = torch.einsum("bmhd,hg->bmgd", o, mix).contiguous()
+            kv = torch.tanh(o[:, :, :4] * 3).contiguous()
+            then()
+            pos = pos + 1
+            if step % 40 == 39:
+                used = c.compact()
+                pos = pos // 2
+                c.truncate(pos)
+                outs.append(used)
+            outs.append(o)
+        torch.cuda.synchronize()
+        c.check()
+        return outs, c
+    a, ca = run(True)
+    for _ in range(3):
+        b, cb = run(False)
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+        assert torch.equal(ca.table, cb.table) and torch.equal(ca.refs, cb.refs)
+        assert torch.equal(ca.pages, cb.pages)
 
 
 def test_calls_on_another_stream():
