@@ -2,8 +2,7 @@
 //
 // pages [n_pages][n_layers][n_kv_heads][2][page][head_dim]: a page is one piece of memory, so that
 // copying or moving one is a single long copy. What an attention reads of a page, a head's keys (a slab)
-// and its values, lies in one piece, too: memory far apart costs it, 1 row of 32 heads over 8 KV heads x 524288
-// keys in scattered pages of 16, 64 and 256 reads 5.6, 6.4 and 6.7 TB/s with all keys in front of all values.
+// and its values, lies in one piece, too.
 #pragma once
 
 #include "kv8.cuh"
@@ -33,7 +32,8 @@ struct PagedView {
 
 // The pages of a sequence's entries in order, for a warp that walks keys kb .. ke - 1: a lane holds one of
 // 32 entries, and the next 32 are on their way meanwhile. (Looked up a stage of 64 keys ahead, an entry that had
-// to come from memory held the copies up: pages of 16, 64 and 256 positions read 5.6, 6.4 and 6.7 TB/s.)
+// to come from memory held the copies up: pages of 16, 64 and 256 positions were read at 5.6, 6.4 and 6.7 TB/s,
+// now at 6.5, 7.2 and 7.4.)
 struct PageWalk {
   const PagedView* view;
   int32_t* err;

@@ -2,13 +2,25 @@
 //   o_r = sum_j p_rj v_j / sum_j p_rj,  p_rj = e^(q_r . k_j / sqrt(hd) - max),
 // over the keys j that row r sees: first .. its own position, at most `window`.
 //
-// k_paged_rows: a block takes a stretch of the plan's units (kv8_plan.cuh), or, for short
-// sequences, a cluster of blocks an item. Stages of keys and values come by cp.async, kNst - 1 of
-// them on their way. Of an item's
-// R tiles of 16 query rows a warp has one, and of each stage the keys of its group; it keeps a
-// running maximum, sum and output of its own, and the block joins the groups once per item.
-// bf16: mma.sync on the rows as they are, probabilities in two bf16 parts (16 bits), so that the
-// output's own rounding is what remains. fp32: fused multiply-adds. Scores, sums and outputs are fp32.
+// Work is dealt out as in the 8-bit attention (kv8_plan.cuh): items of a sequence, tile of query rows and
+// KV head, their keys in units of 64 on a line that all blocks share, parts joined by k_kv8_merge; or, where
+// sequences are short, a cluster of blocks for each item. The kernels, chosen by the rules in front of plan_of:
+// - k_paged_rows: 8 to 64 rows a block, two blocks an SM, clusters; for short sequences, for fp32, and for more
+//   than 16 rows of head_dim 64;
+// - k_paged_stream (paged_stream.cuh): up to 16 rows over long sequences, one block an SM;
+// - k_paged_wide (paged_wide.cuh): more rows, on tcgen05.
+//
+// k_paged_rows: stages of 32 or 64 keys and values come by cp.async, kNst - 1 of them on their way. A warp has
+// a tile of the item's rows and, of each stage, the keys of its group; it keeps a running maximum,
+// sum and output of its own, and the block joins the groups once per item. bf16: mma.sync on the rows as they
+// are, probabilities in two bf16 parts (16 bits), so that the output's own rounding is what
+// remains. fp32: fused multiply-adds. Scores, sums and outputs are fp32. A cluster's blocks write their parts to
+// the shared memory of the block that joins the row, so one barrier lies between them and its sums.
+//
+// Bound by bytes for long sequences: 1 row of 32 heads over 8 KV heads x 131072 keys in pages of 64, 83.9 us = 6.4 TB/s
+// (7.2 once it runs; 5 us are the start, 4 the join), fp32 1 row over 4 x 100000 keys of head_dim 64 40 us = 5.1
+// TB/s. By round trips of memory for short ones: 1 row at 1100 keys 8.9 us, of which 1.0 are positions, 1.3 table
+// and queries, 0.7 the first keys, 1.8 three stages, 3.6 the joins of warps and blocks.
 //
 // A key that some row of the tile does not see can hold anything: its scores are dropped by
 // position, and a value there that is no number is zeroed before the product. A row that sees one
@@ -898,8 +910,29 @@ cudaError_t paged_device(int* sms) {
 }
 
 // Short sequences: a cluster of blocks for each item, which joins its parts itself (no workspace, no
-// second launch): 1, 2, 4 or 8 blocks with 128 keys or more each, as long as there is room for all.
-constexpr int kSplitKeys = 128, kSplitBlocks = 304, kSplitSeq = 512, kSplitMost = 2048;
+// second launch): 1, 2, 4 or 8 blocks with 128 keys or more each, as long as there is room for all, two on each of
+// 152 SMs; up to 512 keys a block and 2048 in all (fp32 1024, and 512 for more than 8 rows, whose blocks are bound by
+// their multiply-adds). What counts is how many keys an item's rows can see: what the caller says
+// of the lengths, or the window. us on the GPU, line / clusters, all sequences of
+//                                   128       512        1024       2048       4096 positions
+//   1 x 8 KV heads, 4 rows       9.5/5.1    9.5/7.2    9.9/7.9  10.2/10.0  11.3/14.3
+//   1 x 8, 16 rows              12.5/6.6   13.2/8.7   13.6/9.5  13.8/11.7  15.0/16.4
+//   1 x 40, 2 rows              10.2/5.5   10.6/7.8  12.8/10.3  15.4/15.3  20.8/25.1
+//   16 x 8, 4 rows              12.9/5.6  16.6/10.5  21.7/15.3  32.3/27.4  51.3/46.9
+//   1 x 8, 32 rows              11.6/8.3  12.5/10.6  13.5/11.2  14.8/15.1  15.8/23.0
+//   fp32, 1 x 4, 1 row           8.5/6.1    8.7/7.8    8.9/8.4   8.7/10.6   9.7/14.6
+//   fp32, 1 x 4, 12 rows       12.4/11.4  12.8/13.1  12.8/14.2  12.9/21.1  15.4/35.5
+// (sequences of one length, for which clusters are at their best.)
+// More than 16 rows a KV head, bf16 and head_dim 128: tcgen05 tiles, but for 17 to 32 rows where there are
+// clusters. us, k_paged_rows / k_paged_wide, 8 KV heads, sequences x keys:
+//                   17 rows       32         33         64
+//   1 x 250       10.5/11.2  10.9/11.7  14.5/12.1  15.9/12.2
+//   1 x 1000      10.7/13.5  11.2/14.0  13.8/14.1  14.7/14.5
+//   1 x 4000      18.0/15.1  18.9/15.8  22.2/15.9  23.9/16.3
+//   16 x 250      12.4/19.0  13.0/20.4  16.9/20.4  18.7/21.1
+//   16 x 1000     26.5/26.1  27.6/27.3  39.9/27.6  42.4/29.1
+//   16 x 16000     269/175    271/177    426/178    436/180
+constexpr int kSplitKeys = 128, kSplitBlocks = 304, kSplitSeq = 512;
 
 struct PagedPlan {
   int wide;   // accumulators of a tile on tcgen05, 0: mma.sync
@@ -924,7 +957,8 @@ PagedPlan plan_of(const ssd_paged_cache* c, int n_heads, int M, int longest, int
   p.split = 1;
   while (p.split < kSplitMax && span > kSplitKeys * p.split && items * p.split * 2 <= kSplitBlocks)
     p.split *= 2;
-  if (span > kSplitSeq * p.split || span > kSplitMost) p.split = 0;
+  const int most = c->dtype == SSD_DTYPE_BF16 ? 2048 : rows > 8 ? 512 : 1024;
+  if (span > kSplitSeq * p.split || span > most) p.split = 0;
   p.wide = 0;
   if (c->dtype == SSD_DTYPE_BF16 && c->head_dim == kWHd && rows > (p.split ? 2 * kTile : kTile)) {
     p.wide = rows > kWRows ? 2 : 1;

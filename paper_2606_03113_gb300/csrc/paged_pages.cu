@@ -1,6 +1,10 @@
 // paged_pages.cu -- the pages of a paged KV cache: reserved, copied on write, forked, given back,
 // compacted, and rows appended to them.
 //
+// us on the GPU: a reserve that finds its pages there 4.2 (two launches), a fork 1.5 to 3.6, a step of 64 sequences
+// with 24 copies of 5.2 MB 39.6 (6.2 TB/s), 100 pages of 5.2 MB moved by a compaction 172 (6.1 TB/s), 2047 rows of 40
+// heads appended 14.6 a call (5.8 TB/s), 16 rows of 8 heads 2.2.
+//
 // Which page goes where is whole-number work on a table and a few counts, bound by round trips of
 // memory (a table entry, its page's count) and not by bytes; what is moved is bound by bytes. So one
 // block plans (its barriers order the steps that have to see each other's counts) and
@@ -615,7 +619,9 @@ const char* check_work(const ssd_paged_cache* c, const void* workspace, size_t b
 }
 
 // Pools for which the planning block has 256 threads, whose barriers cost less, and above which 1024, which
-// look at more counts at once.
+// look at more counts at once. us, fork and reserve, 256 / 1024 threads: 4 sequences and 12 pages 8.7 / 10.7,
+// 64 sequences with 24 copies of 5 MB and 146 pages 39.6 / 40.4, 192 sequences with 1548 new pages of 30961
+// 28.6 / 17.9.
 constexpr int kSmallPool = 8192;
 
 // The launch that carries a plan out: up to four blocks an SM.

@@ -14,8 +14,14 @@
 //    maximum, p = 2^(s - ref) as bf16, which takes the place of S. ref is the row's maximum as of the
 //    last time it grew by more than 8 (in powers of two), so O is rescaled in tensor memory only
 //    then.
-// A probability keeps bf16's 8 bits here (an error of the size of the output's own rounding at most: a
-// second part would take half as many products again, and these tiles are close to bound by them).
+// A probability keeps bf16's 8 bits here, and is summed so rounded (the weights add up to one; an error of the size of
+// the output's own rounding at most): a second part would take half as many products again.
+//
+// 17 rows of 64 heads over 8 x 16000 keys: 28.8 us; 8 x 100000 keys, 64 rows a KV head 79 us (5.2 TB/s), 256 rows
+// 98, 512 rows 175 (1.2 PFLOP/s). Of the 28.8, 6.4 lie in front of the first scores (the plan 1.8, the next
+// item's look-up, the first pages and keys), 13 are 13 steps of 64 keys, 3.3 the outputs, 4 the join. A step takes
+// 0.95 us, 0.7 would be its bytes: the softmax of a row is one chain of scores to registers, their maximum, 64
+// exponentials (512 cycles of a quarter of an SM) and probabilities back.
 #pragma once
 
 #include "attn_wide.cuh"
