@@ -398,22 +398,29 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
                 make_float4(f[4 * x], f[4 * x + 1], f[4 * x + 2], f[4 * x + 3]);
           if (!(q & 1)) continue;
           __syncwarp();
-          const int rows = min(32, it.nr - warp * 32);
-          for (int y = lane >> 4; y < rows; y += 2) {
-            const float4 v = *reinterpret_cast<const float4*>(xs + y * 256 + ((c4 ^ (y & 15)) << 4));
-            const int col = (q >> 1) * 64 + c4 * 4;
-            if (whole) {
+          const int rows = min(32, it.nr - warp * 32), col = (q >> 1) * 64 + c4 * 4;
+          auto from = [&](int y) -> float4 {
+            return *reinterpret_cast<const float4*>(xs + y * 256 + ((c4 ^ (y & 15)) << 4));
+          };
+          if (whole) {
+#pragma unroll 4
+            for (int y = lane >> 4; y < rows; y += 2) {
+              const float4 v = from(y);
               const int r = it.r0 + warp * 32 + y, m = a.byG(r), h = sg.g * a.G + r - m * a.G;
               const __nv_bfloat162 b0 = __floats2bfloat162_rn(v.x, v.y);
               const __nv_bfloat162 b1 = __floats2bfloat162_rn(v.z, v.w);
               *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) +
-                                        ((int64_t)it.b * a.M + m) * a.out_stride +
-                                        (int64_t)h * kWHd + col) =
+                                        ((int64_t)it.b * a.M + m) * a.out_stride + (int64_t)h * kWHd +
+                                        col) =
                   make_uint2(*reinterpret_cast<const uint32_t*>(&b0),
                              *reinterpret_cast<const uint32_t*>(&b1));
-            } else {
-              *reinterpret_cast<float4*>(
-                  a.part + ((size_t)slot * a.part_rows + warp * 32 + y) * kWHd + col) = v;
+            }
+          } else {
+            float* const to = a.part + ((size_t)slot * a.part_rows + warp * 32) * kWHd + col;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int y = (lane >> 4) + 2 * i;
+              if (y < rows) *reinterpret_cast<float4*>(to + y * kWHd) = from(y);
             }
           }
           __syncwarp();
