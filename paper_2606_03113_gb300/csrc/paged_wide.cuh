@@ -14,14 +14,16 @@
 //    maximum, p = 2^(s - ref) as bf16, which takes the place of S. ref is the row's maximum as of the
 //    last time it grew by more than 8 (in powers of two), so O is rescaled in tensor memory only
 //    then.
-// A probability keeps bf16's 8 bits here, and is summed so rounded (the weights add up to one; an error of the size of
-// the output's own rounding at most): a second part would take half as many products again.
+// A probability keeps bf16's 8 bits here, and is summed so rounded (the weights add up to one; an
+// error of the size of the output's own rounding at most): a second part would take half as many
+// products again.
 //
-// 17 rows of 64 heads over 8 x 16000 keys: 28.8 us; 8 x 100000 keys, 64 rows a KV head 79 us (5.2 TB/s), 256 rows
-// 98, 512 rows 175 (1.2 PFLOP/s). Of the 28.8, 6.4 lie in front of the first scores (the plan 1.8, the next
-// item's look-up, the first pages and keys), 13 are 13 steps of 64 keys, 3.3 the outputs, 4 the join. A step takes
-// 0.95 us, 0.7 would be its bytes: the softmax of a row is one chain of scores to registers, their maximum, 64
-// exponentials (512 cycles of a quarter of an SM) and probabilities back.
+// 17 rows of 64 heads over 8 x 16000 keys: 28 us; 8 x 100000 keys, 64 rows a KV head 73 us (5.6 TB/s),
+// 256 rows 98, 512 rows 172 (1.2 PFLOP/s). Of the 28, 6.4 lie in front of the first scores (the plan 1.8,
+// the next item's look-up, the first pages and keys), 12 are 13 steps of 64 keys, 3 the outputs, 4 the
+// join. A step of two accumulators takes 0.95 us, 0.7 would be its bytes: the softmax's warps, two a
+// quarter of an SM, issue 0.7 of it. Two threads a row halve a row's chain, but add instructions and
+// barriers: 17 to 128 rows were as fast as now, 136 and more 10 to 15 % slower.
 #pragma once
 
 #include "attn_wide.cuh"
@@ -49,11 +51,12 @@ constexpr float kPFar = 1048576.f;  // 2^20: half a unit there is 2^-4
 constexpr uint32_t kPIdesc = idesc_bf16_f32(128, kWKeys);
 constexpr uint32_t kPIdescV = idesc_bf16_f32(128, kWHd) | 1u << 16;
 
-// Barriers: a ring step's keys and values stored, and free again; of the two buffers of S: scores
-// there, probabilities there, output added; queries of the segment stored.
+// Barriers: a ring step's keys and values stored, and free again (one each for both: with barriers of
+// their own, which 128 threads arrive at, 8 x 100000 keys took 78 us for 72); of the two buffers of S:
+// scores there, probabilities there, output added; queries of the segment stored.
 template <int TILES>
 struct PWideBars {
-  uint64_t k_full[5], v_full[5], k_free[5], v_free[5];
+  uint64_t full[PWideL<TILES>::kNst], free[PWideL<TILES>::kNst];
   uint64_t s_done[TILES][2], p_full[TILES][2], o_done[TILES][2], q_full[TILES];
   uint64_t drained;  // after a wait that gave up: the products still in flight are done
 };
@@ -85,10 +88,8 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
   pdl_wait();
   if (tid == 0) {
     for (int i = 0; i < L::kNst; ++i) {
-      mbar_init(&bar.k_full[i], 128);
-      mbar_init(&bar.v_full[i], 128);
-      mbar_init(&bar.k_free[i], TILES);
-      mbar_init(&bar.v_free[i], TILES);
+      mbar_init(&bar.full[i], 128);
+      mbar_init(&bar.free[i], TILES);
     }
     for (int t = 0; t < TILES; ++t) {
       for (int i = 0; i < 2; ++i) {
@@ -127,7 +128,7 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
     for (uint32_t seg = 0; kv8_next<L::kRows, kWKeys>(a, cur, sg); ++seg) {
       p_wait(&bar.q_full[t], seg & 1, bad);
       for (int i = 0; i < sg.nu; ++i, ++n, ring.next()) {
-        p_wait(&bar.k_full[ring.at], ring.phase, bad);
+        p_wait(&bar.full[ring.at], ring.phase, bad);
         if (n >= 2) p_wait2(bar.o_done[t], n - 2, bad);  // P of that step was read there
         w_smem_fence();
         __syncwarp();
@@ -139,10 +140,7 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
             w_mma(tmS + buf * kWKeys, dq + (((k >> 2) * kWQHalf + (k & 3) * 32) >> 4),
                   dk + ((ring.at * L::kStep + (k >> 2) * kWKHalf + (k & 3) * 32) >> 4), kPIdesc, k > 0,
                   one);
-        if (one) {
-          tc_commit(&bar.s_done[t][buf]);
-          tc_commit(&bar.k_free[ring.at]);
-        }
+        if (one) tc_commit(&bar.s_done[t][buf]);
       }
     }
   } else if (warp >= L::kPv) {
@@ -154,7 +152,7 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
     const uint64_t dv = w_desc_mn(smem_u32(Ks + kWKTile));
     while (kv8_next<L::kRows, kWKeys>(a, cur, sg))
       for (int i = 0; i < sg.nu; ++i, ++n, ring.next()) {
-        p_wait(&bar.v_full[ring.at], ring.phase, bad);
+        p_wait(&bar.full[ring.at], ring.phase, bad);
         p_wait2(bar.p_full[t], n, bad);
         w_smem_fence();
         __syncwarp();
@@ -167,7 +165,7 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
                      kPIdescV, i > 0 || k > 0, one);
         if (one) {
           tc_commit(&bar.o_done[t][buf]);
-          tc_commit(&bar.v_free[ring.at]);
+          tc_commit(&bar.free[ring.at]);
         }
       }
   } else if (warp >= L::kSoft) {
@@ -205,19 +203,17 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
         const uint32_t dst = smem_u32(Ks) + ring.at * L::kStep + to + w_place(r0, ch & 7);
         size_t off[kWKeys / 16];
         find_keys<kWKeys, kWHd * 2>(walk, k0, off);
-        if (n >= (uint32_t)L::kNst) p_wait(&bar.k_free[ring.at], ring.phase ^ 1, bad);
+        if (n >= (uint32_t)L::kNst) p_wait(&bar.free[ring.at], ring.phase ^ 1, bad);
         copy_keys<kWKeys, kWHd * 2, 8>(off, kp, r0, k0, it.lo, it.hi + 1,
                                        [&](int r) { return dst + (uint32_t)(r * 128); });
-        p_arrive(&bar.k_full[ring.at]);
-        if (n >= (uint32_t)L::kNst) p_wait(&bar.v_free[ring.at], ring.phase ^ 1, bad);
         copy_keys<kWKeys, kWHd * 2, 8>(off, vp, r0, k0, it.lo, it.hi + 1,
                                        [&](int r) { return dst + kWKTile + (uint32_t)(r * 128); });
         if (k0 >= full_lo && k0 + kWKeys - 1 <= full_hi) {
-          p_arrive(&bar.v_full[ring.at]);
+          p_arrive(&bar.full[ring.at]);
         } else {
           asm volatile("cp.async.wait_all;" ::: "memory");
           clean();
-          mbar_arrive(&bar.v_full[ring.at]);
+          mbar_arrive(&bar.full[ring.at]);
         }
       }
     }
