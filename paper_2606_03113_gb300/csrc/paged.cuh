@@ -30,10 +30,10 @@ struct PagedView {
   __host__ __device__ __forceinline__ size_t head() const { return (size_t)2 * slab; }
 };
 
-// The pages of a sequence's entries in order, for a warp that walks keys kb .. ke - 1: a lane holds one of
-// 32 entries, and the next 32 are on their way meanwhile. (Looked up a stage of 64 keys ahead, an entry that had
-// to come from memory held the copies up: pages of 16, 64 and 256 positions were read at 5.6, 6.4 and 6.7 TB/s,
-// now at 6.5, 7.2 and 7.4.)
+// The pages of a sequence's entries in order, for a warp that walks keys kb .. ke - 1: a lane holds one
+// of 32 entries, and the next 32 are on their way meanwhile. (Looked up a stage of 64 keys ahead, an
+// entry that had to come from memory held the copies up: pages of 16, 64 and 256 positions were read at
+// 5.6, 6.4 and 6.7 TB/s, now at 6.5, 7.2 and 7.4.)
 struct PageWalk {
   const PagedView* view;
   int32_t* err;
@@ -67,7 +67,8 @@ struct PageWalk {
   }
 };
 
-// Where keys k0 .. k0 + KEYS - 1 stand, by sixteens, which lie in one page each: bytes from position 0 of page 0.
+// Where keys k0 .. k0 + KEYS - 1 stand, by sixteens, which lie in one page each: bytes from position 0
+// of page 0.
 template <int KEYS, int ROW_BYTES>
 __device__ __forceinline__ void find_keys(PageWalk& walk, int k0, size_t (&off)[KEYS / 16]) {
 #pragma unroll
@@ -75,9 +76,9 @@ __device__ __forceinline__ void find_keys(PageWalk& walk, int k0, size_t (&off)[
     off[j] = (size_t)walk.page(k0 + 16 * j) * walk.view->bytes +
              (size_t)((k0 + 16 * j) & ((1 << walk.view->shift) - 1)) * ROW_BYTES;
 }
-// Copies them (or their values) to shared memory, zeros for those outside of kb .. ke - 1, as one of the
-// threads that hold PASS rows at a time: p at its chunk of its row (r0, below PASS) of position 0 of page 0, to(r)
-// where that chunk of row r0 + r goes.
+// Copies them (or their values) to shared memory, zeros for those outside of kb .. ke - 1, as one of
+// the threads that hold PASS rows at a time: p at its chunk of its row (r0, below PASS) of position 0
+// of page 0, to(r) where that chunk of row r0 + r goes.
 template <int KEYS, int ROW_BYTES, int PASS, typename To>
 __device__ __forceinline__ void copy_keys(const size_t (&off)[KEYS / 16], const char* p, int r0, int k0,
                                           int kb, int ke, To to) {
@@ -90,10 +91,11 @@ __device__ __forceinline__ void copy_keys(const size_t (&off)[KEYS / 16], const 
   }
 }
 
-// Launches a call's first kernel, which begins with pdl_wait(): its blocks take their places while the kernel before
-// it in the stream ends (a call of 9 us takes 12 otherwise; not while a graph is captured, where what comes before
-// need not be a kernel). What that kernel may have written is read by plain loads, not as read-only data, which
-// has to be constant while a kernel is resident. cluster: blocks of a cluster, or 1.
+// Launches a call's first kernel, which begins with pdl_wait(): its blocks take their places while the
+// kernel before it in the stream ends (a call of 9 us takes 12 otherwise; not while a graph is
+// captured, where what comes before need not be a kernel). What that kernel may have written is read by
+// plain loads, not as read-only data, which has to be constant while a kernel is resident. cluster:
+// blocks of a cluster, or 1.
 template <typename Kern, typename... Args>
 cudaError_t launch_first(Kern k, dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st,
                          Args... args) {

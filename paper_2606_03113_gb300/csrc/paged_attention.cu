@@ -2,25 +2,28 @@
 //   o_r = sum_j p_rj v_j / sum_j p_rj,  p_rj = e^(q_r . k_j / sqrt(hd) - max),
 // over the keys j that row r sees: first .. its own position, at most `window`.
 //
-// Work is dealt out as in the 8-bit attention (kv8_plan.cuh): items of a sequence, tile of query rows and
-// KV head, their keys in units of 64 on a line that all blocks share, parts joined by k_kv8_merge; or, where
-// sequences are short, a cluster of blocks for each item. The kernels, chosen by the rules in front of plan_of:
-// - k_paged_rows: 8 to 64 rows a block, two blocks an SM, clusters; for short sequences, for fp32, and for more
-//   than 16 rows of head_dim 64;
+// Work is dealt out as in the 8-bit attention (kv8_plan.cuh): items of a sequence, tile of query rows
+// and KV head, their keys in units of 64 on a line that all blocks share, parts joined by k_kv8_merge;
+// or, where sequences are short, a cluster of blocks for each item. The kernels, chosen by the rules in
+// front of plan_of:
+// - k_paged_rows: 8 to 64 rows a block, two blocks an SM, clusters; for short sequences, for fp32, and
+//   for more than 16 rows of head_dim 64;
 // - k_paged_stream (paged_stream.cuh): up to 16 rows over long sequences, one block an SM;
 // - k_paged_wide (paged_wide.cuh): more rows, on tcgen05.
 //
-// k_paged_rows: stages of 32 or 64 keys and values come by cp.async, kNst - 1 of them on their way. A warp has
-// a tile of the item's rows and, of each stage, the keys of its group; it keeps a running maximum,
-// sum and output of its own, and the block joins the groups once per item. bf16: mma.sync on the rows as they
-// are, probabilities in two bf16 parts (16 bits), so that the output's own rounding is what
-// remains. fp32: fused multiply-adds. Scores, sums and outputs are fp32. A cluster's blocks write their parts to
-// the shared memory of the block that joins the row, so one barrier lies between them and its sums.
+// k_paged_rows: stages of 32 or 64 keys and values come by cp.async, kNst - 1 of them on their way. A
+// warp has a tile of the item's rows and, of each stage, the keys of its group; it keeps a running
+// maximum, sum and output of its own, and the block joins the groups once per item. bf16: mma.sync on
+// the rows as they are, probabilities in two bf16 parts (16 bits), so that the output's own rounding is
+// what remains. fp32: fused multiply-adds. Scores, sums and outputs are fp32. A cluster's blocks write
+// their parts to the shared memory of the block that joins the row, so one barrier lies between them
+// and its sums.
 //
-// Bound by bytes for long sequences: 1 row of 32 heads over 8 KV heads x 131072 keys in pages of 64, 83.9 us = 6.4 TB/s
-// (7.2 once it runs; 5 us are the start, 4 the join), fp32 1 row over 4 x 100000 keys of head_dim 64 40 us = 5.1
-// TB/s. By round trips of memory for short ones: 1 row at 1100 keys 8.9 us, of which 1.0 are positions, 1.3 table
-// and queries, 0.7 the first keys, 1.8 three stages, 3.6 the joins of warps and blocks.
+// Bound by bytes for long sequences: 1 row of 32 heads over 8 KV heads x 131072 keys in pages of 64,
+// 83.9 us = 6.4 TB/s (7.2 once it runs; 5 us are the start, 4 the join), fp32 1 row over 4 x 100000
+// keys of head_dim 64 40 us = 5.1 TB/s. By round trips of memory for short ones: 1 row at 1100 keys 8.9
+// us, of which 1.0 are positions, 1.3 table and queries, 0.7 the first keys, 1.8 three stages, 3.6 the
+// joins of warps and blocks.
 //
 // A key that some row of the tile does not see can hold anything: its scores are dropped by
 // position, and a value there that is no number is zeroed before the product. A row that sees one
@@ -42,7 +45,8 @@ constexpr int kUnit = kKv8Block;  // keys of a unit of the plan
 constexpr int kTile = 16;         // query rows of a warp, at most
 constexpr int kSplitMax = 8;      // blocks of a short sequence's item, a cluster, at most
 
-// The cluster's barrier in two halves (a warp's lanes can come apart), and writes to another block's shared memory.
+// The cluster's barrier in two halves (a warp's lanes can come apart), and writes to another block's
+// shared memory.
 __device__ __forceinline__ void cluster_arrive() {
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
 }
@@ -113,8 +117,8 @@ __device__ __forceinline__ float4 lds4(const unsigned char* p) {
   return *reinterpret_cast<const float4*>(p);
 }
 
-// What a warp holds of up to 8 query rows, fp32: every lane has all rows, HD / 32 columns of each; a step is of
-// KEYS keys, a key's score the sum of 32 / KEYS lanes.
+// What a warp holds of up to 8 query rows, fp32: every lane has all rows, HD / 32 columns of each; a
+// step is of KEYS keys, a key's score the sum of 32 / KEYS lanes.
 template <int HD, int KEYS>
 struct FewTile {
   static constexpr int kRows = 8, C = HD / 32, SUB = 32 / KEYS;
@@ -291,11 +295,11 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   return r;
 }
 
-// What a warp holds of 8 NB query rows, bf16. Keys are the matrix rows of its products (S^T = K Q^T, 16 keys
-// x 8 query rows an instruction, and O^T = V^T P^T), so that the few rows of a decode step take half of
-// the instructions that a tile of 16 would: mma.sync is what a step of 16 keys takes longest for (24 of them for 8
-// rows, 48 for 16; about 19 cycles each of a quarter of an SM). Lane n8, t has keys n8 and n8 + 8, rows
-// 8 b + 2 t and + 1.
+// What a warp holds of 8 NB query rows, bf16. Keys are the matrix rows of its products (S^T = K Q^T, 16
+// keys x 8 query rows an instruction, and O^T = V^T P^T), so that the few rows of a decode step take
+// half of the instructions that a tile of 16 would: mma.sync is what a step of 16 keys takes longest
+// for (24 of them for 8 rows, 48 for 16; about 19 cycles each of a quarter of an SM). Lane n8, t has
+// keys n8 and n8 + 8, rows 8 b + 2 t and + 1.
 template <int HD, int NB>
 struct ColTile {
   float o[HD / 16][NB][4], mx[NB][2], ls[NB][2];  // outputs (columns 16 j + n8, + 8), maxima, sums
@@ -413,8 +417,8 @@ struct ColTile {
 };
 
 // The rows of a block's part of an item, from what GROUPS groups of warps left: outputs in Ox
-// [GROUPS][ROWS][HD + 4], weights s_w (NULL: 1), the rows' maxima and sums. Of keys kb .. ke - 1. To the output,
-// to the workspace, or, for a cluster's join, where `put` says.
+// [GROUPS][ROWS][HD + 4], weights s_w (NULL: 1), the rows' maxima and sums. Of keys kb .. ke - 1. To
+// the output, to the workspace, or, for a cluster's join, where `put` says.
 template <typename T, int HD, int GROUPS, int ROWS, int THREADS, typename Put>
 __device__ __forceinline__ void finish_rows(const PagedAttn& a, const Kv8Seg& sg, int kb, int ke,
                                             const float* Ox, const float (*s_w)[ROWS],
@@ -746,7 +750,8 @@ __global__ void __launch_bounds__(PL<T, HD, R, NB>::kThreads, 2) k_paged_rows(co
       for (int r = 0; r < 8; ++r)
         if (r < it.nr)
 #pragma unroll
-          for (int c = 0; c < C; ++c) Ox[(size_t)(grp * L::kRows + r) * L::kOPad + lane * C + c] = w.o[r][c];
+          for (int c = 0; c < C; ++c)
+            Ox[(size_t)(grp * L::kRows + r) * L::kOPad + lane * C + c] = w.o[r][c];
     } else {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -910,10 +915,10 @@ cudaError_t paged_device(int* sms) {
 }
 
 // Short sequences: a cluster of blocks for each item, which joins its parts itself (no workspace, no
-// second launch): 1, 2, 4 or 8 blocks with 128 keys or more each, as long as there is room for all, two on each of
-// 152 SMs; up to 512 keys a block and 2048 in all (fp32 1024, and 512 for more than 8 rows, whose blocks are bound by
-// their multiply-adds). What counts is how many keys an item's rows can see: what the caller says
-// of the lengths, or the window. us on the GPU, line / clusters, all sequences of
+// second launch): 1, 2, 4 or 8 blocks with 128 keys or more each, as long as there is room for all, two
+// on each of 152 SMs; up to 512 keys a block and 2048 in all (fp32 1024, and 512 for more than 8 rows,
+// whose blocks are bound by their multiply-adds). What counts is how many keys an item's rows can see:
+// what the caller says of the lengths, or the window. us on the GPU, line / clusters, all sequences of
 //                                   128       512        1024       2048       4096 positions
 //   1 x 8 KV heads, 4 rows       9.5/5.1    9.5/7.2    9.9/7.9  10.2/10.0  11.3/14.3
 //   1 x 8, 16 rows              12.5/6.6   13.2/8.7   13.6/9.5  13.8/11.7  15.0/16.4

@@ -1,9 +1,9 @@
 // paged_pages.cu -- the pages of a paged KV cache: reserved, copied on write, forked, given back,
 // compacted, and rows appended to them.
 //
-// us on the GPU: a reserve that finds its pages there 4.2 (two launches), a fork 1.5 to 3.6, a step of 64 sequences
-// with 24 copies of 5.2 MB 39.6 (6.2 TB/s), 100 pages of 5.2 MB moved by a compaction 172 (6.1 TB/s), 2047 rows of 40
-// heads appended 14.6 a call (5.8 TB/s), 16 rows of 8 heads 2.2.
+// us on the GPU: a reserve that finds its pages there 4.2 (two launches), a fork 1.5 to 3.6, a step of
+// 64 sequences with 24 copies of 5.2 MB 39.6 (6.2 TB/s), 100 pages of 5.2 MB moved by a compaction 172
+// (6.1 TB/s), 2047 rows of 40 heads appended 14.6 a call (5.8 TB/s), 16 rows of 8 heads 2.2.
 //
 // Which page goes where is whole-number work on a table and a few counts, bound by round trips of
 // memory (a table entry, its page's count) and not by bytes; what is moved is bound by bytes. So one
@@ -618,10 +618,10 @@ const char* check_work(const ssd_paged_cache* c, const void* workspace, size_t b
   return nullptr;
 }
 
-// Pools for which the planning block has 256 threads, whose barriers cost less, and above which 1024, which
-// look at more counts at once. us, fork and reserve, 256 / 1024 threads: 4 sequences and 12 pages 8.7 / 10.7,
-// 64 sequences with 24 copies of 5 MB and 146 pages 39.6 / 40.4, 192 sequences with 1548 new pages of 30961
-// 28.6 / 17.9.
+// Pools for which the planning block has 256 threads, whose barriers cost less, and above which 1024,
+// which look at more counts at once. us, fork and reserve, 256 / 1024 threads: 4 sequences and 12 pages
+// 8.7 / 10.7, 64 sequences with 24 copies of 5 MB and 146 pages 39.6 / 40.4, 192 sequences with 1548
+// new pages of 30961 28.6 / 17.9.
 constexpr int kSmallPool = 8192;
 
 // The launch that carries a plan out: up to four blocks an SM.
@@ -671,9 +671,9 @@ extern "C" ssd_status ssd_paged_reserve(const ssd_paged_cache* c, const int32_t*
   const PagedView v = paged_view(c);
   const PlanWork w = plan_work(workspace, c->n_pages);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = c->n_pages <= kSmallPool
-                      ? launch_first(k_paged_reserve<256>, dim3(1), 256, 0, 1, st, v, w, pos, rows, M, err_dev)
-                      : launch_first(k_paged_reserve<1024>, dim3(1), 1024, 0, 1, st, v, w, pos, rows, M, err_dev);
+  const bool small = c->n_pages <= kSmallPool;
+  cudaError_t e = launch_first(small ? k_paged_reserve<256> : k_paged_reserve<1024>, dim3(1),
+                               small ? 256 : 1024, 0, 1, st, v, w, pos, rows, M, err_dev);
   if (e == cudaSuccess)
     e = carry_out(k_paged_copy, v, w, c->n_seq < c->n_pages ? c->n_seq : c->n_pages, 1, st);
   return e == cudaSuccess ? SSD_OK : fail_op_cuda("ssd_paged_reserve", e);

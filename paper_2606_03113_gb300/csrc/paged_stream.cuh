@@ -6,11 +6,12 @@
 // eight take every other stage by fours, 16 keys each, and at an item's end join what they have while the
 // ring fills with the next one's.
 //
-// Bound by bytes: pages of 16, 64 and 256 positions are read at 6.5, 7.2 and 7.4 TB/s (262144 keys more of 8 KV heads);
-// 24 ragged sequences of 32 heads, 5 rows each, window 2500, pages of 16: 117 us = 5.8 TB/s, where an item of
-// 20 stages takes 2 us longer than its bytes, since the copying warps' 160 KB do not last for the joins of
-// eight warps. mma.sync is the next bound: 24 instructions of about 19 cycles a warp's step (9 to 16 rows: 48), two warps
-// a quarter of an SM, are 0.25 of the 0.7 us that a stage's bytes take.
+// Bound by bytes: pages of 16, 64 and 256 positions are read at 6.5, 7.2 and 7.4 TB/s (262144 keys more
+// of 8 KV heads); 24 ragged sequences of 32 heads, 5 rows each, window 2500, pages of 16: 117 us = 5.8
+// TB/s, where an item of 20 stages takes 2 us longer than its bytes, since the copying warps' 160 KB do
+// not last for the joins of eight warps. mma.sync is the next bound: 24 instructions of about 19 cycles
+// a warp's step (9 to 16 rows: 48), two warps a quarter of an SM, are 0.25 of the 0.7 us that a stage's
+// bytes take.
 #pragma once
 
 #include "attn_wide.cuh"

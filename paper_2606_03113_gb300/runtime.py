@@ -448,9 +448,9 @@ class KV8Cache:
 class PagedKVCache:
     """A decoder's KV cache in pages that sequences share and give back (ssd_paged_cache,
     include/ssd_ops.h): `pages` [n_pages, n_layers, 2 (K, V), n_kv_heads, page, head_dim] (a view: in
-    memory the heads stand in front of K and V), the pages of each sequence in `table` [n_seq, max_seq / page] (-1: none), how many entries name each page in
-    `refs` [n_pages] (0: free).  `max_seq` is rounded up to a multiple of `page` (a power of
-    two from 16 to 256).
+    memory the heads stand in front of K and V), the pages of each sequence in `table`
+    [n_seq, max_seq / page] (-1: none), how many entries name each page in `refs` [n_pages] (0: free).
+    `max_seq` is rounded up to a multiple of `page` (a power of two from 16 to 256).
 
     A step of decoding: `fork` where sequences branch, are cut back or end; `reserve` the places of the new
     rows (a shared page is copied before it is written); for each layer `append` their K and V and
