@@ -309,8 +309,9 @@ size_t ssd_paged_attention_bytes(const ssd_paged_cache* cache, int32_t n_heads, 
  * alone (SSD_DEV_ERR_CAPACITY).  A row that sees no key is zero.  Rows from rows[b] on are left as they
  * were.  What stands in a key or value that a row does not see never reaches it; an infinity or NaN
  * in one that it sees does.  A sequence some visible position of which has no page
- * (SSD_PAGED_ERR_TABLE) has undefined rows.  Scores, sums and outputs are fp32.  Equal calls give
- * equal bits. */
+ * (SSD_PAGED_ERR_TABLE) has undefined rows.  Scores, sums and outputs are fp32, and so are the
+ * probabilities of an fp32 cache; those of a bf16 cache are multiplied with the values with 16 bits
+ * (2^-16 of each), whatever the sizes and `longest`.  Equal calls give equal bits. */
 ssd_status ssd_paged_attention(const ssd_paged_cache* cache, int32_t layer, const void* q,
                                int32_t n_heads, int64_t q_stride, int32_t M, const int32_t* pos,
                                const int32_t* rows, const int32_t* first, int32_t window,

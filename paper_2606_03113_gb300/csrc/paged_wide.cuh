@@ -11,19 +11,22 @@
 //    buffers) for a step while the softmax of the step before is at work, another one O += P V,
 //    P read from tensor memory, as soon as a softmax is done;
 //  - four an accumulator do the softmax, a thread per row: the row's 64 scores into registers, their
-//    maximum, p = 2^(s - ref) as bf16, which takes the place of S. ref is the row's maximum as of the
-//    last time it grew by more than 8 (in powers of two), so O is rescaled in tensor memory only
-//    then.
-// A probability keeps bf16's 8 bits here, and is summed so rounded (the weights add up to one; an
-// error of the size of the output's own rounding at most): a second part would take half as many
-// products again.
+//    maximum, p = 2^(s - ref) as two bf16 parts, which take the place of S. ref is the row's maximum
+//    as of the last time it grew by more than 8 (in powers of two), so O is rescaled in tensor
+//    memory only then.
+// A probability's two parts keep 16 bits of it, as in the kernels for fewer rows. One part is not enough: an
+// error of 2^-8 of each weight is one of up to 2^-8 sum w |v|, many units of an output whose values
+// cancel (17 rows of 64 heads over 16000 keys were 0.0022 off for 0.0017 with fp32 weights, which two
+// parts give back). The second part is half as many products again, conversions and stores: 28 -> 31 us,
+// 73 -> 77.5, 98 -> 126 and 174 -> 227 for the sizes below.
 //
-// 17 rows of 64 heads over 8 x 16000 keys: 28 us; 8 x 100000 keys, 64 rows a KV head 73 us (5.6 TB/s),
-// 256 rows 98, 512 rows 172 (1.2 PFLOP/s). Of the 28, 6.4 lie in front of the first scores (the plan 1.8,
-// the next item's look-up, the first pages and keys), 12 are 13 steps of 64 keys, 3 the outputs, 4 the
-// join. A step of two accumulators takes 0.95 us, 0.7 would be its bytes: the softmax's warps, two a
-// quarter of an SM, issue 0.7 of it. Two threads a row halve a row's chain, but add instructions and
-// barriers: 17 to 128 rows were as fast as now, 136 and more 10 to 15 % slower.
+// 17 rows of 64 heads over 8 x 16000 keys: 31 us; 8 x 100000 keys, 64 rows a KV head 77.5 us (5.3 TB/s),
+// 256 rows 126, 512 rows 227 (0.92 PFLOP/s, the second parts' products not counted). Of the 31, 6.4 lie in
+// front of the first scores (the plan 1.8, the next item's look-up, the first pages and keys), 15 are
+// 13 steps of 64 keys, 3 the outputs, 4 the join. A step of two accumulators takes 1.1 us with 136 rows,
+// 1.35 with 256, where 0.7 would be its bytes and 0.85 the products of 256 rows at the nominal rate: the
+// softmax's warps, two a quarter of an SM. (With one part and two threads a row, which halve a row's chain
+// but add instructions and barriers, 17 to 128 rows were no faster, 136 and more 10 to 15 % slower.)
 #pragma once
 
 #include "attn_wide.cuh"
@@ -160,9 +163,11 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
         const uint32_t buf = n & 1;
         if (t == 0 || sg.it.nr > t * kWRows)
 #pragma unroll
-          for (int k = 0; k < kWKeys / 16; ++k)  // 16 keys: 8 words of P, two 8-row groups of V
-            w_mma_ts(tmO, tmS + buf * kWKeys + 8 * k, dv + ((ring.at * L::kStep + k * 2048) >> 4),
-                     kPIdescV, i > 0 || k > 0, one);
+          for (int k = 0; k < kWKeys / 16; ++k)  // 16 keys: 8 words of a part of P, two 8-row groups of V
+#pragma unroll
+            for (int x = 1; x >= 0; --x)  // (second parts first, as the small ones)
+              w_mma_ts(tmO, tmS + buf * kWKeys + x * (kWKeys / 2) + 8 * k,
+                       dv + ((ring.at * L::kStep + k * 2048) >> 4), kPIdescV, i > 0 || k > 0 || x == 0, one);
         if (one) {
           tc_commit(&bar.o_done[t][buf]);
           tc_commit(&bar.free[ring.at]);
@@ -321,22 +326,22 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
               if (own) c = 1.f, base = 0.f;
             }
           }
-          // A probability's rounding to 8 bits is in the sum, too: the weights add up to one.
           const float top = base == -INFINITY ? 0.f : base;
           const uint64_t c2 = pack2(c, c), t2 = pack2(-top, -top);
           uint64_t sum2 = 0;
+          uint32_t lo[32];  // the probabilities' second parts
 #pragma unroll
           for (int x = 0; x < 64; x += 2) {
             const float2 z =
                 unpack2(fma2(pack2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), c2, t2));
-            const __nv_bfloat162 h = __floats2bfloat162_rn(ex2_approx(z.x), ex2_approx(z.y));
-            const uint32_t u = *reinterpret_cast<const uint32_t*>(&h);
-            sum2 = add2(sum2, pack2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)));
-            r[x / 2] = u;
+            const float p0 = ex2_approx(z.x), p1 = ex2_approx(z.y);
+            sum2 = add2(sum2, pack2(p0, p1));
+            split2(p0, p1, r[x / 2], lo[x / 2]);
           }
           const float2 sum = unpack2(sum2);
           ls += sum.x + sum.y;
           w_st32(at, r);
+          w_st32(at + kWKeys / 2, lo);
           w_st_wait();
         }
         tc_fence_before();

@@ -632,7 +632,8 @@ class PagedKVCache:
         """softmax(q k^T / sqrt(head_dim)) v over a layer's pages for q [n_seq, M, n_heads,
         head_dim]: row m < rows[b] of sequence b sits at position pos[b] + m, whose key has been
         appended, and sees the keys up to its own from first[b] on, at most `window` of them
-        (0: all).  A row that sees none is zero.  `longest`: no sequence's pos[b] + rows[b] exceeds
+        (0: all).  A row that sees none is zero.  Scores and sums are fp32, probabilities too, or of
+        16 bits in a bf16 cache.  `longest`: no sequence's pos[b] + rows[b] exceeds
         it (0: max_seq), which short sequences in a large table gain by.  Returns `out`, which keeps
         its rows from rows[b] on; without it a new tensor, where those are zero (a sequence with
         bad positions leaves its own unset)."""
