@@ -311,7 +311,8 @@ size_t ssd_paged_attention_bytes(const ssd_paged_cache* cache, int32_t n_heads, 
  * in one that it sees does.  A sequence some visible position of which has no page
  * (SSD_PAGED_ERR_TABLE) has undefined rows.  Scores, sums and outputs are fp32, and so are the
  * probabilities of an fp32 cache; those of a bf16 cache are multiplied with the values with 16 bits
- * (2^-16 of each), whatever the sizes and `longest`.  Equal calls give equal bits. */
+ * (2^-16 of each), whatever the sizes and `longest`.  Sums are divided at their end: values above
+ * 2^127 over the number of visible keys can give an infinity.  Equal calls give equal bits. */
 ssd_status ssd_paged_attention(const ssd_paged_cache* cache, int32_t layer, const void* q,
                                int32_t n_heads, int64_t q_stride, int32_t M, const int32_t* pos,
                                const int32_t* rows, const int32_t* first, int32_t window,

@@ -11,9 +11,9 @@
 //    buffers) for a step while the softmax of the step before is at work, another one O += P V,
 //    P read from tensor memory, as soon as a softmax is done;
 //  - four an accumulator do the softmax, a thread per row: the row's 64 scores into registers, their
-//    maximum, p = 2^(s - ref) as two bf16 parts, which take the place of S. ref is the row's maximum
-//    as of the last time it grew by more than 8 (in powers of two), so O is rescaled in tensor
-//    memory only then.
+//    maximum, p = 2^(s - ref) as two bf16 parts, which take the place of S. ref lies 8 (in powers of
+//    two) above what the row's maximum was the last time it passed ref, so O is rescaled in tensor
+//    memory only then, and no p is above 1: sums stay as far from fp32's end as in the other kernels.
 // A probability's two parts keep 16 bits of it, as in the kernels for fewer rows. One part is not enough: an
 // error of 2^-8 of each weight is one of up to 2^-8 sum w |v|, many units of an output whose values
 // cancel (17 rows of 64 heads over 16000 keys were 0.0022 off for 0.0017 with fp32 weights, which two
@@ -48,7 +48,7 @@ struct PWideL {
   static constexpr uint32_t kCols = 256 * TILES;  // tensor memory: S and P (2 x 64 each), O
 };
 constexpr float kPGrow = 8.f;
-constexpr float kPFar = 1048576.f;  // 2^20: half a unit there is 2^-4
+constexpr float kPFar = 1048576.f;  // 2^20: half a unit there is 2^-4, and ref is rounded twice
 
 // Instruction descriptors: bf16 operands, fp32 accumulator, M = 128; values are MN-major (bit 16).
 constexpr uint32_t kPIdesc = idesc_bf16_f32(128, kWKeys);
@@ -290,14 +290,14 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
             for (int y = 0; y < 4; ++y)
               m[y] = w_max3(m[y], __uint_as_float(r[x + 2 * y]), __uint_as_float(r[x + 2 * y + 1]));
           const float mx = fmaxf(w_max3(m[0], m[1], m[2]), m[3]) * a.scale;
-          // (rounded down: what stays is not above ref + 8, whatever ref's unit is)
-          const bool grow = mx > __fadd_rd(ref, kPGrow) || (ref == -INFINITY && mx > ref);
+          const bool grow = mx > ref;
           float c = a.scale, base = ref;  // what the exponents below are taken from
           if (__any_sync(0xffffffffu, grow || far)) {
             float f = 1.f;
             if (grow) {
-              f = ref == -INFINITY ? 0.f : exp2f(ref - mx);
-              ref = mx;
+              const float up = mx + kPGrow;
+              f = ref == -INFINITY ? 0.f : exp2f(ref - up);
+              ref = up;
               ls *= f;
             }
             if (i > 0) {

@@ -156,3 +156,28 @@ def test_values_that_cancel_show_the_bits_of_a_probability(form, dtype, heads, k
     c.pages[held, 0, 1] = full.view(len(held), page, kvh, hd).transpose(1, 2).to(c.dtype).cuda()
     _held(c, 0, q, [keys], [M])
     c.check()
+
+
+@pytest.mark.parametrize("form,dtype,heads,kvh,hd,M,cap", SHAPES)
+def test_large_values_stay_finite(form, dtype, heads, kvh, hd, M, cap):
+    """A few hundred values of up to 2^119, all of one sign, their largest scores behind the first ones by a little
+    less than what moves a running maximum's stand-in: the sums stay within fp32. So many sequences (all
+    of the same pages) that a block walks whole items."""
+    torch = _torch()
+    keys, page, n = 300, 32, 48
+    c, g = _filled(dtype, 1, kvh, hd, page, n, (keys + M) // page + 1, seed=M,
+                   room=cap // page - (keys + M) // page - 1 if cap > 640 else 0)
+    assert _forms(c, heads, M) == {form}
+    c.table[:] = c.table[0]
+    score = np.full(keys, 7.5 * np.log(2.0))
+    score[:64] = 0.0
+    q, held, _ = _one_key_column(c, heads, M, keys, score)
+    v = (1.0 + torch.rand(len(held), kvh, page, hd, generator=g, device="cuda")) * 2.0 ** 118
+    c.pages[held, 0, 1] = v.to(c.dtype)
+    got = c.attention(0, q.expand(n, M, heads, hd).contiguous(), _ints([keys] * n)).double().cpu().numpy()
+    bits, half = (24, 2.0 ** -24) if dtype == "f32" else (16, 2.0 ** -8)
+    want, bound = R.attention(_twin(c), 0, q.float().cpu().numpy(), [keys], [M], [0], 0, bits)
+    assert np.isfinite(want).all() and want.min() > 2.0 ** 118
+    off = np.abs(got - want) - (bound + half * (want + bound))
+    assert off.max() <= 0, off.max()
+    c.check()
