@@ -78,7 +78,11 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
   __shared__ Kv8PlanSmem s_plan;
   __shared__ PWideBars<TILES> bar;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_bad, s_fail, s_more[TILES];
+  __shared__ int s_fail, s_more[TILES];
+  // i + 1 at i % 8 where a value of the block's segment i was zeroed. Segments have a step or more, so the
+  // copies are at most kNst segments ahead of a softmax that has not begun its next one.
+  __shared__ uint32_t s_odd[8];
+  static_assert(L::kNst < 8, "a place for each segment under way");
   __shared__ Kv8Cursor s_cur[TILES];  // of the softmax warps
   __shared__ Kv8Seg s_seg[TILES];
   unsigned char* const smem =
@@ -104,7 +108,8 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
     }
     mbar_init(&bar.drained, 2 * TILES);
     mbar_init_fence();
-    s_bad = s_fail = 0;
+    for (int i = 0; i < 8; ++i) s_odd[i] = 0;
+    s_fail = 0;
     a.desc[blockIdx.x].nr = 0;
   }
   if (warp == L::kQk) tc_alloc(&s_tmem, L::kCols);
@@ -180,6 +185,7 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
     const uint32_t to = (ch >> 3) * kWKHalf;
     // values that are no numbers to zero, in a step that not every row sees whole (each thread in the
     // chunks that it copied)
+    uint32_t seg = 0;
     auto clean = [&]() {
       unsigned char* const st = Ks + ring.at * L::kStep + kWKTile + to;
       uint32_t any = 0;
@@ -191,11 +197,10 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
         u.z = numbers(u.z, any), u.w = numbers(u.w, any);
         *p = u;
       }
-      // (published by the arrival that follows; it stays set for the block's later tiles)
-      if (any) s_bad = 1;
+      if (any) s_odd[seg & 7] = seg + 1;  // (published by the arrival that follows)
     };
     Kv8Seg sg;
-    while (kv8_next<L::kRows, kWKeys>(a, cur, sg)) {
+    for (; kv8_next<L::kRows, kWKeys>(a, cur, sg); ++seg) {
       const Kv8Item& it = sg.it;
       const int k00 = (it.unit0 + sg.u0) * kWKeys;
       const int full_lo = kv8_row_lo(it, it.hi, a.window), full_hi = kv8_row_pos(a, it, it.r0);
@@ -229,7 +234,7 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
     const int row = tid;  // of the tile
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tmS = tm + t * kS + lanes, tmO = tm + kO + t * kWHd + lanes;
-    for (;;) {
+    for (uint32_t seg = 0;; ++seg) {
       // the segment stands in shared memory: the steps need the registers
       if (ttid == 0) s_more[t] = kv8_next<L::kRows, kWKeys>(a, s_cur[t], s_seg[t]);
       named_sync(1 + t, 128);
@@ -352,7 +357,7 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
       tc_fence_after();
       // ---- the rows' outputs, or the block's part of them
       if (live) {
-        const bool whole = sg.whole(), odd = *(volatile int*)&s_bad;
+        const bool whole = sg.whole(), odd = *(volatile uint32_t*)&s_odd[seg & 7] == seg + 1;
         const int slot = 2 * blockIdx.x + (sg.u0 == 0);
         const bool in = row < it.nr, sees = plo <= phi;
         const float unit = ls == 0.f ? 0.f : 1.f / ls;
@@ -371,21 +376,45 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
             f[x] = ls == 0.f ? 0.f : __uint_as_float(o[x]) * unit;
             nan |= f[x] != f[x];
           }
-          if ((odd || nan) && in && ls == ls) {  // as in k_paged_rows
+          const bool mend = (odd || nan) && in && ls == ls;  // as in k_paged_rows
+          if (__any_sync(0xffffffffu, mend)) {
             uint32_t seen = 0;  // columns with such a value: their sum takes the column's place
-            const int kb = max(k00, plo), ke = min(k00 + sg.nu * kWKeys - 1, phi);
-            for (int key = kb; key <= ke; ++key) {
+            const int last = min(k00 + sg.nu * kWKeys - 1, it.hi);
+            const int kb = max(k00, plo), ke = min(last, phi);
+            const char* const v0 = a.v + sg.g * a.c.head() + 64 * q;
+            auto at = [&](int key) -> const char* {
               const int e = max(a.c.entry(it.b, key >> a.c.shift), 0);
-              const char* v = a.v + sg.g * a.c.head() + (size_t)e * a.c.bytes +
-                              (size_t)(key & pmask) * (kWHd * 2) + 64 * q;
-#pragma unroll 1
-              for (int x = 0; x < 32; ++x) {
-                const float y = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(v)[x]);
-                if (!no_number(y)) continue;
+              return v0 + (size_t)e * a.c.bytes + (size_t)(key & pmask) * (kWHd * 2);
+            };
+            // a lane a key looks for them (an exponent of ones and one more is a carry), each row takes what
+            // it sees (a thread a row that walked 3000 keys by itself took 25 ms)
+            for (int k1 = max(k00, it.lo); k1 <= last; k1 += 32) {
+              uint32_t carry = 0;
+              if (k1 + lane <= last) {
+                const uint4* v = reinterpret_cast<const uint4*>(at(k1 + lane));
 #pragma unroll
-                for (int z = 0; z < 32; ++z)
-                  if (z == x) f[z] = seen >> x & 1 ? f[z] + y : y;
-                seen |= 1u << x;
+                for (int x = 0; x < 4; ++x) {
+                  const uint4 u = v[x];
+                  carry |= (u.x & 0x7f807f80u) + 0x00800080u;
+                  carry |= (u.y & 0x7f807f80u) + 0x00800080u;
+                  carry |= (u.z & 0x7f807f80u) + 0x00800080u;
+                  carry |= (u.w & 0x7f807f80u) + 0x00800080u;
+                }
+              }
+              uint32_t hits = __ballot_sync(0xffffffffu, (carry & 0x80008000u) != 0);
+              for (; hits; hits &= hits - 1) {
+                const int key = k1 + __ffs(hits) - 1;
+                if (!mend || key < kb || key > ke) continue;
+                const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(at(key));
+#pragma unroll 1
+                for (int x = 0; x < 32; ++x) {
+                  const float y = __bfloat162float(v[x]);
+                  if (!no_number(y)) continue;
+#pragma unroll
+                  for (int z = 0; z < 32; ++z)
+                    if (z == x) f[z] = seen >> x & 1 ? f[z] + y : y;
+                  seen |= 1u << x;
+                }
               }
             }
           }

@@ -181,3 +181,43 @@ def test_large_values_stay_finite(form, dtype, heads, kvh, hd, M, cap):
     off = np.abs(got - want) - (bound + half * (want + bound))
     assert off.max() <= 0, off.max()
     c.check()
+
+
+def test_what_is_no_number_slows_its_own_rows_alone():
+    """An infinity that one sequence's last row sees, in one head: the others' rows keep their bits. Where the
+    sequence is short, the call takes its time (each of the others' keys walked again by one thread a row took
+    160 times as long), where it has 3000 keys, a few times that at most (they are looked through by 32 at a
+    time, a round trip of a page's number and 64 bytes, for each quarter of the columns: 0.2 ms beside 0.15)."""
+    torch = _torch()
+    n, M, heads, kvh = 41, 17, 64, 8
+    c, g = _filled("bf16", 1, kvh, 128, 64, n, 50, seed=3)
+    assert _forms(c, heads, M) == {"wide2"}
+    at = [0] + [3000 + 3 * b for b in range(n - 1)]
+    pos = _ints(at)
+    q = torch.randn(n, M, heads, 128, generator=g, device="cuda").bfloat16()
+
+    def timed():
+        took = []
+        for _ in range(7):
+            a, z = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            torch.cuda.synchronize()
+            a.record()
+            got = c.attention(0, q, pos)
+            z.record()
+            torch.cuda.synchronize()
+            took.append(a.elapsed_time(z))
+        return got, sorted(took)[3]
+    want, before = timed()
+    for b, times in ((0, 4), (20, 16)):
+        p = at[b] + M - 1
+        e = int(c.table[b, p // 64])
+        was = c.pages[e, 0, 1, 0, p % 64, 5].clone()
+        c.pages[e, 0, 1, 0, p % 64, 5] = float("inf")
+        got, after = timed()
+        hit = got[b, M - 1, :heads // kvh, 5]
+        assert (hit == float("inf")).all()
+        got[b, M - 1, :heads // kvh, 5] = want[b, M - 1, :heads // kvh, 5]
+        assert torch.equal(got, want)
+        assert after <= times * before, (b, before, after)
+        c.pages[e, 0, 1, 0, p % 64, 5] = was
+    c.check()
