@@ -16,6 +16,7 @@ from typing import NamedTuple
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 import synth
 from synth.workloads import ModelShape, Workload
@@ -265,6 +266,8 @@ def _on(t, device: torch.device, what: str) -> int:
         raise ValueError(f"{what} is on {t.device}, not on {device}")
     if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{what} requires a gradient: there is no backward pass")
+    if forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{what} has a tangent: there is no forward-mode derivative")
     return t.data_ptr()
 
 
@@ -528,8 +531,8 @@ class PagedKVCache:
         if x.dtype is not self.dtype:
             raise ValueError(f"{what} must be {self.dtype}, as the cache, not {x.dtype}")
         M, row = _rows_of(x, self.n_seq, heads, self.head_dim, what)
-        at = x.data_ptr() if x.get_device() == self._index and not x.requires_grad else \
-            _on(x, self.device, what)
+        at = x.data_ptr() if x.get_device() == self._index and not x.requires_grad and \
+            forward_ad._current_level < 0 else _on(x, self.device, what)
         return at, M, row
 
     def _here(self, stream) -> bool:

@@ -174,6 +174,25 @@ def test_python_calls_refuse():
             call()
 
 
+def test_tangents_are_refused():
+    """No entry point has a forward-mode derivative: a dual tensor's tangent would be lost."""
+    from torch.autograd import forward_ad
+    from paper_2606_03113_gb300.runtime import KV8Cache, token_logprobs
+    c, c8 = py_cache(), KV8Cache(4, 64, 64, n_seq=3, device="cpu")
+    pos = torch.zeros(3, dtype=torch.int32)
+    k, q, z = torch.zeros(3, 2, 4, 64), torch.zeros(3, 2, 8, 64), torch.zeros(2, 9)
+    with forward_ad.dual_level():
+        dk, dq, dz = (forward_ad.make_dual(x, torch.ones_like(x)) for x in (k, q, z))
+        for call in (lambda: c.append(0, dk, k, pos), lambda: c.append(0, k, dk, pos),
+                     lambda: c.attention(0, dq, pos), lambda: c.attention(0, q, pos, out=dq),
+                     lambda: c8.append(dk, k, pos), lambda: c8.attention(dq, pos),
+                     lambda: token_logprobs(dz)):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+        with pytest.raises(ValueError, match="CUDA"):  # others are as ever
+            c.append(0, k, k, pos)
+
+
 def test_every_error_bit_of_the_kernels_is_named():
     import re
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
