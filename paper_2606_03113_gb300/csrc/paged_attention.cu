@@ -994,6 +994,9 @@ const char* check_attention(const ssd_paged_cache* c, int32_t n_heads, int32_t M
   const int cap = c->max_pages * c->page;
   if (M > cap) return "more rows than the cache has positions";
   if (longest > cap) return "longest: more than the cache has positions";
+  // (a tile's first row is an int, also of those behind the rows that a short `longest` leaves)
+  if ((long long)M * (n_heads / c->n_kv_heads) > 0x7fffffffll - 256)
+    return "M x n_heads / n_kv_heads: more than 2^31 rows of a KV head";
   *plan = plan_of(c, n_heads, M, longest ? longest : cap, window);
   if (plan->units > 0x7fffffffll) return "n_seq x M x longest: more than 2^31 units of work";
   *status = SSD_OK;

@@ -118,6 +118,19 @@ def test_attention_refuses(kw, status):
     assert e.value.status == status
 
 
+def test_attention_counts_rows_in_31_bits():
+    """Rows of a KV head are numbered in 31 bits, by tiles of up to 256: more are refused, also where `longest`
+    keeps the work itself small."""
+    c = cache(n_seq=1, n_kv_heads=1, head_dim=64, max_pages=1 << 20)
+    assert S.ssd_paged_attention_bytes(c, 65536, (1 << 15) - 1, 0, 1) > 0
+    for M in (1 << 15, 40000, 1 << 24):
+        assert S.ssd_paged_attention_bytes(c, 65536, M, 0, 1) == 0
+        with pytest.raises(S.SsdError) as e:
+            S.ssd_paged_attention(c, 0, BUF, 65536, 65536 * 64, M, BUF, 0, 0, 0, 1, BUF, 65536 * 64, BUF,
+                                  1 << 40)
+        assert e.value.status == CAPACITY and "rows" in str(e.value)
+
+
 # ------------------------------------------------------------- the Python entry points
 
 def py_cache(**kw):
