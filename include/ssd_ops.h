@@ -266,8 +266,9 @@ size_t ssd_paged_workspace_bytes(const ssd_paged_cache* cache);
  *   where all who share a page ask for it in this call, it stays with the last of them;
  * - any other stays.
  * Free pages are taken lowest first, for the sequences in their order and each one's positions in
- * theirs; the result is that of looking at the sequences one by one.  Positions from pos[b] + rows[b] on
- * keep their pages.  Where the free pages do not suffice, nothing is changed, and the error bit
+ * theirs; the result is that of looking at the sequences one by one.  Pages behind the one that holds
+ * position pos[b] + rows[b] - 1 stay as they are; in a page that was copied, what stood from
+ * pos[b] on is left behind.  Where the free pages do not suffice, nothing is changed, and the error bit
  * SSD_PAGED_ERR_PAGES is set.  A sequence whose positions do not lie in the cache, or whose rows[b]
  * does not in 0 .. M, is left alone, with its error bit. */
 ssd_status ssd_paged_reserve(const ssd_paged_cache* cache, const int32_t* pos, const int32_t* rows,

@@ -546,8 +546,8 @@ class PagedKVCache:
 
     def reserve(self, pos: torch.Tensor, rows: torch.Tensor | int = 1, stream=None):
         """Pages for rows[b] new rows (or `rows` of each sequence) at positions pos[b] and up: missing
-        ones, and copies of shared ones up to pos[b], are taken lowest first.  Changes nothing where
-        too few pages are free (`check` raises)."""
+        ones, and copies of shared ones up to pos[b] (what stood from there on in such a page is left
+        behind), are taken lowest first.  Changes nothing where too few pages are free (`check` raises)."""
         if pos is None:
             raise ValueError("pos is missing")
         pp = self._ints(pos, "pos")

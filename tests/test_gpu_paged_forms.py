@@ -7,7 +7,7 @@ import pytest
 
 import paged_ref as R
 from parity import has_gpu
-from test_gpu_paged import _dtype, _filled, _ints, _torch, _twin
+from test_gpu_paged import _agree, _cache, _dtype, _err, _filled, _ints, _torch, _twin
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not has_gpu(), reason="needs a CUDA GPU")]
 
@@ -221,3 +221,52 @@ def test_what_is_no_number_slows_its_own_rows_alone():
         assert after <= times * before, (b, before, after)
         c.pages[e, 0, 1, 0, p % 64, 5] = was
     c.check()
+
+
+# ------------------------------------------------------------------ rows and pages beyond one pass
+
+@pytest.mark.parametrize("dtype,heads,M", [("bf16", 41, 1), ("bf16", 64, 3), ("bf16", 80, 2), ("f32", 24, 2)])
+def test_rows_of_more_chunks_than_threads_hold_at_once(dtype, heads, M):
+    """Rows of more than 5 x 128 pieces of 16 bytes: a whole second batch of them, and a part of one."""
+    torch = _torch()
+    c = _cache(dtype, 2, heads, 128, 9, 16, 2, 4, fill=2.0)
+    r = _twin(c)
+    k, v = (torch.randn(2, M, heads, 128, device="cuda").to(_dtype(dtype)) for _ in range(2))
+    pos, rows = [15, 30], [M, M - 1]
+    for x in (c, r):
+        x.reserve(*((_ints(pos), _ints(rows)) if x is c else (pos, rows)))
+    c.append(1, k, v, _ints(pos), rows=_ints(rows))
+    r.append(1, k.float().cpu().numpy(), v.float().cpu().numpy(), pos, rows)
+    _agree(c, r)
+    c.check()
+
+
+@pytest.mark.parametrize("pool", [2399, 9000])
+def test_too_few_pages_for_thousands_of_claims(pool):
+    """More wanted entries than a reserve keeps in registers, shared and missing ones, in a pool that is one page
+    short: claims are taken back, nothing changes, and what fits works."""
+    torch = _torch()
+    c = _cache("f32", 1, 1, 64, pool, 16, 3, 1300)
+    r = _twin(c)
+    taken = pool - 2399  # pages that nobody here names
+    c.refs[:taken] = 1
+    r.refs[:taken] = [1] * taken
+    for x, ints in ((c, _ints), (r, list)):
+        x.reserve(ints([0, 0, 0]), ints([16 * 1200, 0, 0]))
+        x.fork(ints([0, 0, 2]))
+    c.refs[:taken] = 1
+    r.refs[:taken] = [1] * taken
+    c.pages.copy_(torch.arange(pool, device="cuda").view(-1, 1, 1, 1, 1, 1).expand_as(c.pages))
+    r.pages = c.pages.float().cpu().numpy()
+    # 1100 pages that both ask for, of which the first sequence needs new ones, and 100 missing ones
+    pos, rows = [7, 7, 0], [1100 * 16 - 7, 1100 * 16 - 7, 1600]
+    for x, ints in ((c, _ints), (r, list)):
+        x.reserve(ints(pos), ints(rows))
+    assert _err(c) == r.err == R.PAGES
+    _agree(c, r)
+    r.err = 0
+    rows[2] = 1584
+    for x, ints in ((c, _ints), (r, list)):
+        x.reserve(ints(pos), ints(rows))
+    assert _err(c) == r.err == 0
+    _agree(c, r)
