@@ -931,12 +931,12 @@ cudaError_t paged_device(int* sms) {
 // More than 16 rows a KV head, bf16 and head_dim 128: tcgen05 tiles, but for 17 to 32 rows where there are
 // clusters. us, k_paged_rows / k_paged_wide, 8 KV heads, sequences x keys:
 //                   17 rows       32         33         64
-//   1 x 250       10.5/11.2  10.9/11.7  14.5/12.1  15.9/12.2
-//   1 x 1000      10.7/13.5  11.2/14.0  13.8/14.1  14.7/14.5
-//   1 x 4000      18.0/15.1  18.9/15.8  22.2/15.9  23.9/16.3
-//   16 x 250      12.4/19.0  13.0/20.4  16.9/20.4  18.7/21.1
-//   16 x 1000     26.5/26.1  27.6/27.3  39.9/27.6  42.4/29.1
-//   16 x 16000     269/175    271/177    426/178    436/180
+//   1 x 250       10.5/11.8  10.9/11.8  14.5/12.1  15.9/12.2
+//   1 x 1000      10.7/14.2  11.2/14.2  13.8/14.3  14.7/14.7
+//   1 x 4000      18.0/15.9  18.9/16.2  22.2/16.2  23.9/16.7
+//   16 x 250      12.4/20.3  13.0/20.5  16.9/20.6  18.7/21.4
+//   16 x 1000     26.5/28.7  27.6/29.0  39.9/29.4  42.4/30.8
+//   16 x 16000     269/179    271/182    426/183    436/187
 constexpr int kSplitKeys = 128, kSplitBlocks = 304, kSplitSeq = 512;
 
 struct PagedPlan {

@@ -14,17 +14,17 @@
 //    maximum, p = 2^(s - ref) as two bf16 parts, which take the place of S. ref lies 8 (in powers of
 //    two) above what the row's maximum was the last time it passed ref, so O is rescaled in tensor
 //    memory only then, and no p is above 1: sums stay as far from fp32's end as in the other kernels.
-// A probability's two parts keep 16 bits of it, as in the kernels for fewer rows. One part is not enough: an
-// error of 2^-8 of each weight is one of up to 2^-8 sum w |v|, many units of an output whose values
+// A probability's two parts keep 16 bits of it, as in the kernels for fewer rows. One part is not enough:
+// an error of 2^-8 of each weight is one of up to 2^-8 sum w |v|, many units of an output whose values
 // cancel (17 rows of 64 heads over 16000 keys were 0.0022 off for 0.0017 with fp32 weights, which two
 // parts give back). The second part is half as many products again, conversions and stores: 28 -> 31 us,
-// 73 -> 77.5, 98 -> 126 and 174 -> 227 for the sizes below.
+// 73 -> 78, 98 -> 118 and 174 -> 210 for the sizes below.
 //
-// 17 rows of 64 heads over 8 x 16000 keys: 31 us; 8 x 100000 keys, 64 rows a KV head 77.5 us (5.3 TB/s),
-// 256 rows 126, 512 rows 227 (0.92 PFLOP/s, the second parts' products not counted). Of the 31, 6.4 lie in
+// 17 rows of 64 heads over 8 x 16000 keys: 31 us; 8 x 100000 keys, 64 rows a KV head 78 us (5.3 TB/s),
+// 256 rows 118, 512 rows 210 (1.0 PFLOP/s, the second parts' products not counted). Of the 31, 6.4 lie in
 // front of the first scores (the plan 1.8, the next item's look-up, the first pages and keys), 15 are
 // 13 steps of 64 keys, 3 the outputs, 4 the join. A step of two accumulators takes 1.1 us with 136 rows,
-// 1.35 with 256, where 0.7 would be its bytes and 0.85 the products of 256 rows at the nominal rate: the
+// 1.27 with 256, where 0.7 would be its bytes and 0.85 the products of 256 rows at the nominal rate: the
 // softmax's warps, two a quarter of an SM. (With one part and two threads a row, which halve a row's chain
 // but add instructions and barriers, 17 to 128 rows were no faster, 136 and more 10 to 15 % slower.)
 #pragma once
@@ -55,8 +55,8 @@ constexpr uint32_t kPIdesc = idesc_bf16_f32(128, kWKeys);
 constexpr uint32_t kPIdescV = idesc_bf16_f32(128, kWHd) | 1u << 16;
 
 // Barriers: a ring step's keys and values stored, and free again (one each for both: with barriers of
-// their own, which 128 threads arrive at, 8 x 100000 keys took 78 us for 72); of the two buffers of S:
-// scores there, probabilities there, output added; queries of the segment stored.
+// their own, which 128 threads arrive at, 8 x 100000 keys took 78 us where they took 72 so, a
+// probability in one part); of the two buffers of S: scores there, probabilities there, output added; queries of the segment stored.
 template <int TILES>
 struct PWideBars {
   uint64_t full[PWideL<TILES>::kNst], free[PWideL<TILES>::kNst];
@@ -172,7 +172,8 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
 #pragma unroll
             for (int x = 1; x >= 0; --x)  // (second parts first, as the small ones)
               w_mma_ts(tmO, tmS + buf * kWKeys + x * (kWKeys / 2) + 8 * k,
-                       dv + ((ring.at * L::kStep + k * 2048) >> 4), kPIdescV, i > 0 || k > 0 || x == 0, one);
+                       dv + ((ring.at * L::kStep + k * 2048) >> 4), kPIdescV, i > 0 || k > 0 || x == 0,
+                       one);
         if (one) {
           tc_commit(&bar.o_done[t][buf]);
           tc_commit(&bar.free[ring.at]);
@@ -386,8 +387,8 @@ __global__ void __launch_bounds__(PWideL<TILES>::kThreads, 1) k_paged_wide(const
               const int e = max(a.c.entry(it.b, key >> a.c.shift), 0);
               return v0 + (size_t)e * a.c.bytes + (size_t)(key & pmask) * (kWHd * 2);
             };
-            // a lane a key looks for them (an exponent of ones and one more is a carry), each row takes what
-            // it sees (a thread a row that walked 3000 keys by itself took 25 ms)
+            // a lane a key looks for them (an exponent of ones and one more is a carry), each row takes
+            // what it sees (a thread a row that walked 3000 keys by itself took 25 ms)
             for (int k1 = max(k00, it.lo); k1 <= last; k1 += 32) {
               uint32_t carry = 0;
               if (k1 + lane <= last) {
