@@ -56,7 +56,8 @@ constexpr uint32_t kPIdescV = idesc_bf16_f32(128, kWHd) | 1u << 16;
 
 // Barriers: a ring step's keys and values stored, and free again (one each for both: with barriers of
 // their own, which 128 threads arrive at, 8 x 100000 keys took 78 us where they took 72 so, a
-// probability in one part); of the two buffers of S: scores there, probabilities there, output added; queries of the segment stored.
+// probability in one part); of the two buffers of S: scores there, probabilities there, output added;
+// queries of the segment stored.
 template <int TILES>
 struct PWideBars {
   uint64_t full[PWideL<TILES>::kNst], free[PWideL<TILES>::kNst];
